@@ -32,6 +32,24 @@ LAYER_EXPORTS = ["okv_pack_linear_weight", "okv_linear", "okv_linear_qkv", "okv_
                  "okv_decoder_scratch_bytes", "okv_decoder_step"]
 
 
+# every symbol include/okv_cache8.h declares (same library)
+CACHE8_EXPORTS = ["okv8_codes_bytes", "okv8_scales_bytes", "okv8_tails_bytes", "okv8_workspace_bytes", "okv8_store", "okv8_load", "okv8_step_begin",
+                  "okv8_decode_attn", "okv8_decode_step"]
+
+
+class Okv8Cache(ctypes.Structure):
+    """okv8_cache of include/okv_cache8.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "page_tokens", "format", "out_dtype", "max_seqs",
+                                              "max_pages_per_seq")] + [("n_pages", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("codes", "scales", "tails", "page_table")]
+
+
+class Okv8Step(ctypes.Structure):
+    """okv8_step of include/okv_cache8.h."""
+    _fields_ = [("batch", ctypes.c_int32), ("appends", ctypes.c_int32), ("seqs", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64), ("stream", ctypes.c_void_p)]
+
+
 class OkvDecoderLayer(ctypes.Structure):
     """okv_decoder_layer of include/okv_layer.h: twelve device pointers."""
     FIELDS = ("ln1_gamma", "ln1_beta", "w_qkv", "b_qkv", "w_o", "b_o", "ln2_gamma", "ln2_beta", "w_ff1", "b_ff1", "w_ff2", "b_ff2")
@@ -144,6 +162,15 @@ def lib():
             "okv_waves_per_pair": (I32, [I32, I32, I32, I64, I64]),
             "okv_layers_per_launch": (I32, [P]),
             "okv_decode_attn_static": (ctypes.c_int, [ctypes.POINTER(OkvStaticAttn)]),
+            "okv8_codes_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),
+            "okv8_scales_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),
+            "okv8_tails_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),
+            "okv8_workspace_bytes": (I64, [ctypes.POINTER(Okv8Cache), I32]),
+            "okv8_store": (ctypes.c_int, [ctypes.POINTER(Okv8Cache), I32, I32, I32, P, P, P, I64, P, P, I64, I64, P]),
+            "okv8_load": (ctypes.c_int, [ctypes.POINTER(Okv8Cache), I32, I32, I32, P, P, P, I64, P, P, I64, I64, P]),
+            "okv8_step_begin": (ctypes.c_int, [ctypes.POINTER(Okv8Cache), ctypes.POINTER(Okv8Step)]),
+            "okv8_decode_attn": (ctypes.c_int, [ctypes.POINTER(Okv8Cache), ctypes.POINTER(Okv8Step), I32, P, I64, P, P, I64, P]),
+            "okv8_decode_step": (ctypes.c_int, [ctypes.POINTER(Okv8Cache), ctypes.POINTER(Okv8Step), P, P, P, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)

@@ -16,6 +16,7 @@
 #include "../../include/okv_layer.h"
 #include "okv_host.h"
 #include "okv_kernels.h"
+#include "okv_report.h"
 
 using okv::Op;
 
@@ -196,6 +197,18 @@ struct okv_ctx {
 
   std::string err;
 };
+
+namespace okv {
+int report(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_error = buf;
+  return code;
+}
+}  // namespace okv
 
 namespace {
 
