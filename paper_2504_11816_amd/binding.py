@@ -50,6 +50,32 @@ class Okv8Step(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64), ("stream", ctypes.c_void_p)]
 
 
+# every symbol include/okv_pages.h declares (same library)
+PAGES_EXPORTS = ["okv_pages_workspace_bytes", "okv_pages_extend", "okv_pages_fork", "okv_pages_free", "okv_pages_compact", "okv_pages_copy"]
+
+
+# every symbol include/okv_linear4.h declares (same library)
+LINEAR4_EXPORTS = ["okv_linear4_packed_bytes", "okv_linear4_pack", "okv_linear4_quantize", "okv_linear4", "okv_linear4_workspace_bytes"]
+
+
+class OkvPageArray(ctypes.Structure):
+    """okv_page_array of include/okv_pages.h."""
+    _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64), ("layer_stride", ctypes.c_int64), ("unit_tokens", ctypes.c_int32),
+                ("whole_units", ctypes.c_int32)]
+
+
+class OkvRowArray(ctypes.Structure):
+    """okv_row_array of include/okv_pages.h."""
+    _fields_ = [("base", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("groups", ctypes.c_int32), ("rows", ctypes.c_int32), ("row_bytes", ctypes.c_int32)]
+
+
+class OkvPages(ctypes.Structure):
+    """okv_pages of include/okv_pages.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "page_tokens", "max_seqs", "max_pages_per_seq", "n_pages", "n_arrays", "n_rows")] + [
+        ("arrays", OkvPageArray * 4), ("rows", OkvRowArray * 2)] + [(n, ctypes.c_void_p) for n in ("table", "lens", "refs", "status", "workspace")] + [
+        ("workspace_bytes", ctypes.c_int64)]
+
+
 class OkvDecoderLayer(ctypes.Structure):
     """okv_decoder_layer of include/okv_layer.h: twelve device pointers."""
     FIELDS = ("ln1_gamma", "ln1_beta", "w_qkv", "b_qkv", "w_o", "b_o", "ln2_gamma", "ln2_beta", "w_ff1", "b_ff1", "w_ff2", "b_ff2")
@@ -162,6 +188,17 @@ def lib():
             "okv_waves_per_pair": (I32, [I32, I32, I32, I64, I64]),
             "okv_layers_per_launch": (I32, [P]),
             "okv_decode_attn_static": (ctypes.c_int, [ctypes.POINTER(OkvStaticAttn)]),
+            "okv_linear4_packed_bytes": (I64, [I32, I32, I32, I32]),
+            "okv_linear4_pack": (ctypes.c_int, [P, P, I32, P, P, I32, I32, I32, P]),
+            "okv_linear4_quantize": (ctypes.c_int, [P, P, I32, I32, I32, I32, P]),
+            "okv_linear4": (ctypes.c_int, [P, P, P, P, ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(I32), I32, I32, I32, I32, I32, I32, I32, P, I64, P]),
+            "okv_linear4_workspace_bytes": (I64, [I32, I32, I32]),
+            "okv_pages_workspace_bytes": (I64, [I32]),
+            "okv_pages_extend": (ctypes.c_int, [ctypes.POINTER(OkvPages), I32, P, P, P]),
+            "okv_pages_fork": (ctypes.c_int, [ctypes.POINTER(OkvPages), I32, P, P, P]),
+            "okv_pages_free": (ctypes.c_int, [ctypes.POINTER(OkvPages), I32, P, P]),
+            "okv_pages_compact": (ctypes.c_int, [ctypes.POINTER(OkvPages), P]),
+            "okv_pages_copy": (ctypes.c_int, [ctypes.POINTER(OkvPages), I32, P, P, ctypes.POINTER(OkvPageArray), I32, P]),
             "okv8_codes_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),
             "okv8_scales_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),
             "okv8_tails_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),

@@ -15,6 +15,7 @@ import ctypes
 import torch
 
 from . import binding
+from .pages import PageArray, Pages, RowArray
 
 FORMATS = {"int8": 0, "e4m3": 1}
 TILE = 32
@@ -70,6 +71,10 @@ class Cache8:
         self.table = table
         self.lens = torch.zeros(max_seqs, dtype=torch.int32, device=self.device)
         c.codes, c.scales, c.tails, c.page_table = (x.data_ptr() for x in (self.codes, self.scales, self.tails, self.table))
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device=self.device)
+        self.pages = Pages(table=self.table, lens=self.lens, refs=self.refs, page_tokens=page_tokens,
+                           arrays=[PageArray(self.codes, TILE, whole_units=True), PageArray(self.scales, TILE, whole_units=True)],
+                           rows=[RowArray(self.tails, 2 * n_kv_heads, TILE)])
         # the workspace of a whole batch; steps of one cache follow one another on one stream
         n = min(max_seqs, 4096)
         self.workspace = torch.empty(bytes_of("okv8_workspace_bytes", n), dtype=torch.uint8, device=self.device)

@@ -1,0 +1,356 @@
+// Linear layers with 4-bit weights (include/okv_linear4.h), for gfx950.
+//
+// y[m][n] = sum_g scale[n][g] sum_{k in g} x[m][k] (code[n][k] - zero[n][g]) for a decode batch's few rows: bound by reading the codes.
+//
+//   * one 16-byte load per lane brings a wavefront a block of 16 features x 128 inputs, in operand order for four 16x16x32
+//     matrix-core instructions: nothing moves between lanes;
+//   * a code becomes an fp16 number with one and-or (0x6400 | code is 1024 + code; four bits further up it is 1024 + 16 code) and one packed
+//     subtraction or fused multiply-add that also takes the zero point off: code - zero, exactly, at about one instruction a weight;
+//   * the sums of a group stay apart from the others' in fp32 and are multiplied by its scale there: one fma per result and group
+//     instead of one rounding per weight;
+//   * a workgroup has the whole input dimension of its features, its wavefronts take blocks of 128 inputs in turn and add up
+//     through LDS: one launch per product.
+#include "okv_linear4.h"
+#include "okv_report.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "okv.h"
+
+namespace okv {
+
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kBlockIn = 128;            // inputs of a block
+constexpr int kWaves4 = 8;               // wavefronts of a workgroup
+
+struct Linear4Args {
+  const _Float16 *x;
+  const u32x4 *codes;                    // [n_out / 16][blocks][64]
+  const _Float16 *scales;                // [n_out / 16][blocks * groups of a block][16]
+  const uint8_t *zeros;
+  const _Float16 *bias, *residual;
+  _Float16 *out[3];
+  int32_t end[3];                        // first feature behind run s
+  int32_t m, n_out, n_in, blocks, relu;
+};
+
+// 8 codes -> code - zero.  near: -(1024 + zero) twice, far: -(64 + zero) twice
+__device__ __forceinline__ half8 unpack4bit(const uint32_t w, const half2v near, const half2v far) {
+  const half2v by = {(_Float16)0.0625f, (_Float16)0.0625f};
+  const uint32_t v = w >> 8;
+  const half2v a = __builtin_bit_cast(half2v, (w & 0x000f000fu) | 0x64006400u) + near;
+  const half2v b = __builtin_elementwise_fma(__builtin_bit_cast(half2v, (w & 0x00f000f0u) | 0x64006400u), by, far);
+  const half2v c = __builtin_bit_cast(half2v, (v & 0x000f000fu) | 0x64006400u) + near;
+  const half2v d = __builtin_elementwise_fma(__builtin_bit_cast(half2v, (v & 0x00f000f0u) | 0x64006400u), by, far);
+  return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// MF fragments of 16 rows, NT tiles of 16 features per workgroup, GROUPS groups in a block of 128 inputs, DEPTH blocks in flight per wavefront
+template <int MF, int NT, int GROUPS, bool ZEROS, int DEPTH>
+__global__ void __launch_bounds__(64 * kWaves4) linear4_kernel(Linear4Args a) {
+  __shared__ floatx4 shares[kWaves4][MF * NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tile0 = blockIdx.x * NT, row0 = blockIdx.y * 16 * MF, n_tiles = a.n_out / 16;
+  const int r = lane % 16, quarter = lane / 16;
+  floatx4 sum[MF][NT] = {};
+  const half8 none = {};
+
+  for (int b0 = wave; b0 < a.blocks; b0 += kWaves4 * DEPTH) {
+    u32x4 w[DEPTH][NT];
+    half4v scale[DEPTH][NT][GROUPS];
+    uint8_t zero[DEPTH][NT][GROUPS];
+    half8 x[DEPTH][MF][4];
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      const int b = min(b0 + i * kWaves4, a.blocks - 1);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int64_t at = (int64_t)min(tile0 + t, n_tiles - 1) * a.blocks + b;
+        w[i][t] = __builtin_nontemporal_load(a.codes + at * 64 + lane);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          scale[i][t][g] = *reinterpret_cast<const half4v *>(a.scales + (at * GROUPS + g) * 16 + 4 * quarter);
+          if (ZEROS) zero[i][t][g] = a.zeros[(at * GROUPS + g) * 16 + r];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      const int b = b0 + i * kWaves4;
+#pragma unroll
+      for (int f = 0; f < MF; ++f) {
+        const int row = row0 + 16 * f + r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int k = b * kBlockIn + 32 * j;
+          x[i][f][j] = row < a.m && k < a.n_in ? *reinterpret_cast<const half8 *>(a.x + (int64_t)row * a.n_in + k + 8 * quarter) : none;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      if (b0 + i * kWaves4 >= a.blocks) break;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          half2v near = {(_Float16)-1032.f, (_Float16)-1032.f}, far = {(_Float16)-72.f, (_Float16)-72.f};
+          if (ZEROS) {
+            near = __builtin_bit_cast(half2v, 0xe400e400u + zero[i][t][g] * 0x00010001u);
+            far = __builtin_bit_cast(half2v, 0xd400d400u + zero[i][t][g] * 0x00100010u);
+          }
+          floatx4 part[MF] = {};
+#pragma unroll
+          for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) {
+            const half8 v = unpack4bit(w[i][t][j], near, far);
+#pragma unroll
+            for (int f = 0; f < MF; ++f) part[f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, x[i][f][j], part[f], 0, 0, 0);
+          }
+#pragma unroll
+          for (int f = 0; f < MF; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[f][t][e] = fmaf(part[f][e], (float)scale[i][t][g][e], sum[f][t][e]);
+        }
+    }
+  }
+#pragma unroll
+  for (int f = 0; f < MF; ++f)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) shares[wave][f * NT + t][lane] = sum[f][t];
+  __syncthreads();
+  // 4 consecutive features of a row per thread
+  for (int i = threadIdx.x; i < MF * NT * 64; i += 64 * kWaves4) {
+    const int frag = i >> 6, l = i & 63, f = frag / NT, t = frag - f * NT;
+    floatx4 y = shares[0][frag][l];
+#pragma unroll
+    for (int w = 1; w < kWaves4; ++w) y += shares[w][frag][l];
+    const int row = row0 + 16 * f + l % 16, n = (tile0 + t) * 16 + 4 * (l / 16);
+    if (row >= a.m || n >= a.n_out) continue;
+    if (a.bias) {
+      const half4v bias = *reinterpret_cast<const half4v *>(a.bias + n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += (float)bias[e];
+    }
+    if (a.relu)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = fmaxf(y[e], 0.f);
+    if (a.residual) {
+      const half4v more = *reinterpret_cast<const half4v *>(a.residual + (int64_t)row * a.n_out + n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += (float)more[e];
+    }
+    const int s = n < a.end[0] ? 0 : n < a.end[1] ? 1 : 2, first = s == 0 ? 0 : s == 1 ? a.end[0] : a.end[1];
+    _Float16 *to = s == 0 ? a.out[0] : s == 1 ? a.out[1] : a.out[2];
+    const int width = (s == 0 ? a.end[0] : s == 1 ? a.end[1] : a.end[2]) - first;
+    half4v h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = (_Float16)y[e];
+    *reinterpret_cast<half4v *>(to + (int64_t)row * width + n - first) = h;
+  }
+}
+
+// ---- packing ----------------------------------------------------------------------------------------
+
+struct Packed {
+  uint32_t *codes;
+  _Float16 *scales;
+  uint8_t *zeros;
+};
+
+// What a thread writes: one 32-bit word (8 inputs of a feature); code(n, k) is asked for inputs below n_in
+template <class Code>
+__device__ __forceinline__ uint32_t pack_word(const int64_t i, const int blocks, const int n_in, const Code &code) {
+  const int64_t block = i >> 8;
+  const int lane = (i >> 2) & 63, j = i & 3, n = (int)(block / blocks) * 16 + lane % 16;
+  const int k = (int)(block % blocks) * kBlockIn + 32 * j + 8 * (lane / 16);
+  uint32_t w = 0;
+  if (k < n_in)
+#pragma unroll
+    for (int p = 0; p < 4; ++p) w |= code(n, k + 2 * p) << (4 * p) | code(n, k + 2 * p + 1) << (16 + 4 * p);
+  return w;
+}
+
+__global__ void __launch_bounds__(256) pack4_kernel(Packed to, const uint8_t *codes, int per_byte, const _Float16 *scales, const uint8_t *zeros, int n_out,
+                                                    int n_in, int group) {
+  const int blocks = (n_in + kBlockIn - 1) / kBlockIn, groups = n_in / group, padded = blocks * (kBlockIn / group);
+  const int64_t words = (int64_t)n_out / 16 * blocks * 256, all = (int64_t)n_out * padded;
+  const int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = i0; i < words; i += step)
+    to.codes[i] = pack_word(i, blocks, n_in, [&](int n, int k) -> uint32_t {
+      return per_byte == 1 ? codes[(int64_t)n * n_in + k] & 15u : codes[((int64_t)n * n_in + k) >> 1] >> (4 * (k & 1)) & 15u;
+    });
+  for (int64_t i = i0; i < all; i += step) {
+    const int g = (int)(i / 16 % padded), n = (int)(i / 16 / padded) * 16 + (int)(i % 16);
+    to.scales[i] = g < groups ? scales[(int64_t)n * groups + g] : (_Float16)0.f;
+    if (to.zeros) to.zeros[i] = g < groups ? zeros[(int64_t)n * groups + g] & 15u : 8;
+  }
+}
+
+// The scale and zero point of every group (a thread each)
+__global__ void __launch_bounds__(256) scales4_kernel(Packed to, const _Float16 *src, int n_out, int n_in, int group) {
+  const int blocks = (n_in + kBlockIn - 1) / kBlockIn, groups = n_in / group, padded = blocks * (kBlockIn / group);
+  const int64_t all = (int64_t)n_out * padded;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int g = (int)(i / 16 % padded), n = (int)(i / 16 / padded) * 16 + (int)(i % 16);
+    float lo = 0.f, hi = 0.f;
+    if (g < groups)
+      for (int k = 0; k < group; k += 8) {
+        const half8 w = *reinterpret_cast<const half8 *>(src + (int64_t)n * n_in + (int64_t)g * group + k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) lo = fminf(lo, (float)w[e]), hi = fmaxf(hi, (float)w[e]);
+      }
+    const _Float16 scale = (_Float16)(to.zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f);
+    to.scales[i] = scale;
+    if (to.zeros) to.zeros[i] = (float)scale > 0.f ? (uint8_t)fminf(__builtin_rintf(-lo / (float)scale), 15.f) : 8;
+  }
+}
+__global__ void __launch_bounds__(256) codes4_kernel(Packed to, const _Float16 *src, int n_out, int n_in, int group) {
+  const int blocks = (n_in + kBlockIn - 1) / kBlockIn, padded = blocks * (kBlockIn / group);
+  const int64_t words = (int64_t)n_out / 16 * blocks * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256)
+    to.codes[i] = pack_word(i, blocks, n_in, [&](int n, int k) -> uint32_t {
+      const int64_t at = ((int64_t)(n / 16) * padded + k / group) * 16 + n % 16;
+      const float scale = (float)to.scales[at], zero = to.zeros ? (float)to.zeros[at] : 8.f;
+      const float q = scale > 0.f ? __builtin_rintf((float)src[(int64_t)n * n_in + k] / scale) : 0.f;
+      return (uint32_t)fminf(fmaxf(q + zero, 0.f), 15.f);
+    });
+}
+
+// ---- host -------------------------------------------------------------------------------------------
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+const char *shape_problem(int32_t n_out, int32_t n_in, int32_t group) {
+  if (n_out < 16 || n_out % 16 || n_out > 1 << 24) return "n_out must be a multiple of 16, at most 2^24";
+  if (group != 32 && group != 64 && group != 128) return "group must be 32, 64 or 128";
+  if (n_in < 32 || n_in % 32 || n_in % group || n_in > 1 << 24) return "n_in must be a multiple of 32 and of group, at most 2^24";
+  return nullptr;
+}
+
+struct PackedLayout {
+  int64_t blocks, scales, zeros, bytes;  // blocks of 128 inputs; byte offsets
+};
+PackedLayout layout_of(int32_t n_out, int32_t n_in, int32_t group, bool zeros) {
+  PackedLayout l;
+  l.blocks = (n_in + kBlockIn - 1) / kBlockIn;
+  const int64_t groups = (int64_t)n_out * l.blocks * (kBlockIn / group);
+  l.scales = (int64_t)n_out / 16 * l.blocks * 1024;
+  l.zeros = l.scales + 2 * groups;
+  l.bytes = l.zeros + (zeros ? groups : 0);
+  return l;
+}
+Packed packed_at(void *p, const PackedLayout &l, bool zeros) {
+  char *c = static_cast<char *>(p);
+  return {reinterpret_cast<uint32_t *>(c), reinterpret_cast<_Float16 *>(c + l.scales), zeros ? reinterpret_cast<uint8_t *>(c + l.zeros) : nullptr};
+}
+
+int hip_result(const char *who) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? OKV_OK : report(OKV_EHIP, "%s: %s", who, hipGetErrorString(e));
+}
+
+template <int MF, int NT, int DEPTH>
+void launch(const Linear4Args &a, int group, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.n_out / 16 + NT - 1) / NT), (unsigned)((a.m + 16 * MF - 1) / (16 * MF))), block(64 * kWaves4);
+  if (a.zeros) {
+    if (group == 128) hipLaunchKernelGGL((linear4_kernel<MF, NT, 1, true, DEPTH>), grid, block, 0, stream, a);
+    else if (group == 64) hipLaunchKernelGGL((linear4_kernel<MF, NT, 2, true, DEPTH>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((linear4_kernel<MF, NT, 4, true, DEPTH>), grid, block, 0, stream, a);
+  } else {
+    if (group == 128) hipLaunchKernelGGL((linear4_kernel<MF, NT, 1, false, DEPTH>), grid, block, 0, stream, a);
+    else if (group == 64) hipLaunchKernelGGL((linear4_kernel<MF, NT, 2, false, DEPTH>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((linear4_kernel<MF, NT, 4, false, DEPTH>), grid, block, 0, stream, a);
+  }
+}
+
+}  // namespace
+
+}  // namespace okv
+
+using namespace okv;
+
+extern "C" {
+
+int64_t okv_linear4_packed_bytes(int32_t n_out, int32_t n_in, int32_t group, int32_t zeros) {
+  if (const char *why = shape_problem(n_out, n_in, group)) return report(OKV_EINVAL, "okv_linear4_packed_bytes: %s", why);
+  return layout_of(n_out, n_in, group, zeros != 0).bytes;
+}
+
+int okv_linear4_pack(void *dst, const void *codes, int32_t per_byte, const void *scales, const void *zeros, int32_t n_out, int32_t n_in, int32_t group,
+                     void *stream) {
+  if (const char *why = shape_problem(n_out, n_in, group)) return report(OKV_EINVAL, "okv_linear4_pack: %s", why);
+  if (!dst || !codes || !scales || !aligned16(dst)) return report(OKV_EINVAL, "okv_linear4_pack: NULL or misaligned pointer");
+  if (per_byte != 1 && per_byte != 2) return report(OKV_EINVAL, "okv_linear4_pack: per_byte must be 1 or 2");
+  const PackedLayout l = layout_of(n_out, n_in, group, zeros != nullptr);
+  const int64_t words = (int64_t)n_out / 16 * l.blocks * 256;
+  hipLaunchKernelGGL(pack4_kernel, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 1 << 14)), dim3(256), 0, static_cast<hipStream_t>(stream),
+                     packed_at(dst, l, zeros != nullptr), static_cast<const uint8_t *>(codes), per_byte, static_cast<const _Float16 *>(scales),
+                     static_cast<const uint8_t *>(zeros), n_out, n_in, group);
+  return hip_result("okv_linear4_pack");
+}
+
+int okv_linear4_quantize(void *dst, const void *src, int32_t n_out, int32_t n_in, int32_t group, int32_t zeros, void *stream) {
+  if (const char *why = shape_problem(n_out, n_in, group)) return report(OKV_EINVAL, "okv_linear4_quantize: %s", why);
+  if (!dst || !src || !aligned16(dst) || !aligned16(src)) return report(OKV_EINVAL, "okv_linear4_quantize: NULL or misaligned pointer");
+  const PackedLayout l = layout_of(n_out, n_in, group, zeros != 0);
+  const Packed to = packed_at(dst, l, zeros != 0);
+  const int64_t words = (int64_t)n_out / 16 * l.blocks * 256, groups = (int64_t)n_out * l.blocks * (kBlockIn / group);
+  hipLaunchKernelGGL(scales4_kernel, dim3((unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 14)), dim3(256), 0, static_cast<hipStream_t>(stream), to,
+                     static_cast<const _Float16 *>(src), n_out, n_in, group);
+  hipLaunchKernelGGL(codes4_kernel, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 1 << 14)), dim3(256), 0, static_cast<hipStream_t>(stream), to,
+                     static_cast<const _Float16 *>(src), n_out, n_in, group);
+  return hip_result("okv_linear4_quantize");
+}
+
+int64_t okv_linear4_workspace_bytes(int32_t m, int32_t n_out, int32_t n_in) {
+  if (const char *why = shape_problem(n_out, n_in, 32)) return report(OKV_EINVAL, "okv_linear4_workspace_bytes: %s", why);
+  if (m < 1 || m > OKV_LINEAR4_MAX_BATCH) return report(OKV_EINVAL, "okv_linear4_workspace_bytes: m must be in [1, %d]", OKV_LINEAR4_MAX_BATCH);
+  return 0;
+}
+
+int okv_linear4(const void *x, const void *packed, const void *bias, const void *residual, void *const *out, const int32_t *cols, int32_t n_seg, int32_t m,
+                int32_t n_out, int32_t n_in, int32_t group, int32_t zeros, int32_t relu, void *workspace, int64_t workspace_bytes, void *stream) {
+  (void)workspace, (void)workspace_bytes;
+  if (const char *why = shape_problem(n_out, n_in, group)) return report(OKV_EINVAL, "okv_linear4: %s", why);
+  if (m < 1 || m > OKV_LINEAR4_MAX_BATCH) return report(OKV_EINVAL, "okv_linear4: m must be in [1, %d]", OKV_LINEAR4_MAX_BATCH);
+  if (!x || !packed || !out) return report(OKV_EINVAL, "okv_linear4: NULL pointer");
+  if (!aligned16(x) || !aligned16(packed) || !aligned16(bias) || !aligned16(residual)) return report(OKV_EINVAL, "okv_linear4: misaligned pointer");
+  if (n_seg < 1 || n_seg > 3) return report(OKV_EINVAL, "okv_linear4: n_seg must be 1, 2 or 3");
+  if (residual && n_seg != 1) return report(OKV_EINVAL, "okv_linear4: a residual goes with one output tensor");
+  Linear4Args a;
+  int64_t end = 0;
+  for (int s = 0; s < 3; ++s) {
+    if (s < n_seg) {
+      const int64_t width = cols ? cols[s] : n_out / n_seg;
+      if (width < 16 || width % 16) return report(OKV_EINVAL, "okv_linear4: the runs of output features must be multiples of 16");
+      if (!out[s] || !aligned16(out[s])) return report(OKV_EINVAL, "okv_linear4: NULL or misaligned output");
+      end += width;
+    }
+    a.out[s] = static_cast<_Float16 *>(out[std::min(s, n_seg - 1)]);
+    a.end[s] = (int32_t)std::min<int64_t>(end, 0x7fffffff);
+  }
+  if (end != n_out) return report(OKV_EINVAL, "okv_linear4: the runs of output features must add up to n_out");
+  const PackedLayout l = layout_of(n_out, n_in, group, zeros != 0);
+  const Packed p = packed_at(const_cast<void *>(packed), l, zeros != 0);
+  a.x = static_cast<const _Float16 *>(x);
+  a.codes = reinterpret_cast<const u32x4 *>(p.codes), a.scales = p.scales, a.zeros = p.zeros;
+  a.bias = static_cast<const _Float16 *>(bias), a.residual = static_cast<const _Float16 *>(residual);
+  a.m = m, a.n_out = n_out, a.n_in = n_in, a.blocks = (int32_t)l.blocks, a.relu = relu != 0;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const int tiles = n_out / 16;
+  if (m <= 16) tiles >= 1024 ? launch<1, 4, 2>(a, group, st) : tiles >= 512 ? launch<1, 2, 2>(a, group, st) : launch<1, 1, 4>(a, group, st);
+  else if (m <= 32) tiles >= 1024 ? launch<2, 4, 1>(a, group, st) : tiles >= 512 ? launch<2, 2, 2>(a, group, st) : launch<2, 1, 2>(a, group, st);
+  else tiles >= 1024 ? launch<4, 4, 1>(a, group, st) : launch<4, 2, 1>(a, group, st);
+  return hip_result("okv_linear4");
+}
+
+}  // extern "C"
