@@ -91,7 +91,7 @@ class Cache8:
         for name, t in (("k", k), ("v", v)):
             if t.dtype != torch.float16 or t.device != self.device or tuple(t.shape) != shape or t.dim() not in (3, 4):
                 raise ValueError(f"{name} must be fp16 [layers][rows][{self.G}][{self.d}] (or one layer's) on {self.device}")
-            if t.stride(-1) != 1 or t.stride(-2) != self.d or t.stride() != k.stride():
+            if t.numel() and (t[..., 0, :, :].stride()[-2:] != (self.d, 1) or any(a != b for a, b, n in zip(t.stride(), k.stride(), k.shape) if n > 1)):
                 raise ValueError("the heads of a row must be contiguous, k and v laid out alike")
         self._seqs(seqs, batch)
         need("starts", starts, torch.int32, self.device, dims=1)

@@ -1,0 +1,311 @@
+"""The 8-bit KV cache against its definition in 64 bits.
+
+Codes, scales and what is read back are exact (bits).  Attention: weights go into the second product with 22 bits and scores are fp32 sums of d
+products whose magnitudes add up to some 8 sqrt(d) at most here, so an output vector is within d 2^-24 8 + a few 2^-22 of the definition: 7e-5, and
+2^-11 more where it is rounded to fp16.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache8 as oracle
+from paper_2504_11816_amd import binding
+from paper_2504_11816_amd.cache8 import Cache8
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TILE = 32
+
+
+def rows_of(rng, n, G, d):
+    return (rng.standard_normal((n, G, d)) * np.exp(0.5 * rng.standard_normal((G, d)))).astype(np.float16)
+
+
+def dev(x, dtype=None):
+    return torch.tensor(np.ascontiguousarray(x), dtype=dtype, device=DEV)
+
+
+def make(rng, lens, *, L=1, H=4, G=2, d=64, T=64, fmt="int8", fp32=True, spare=2, max_seqs=None):
+    """A cache whose sequences will have `lens` tokens: random pages, everything that is not stored yet poisoned."""
+    S, width = max_seqs or len(lens), max(1, max(-(-n // T) for n in lens)) + 1
+    n_pages = sum(-(-n // T) for n in lens) + spare
+    c = Cache8(n_layers=L, n_q_heads=H, n_kv_heads=G, head_dim=d, page_tokens=T, n_pages=n_pages, max_seqs=S, max_pages_per_seq=width, format=fmt,
+               out_dtype=torch.float32 if fp32 else torch.float16, device=DEV)
+    ids, table = list(rng.permutation(n_pages)), np.full((S, width), -1, np.int32)
+    for b, n in enumerate(lens):
+        for p in range(-(-n // T)):
+            table[b, p] = ids.pop()
+    c.table.copy_(dev(table))
+    c.codes.fill_(0xff)                                      # the E4M3 code of NaN
+    c.scales.fill_(float("nan"))
+    c.tails.fill_(float("nan"))
+    return c
+
+
+def store(c, parts_k, parts_v, lens, seqs=None):
+    starts = np.concatenate([[0], np.cumsum([p.shape[0] for p in parts_k])])
+    full = torch.zeros(c.max_seqs, dtype=torch.int32, device=DEV)
+    at = np.arange(len(lens)) if seqs is None else np.asarray(seqs)
+    full[torch.tensor(at, device=DEV, dtype=torch.long)] = dev(lens, torch.int32)
+    k, v = (dev(np.concatenate(p)[None].repeat(c.L, 0)) for p in (parts_k, parts_v))
+    c.store(k, v, dev(starts, torch.int32), full, None if seqs is None else dev(seqs, torch.int32))
+    return full
+
+
+def tile_bits(c, lens):
+    """The raw bits of everything that the sequences' tiles and tails hold."""
+    table, out = c.table.cpu().numpy(), []
+    codes, scales, tails = c.codes.cpu().numpy(), c.scales.cpu().numpy().view(np.uint32), c.tails.cpu().numpy().view(np.uint16)
+    tpp = c.T // TILE
+    for b, n in enumerate(lens):
+        for t in range(n // TILE):
+            page = table[b, t // tpp]
+            out += [codes[:, page, t % tpp], scales[:, page, t % tpp]]
+        out.append(tails[:, b, :, :, :n % TILE])
+    return out
+
+
+def equal(a, b):
+    return all(np.array_equal(x, y) for x, y in zip(a, b, strict=True))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("d,G,T", [(64, 1, 32), (64, 5, 64), (128, 2, 128), (128, 12, 32)])
+def test_store_and_load(fmt, d, G, T):
+    rng = np.random.default_rng(d + G)
+    lens = [1, 31, 32, 33, 64, 95, 200, 7]
+    c = make(rng, lens, L=2, H=G, G=G, d=d, T=T, fmt=fmt)
+    k, v = ([rows_of(rng, n, G, d) for n in lens] for _ in range(2))
+    after = store(c, k, v, lens)
+    starts = dev(np.concatenate([[0], np.cumsum(lens)]), torch.int32)
+    out = [torch.full((2, sum(lens), G, d), float("nan"), dtype=torch.float16, device=DEV) for _ in range(2)]
+    c.load(out[0], out[1], starts, after)
+    for got, rows in zip(out, (k, v)):
+        want = np.concatenate([oracle.held(r, fmt, r.shape[0] // TILE * TILE) for r in rows]).astype(np.float16)
+        for layer in got.cpu().numpy():
+            assert np.array_equal(layer, want)               # (values: a whole number has no -0)
+    # the documented layout, byte by byte
+    b, t = 6, 3
+    page = int(c.table[b, t * TILE // T])
+    raw = oracle.unpack(c.codes[1].cpu().numpy(), c.scales[1].cpu().numpy(), G=G, gg=binding.okv_kv_head_group(G, d), d=d, T=T, fmt=fmt, page=page, tile=t % (T // TILE))
+    for kv, rows in enumerate((k, v)):
+        assert np.array_equal(raw[kv], oracle.held(rows[b], fmt, 192)[t * TILE:(t + 1) * TILE])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_chunks_leave_the_same_bits(fmt):
+    """A prompt at once; in chunks that begin and end anywhere, of some of the sequences, in another order; the last rows by decode steps."""
+    rng = np.random.default_rng(7)
+    lens, G, d, T = [130, 97, 64, 33], 3, 64, 64
+    k, v = ([rows_of(rng, n, G, d) for n in lens] for _ in range(2))
+    whole = make(np.random.default_rng(1), lens, G=G, H=G, d=d, T=T, fmt=fmt)
+    store(whole, k, v, lens)
+    want = tile_bits(whole, lens)
+    chunks = make(np.random.default_rng(1), lens, G=G, H=G, d=d, T=T, fmt=fmt)
+    done = [0, 0, 0, 0]
+    for size in (1, 30, 2, 40, 5, 33, 64, 100):
+        todo = [b for b in (2, 0, 3, 1) if done[b] < lens[b]]
+        if not todo:
+            break
+        upto = [min(lens[b], done[b] + size) for b in todo]
+        store(chunks, [k[b][done[b]:u] for b, u in zip(todo, upto)], [v[b][done[b]:u] for b, u in zip(todo, upto)], upto, seqs=todo)
+        for b, u in zip(todo, upto):
+            done[b] = u
+    assert done == lens and equal(tile_bits(chunks, lens), want)
+    steps = make(np.random.default_rng(1), lens, G=G, H=G, d=d, T=T, fmt=fmt)
+    back = 35
+    store(steps, [x[:max(0, len(x) - back)] for x in k], [x[:max(0, len(x) - back)] for x in v], [max(0, n - back) for n in lens])
+    for i in range(back, 0, -1):
+        seqs = [b for b in range(4) if lens[b] >= i]
+        now = torch.zeros(4, dtype=torch.int32, device=DEV)
+        now[seqs] = dev([lens[b] - i + 1 for b in seqs], torch.int32)
+        out = torch.empty((1, len(seqs), G, d), device=DEV)
+        steps.step(torch.zeros((1, len(seqs), G, d), dtype=torch.float16, device=DEV), dev(np.stack([k[b][lens[b] - i] for b in seqs])[None]),
+                   dev(np.stack([v[b][lens[b] - i] for b in seqs])[None]), out, now, dev(seqs, torch.int32))
+    assert equal(tile_bits(steps, lens), want)
+
+
+def test_extreme_numbers():
+    """The largest and the smallest fp16 numbers, tiles of zeros, and numbers that are none: those make their tile NaN and no other."""
+    rng = np.random.default_rng(5)
+    k = rows_of(rng, 192, 2, 64)
+    k[0:32, 0] = 65504 * np.sign(k[0:32, 0])
+    k[32:64, 0] = (rng.integers(-2, 3, (32, 64)) * 2.0 ** -24).astype(np.float16)
+    k[64:96] = 0
+    k[100, 1, 3] = np.inf
+    k[130, 0, 0] = np.nan
+    for fmt in ("int8", "e4m3"):
+        c = make(rng, [192], G=2, H=2, d=64, fmt=fmt)
+        after = store(c, [k], [k], [192])
+        out = [torch.empty((1, 192, 2, 64), dtype=torch.float16, device=DEV) for _ in range(2)]
+        c.load(out[0], out[1], dev([0, 192], torch.int32), after)
+        with np.errstate(invalid="ignore"):
+            want = np.stack([np.concatenate([oracle.held(k[t:t + 32, g:g + 1], fmt, 32) if np.isfinite(k[t:t + 32, g]).all() else np.full((32, 1, 64), np.nan)
+                                             for t in range(0, 192, 32)])[:, 0] for g in range(2)], 1).astype(np.float16)
+        for x in out:
+            np.testing.assert_array_equal(x[0].cpu().numpy(), want)
+
+
+def check_step(lens, *, H, G, d, T=64, fmt="int8", fp32=True, seed=0, max_seqs=None, seqs=None, strided=False, scale_q=1.0):
+    """An appending step and one that appends nothing, against the definition."""
+    rng = np.random.default_rng(seed)
+    S = max_seqs or len(lens)
+    seqs = list(range(len(lens))) if seqs is None else seqs
+    by_row = [0] * S
+    for s, n in zip(seqs, lens):
+        by_row[s] = n
+    c = make(rng, by_row, H=H, G=G, d=d, T=T, fmt=fmt, fp32=fp32, max_seqs=S)
+    k, v = ([rows_of(rng, max(n, 1), G, d) for n in lens] for _ in range(2))
+    store(c, [x[:max(n - 1, 0)] for x, n in zip(k, lens)], [x[:max(n - 1, 0)] for x, n in zip(v, lens)], [max(n - 1, 0) for n in lens], seqs=seqs)
+    B = len(lens)
+    q = (scale_q * rng.standard_normal((B, H, d))).astype(np.float16)
+    kn, vn = (np.stack([x[max(n - 1, 0)] for x, n in zip(p, lens)]) for p in (k, v))
+    now = torch.zeros(S, dtype=torch.int32, device=DEV)
+    now[torch.tensor(seqs, device=DEV)] = dev(lens, torch.int32)
+    ids = dev(seqs, torch.int32)
+    out = torch.full((B, H, d), float("nan"), dtype=c.out_dtype, device=DEV)
+    if strided:                                              # q, k and v as one product leaves them
+        row = torch.full((B, (H + 2 * G) * d + 8), float("nan"), dtype=torch.float16, device=DEV)
+        tq, tk, tv = (row[:, a * d:b * d].unflatten(1, (-1, d)) for a, b in ((0, H), (H, H + G), (H + G, H + 2 * G)))
+        for t, x in ((tq, q), (tk, kn), (tv, vn)):
+            t.copy_(dev(x))
+    else:
+        tq, tk, tv = dev(q), dev(kn), dev(vn)
+    tol = 7e-5 + (0 if fp32 else 2.0 ** -11)
+    for appends in (True, False):
+        out.fill_(float("nan"))
+        c.begin(B, now, ids, appends=appends)
+        c.attend(0, tq, tk if appends else None, tv if appends else None, out)
+        got = out.double().cpu().numpy()
+        for b, n in enumerate(lens):
+            want = oracle.attend(q[b], k[b], v[b], n, fmt, appends)
+            if n == 0:
+                assert (got[b] == 0).all()
+                continue
+            err = np.linalg.norm(got[b] - want, axis=1) / np.linalg.norm(want, axis=1)
+            assert err.max() <= tol, (b, n, appends, err.max())
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("H,G,d", [(4, 4, 64), (1, 1, 128), (16, 1, 64), (15, 5, 128), (32, 2, 128), (20, 10, 64), (12, 12, 128)])
+def test_decode_against_the_definition(fmt, H, G, d):
+    check_step([1, 2, 31, 32, 33, 63, 64, 65, 200, 449], H=H, G=G, d=d, fmt=fmt, seed=H + d)
+
+
+@pytest.mark.parametrize("T", [32, 128, 1024])
+@pytest.mark.parametrize("fp32", [True, False])
+def test_page_sizes_and_output_types(T, fp32):
+    check_step([1025, 40, 5, 700], H=8, G=2, d=128, T=T, fp32=fp32, seed=T)
+
+
+def test_empty_sequences_and_rows_of_the_table():
+    check_step([0, 40, 0, 0, 65, 0], H=4, G=2, d=64, seed=3)
+    check_step([0, 0], H=4, G=2, d=64, seed=4)
+    check_step([70, 0, 33], H=4, G=2, d=64, seed=5, max_seqs=9, seqs=[7, 2, 0])
+
+
+def test_strided_rows():
+    check_step([70, 33, 64], H=6, G=2, d=64, strided=True, seed=6)
+    check_step([70, 33, 64], H=5, G=5, d=128, strided=True, seed=7, fp32=False)
+
+
+def test_scores_far_apart():
+    check_step([300, 64, 1000], H=8, G=4, d=128, scale_q=30.0, seed=8)
+
+
+@pytest.mark.parametrize("B", [65, 300])
+def test_many_short_sequences(B):
+    rng = np.random.default_rng(B)
+    check_step([int(n) for n in rng.integers(0, 90, B)], H=2, G=2, d=64, T=32, seed=B)
+
+
+@pytest.mark.parametrize("G,n", [(1, 9000), (8, 3000), (40, 800)])
+def test_long_sequences_are_cut(G, n):
+    check_step([n, 17, n // 2 + 1], H=2 * G, G=G, d=64, T=32, seed=G)
+
+
+def test_more_pages_than_lanes_and_buffers_beyond_4_gib():
+    """Two long sequences in the last pages of buffers of more than 2^32 bytes: page lists of more than 64 entries in 32-token pages."""
+    rng = np.random.default_rng(11)
+    G, d, T, n_pages = 8, 128, 32, 70000                     # 64 KiB a page: 4.6e9 bytes
+    lens = [4500, 2300]
+    c = Cache8(n_layers=1, n_q_heads=8, n_kv_heads=G, head_dim=d, page_tokens=T, n_pages=n_pages, max_seqs=2, max_pages_per_seq=150, out_dtype=torch.float32, device=DEV)
+    ids, table = list(n_pages - 1 - rng.permutation(300)), np.full((2, 150), -1, np.int32)
+    for b, n in enumerate(lens):
+        for p in range(-(-n // T)):
+            table[b, p] = ids.pop()
+    c.table.copy_(dev(table))
+    k, v = ([rows_of(rng, n, G, d) for n in lens] for _ in range(2))
+    store(c, [x[:-1] for x in k], [x[:-1] for x in v], [n - 1 for n in lens])
+    q, out = rng.standard_normal((1, 2, 8, d)).astype(np.float16), torch.empty((1, 2, 8, d), device=DEV)
+    c.step(dev(q), dev(np.stack([x[-1] for x in k])[None]), dev(np.stack([x[-1] for x in v])[None]), out, dev(lens, torch.int32))
+    for b, n in enumerate(lens):
+        want = oracle.attend(q[0, b], k[b], v[b], n, "int8", True)
+        err = np.linalg.norm(out[0, b].double().cpu().numpy() - want, axis=1) / np.linalg.norm(want, axis=1)
+        assert err.max() <= 7e-5
+
+
+def test_layers_in_one_call_are_the_layers_one_by_one():
+    rng = np.random.default_rng(12)
+    L, H, G, d, lens = 3, 8, 2, 128, [200, 64, 1, 95]
+    a, b = (make(np.random.default_rng(2), lens, L=L, H=H, G=G, d=d, fp32=False) for _ in range(2))
+    k, v = ([rows_of(rng, n - 1, G, d) for n in lens] for _ in range(2))
+    for c in (a, b):
+        store(c, k, v, [n - 1 for n in lens])
+    q, kn, vn = (dev(rng.standard_normal((L, 4, h, d)).astype(np.float16)) for h in (H, G, G))
+    now, oa, ob = dev(lens, torch.int32), torch.empty((L, 4, H, d), dtype=torch.float16, device=DEV), torch.empty((L, 4, H, d), dtype=torch.float16, device=DEV)
+    a.step(q, kn, vn, oa, now)
+    b.begin(4, now)
+    for layer in range(L):
+        b.attend(layer, q[layer], kn[layer], vn[layer], ob[layer])
+    assert torch.equal(oa, ob) and equal(tile_bits(a, lens), tile_bits(b, lens))
+
+
+def test_a_captured_step_and_another_stream():
+    """A graph that raises the lengths and steps, replayed with eager work between, against eager steps on another stream."""
+    rng = np.random.default_rng(13)
+    H, G, d, lens = 8, 2, 64, [60, 31, 5]
+    a, b = (make(np.random.default_rng(2), [n + 12 for n in lens], H=H, G=G, d=d) for _ in range(2))
+    k, v = ([rows_of(rng, n, G, d) for n in lens] for _ in range(2))
+    q, kn, vn = (dev(rng.standard_normal((1, 3, h, d)).astype(np.float16)) for h in (H, G, G))
+    outs, nows = [torch.zeros((1, 3, H, d), device=DEV) for _ in range(2)], [dev(lens, torch.int32) for _ in range(2)]
+    for c in (a, b):
+        store(c, k, v, lens)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        nows[0].add_(1)
+        a.step(q, kn, vn, outs[0], nows[0])
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for i in range(6):
+        graph.replay()
+        torch.randn(1 << 16, device=DEV).sum().item()
+        with torch.cuda.stream(other):
+            nows[1].add_(1)
+            b.step(q, kn, vn, outs[1], nows[1])
+        torch.cuda.synchronize()
+        assert torch.equal(nows[0], nows[1]) and torch.equal(outs[0], outs[1]), i
+    assert equal(tile_bits(a, [n + 6 for n in lens]), tile_bits(b, [n + 6 for n in lens]))
+
+
+def test_wrong_tensors_are_refused():
+    c = make(np.random.default_rng(0), [40], G=2, H=4, d=64, fp32=False)
+    q, k = torch.zeros((1, 1, 4, 64), dtype=torch.float16, device=DEV), torch.zeros((1, 1, 2, 64), dtype=torch.float16, device=DEV)
+    out, now = torch.zeros_like(q), dev([40], torch.int32)
+    for bad in (dict(q=q.float()), dict(q=q[:, :, :3]), dict(k_new=None), dict(k_new=k.cpu()), dict(out=out.float()), dict(lens=now.long()), dict(lens=now[:0]),
+                dict(seqs=now.long())):
+        args = dict(q=q, k_new=k, v_new=k, out=out, lens=now)
+        args.update(bad)
+        with pytest.raises(ValueError):
+            c.step(**args)
+    with pytest.raises(ValueError):
+        c.store(k.float(), k, dev([0, 1], torch.int32), now)
+    with pytest.raises(ValueError):
+        c.store(k, k, dev([0, 1], torch.int64), now)
+    with pytest.raises(ValueError):
+        c.attend(0, q[0].transpose(0, 1), None, None, out[0])
+    with pytest.raises(ValueError):
+        Cache8(n_layers=1, n_q_heads=4, n_kv_heads=2, head_dim=64, page_tokens=32, n_pages=4, max_seqs=1, max_pages_per_seq=4, format="int4", device=DEV)
+    with pytest.raises(binding.OkvError):
+        Cache8(n_layers=1, n_q_heads=4, n_kv_heads=2, head_dim=80, page_tokens=32, n_pages=4, max_seqs=1, max_pages_per_seq=4, device=DEV)

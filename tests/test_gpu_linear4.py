@@ -1,0 +1,167 @@
+"""Products with 4-bit weights against their definition in 64 bits.
+
+fp32 sums of n exact products, in any order, are within n 2^-24 of the sum of their magnitudes; a group's scale, the bias and the residual add a few
+roundings more, the result is rounded to fp16 once: |error| <= 2^-11 |y| + (n + 8) 2^-24 (sum |x W| + |bias| + |residual|) + 2^-25."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2504_11816_amd.linear4 import Linear4
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def dev(x):
+    return None if x is None else torch.tensor(x, device=DEV)
+
+
+def weights(rng, n_out, n_in, group, zeros):
+    codes = rng.integers(0, 16, (n_out, n_in)).astype(np.uint8)
+    scales = ((0.5 + rng.random((n_out, n_in // group))) / n_in ** 0.5).astype(np.float16)
+    return codes, scales, rng.integers(0, 16, scales.shape).astype(np.uint8) if zeros else None
+
+
+def expand(codes, scales, zeros):
+    g = codes.shape[1] // scales.shape[1]
+    z = 8.0 if zeros is None else zeros.astype(np.float64).repeat(g, 1)
+    return (codes.astype(np.float64) - z) * scales.astype(np.float64).repeat(g, 1)
+
+
+def check(got, x, w, bias, residual, relu):
+    x = x.astype(np.float64)
+    y, size = x @ w.T, np.abs(x) @ np.abs(w).T
+    if bias is not None:
+        y, size = y + bias.astype(np.float64), size + np.abs(bias.astype(np.float64))
+    if relu:
+        y = np.maximum(y, 0)
+    if residual is not None:
+        y, size = y + residual.astype(np.float64), size + np.abs(residual.astype(np.float64))
+    err = np.abs(got.astype(np.float64) - y)
+    assert (err <= 2.0 ** -11 * np.abs(y) + (w.shape[1] + 8) * 2.0 ** -24 * size + 2.0 ** -25).all(), err.max()
+
+
+def product(m, n_out, n_in, group, zeros, seed=0, bias=True, residual=False, relu=False, alias=False, segments=None, pack=1):
+    rng = np.random.default_rng(seed + m + n_out + n_in)
+    codes, scales, zs = weights(rng, n_out, n_in, group, zeros)
+    b = rng.standard_normal(n_out).astype(np.float16) if bias else None
+    x, r = rng.standard_normal((m, n_in)).astype(np.float16), rng.standard_normal((m, n_out)).astype(np.float16) if residual else None
+    stored = codes if pack == 1 else (codes[:, ::2] | codes[:, 1::2] << 4)
+    w = Linear4(dev(stored), dev(scales), dev(zs), dev(b), n_in=n_in)
+    widths = segments or [n_out]
+    rt = dev(r)
+    # a margin of rows that must stay as they are
+    full = [torch.full((m + 3, n), 7.0, dtype=torch.float16, device=DEV) for n in widths]
+    out = [f[:m] for f in full]
+    if alias:
+        out[0].copy_(rt)
+        rt = out[0]
+    w(dev(x), out if segments else out[0], relu=relu, residual=rt)
+    first = [o.clone() for o in out]
+    check(torch.cat(out, 1).cpu().numpy(), x, expand(codes, scales, zs), b, r, relu)
+    assert all((f[m:] == 7).all() for f in full)
+    if not alias:
+        w(dev(x), out if segments else out[0], relu=relu, residual=rt)       # the same bits every time
+        assert all(torch.equal(a, b) for a, b in zip(first, out))
+
+
+@pytest.mark.parametrize("group,zeros", [(32, False), (32, True), (64, False), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("m", [1, 2, 5, 16, 17, 31, 33, 48, 64, 65, 130, 256])
+def test_rows_and_groups(m, group, zeros):
+    product(m, 144, 640, group, zeros, residual=m % 2 == 0, relu=m % 3 == 0)
+
+
+@pytest.mark.parametrize("n_out", [16, 32, 48, 272, 4096, 8208, 12288, 16400])
+@pytest.mark.parametrize("m", [1, 20, 40, 100])
+def test_features(m, n_out):
+    product(m, n_out, 256, 64, True, relu=True, residual=True)
+
+
+@pytest.mark.parametrize("n_in", [32, 64, 96, 128, 160, 1024, 1056, 1152, 2080, 4096 + 96, 8192, 20480])
+@pytest.mark.parametrize("m", [1, 16, 24, 64])
+def test_inputs(m, n_in):
+    product(m, 80, n_in, 32, n_in % 64 == 0)
+
+
+@pytest.mark.parametrize("m", [1, 3, 33, 70])
+def test_output_tensors_and_packed_codes(m):
+    product(m, 512 + 2 * 64, 512, 64, False, segments=[512, 64, 64])
+    product(m, 96, 512, 64, True, segments=[32, 64])
+    product(m, 96, 512, 64, True, bias=False, pack=2)
+    product(m, 96, 512, 64, False, residual=True, alias=True, relu=True)
+
+
+def test_codes_at_their_ends():
+    """All codes and zero points: code - zero from -15 to 15, products that are whole numbers, exactly."""
+    n_in = 128
+    codes = np.tile(np.arange(16, dtype=np.uint8), (256, n_in // 16))
+    zeros = np.repeat(np.arange(16, dtype=np.uint8), 16)[:, None]
+    scales = np.ones((256, 1), np.float16)
+    x = np.zeros((n_in, n_in), np.float16)
+    x[np.arange(n_in), np.arange(n_in)] = 1
+    out = torch.empty((n_in, 256), dtype=torch.float16, device=DEV)
+    Linear4(dev(codes), dev(scales), dev(zeros))(dev(x), out)
+    assert np.array_equal(out.cpu().numpy(), expand(codes, scales, zeros).T)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_quantised_weights(group, zeros):
+    """Against the header's formulas: codes are seen through products with unit vectors."""
+    rng = np.random.default_rng(group)
+    n_out, n_in = 48, 384
+    w = (rng.standard_normal((n_out, n_in)) * 0.05).astype(np.float16)
+    w[3, :group] = 0
+    w[5, :group] = np.abs(w[5, :group])
+    w[6, :group] = 1e-7
+    t = w.astype(np.float32).reshape(n_out, -1, group)
+    lo, hi = np.minimum(t.min(-1), 0), np.maximum(t.max(-1), 0)
+    s = (((hi - lo) / np.float32(15)) if zeros else np.maximum(hi, -lo) / np.float32(7)).astype(np.float16).astype(np.float32)
+    safe = np.where(s > 0, s, 1)
+    z = np.where(s > 0, np.minimum(np.rint(-lo / safe), 15), 8) if zeros else np.full_like(s, 8)
+    code = np.clip(np.rint(np.where(s[..., None] > 0, t / safe[..., None], 0)) + z[..., None], 0, 15)
+    want = ((code - z[..., None]).astype(np.float64) * s[..., None]).reshape(n_out, n_in)
+    q = Linear4.quantize(dev(w), group=group, zeros=zeros)
+    x = np.eye(n_in, dtype=np.float16)
+    out = torch.empty((n_in, n_out), dtype=torch.float16, device=DEV)
+    q(dev(x), out)
+    assert np.array_equal(out.cpu().numpy(), want.T.astype(np.float16))
+    assert np.abs(want - w).max() <= (s.max() / 2 + 1e-6) * 1.01 + np.abs(w).max() * 2.0 ** -10
+
+
+def test_another_stream_and_a_graph():
+    rng = np.random.default_rng(0)
+    codes, scales, zs = weights(rng, 512, 1024, 128, True)
+    w = Linear4(dev(codes), dev(scales), dev(zs))
+    x, outs = torch.randn((40, 1024), dtype=torch.float16, device=DEV), [torch.zeros((40, 512), dtype=torch.float16, device=DEV) for _ in range(2)]
+    w(x, outs[1])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w(x, outs[0])
+    other = torch.cuda.Stream()
+    for i in range(4):
+        x.normal_()
+        graph.replay()
+        torch.randn(1 << 14, device=DEV).sum().item()
+        other.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(other):
+            w(x, outs[1])
+        torch.cuda.synchronize()
+        assert torch.equal(*outs), i
+
+
+def test_wrong_tensors_are_refused():
+    rng = np.random.default_rng(0)
+    codes, scales, zs = (dev(t) for t in weights(rng, 32, 128, 32, True))
+    w = Linear4(codes, scales, zs)
+    x, out = torch.zeros((2, 128), dtype=torch.float16, device=DEV), torch.zeros((2, 32), dtype=torch.float16, device=DEV)
+    for bad in (dict(x=x.float()), dict(x=x[:, :64]), dict(out=out[:1]), dict(residual=out[:, :16]), dict(out=[out] * 4), dict(x=x.cpu()), dict(out=out.t().contiguous().t())):
+        with pytest.raises(ValueError):
+            w(**{**dict(x=x, out=out), **bad})
+    for bad in ((codes.int(), scales, zs), (codes, scales.float(), zs), (codes, scales[:, :3], zs), (codes, scales, zs[:, :2]), (codes[:, :32], scales, zs)):
+        with pytest.raises((ValueError, RuntimeError)):
+            Linear4(bad[0], bad[1], bad[2], n_in=128)
+    with pytest.raises(RuntimeError):                        # an OkvError: widths that do not add up
+        w(x, [out[:, :16].contiguous()])
+    assert w(x[:0], out[:0]) is not None

@@ -1,0 +1,296 @@
+"""Pages of a cache against a model on plain lists: integers and moved bits are equal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as oracle
+from paper_2504_11816_amd import binding
+from paper_2504_11816_amd.cache8 import Cache8
+from paper_2504_11816_amd.pages import PageArray, Pages, RowArray
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def ids(x):
+    return torch.tensor(list(x), dtype=torch.int32, device=DEV)
+
+
+class Pair:
+    """A cache on the GPU and the model of it: two page arrays (one of 16-byte units, one whose units are 4 bytes) and a row array."""
+
+    def __init__(self, n_pages=40, T=16, S=8, width=9, L=2, unit=4, rows=8, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        self.T, self.unit, self.n_rows = T, unit, rows
+        self.a = torch.randint(0, 1 << 30, (L, n_pages, T // unit, 8), generator=g, dtype=torch.int32).to(DEV)
+        self.b = torch.randint(0, 1 << 30, (L, n_pages, T // unit), generator=g, dtype=torch.int32).to(DEV)
+        self.r = torch.randint(0, 1 << 30, (L, S, 3, rows, 4), generator=g, dtype=torch.int32).to(DEV)
+        self.table = torch.full((S, width), -1, dtype=torch.int32, device=DEV)
+        self.lens, self.refs = (torch.zeros(n, dtype=torch.int32, device=DEV) for n in (S, n_pages))
+        self.pages = Pages(table=self.table, lens=self.lens, refs=self.refs, page_tokens=T,
+                           arrays=[PageArray(self.a, unit), PageArray(self.b, unit, whole_units=True)], rows=[RowArray(self.r, 3, rows)])
+        self.model = oracle.Model(n_pages, T, S, width)
+        self.want = [x.cpu().clone() for x in (self.a, self.b, self.r)]
+
+    def do(self, name, *args):
+        if name == "extend":
+            self.pages.extend(*[ids(x) for x in args])
+            self.model.extend(*args)
+        elif name == "free":
+            self.pages.free(ids(args[0]))
+            self.model.free(args[0])
+        elif name == "fork":
+            before = list(self.model.lens)
+            self.pages.fork(*[ids(x) for x in args])
+            status = self.model.status
+            copies = self.model.fork(*args)
+            for a, b, n in copies:
+                whole = n // self.unit
+                self.want[0][:, b, :-(-n // self.unit)] = self.want[0][:, a, :-(-n // self.unit)]
+                self.want[1][:, b, :whole] = self.want[1][:, a, :whole]
+            if self.model.status == status:
+                for a, b in zip(*args):
+                    if before[a]:
+                        n = before[a] % self.n_rows
+                        self.want[2][:, b, :, :n] = self.want[2][:, a, :, :n]
+        else:
+            self.pages.compact()
+            moves = self.model.compact()
+            for a, b in moves:
+                for x in self.want[:2]:
+                    x[:, b] = x[:, a]
+            assert self.pages.status.tolist()[1:3] == [sum(r > 0 for r in self.model.refs), len(moves)]
+        self.same(name)
+
+    def same(self, what=""):
+        assert self.table.tolist() == self.model.table, what
+        assert self.lens.tolist() == self.model.lens, what
+        assert self.refs.tolist() == self.model.refs, what
+        assert self.pages.status.tolist()[0] == self.model.status, what
+        for got, want in zip((self.a, self.b, self.r), self.want):
+            assert torch.equal(got.cpu(), want), what
+
+
+def test_a_life_of_sequences():
+    p = Pair()
+    p.do("extend", [0, 1, 2], [37, 16, 1])
+    p.do("fork", [0, 1, 0], [3, 4, 5])
+    p.do("extend", [3, 0, 4, 5], [20, 1, 40, 11])
+    p.do("free", [1, 0])
+    p.do("fork", [5, 3], [0, 1])
+    p.do("compact")
+    p.do("extend", [6], [130])
+    p.do("free", [3, 3, 99, -1])                             # twice the same; rows that there are not
+    p.do("compact")
+    p.do("compact")
+    p.do("free", list(range(8)))
+    assert p.refs.sum() == 0
+    p.pages.check()
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_lives(seed):
+    rng = np.random.default_rng(seed)
+    n_pages, T, S, width = [(40, 16, 8, 9), (200, 4, 30, 12), (33, 64, 6, 4), (3000, 8, 60, 50), (9000, 16, 100, 80), (64, 1024, 5, 2)][seed]
+    p = Pair(n_pages=n_pages, T=T, S=S, width=width, L=1 + seed % 3, unit=4, rows=4 << seed % 3, seed=seed)
+    for step in range(40):
+        empty, full = [s for s in range(S) if p.model.lens[s] == 0], [s for s in range(S) if p.model.lens[s]]
+        what = rng.choice(["extend", "extend", "fork", "free", "compact"])
+        if what == "extend":
+            some = [int(x) for x in rng.permutation(S)[:rng.integers(1, S)]]
+            p.do("extend", some, [int(x) for x in rng.integers(0, width * T // 3 + 2, len(some))])
+        elif what == "fork" and empty and full:
+            n = int(rng.integers(1, len(empty) + 1))
+            p.do("fork", [int(rng.choice(full)) for _ in range(n)], [int(x) for x in rng.permutation(empty)[:n]])
+        elif what == "free" and full:
+            p.do("free", [int(x) for x in rng.permutation(full)[:rng.integers(1, len(full) + 1)]])
+        else:
+            p.do("compact")
+        if p.model.status:
+            with pytest.raises(binding.OkvError):
+                p.pages.check()
+            p.model.status = 0
+
+
+def test_what_cannot_be_done_changes_nothing():
+    p = Pair(n_pages=6, T=16, S=4, width=5)
+    p.do("extend", [0], [40])
+    p.do("extend", [1, 2], [32, 17])                         # four pages, three are free
+    assert p.model.status == binding.OKV_ENOSPC
+    with pytest.raises(binding.OkvError) as e:
+        p.pages.check()
+    assert e.value.code == binding.OKV_ENOSPC
+    p.model.status = 0
+    p.do("extend", [0], [41])                                # a page more than a row of the table
+    p.pages.status.zero_()
+    p.model.status = 0
+    p.do("extend", [1, 2], [32, 16])                         # the last pages
+    p.do("fork", [0, 1], [3, 3 - 3])                         # 0 is not empty
+    assert p.model.status == binding.OKV_ESTATE
+    p.pages.status.zero_()
+    p.model.status = 0
+    p.do("fork", [0], [3])                                   # no page for the last one
+    assert p.model.status == binding.OKV_ENOSPC
+    p.pages.status.zero_()
+    p.model.status = 0
+    p.do("fork", [1], [3])                                   # nothing to copy: no page is needed
+    assert p.model.status == 0
+    p.do("fork", [0], [9])                                   # a row that there is not
+    assert p.model.status == binding.OKV_ESTATE
+
+
+def test_forks_of_empty_sequences():
+    p = Pair()
+    p.do("extend", [0], [20])
+    p.do("fork", [1, 0, 2], [2, 1, 3])                       # 1 and 2 are empty as the call begins
+    assert p.lens.tolist()[:4] == [20, 20, 0, 0]
+
+
+def test_copies_of_pages():
+    p = Pair()
+    to = [PageArray(torch.zeros_like(x[:, :10])) for x in (p.a, p.b)]
+    p.pages.copy(ids([3, 39, 7]), ids([9, 0, 4]), to=to)
+    for t, x in zip(to, (p.a, p.b)):
+        want = torch.zeros_like(t.tensor)
+        want[:, [9, 0, 4]] = x[:, [3, 39, 7]]
+        assert torch.equal(t.tensor, want)
+    p.pages.copy(ids([3, 40, -1, 5, 6]), ids([30, 1, 2, 10, -4]), to=to)      # ids that there are not are passed over
+    assert torch.equal(to[0].tensor, torch.zeros_like(to[0].tensor).index_copy_(1, torch.tensor([9, 0, 4], device=DEV), p.a[:, [3, 39, 7]]))
+    p.pages.copy(ids([1, 2]), ids([11, 12]))                 # within the pool
+    for x in p.want[:2]:
+        x[:, [11, 12]] = x[:, [1, 2]]
+    p.same()
+    assert p.pages.copy(ids([]), ids([]), to=to) is None
+
+
+def test_pages_of_odd_sizes():
+    """Pages that end inside a workgroup's piece, moved by 4 bytes and by 16; a copy keeps to the units that hold tokens."""
+    for words, T in ((2052, 4), (8192 + 4, 2), (12 * 1024, 1), (99, 1)):
+        x = torch.randint(0, 1 << 30, (2, 5, T, words), dtype=torch.int32).to(DEV)
+        want = x.clone()
+        table, lens, refs = torch.full((2, 2), -1, dtype=torch.int32, device=DEV), ids([0, 0]), ids([0] * 5)
+        p = Pages(table=table, lens=lens, refs=refs, page_tokens=T, arrays=[PageArray(x, 1)])
+        p.extend(ids([0]), ids([T + (T > 1)]))
+        p.fork(ids([0]), ids([1]))
+        if T > 1:
+            want[:, 2, :1] = want[:, 1, :1]
+        assert torch.equal(x, want)
+        p.copy(ids([1, 0]), ids([4, 3]))
+        want[:, [4, 3]] = want[:, [1, 0]]
+        assert torch.equal(x, want)
+
+
+def test_a_forked_cache_decodes_as_a_copy_would():
+    """Forks of a quantised cache go their own ways: every sequence gives what an unshared cache of its own tokens gives, before and after compaction."""
+    rng = np.random.default_rng(3)
+    L, H, G, d, T = 2, 8, 2, 64, 64
+
+    def cache():
+        return Cache8(n_layers=L, n_q_heads=H, n_kv_heads=G, head_dim=d, page_tokens=T, n_pages=40, max_seqs=6, max_pages_per_seq=6, out_dtype=torch.float32, device=DEV)
+
+    c, lens = cache(), [150, 95]
+    prompt = [torch.randn((L, n, G, d), dtype=torch.float16, device=DEV) for n in lens]
+    c.pages.extend(ids([4]), ids([200]))                     # pages of a sequence that goes
+    c.pages.extend(ids([0, 1]), ids(lens))
+    c.store(torch.cat(prompt, 1), torch.cat(prompt, 1), ids([0, 150, 245]), c.lens, ids([0, 1]))
+    c.pages.free(ids([4]))
+    c.pages.fork(ids([0, 0, 1]), ids([2, 3, 5]))
+    live, tokens = ids([0, 1, 2, 3, 5]), {0: [prompt[0]], 1: [prompt[1]], 2: [prompt[0]], 3: [prompt[0]], 5: [prompt[1]]}
+    for step in range(40):
+        if step == 20:
+            c.pages.compact()
+        q, k = (torch.tensor(rng.standard_normal((L, 5, h, d)), dtype=torch.float16, device=DEV) for h in (H, G))
+        out = torch.empty((L, 5, H, d), device=DEV)
+        c.pages.extend(live)
+        c.step(q, k, k, out, c.lens, live)
+        for i, s in enumerate(live.tolist()):
+            tokens[s].append(k[:, i:i + 1])
+    c.pages.check()
+    assert c.lens.tolist() == [190, 135, 190, 190, 0, 135]
+    for i, s in enumerate(live.tolist()):
+        own, rows = cache(), torch.cat(tokens[s], 1)
+        own.pages.extend(ids([0]), ids([rows.shape[1] - 1]))
+        own.store(rows[:, :-1].contiguous(), rows[:, :-1].contiguous(), ids([0, rows.shape[1] - 1]), own.lens)
+        own.pages.extend(ids([0]))
+        alone = torch.empty((L, 1, H, d), device=DEV)
+        own.step(q[:, i:i + 1].contiguous(), rows[:, -1:].contiguous(), rows[:, -1:].contiguous(), alone, own.lens)
+        # the same numbers, cut among wavefronts in another way: the join's rounding
+        torch.testing.assert_close(out[:, i], alone[:, 0], rtol=0, atol=2e-6)
+
+
+def test_a_forked_fp16_pool_decodes_as_a_copy_would():
+    """Pages that sequences share under okv_decode_attn_static, whose tables are on the GPU as well."""
+    H, G, d, T, n = 8, 4, 64, 16, 70
+    c = binding.OkvConfig
+    pool = torch.randn((1, 30, 2 * G * T * d), dtype=torch.float16, device=DEV)
+    table, lens, refs = torch.full((3, 8), -1, dtype=torch.int32, device=DEV), ids([0, 0, 0]), ids([0] * 30)
+    p = Pages(table=table, lens=lens, refs=refs, page_tokens=T, arrays=[PageArray(pool, unit_tokens=16)])
+    p.extend(ids([1]), ids([n]))
+    p.fork(ids([1, 1]), ids([0, 2]))
+    assert c is not None and refs.tolist().count(3) == 4
+    own = torch.zeros_like(pool)                             # the same sequences without sharing
+    own_table = torch.arange(24, dtype=torch.int32, device=DEV).view(3, 8)
+    for s in range(3):
+        for i, page in enumerate(table[s].tolist()):
+            if page >= 0:
+                own[:, 8 * s + i] = pool[:, page]
+    q = torch.randn((3, H, d), dtype=torch.float16, device=DEV)
+    for _ in range(20):
+        p.extend(ids([0, 1, 2]))
+        k, v = (torch.randn((3, G, d), dtype=torch.float16, device=DEV) for _ in range(2))
+        outs = [torch.empty((3, H, d), dtype=torch.float16, device=DEV) for _ in range(2)]
+        for x, t, o in ((pool, table, outs[0]), (own, own_table, outs[1])):
+            binding.okv_decode_attn_static(n_q_heads=H, n_kv_heads=G, head_dim=d, block_tokens=T, max_blocks_per_seq=8, max_ctx=0, out_dtype=0, B=3, pool=x[0],
+                                           block_table=t, ctx_lens=lens, q=q, out=o, k_new=k, v_new=v, stream=torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(*outs)
+    p.check()
+
+
+def test_captured_calls():
+    """Extend, fork, free and compact in a graph, replayed with eager work between, against the model."""
+    p = Pair(n_pages=60)
+    p.do("extend", [0, 1], [37, 50])
+    p.do("fork", [0], [2])                                   # (loads the kernels)
+    p.do("free", [2])
+    p.do("compact")
+    one, src, dst, gone, both = ids([0]), ids([0, 1]), ids([2, 3]), ids([2, 3]), ids([0, 1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.pages.extend(both)
+        p.pages.fork(src, dst)
+        p.pages.free(one)
+        p.pages.fork(ids_of := dst[:1], one)
+        p.pages.free(gone)
+        p.pages.compact()
+    assert ids_of is not None
+    for i in range(5):
+        graph.replay()
+        torch.randn(1 << 14, device=DEV).sum().item()
+        for name, *args in (("extend", [0, 1], [1, 1]), ("fork", [0, 1], [2, 3]), ("free", [0]), ("fork", [2], [0]), ("free", [2, 3])):
+            before = list(p.model.lens)
+            copies = getattr(p.model, name)(*args)
+            if name == "fork":
+                for a, b, n in copies:
+                    p.want[0][:, b, :-(-n // 4)] = p.want[0][:, a, :-(-n // 4)]
+                    p.want[1][:, b, :n // 4] = p.want[1][:, a, :n // 4]
+                for a, b in zip(*args):
+                    p.want[2][:, b, :, :before[a] % 8] = p.want[2][:, a, :, :before[a] % 8]
+        for a, b in p.model.compact():
+            for x in p.want[:2]:
+                x[:, b] = x[:, a]
+        p.same(i)
+
+
+def test_wrong_tensors_are_refused():
+    p = Pair()
+    for bad in (torch.zeros(2, device=DEV), torch.zeros(2, dtype=torch.int32), ids([1, 2, 3, 4])[::2], ids([1, 2]).view(1, 2)):
+        with pytest.raises(ValueError):
+            p.pages.free(bad)
+    with pytest.raises(ValueError):
+        p.pages.fork(ids([1, 2]), ids([3]))
+    with pytest.raises(ValueError):
+        p.pages.copy(ids([1]), ids([2]), to=[PageArray(p.a, 4)])
+    with pytest.raises(ValueError):
+        Pages(table=p.table, lens=p.lens, refs=p.refs, page_tokens=16, arrays=[PageArray(p.a[:, :20].contiguous(), 4)])
+    with pytest.raises(binding.OkvError):
+        Pages(table=p.table, lens=p.lens, refs=p.refs, page_tokens=24, arrays=[PageArray(p.a, 4)]).compact()
