@@ -25,8 +25,9 @@ extern "C" {
 /* Bytes of a packed matrix: n_out a multiple of 16, n_in a multiple of 32 and of group, group 32, 64 or 128.
  * Codes first: blocks of 16 features x 128 inputs (the last block's inputs padded), as the 64 x 16 bytes that a
  * wavefront loads with one instruction: 32-bit word j of lane l holds inputs 32 j + 8 (l / 16) .. + 7 of feature l % 16, input 2 p
- * of them in bits 4 p .. 4 p + 3 and input 2 p + 1 in bits 16 + 4 p .. 19 + 4 p.  Then the scales,
- * [n_out / 16][groups][16] fp16 (groups of the padded inputs), and, with zeros, the zeros in the same order, a byte each. */
+ * of them in bits 4 p .. 4 p + 3 and input 2 p + 1 in bits 16 + 4 p .. 19 + 4 p.  Then the scales, fp16
+ * [n_out / 16][blocks][4][128 / group][4] (feature 4 i + j of the 16 at [..][i][..][j]), and, with zeros, the zeros, bytes
+ * [n_out / 16][blocks][16][128 / group]. */
 int64_t okv_linear4_packed_bytes(int32_t n_out, int32_t n_in, int32_t group, int32_t zeros);
 
 /* Packs a matrix that is quantised already.

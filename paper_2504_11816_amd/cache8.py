@@ -21,10 +21,6 @@ FORMATS = {"int8": 0, "e4m3": 1}
 TILE = 32
 
 
-def _stream():
-    return torch.cuda.current_stream().cuda_stream
-
-
 def _address(t):
     return 0 if t is None else t.data_ptr()
 
@@ -99,7 +95,7 @@ class Cache8:
         if lens.numel() < (self.max_seqs if seqs is not None else batch):
             raise ValueError("lens has an entry per row of the table (per sequence where seqs is None)")
         binding._check(fn(self.ref, layer, n_layers, batch, _address(seqs), starts.data_ptr(), lens.data_ptr(), k.shape[-3], k.data_ptr(), v.data_ptr(),
-                          k.stride(-3) if k.shape[-3] > 1 else self.G * self.d, k.stride(0) if n_layers > 1 else 0, _stream()))
+                          k.stride(-3) if k.shape[-3] > 1 else self.G * self.d, k.stride(0) if n_layers > 1 else 0, binding.current_stream(self.device)))
 
     def _seqs(self, seqs, batch):
         if seqs is not None:
@@ -121,7 +117,7 @@ class Cache8:
             raise ValueError("lens must be int32 with an entry per row of the table (per sequence where seqs is None)")
         self._seqs(seqs, batch)
         s = self._step
-        s.batch, s.appends, s.seqs, s.lens, s.stream = batch, appends, _address(seqs), lens.data_ptr(), _stream()
+        s.batch, s.appends, s.seqs, s.lens, s.stream = batch, appends, _address(seqs), lens.data_ptr(), binding.current_stream(self.device)
 
     def begin(self, batch, lens, seqs=None, appends=True):
         """Describes a step whose layers come one by one (attend)."""

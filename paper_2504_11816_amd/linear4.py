@@ -13,6 +13,9 @@ import torch
 from . import binding
 
 
+_One = ctypes.c_void_p * 1
+
+
 class Linear4:
     """W[n][k] = (codes[n][k] - zeros[n][k / group]) * scales[n][k / group], packed for the product kernels.
 
@@ -39,9 +42,8 @@ class Linear4:
     def _shape(self, n_out, n_in, group, zeros, device):
         self.n_out, self.n_in, self.group, self.zeros, self.device = n_out, n_in, group, int(zeros), device
 
-    @staticmethod
-    def _stream():
-        return torch.cuda.current_stream().cuda_stream
+    def _stream(self):
+        return binding.current_stream(self.device)
 
     def _allocate(self, bias):
         n = int(binding.lib().okv_linear4_packed_bytes(self.n_out, self.n_in, self.group, self.zeros))
@@ -50,8 +52,8 @@ class Linear4:
             raise ValueError(f"bias must be a contiguous fp16 vector of {self.n_out} on {self.device}")
         self.bias = bias
         self.packed = torch.empty(n, dtype=torch.uint8, device=self.device)
-        self.workspace = None
-        self._call = binding.lib().okv_linear4
+        self.workspace, self._workspace_bytes, self._wants = None, 0, {}
+        self._call, self._packed_at, self._bias_at = binding.lib().okv_linear4, self.packed.data_ptr(), bias.data_ptr() if bias is not None else None
 
     @classmethod
     def quantize(cls, weight, group=128, zeros=False, bias=None):
@@ -65,25 +67,42 @@ class Linear4:
         binding._check(binding.lib().okv_linear4_quantize(w.packed.data_ptr(), weight.data_ptr(), w.n_out, w.n_in, group, w.zeros, w._stream()))
         return w
 
+    def _bad(self, what, t, m, width):
+        raise ValueError(f"{what} must be a contiguous fp16 matrix [{m}][{width}] on {self.device}, it is {t.dtype} {list(t.shape)} on {t.device}")
+
     def __call__(self, x, out, relu=False, residual=None):
         """out = act(x W^T + bias) + residual: x fp16 [m][n_in], out fp16 [m][n_out] or a list of up to three tensors that share the
         output features, in order.  Products of one Linear4 that may run at the same time need copies of it (they share its workspace)."""
-        outs = out if isinstance(out, (list, tuple)) else (out,)
-        m, n = x.shape[0], len(outs)
-        if not 1 <= n <= 3:
-            raise ValueError("one to three output tensors")
-        for t, width in ((x, self.n_in), *((o, None) for o in outs), *(((residual, self.n_out),) if residual is not None else ())):
-            if t.dtype != torch.float16 or t.dim() != 2 or t.shape[0] != m or (width is not None and t.shape[1] != width) or not t.is_contiguous() or t.device != self.device:
-                raise ValueError(f"x, out and residual must be contiguous fp16 matrices of {m} rows on {self.device}, of the layer's widths")
+        # A call is 5 us of host time, with kernels of as little: checks are written out, and what depends on the shape alone is kept.
+        m, half, device = x.shape[0], torch.float16, self.device
+        if x.dtype is not half or x.shape != (m, self.n_in) or not x.is_contiguous() or x.device != device:
+            self._bad("x", x, m, self.n_in)
+        if type(out) in (list, tuple):
+            n = len(out)
+            if not 1 <= n <= 3:
+                raise ValueError("one to three output tensors")
+            for o in out:
+                if o.dtype is not half or o.dim() != 2 or o.shape[0] != m or not o.is_contiguous() or o.device != device:
+                    self._bad("out", o, m, "width")
+            arr, cols = (ctypes.c_void_p * n)(*[o.data_ptr() for o in out]), (ctypes.c_int32 * n)(*[o.shape[1] for o in out])
+        else:
+            n, cols = 1, None
+            if out.dtype is not half or out.shape != (m, self.n_out) or not out.is_contiguous() or out.device != device:
+                self._bad("out", out, m, self.n_out)
+            arr = _One(out.data_ptr())
+        if residual is not None and (residual.dtype is not half or residual.shape != (m, self.n_out) or not residual.is_contiguous() or residual.device != device):
+            self._bad("residual", residual, m, self.n_out)
         if m == 0:
             return out
-        arr = (ctypes.c_void_p * n)(*[o.data_ptr() for o in outs])
-        cols = (ctypes.c_int32 * n)(*[o.shape[1] for o in outs])
-        want = binding.lib().okv_linear4_workspace_bytes(m, self.n_out, self.n_in)
-        if want > 0 and (self.workspace is None or self.workspace.numel() < want):
-            self.workspace = torch.empty(want, dtype=torch.uint8, device=self.device)
+        want = self._wants.get(m)
+        if want is None:
+            want = self._wants[m] = max(0, int(binding.lib().okv_linear4_workspace_bytes(m, self.n_out, self.n_in)))
         ws = self.workspace
-        binding._check(self._call(x.data_ptr(), self.packed.data_ptr(), self.bias.data_ptr() if self.bias is not None else None,
-                                  residual.data_ptr() if residual is not None else None, arr, cols, n, m, self.n_out, self.n_in, self.group, self.zeros,
-                                  int(relu), ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, self._stream()))
+        if want and (ws is None or self._workspace_bytes < want):
+            ws = self.workspace = torch.empty(want, dtype=torch.uint8, device=device)
+            self._workspace_bytes = want
+        rc = self._call(x.data_ptr(), self._packed_at, self._bias_at, None if residual is None else residual.data_ptr(), arr, cols, n, m, self.n_out, self.n_in,
+                        self.group, self.zeros, 1 if relu else 0, None if ws is None else ws.data_ptr(), self._workspace_bytes, self._stream())
+        if rc:
+            binding._check(rc)
         return out

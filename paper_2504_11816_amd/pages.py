@@ -80,20 +80,20 @@ class Pages:
         """Sequence seqs[i] grows by n_new[i] tokens (None: one each) and takes the pages that it lacks."""
         at = self._ids("seqs", seqs)
         binding._check(binding.lib().okv_pages_extend(self.ref, seqs.numel(), at, None if n_new is None else self._ids("n_new", n_new, seqs.numel()),
-                                                      torch.cuda.current_stream().cuda_stream))
+                                                      binding.current_stream(self.device)))
 
     def fork(self, src, dst):
         """Sequence dst[i] (empty) becomes a fork of src[i]: shares its full pages, copies the rest."""
         at = self._ids("src", src)
-        binding._check(binding.lib().okv_pages_fork(self.ref, src.numel(), at, self._ids("dst", dst, src.numel()), torch.cuda.current_stream().cuda_stream))
+        binding._check(binding.lib().okv_pages_fork(self.ref, src.numel(), at, self._ids("dst", dst, src.numel()), binding.current_stream(self.device)))
 
     def free(self, seqs):
         at = self._ids("seqs", seqs)
-        binding._check(binding.lib().okv_pages_free(self.ref, seqs.numel(), at, torch.cuda.current_stream().cuda_stream))
+        binding._check(binding.lib().okv_pages_free(self.ref, seqs.numel(), at, binding.current_stream(self.device)))
 
     def compact(self):
         """Pages in use become 0 .. n_used - 1 (status[1] says how many, status[2] how many were moved)."""
-        binding._check(binding.lib().okv_pages_compact(self.ref, torch.cuda.current_stream().cuda_stream))
+        binding._check(binding.lib().okv_pages_compact(self.ref, binding.current_stream(self.device)))
 
     def copy(self, src_ids, dst_ids, to=None):
         """Copies pages src_ids[i] to pages dst_ids[i] of the arrays `to` (PageArrays like this cache's; None: this cache's own)."""
@@ -106,7 +106,7 @@ class Pages:
         c = (binding.OkvPageArray * len(to))(*[t.c for t in to])
         at = self._ids("src_ids", src_ids)
         binding._check(binding.lib().okv_pages_copy(self.ref, src_ids.numel(), at, self._ids("dst_ids", dst_ids, src_ids.numel()), c,
-                                                    min(t.tensor.shape[1] for t in to), torch.cuda.current_stream().cuda_stream))
+                                                    min(t.tensor.shape[1] for t in to), binding.current_stream(self.device)))
 
     def check(self):
         """Waits for the GPU; raises if a call could not be carried out since the last check."""
