@@ -8,7 +8,7 @@
 //     query heads of the KV head), and the result's layout -- lane l has keys 4 (l / 16) + 0..3 of query l % 16, twice -- is,
 //     with V's keys stored in that order, the operand layout of the second product, V^T (rows: elements) times the weights;
 //   * codes become fp16 numbers exactly (int8: a byte shuffle that makes 1024 + u, and a subtraction; e4m3: the conversion instruction), the
-//     scale multiplies the 16 scores and the 16-row results in fp32;
+//     scale of K multiplies the scores in fp32, that of V goes into the weights' exponent;
 //   * weights go into the second product as two fp16 numbers, w = hi + lo, w - hi - lo below 2^-22: one rounded to 11 bits would leave
 //     errors of 1e-4 of the result, which an fp32 output would show;
 //   * only whole tiles are in codes, so the loop over them has no masks; the up to 32 keys in a sequence's fp16 tail are attended
@@ -435,29 +435,37 @@ struct Softmax8 {
     m = -__builtin_inff(), l = 0.f;
   }
 
-  // The lane's 8 scores of 32 keys (in log2 units) -> its weights as two fp16 numbers each; returns what earlier results are multiplied with
-  __device__ __forceinline__ float weigh(const float (&s)[8], half8 &hi, half8 &lo) {
-    float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    top = fmaxf(m, max_with_lane_xor<16>(max_with_lane_xor<32>(top)));
-    const float base = top == -__builtin_inff() ? 0.f : top;          // no key yet: every weight is 0
-    const float alpha = __builtin_amdgcn_exp2f(m - base);
-    m = top;
-    float sum = 0.f;
+  // The lane's 8 scores of 32 keys, in log2 units and with log2 of the tile's V scale added -> weights w = 2^(s - m) as two fp16 numbers each,
+  // w = hi + lo to 22 bits.  The scale is in the weights, so that the products add up in the accumulators of the matrix cores;
+  // l counts the weights without it.  m is raised, and what is there multiplied down, only when a score is 8 or more above it
+  // (weights stay below 2^8): hardly ever after a piece's first tile.
+  __device__ __forceinline__ void weigh(const float (&s)[8], half8 &hi, half8 &lo, const float scale) {
+    const float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+    if (__any(top > m + 8.f)) {
+      const float now = fmaxf(m, max_with_lane_xor<16>(max_with_lane_xor<32>(top)));
+      const float alpha = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= alpha;
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) o[e] *= alpha;
+    }
+    float w[8], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float p = __builtin_amdgcn_exp2f(s[i] - base);
-      sum += p;
-      hi[i] = (_Float16)p;
-      lo[i] = (_Float16)(p - (float)hi[i]);
+      w[i] = __builtin_amdgcn_exp2f(s[i] - m);
+      sum += w[i];
     }
-    l = l * alpha + sum;
-    return alpha;
-  }
-  __device__ __forceinline__ void add(const int e, const half8 v, const half8 hi, const half8 lo, const float alpha, const float scale) {
-    floatx4 t = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-    t = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo, t, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[e][i] = fmaf(t[i], scale, o[e][i] * alpha);
+    for (int i = 0; i < 8; i += 2) {
+      const half2v h = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[i], w[i + 1]));
+      const half2v r = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[i] - (float)h[0], w[i + 1] - (float)h[1]));
+      hi[i] = h[0], hi[i + 1] = h[1], lo[i] = r[0], lo[i + 1] = r[1];
+    }
+    l = fmaf(sum, scale, l);
+  }
+  __device__ __forceinline__ void add(const int e, const half8 v, const half8 hi, const half8 lo) {
+    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, o[e], 0, 0, 0);
+    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo, o[e], 0, 0, 0);
   }
   __device__ __forceinline__ void write(const Attn8 &a, const int64_t slot, const int g, const int lane) const {
     const float sum = sum_with_lane_xor<16>(sum_with_lane_xor<32>(l));
@@ -513,9 +521,9 @@ __device__ __forceinline__ void attend_tail(const Attn8 &a, const int unit, _Flo
       for (int i = 0; i < 4; ++i) score[4 * h + i] = 16 * h + 4 * (lane / 16) + i < rows ? t[i] * a.scale_log2e : -__builtin_inff();
     }
     half8 hi, lo;
-    const float alpha = acc.weigh(score, hi, lo);
+    acc.weigh(score, hi, lo, 1.f);
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) acc.add(e, x.v[e], hi, lo, alpha, 1.f);
+    for (int e = 0; e < D / 16; ++e) acc.add(e, x.v[e], hi, lo);
     if (a.appends && rows == kTile) {
       const int page = clamp_page(a.c.table[(int64_t)row * s.max_pages + (held >> s.log2_T)], s.n_pages);
       x.template quantise_to<FMT>(a.c, page, (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
@@ -583,7 +591,7 @@ __global__ void __launch_bounds__(256) attn8_kernel(Attn8 a) {
     acc.clear();
     for (int i = 0; i < piece; ++i) {
       float score[8];
-      const float by = scale.x * a.scale_log2e, scale_v = scale.y;
+      const float by = scale.x * a.scale_log2e, scale_v = scale.y == 0.f ? 1.f : scale.y, log2_v = __builtin_amdgcn_logf(scale_v);      // (scale 0: codes 0)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
@@ -593,7 +601,7 @@ __global__ void __launch_bounds__(256) attn8_kernel(Attn8 a) {
           x = __builtin_amdgcn_mfma_f32_16x16x32_f16(unpack8<FMT>(w[2 * (c % 2)], w[2 * (c % 2) + 1]), q[c], x, 0, 0, 0);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) score[4 * h + j] = x[j] * by;
+        for (int j = 0; j < 4; ++j) score[4 * h + j] = fmaf(x[j], by, log2_v);
       }
       --left;
       if (left > 0) {
@@ -614,9 +622,9 @@ __global__ void __launch_bounds__(256) attn8_kernel(Attn8 a) {
         scale = *reinterpret_cast<const float2 *>(scale_from);
       }
       half8 hi, lo;
-      const float alpha = acc.weigh(score, hi, lo);
+      acc.weigh(score, hi, lo, __builtin_amdgcn_rcpf(scale_v));
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) acc.add(e, unpack8<FMT>(wv[e / 2][2 * (e % 2)], wv[e / 2][2 * (e % 2) + 1]), hi, lo, alpha, scale_v);
+      for (int e = 0; e < D / 16; ++e) acc.add(e, unpack8<FMT>(wv[e / 2][2 * (e % 2)], wv[e / 2][2 * (e % 2) + 1]), hi, lo);
       if (left > 0) load_codes<D, FMT, NT>(wv, at + v_step);
     }
     acc.write(a, str + b, g, lane);
