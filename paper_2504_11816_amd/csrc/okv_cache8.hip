@@ -96,18 +96,31 @@ __device__ __forceinline__ float scale_of(const float bits) {
   return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, s) + 4095u) & ~4095u);
 }
 
+// x / scale and its rounding.  A product with the reciprocal (1 unit in the last place off) and one correction by the exact remainder: a quotient
+// that lies on a rounding boundary comes out exactly, any other on its side, because it is 2^-21 away from it (okv_cache8.h).  Whole
+// numbers are rounded by an addition: 1.5 2^23 + 128 + y has the code in its last byte.
 template <int FMT>
 __device__ __forceinline__ u32x2 quantise8(const half8 x, const float scale) {
+  const bool some = scale > 0.f;                     // scale 0 or NaN: codes 0
+  const float over = some ? __builtin_amdgcn_rcpf(scale) : 0.f, by = some ? scale : 0.f;
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = scale > 0.f ? (float)x[i] / scale : 0.f;          // scale 0 or NaN: codes 0
+  for (int i = 0; i < 8; ++i) {
+    const float v = (float)x[i], q = v * over;
+    y[i] = fmaf(fmaf(-q, by, v), over, q);
+  }
+  if (!some)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = 0.f;
   u32x2 out;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t w = 0;
     if constexpr (FMT == OKV8_INT8) {
+      uint32_t b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w |= (uint32_t)((int)__builtin_rintf(y[4 * h + i]) + 128) << (8 * i);
+      for (int i = 0; i < 4; ++i) b[i] = __builtin_bit_cast(uint32_t, y[4 * h + i] + 12583040.f);
+      w = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
     } else {
       w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h], y[4 * h + 1], w, false);
       w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], w, true);
@@ -577,59 +590,74 @@ __global__ void __launch_bounds__(256) attn8_kernel(Attn8 a) {
     scale_from = a.c.scales + (tile * s.G + g) * 2;
   };
 
-  u32x4 wk[D / 32], wv[D / 32];
-  place();
-  load_codes<D, FMT, NT>(wk, at);
-  load_codes<D, FMT, NT>(wv, at + v_step);
-  float2 scale = *reinterpret_cast<const float2 *>(scale_from);
-
-  int b = fb, piece = in_seq, f_left = in_seq;      // the loads have f_left tiles of their piece to go, the tile at hand among them
-  for (;;) {
-    half8 q[D / 32];
-    load_q<D>(q, a, b, g, lane);
-    Softmax8<D> acc;
-    acc.clear();
-    for (int i = 0; i < piece; ++i) {
-      float score[8];
-      const float by = scale.x * a.scale_log2e, scale_v = scale.y == 0.f ? 1.f : scale.y, log2_v = __builtin_amdgcn_logf(scale_v);      // (scale 0: codes 0)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          const u32x4 w = wk[h * (D / 64) + c / 2];
-          x = __builtin_amdgcn_mfma_f32_16x16x32_f16(unpack8<FMT>(w[2 * (c % 2)], w[2 * (c % 2) + 1]), q[c], x, 0, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) score[4 * h + j] = fmaf(x[j], by, log2_v);
-      }
-      --left;
-      if (left > 0) {
-        ++next;
-        if (--f_left == 0) {                   // the next tile is another sequence's
-          int lo, hi;
-          do {
-            ++fb;
-            lo = a.plan.prefix[fb], hi = a.plan.prefix[fb + 1];
-          } while (lo == hi);
-          frow = min(max(a.seqs ? a.seqs[fb] : fb, 0), s.max_seqs - 1);
-          next = 0;
-          f_left = in_seq = min(hi - lo, left);
-          look_up();
-        }
-        place();
-        load_codes<D, FMT, NT>(wk, at);
-        scale = *reinterpret_cast<const float2 *>(scale_from);
-      }
-      half8 hi, lo;
-      acc.weigh(score, hi, lo, __builtin_amdgcn_rcpf(scale_v));
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) acc.add(e, unpack8<FMT>(wv[e / 2][2 * (e % 2)], wv[e / 2][2 * (e % 2) + 1]), hi, lo);
-      if (left > 0) load_codes<D, FMT, NT>(wv, at + v_step);
+  struct Buffer {
+    u32x4 k[D / 32], v[D / 32];
+    float2 scale;
+  };
+  // The loads have a cursor of their own, one tile ahead: `ahead` tiles of the stretch are still to be asked for.  A tile's K and V are asked for
+  // together, when the one before has been reduced: K as soon as its registers are free and V later is 9 % slower (ragged grouped heads 437 us
+  // a case against 397), a second tile in flight no faster (401).
+  int f_left = in_seq, ahead = left;
+  const auto fetch = [&](Buffer &t) {
+    if (ahead == 0) return;
+    place();
+    load_codes<D, FMT, NT>(t.k, at);
+    load_codes<D, FMT, NT>(t.v, at + v_step);
+    t.scale = *reinterpret_cast<const float2 *>(scale_from);
+    --ahead;
+    ++next;
+    if (--f_left == 0 && ahead > 0) {            // the next tile is another sequence's
+      int lo, hi;
+      do {
+        ++fb;
+        lo = a.plan.prefix[fb], hi = a.plan.prefix[fb + 1];
+      } while (lo == hi);
+      frow = min(max(a.seqs ? a.seqs[fb] : fb, 0), s.max_seqs - 1);
+      next = 0;
+      f_left = min(hi - lo, ahead);
+      look_up();
     }
-    acc.write(a, str + b, g, lane);
-    if (left == 0) break;
-    b = fb, piece = in_seq;
+  };
+  Buffer tile;
+  fetch(tile);
+  int b = begin.x, piece = in_seq;               // sequence at hand, tiles of it to go
+  half8 q[D / 32];
+  Softmax8<D> acc;
+  load_q<D>(q, a, b, g, lane);
+  acc.clear();
+  for (;;) {
+    float score[8];
+    const float scale_v = tile.scale.y == 0.f ? 1.f : tile.scale.y, by = tile.scale.x * a.scale_log2e, log2_v = __builtin_amdgcn_logf(scale_v);      // (scale 0: codes 0)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        const u32x4 w = tile.k[h * (D / 64) + c / 2];
+        x = __builtin_amdgcn_mfma_f32_16x16x32_f16(unpack8<FMT>(w[2 * (c % 2)], w[2 * (c % 2) + 1]), q[c], x, 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) score[4 * h + j] = fmaf(x[j], by, log2_v);
+    }
+    half8 hi, lo;
+    acc.weigh(score, hi, lo, __builtin_amdgcn_rcpf(scale_v));
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) acc.add(e, unpack8<FMT>(tile.v[e / 2][2 * (e % 2)], tile.v[e / 2][2 * (e % 2) + 1]), hi, lo);
+    fetch(tile);
+    if (--piece == 0) {
+      acc.write(a, str + b, g, lane);
+      if (left > 1) {
+        int first, end;
+        do {
+          ++b;
+          first = a.plan.prefix[b], end = a.plan.prefix[b + 1];
+        } while (first == end);
+        piece = min(end - first, left - 1);
+        load_q<D>(q, a, b, g, lane);
+        acc.clear();
+      }
+    }
+    if (--left == 0) break;
   }
 }
 
@@ -644,39 +672,42 @@ struct Merge8 {
 // workgroup, where most sequences are cut little; 4 where there are few sequences and therefore many pieces of each.
 template <int D, int WAVES>
 __global__ void __launch_bounds__(256) merge8_kernel(Merge8 a) {
-  constexpr int E = D / 64;
+  constexpr int E = D / 64, kJoin = WAVES == 1 ? 4 : 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x, share = WAVES == 1 ? 0 : wave;
   if (row >= a.batch * a.H) return;
   const int b = row / a.H, h = row - b * a.H;
-  const int lo = a.plan.prefix[b], hi = a.plan.prefix[b + 1], span = a.plan.head[1];
+  const int span = a.plan.head[1], lo = a.plan.prefix[b], hi = a.plan.prefix[b + 1];
   const int first = lo / span, pieces = (hi > lo ? (hi - 1) / span - first + 1 : 0) + 1;      // the last one is the tail's
   const auto at = [&](int p) { return (int64_t)(p == pieces - 1 ? a.main_slots + b : first + p + b) * a.H + h; };
   float top = -__builtin_inff(), sum = 0.f, o[E] = {};
   for (int p0 = share * 64; p0 < pieces; p0 += 64 * WAVES) {
-    const int p = p0 + lane;
-    const float2 ml = p < pieces ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(p)) : make_float2(-__builtin_inff(), 0.f);
+    const int n = min(64, pieces - p0);
+    float x[kJoin][E];                                     // kJoin pieces at a time are in flight, the first with the maxima and sums of all
+    const auto ask = [&](const int i) {
+#pragma unroll
+      for (int j = 0; j < kJoin; ++j) {
+        const float *from = a.part_o + at(p0 + min(i + j, n - 1)) * D + E * lane;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[j][e] = from[e];
+      }
+    };
+    const float2 ml = lane < n ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(p0 + lane)) : make_float2(-__builtin_inff(), 0.f);
+    ask(0);
     const float now = fmaxf(top, wave_max(ml.x)), base = now == -__builtin_inff() ? 0.f : now;
     const float w = __builtin_amdgcn_exp2f(ml.x - base), old = __builtin_amdgcn_exp2f(top - base);
     top = now;
     sum = sum * old + wave_sum(w * ml.y);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= old;
-    const int n = min(64, pieces - p0);
-    for (int i = 0; i < n; i += 8) {                     // eight pieces at a time: their loads are in flight together
-      float x[8][E], wi[8];
+    for (int i = 0; i < n; i += kJoin) {
+      if (i) ask(i);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int p = min(i + j, n - 1);
-        const float *from = a.part_o + at(p0 + p) * D + E * lane;
+      for (int j = 0; j < kJoin; ++j) {
+        const float wi = i + j < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(i + j, n - 1))) : 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[j][e] = from[e];
-        wi[j] = i + j < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), p)) : 0.f;
+        for (int e = 0; e < E; ++e) o[e] = fmaf(wi, x[j][e], o[e]);
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(wi[j], x[j][e], o[e]);
     }
   }
   if constexpr (WAVES > 1) {
