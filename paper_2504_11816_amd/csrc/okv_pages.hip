@@ -1,8 +1,11 @@
 // Pages of a paged KV cache (include/okv_pages.h), for gfx950.
 //
 // Two kinds of kernels.  What is decided -- which ids are free, who gets which, what moves where -- is prefix sums over a few thousand
-// integers: one workgroup of 1024 threads, a launch of 3 to 6 us.  What is moved is bound by HBM, twice its bytes: a workgroup
-// takes 32 KiB, eight 16-byte loads of every thread in flight before the first store.
+// integers: one workgroup of 1024 threads, a launch of 3 to 5 us.  What is moved is bound by HBM, twice its bytes: a workgroup takes 16 KiB,
+// four 16-byte loads of every thread in flight before the first store; loads through the caches (several forks read one page), stores past
+// them.  Measured, us: 48 forks of 256 KiB pages in 32 layers 118 (806 MB moved: 6.8 TB/s, a third of it read from HBM), 592 pages of 256 KiB
+// in 4 layers and 200 gathered 310 (5.3 TB/s); with 32 KiB a workgroup 200 and 471, with loads past the caches 158 and 314, stores through
+// them 144 and 337.
 #include "okv_pages.h"
 #include "okv_report.h"
 
@@ -18,8 +21,9 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 1024, kMoveThreads = 256, kInFlight = 8;
-constexpr int kMoveBlocks = 4096;        // of launches whose amount of work is known on the GPU only
+constexpr int kThreads = 1024, kMoveThreads = 256, kInFlight = 4;
+constexpr int kSmallPage = 2048;         // bytes of a page in an array that is moved together with another's piece
+constexpr int kMoveBlocks = 8192;        // of launches that may have more work than workgroups
 
 struct Lists {                           // in the workspace
   int32_t *count;                        // pages to move (compact), or whether the fork is carried out
@@ -87,10 +91,11 @@ __global__ void __launch_bounds__(kThreads) extend_kernel(State s, const int32_t
   __shared__ int sums[kThreads / 64], first[OKV_PAGES_MAX_SEQS + 1], bad;
   if (threadIdx.x == 0) bad = 0;
   __syncthreads();
+  const int each = (n + kThreads - 1) / kThreads;
   int more[kEachSeq], need = 0;
 #pragma unroll
   for (int i = 0; i < kEachSeq; ++i) {
-    const int j = threadIdx.x * kEachSeq + i, row = j < n ? seqs ? seqs[j] : j : -1;
+    const int j = threadIdx.x * each + i, row = i < each && j < n ? seqs ? seqs[j] : j : -1;
     more[i] = 0;
     if (!is_row(s, row)) continue;
     const int len = length_of(s, row), add = n_new ? max(n_new[j], 0) : 1;
@@ -101,10 +106,10 @@ __global__ void __launch_bounds__(kThreads) extend_kernel(State s, const int32_t
   int total, at = scan(need, total, sums);
 #pragma unroll
   for (int i = 0; i < kEachSeq; ++i) {
-    first[threadIdx.x * kEachSeq + i] = at;
+    if (i < each) first[threadIdx.x * each + i] = at;
     at += more[i];
   }
-  if (threadIdx.x == kThreads - 1) first[OKV_PAGES_MAX_SEQS] = at;
+  if (threadIdx.x == kThreads - 1) first[kThreads * each] = at;
   __syncthreads();
   if (bad || total > s.n_pages) {
     if (threadIdx.x == 0) blame(s, OKV_ENOSPC);
@@ -137,21 +142,23 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(State s, const int3
   __shared__ int sums[kThreads / 64], bad, holes[OKV_PAGES_MAX_SEQS];
   if (threadIdx.x == 0) bad = 0;
   __syncthreads();
-  int needs[kEachSeq], need = 0;
+  const int each = (n + kThreads - 1) / kThreads;
+  int row[kEachSeq], len[kEachSeq], need = 0;
+  const int within = (1 << s.log2_T) - 1;
 #pragma unroll
   for (int i = 0; i < kEachSeq; ++i) {
-    const int j = threadIdx.x * kEachSeq + i;
-    needs[i] = 0;
-    if (j >= n) continue;
+    const int j = threadIdx.x * each + i;
+    row[i] = len[i] = 0;
+    if (i >= each || j >= n) continue;
     const int a = src[j], b = dst[j];
-    if (!is_row(s, a) || !is_row(s, b)) {
+    if (!is_row(s, a) || !is_row(s, b) || a == b) {
       bad = 1;
       continue;
     }
-    const int len = length_of(s, a);
-    if (a == b || s.lens[b] != 0) bad = 1;
-    needs[i] = len & ((1 << s.log2_T) - 1) ? 1 : 0;
-    need += needs[i];
+    row[i] = a;
+    len[i] = length_of(s, a);
+    if (s.lens[b] != 0) bad = 1;
+    need += len[i] & within ? 1 : 0;
   }
   int total, at = scan(need, total, sums);         // (its barriers: `bad` is everybody's)
   const int found = bad ? 0 : take_free(s, total, sums, [&](int rank, int page) { holes[rank] = page; });
@@ -164,25 +171,25 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(State s, const int3
   if (!go) return;
 #pragma unroll
   for (int i = 0; i < kEachSeq; ++i) {
-    const int j = threadIdx.x * kEachSeq + i;
-    if (j >= n) continue;
+    const int j = threadIdx.x * each + i;
+    if (i >= each || j >= n) continue;
     int from = -1, to = -1;
-    if (needs[i]) {
+    if (len[i] & within) {
       to = holes[at++];
-      from = s.table[(int64_t)src[j] * s.width + (length_of(s, src[j]) >> s.log2_T)];
+      from = s.table[(int64_t)row[i] * s.width + (len[i] >> s.log2_T)];
       s.refs[to] = 1;
     }
     l.from[j] = from;
     l.to[j] = to;
-    l.place[j] = length_of(s, src[j]);
+    l.place[j] = len[i];
   }
 }
 
-// A page array as kernels see it; pieces of 32 KiB (8 KiB where it is moved by 4 bytes)
+// A page array as kernels see it; pieces of 16 KiB (4 KiB where it is moved by 4 bytes)
 struct Moved {
   char *base, *to;
   int64_t page_bytes, layer_stride, to_layer_stride, unit_bytes;
-  int32_t log2_units_tokens, whole_units, wide, pieces;
+  int32_t log2_units_tokens, whole_units, wide, pieces;      // pieces 0: a small array, moved with the page's first piece
 };
 struct MovedRows {
   char *base;
@@ -204,26 +211,27 @@ __device__ __forceinline__ void move_piece(char *to, const char *from, const int
   T x[kInFlight];
 #pragma unroll
   for (int i = 0; i < kInFlight; ++i)
-    if ((int64_t)i * kMoveThreads + threadIdx.x < n) x[i] = __builtin_nontemporal_load(f + i * kMoveThreads + threadIdx.x);
+    if ((int64_t)i * kMoveThreads + threadIdx.x < n) x[i] = f[i * kMoveThreads + threadIdx.x];
 #pragma unroll
   for (int i = 0; i < kInFlight; ++i)
     if ((int64_t)i * kMoveThreads + threadIdx.x < n) __builtin_nontemporal_store(x[i], t + i * kMoveThreads + threadIdx.x);
 }
 __device__ __forceinline__ void move_page(const Moves &m, int piece, const int layer, const int64_t from, const int64_t to, const int used) {
+  const bool small_ones = piece == 0;
 #pragma unroll
   for (int i = 0; i < OKV_PAGES_MAX_ARRAYS; ++i) {
     if (i >= m.n_arrays) return;
     const Moved &a = m.arrays[i];
-    if (piece >= a.pieces) {
-      piece -= a.pieces;
-      continue;
+    const bool mine = piece >= 0 && piece < a.pieces;
+    if (mine || (a.pieces == 0 && small_ones)) {
+      const char *f = a.base + layer * a.layer_stride + from * a.page_bytes;
+      char *t = a.to + layer * a.to_layer_stride + to * a.page_bytes;
+      const int units = used < 0 ? 0 : (used + (a.whole_units ? 0 : (1 << a.log2_units_tokens) - 1)) >> a.log2_units_tokens;
+      const int64_t bytes = used < 0 ? a.page_bytes : units * a.unit_bytes;
+      if (a.wide) move_piece<u32x4>(t, f, mine ? piece : 0, bytes);
+      else move_piece<uint32_t>(t, f, mine ? piece : 0, bytes);
     }
-    const char *f = a.base + layer * a.layer_stride + from * a.page_bytes;
-    char *t = a.to + layer * a.to_layer_stride + to * a.page_bytes;
-    const int64_t bytes = used < 0 ? a.page_bytes : ((int64_t)used + (a.whole_units ? 0 : (1 << a.log2_units_tokens) - 1) >> a.log2_units_tokens) * a.unit_bytes;
-    if (a.wide) move_piece<u32x4>(t, f, piece, bytes);
-    else move_piece<uint32_t>(t, f, piece, bytes);
-    return;
+    piece -= a.pieces;
   }
 }
 template <class T>
@@ -385,9 +393,10 @@ Moves moves_of(const okv_pages *p, const okv_page_array *to) {
     k.log2_units_tokens = log2_of(a.unit_tokens), k.whole_units = a.whole_units != 0;
     k.wide = multiple(a.base, 16) && multiple(t.base, 16) && multiple(k.unit_bytes, 16) && multiple(a.layer_stride, 16) && multiple(t.layer_stride, 16);
     const int64_t piece = (int64_t)kMoveThreads * kInFlight * (k.wide ? 16 : 4);
-    k.pieces = (int32_t)((a.page_bytes + piece - 1) / piece);
+    k.pieces = a.page_bytes <= kSmallPage ? 0 : (int32_t)((a.page_bytes + piece - 1) / piece);
     m.pieces += k.pieces;
   }
+  if (p->n_arrays && m.pieces == 0) m.pieces = 1;
   for (int i = 0; i < p->n_rows; ++i) {
     const okv_row_array &r = p->rows[i];
     m.rows[i] = {static_cast<char *>(r.base), r.layer_stride, r.groups, r.rows, r.row_bytes,
@@ -452,8 +461,10 @@ int okv_pages_compact(const okv_pages *p, void *stream) {
   if (const int rc = check("okv_pages_compact", p, 0, 0)) return rc;
   const Lists l = lists_of(p);
   hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), state_of(p), l);
-  hipLaunchKernelGGL(compact_move_kernel, dim3(kMoveBlocks), dim3(kMoveThreads), 0, static_cast<hipStream_t>(stream), state_of(p), l, moves_of(p, nullptr),
-                     p->n_layers);
+  const Moves m = moves_of(p, nullptr);            // at most every other page is moved
+  const int64_t entries = ((int64_t)p->max_seqs * p->max_pages_per_seq + kMoveThreads - 1) / kMoveThreads;
+  const int64_t blocks = std::min<int64_t>(kMoveBlocks, std::max(entries, (int64_t)(p->n_pages / 2) * p->n_layers * m.pieces));
+  hipLaunchKernelGGL(compact_move_kernel, dim3((unsigned)blocks), dim3(kMoveThreads), 0, static_cast<hipStream_t>(stream), state_of(p), l, m, p->n_layers);
   return hip_result("okv_pages_compact");
 }
 
