@@ -103,13 +103,15 @@ typedef struct okv8_step {
   const int32_t *seqs;         /* [batch] or NULL, as above                                  */
   const int32_t *lens;         /* [max_seqs] keys that are attended, an appended one included.
                                   0: nothing is appended, the output is 0                    */
-  void *workspace;             /* okv8_workspace_bytes(c, batch) bytes, 256-byte aligned     */
+  void *workspace;             /* up to okv8_workspace_bytes(c, batch) bytes, 256-byte aligned */
   int64_t workspace_bytes;
   void *stream;
 } okv8_step;
 
-/* Workspace of a step of up to max_batch sequences; < 0 on a bad shape.  Its contents mean nothing
- * between steps.  Steps that may run at the same time need workspaces of their own. */
+/* Workspace of a step of up to max_batch sequences; < 0 on a bad shape.  okv8_decode_step attends up to 32 layers in one launch
+ * with it; what this returns for a cache of one layer is enough for okv8_decode_attn, and okv8_decode_step then takes fewer
+ * layers at a time.  Its contents mean nothing between steps.  Steps that may run at the same time need
+ * workspaces of their own. */
 int64_t okv8_workspace_bytes(const okv8_cache *c, int32_t max_batch);
 
 /* Shares the step's keys out over the wavefronts: once per step, before the first okv8_decode_attn. */
@@ -126,7 +128,8 @@ int okv8_step_begin(const okv8_cache *c, const okv8_step *s);
 int okv8_decode_attn(const okv8_cache *c, const okv8_step *s, int32_t layer, const void *q, int64_t q_stride,
                      const void *k_new, const void *v_new, int64_t kv_stride, void *out);
 
-/* okv8_step_begin and every layer's okv8_decode_attn, for inputs that are there for all layers:
+/* A step whose inputs are there for all layers, in three launches (okv8_step_begin and okv8_decode_attn for every layer
+ * give the same up to the order in which partial results are added):
  * q [L][batch][H][d], k_new / v_new [L][batch][G][d] (or NULL), out [L][batch][H][d], all contiguous. */
 int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, const void *k_new,
                      const void *v_new, void *out);

@@ -15,7 +15,8 @@
 //     by wavefronts of their own in the same launch, which also store the appended row and quantise a tail that is full.
 //
 // The keys of a launch are cut into equal stretches of tiles over the sequences laid end to end, a wavefront per (stretch, KV head);
-// partial results (max, sum, weighted sum) are joined by a second launch.
+// partial results (max, sum, weighted sum) are joined by a second launch.  A step whose layers' inputs are all there attends up to 32 layers in one
+// launch, the stretches that much longer.
 #include "okv_cache8.h"
 #include "okv_host.h"
 #include "okv_lanes.h"
@@ -433,9 +434,22 @@ struct Attn8 {
   const _Float16 *q, *k_new, *v_new;
   float *part_o, *part_ml;         // partial results by [slot][G][R]; sequence b's tail in slot main_slots + b
   int64_t q_stride, kv_stride;
+  int64_t q_layer, kv_layer, codes_layer, scales_layer, tails_layer;      // from a layer's to the next one's
   float scale_log2e;               // log2(e) / sqrt(d)
-  int32_t batch, main_slots, main_blocks, appends;
+  int32_t batch, main_slots, main_blocks, layers, appends;      // main_blocks: of a layer
+  int32_t slot0;                   // of the layer's partial results
 };
+
+// The launch covers `layers` layers; a wavefront works for one of them.
+__device__ __forceinline__ void of_layer(Attn8 &a, const int layer) {
+  a.c.codes += layer * a.codes_layer;
+  a.c.scales += layer * a.scales_layer;
+  a.c.tails += layer * a.tails_layer;
+  a.q += layer * a.q_layer;
+  a.k_new += layer * a.kv_layer;
+  a.v_new += layer * a.kv_layer;
+  a.slot0 = layer * (a.main_slots + a.batch);
+}
 
 template <int D>
 struct Softmax8 {
@@ -484,7 +498,7 @@ struct Softmax8 {
     const float sum = sum_with_lane_xor<16>(sum_with_lane_xor<32>(l));
     const int R = a.c.s.R, r = lane % 16;
     if (r >= R) return;
-    const int64_t at = (slot * a.c.s.G + g) * R + r;
+    const int64_t at = ((a.slot0 + slot) * a.c.s.G + g) * R + r;
     if (lane < 16) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, sum);
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) *reinterpret_cast<floatx4 *>(a.part_o + at * D + 16 * e + 4 * (lane / 16)) = o[e];
@@ -555,15 +569,22 @@ __device__ __forceinline__ void load_codes(u32x4 (&w)[D / 32], const uint8_t *fr
 }
 
 template <int D, int FMT, bool NT>
-__global__ void __launch_bounds__(256) attn8_kernel(Attn8 a) {
+__global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
   __shared__ _Float16 lds_all[4][kTile * lds_row(D)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int)blockIdx.x >= a.main_blocks) {
-    attend_tail<D, FMT>(a, (blockIdx.x - a.main_blocks) * 4 + wave, lds_all[wave], lane);
+  Attn8 a = launch;
+  // the layers' code readers first, then their tails, which take the places beside them
+  int block = blockIdx.x;
+  if (block >= a.main_blocks * a.layers) {
+    block -= a.main_blocks * a.layers;
+    const int per_layer = (a.batch * a.c.s.G + 3) >> 2, layer = block / per_layer;
+    of_layer(a, layer);
+    attend_tail<D, FMT>(a, (block - layer * per_layer) * 4 + wave, lds_all[wave], lane);
     return;
   }
   const Shape8 s = a.c.s;
-  const int unit = blockIdx.x * 4 + wave, str = unit / s.G, g = unit - str * s.G;
+  const int layer = block / a.main_blocks, unit = (block - layer * a.main_blocks) * 4 + wave, str = unit / s.G, g = unit - str * s.G;
+  of_layer(a, layer);
   const int total = a.plan.head[0], span = a.plan.head[1];
   if (str * span >= total) return;
   const int4 begin = a.plan.stretch[str];
@@ -664,8 +685,8 @@ __global__ void __launch_bounds__(256) attn8_kernel(Attn8 a) {
 struct Merge8 {
   Plan8 plan;
   const float *part_o, *part_ml;
-  void *out;
-  int32_t batch, H, G, R, main_slots, out_fp32;
+  void *out;                       // [layers][batch][H][d]
+  int32_t batch, H, main_slots, layers, out_fp32;
 };
 
 // out = sum_p w_p o_p / sum_p w_p l_p with w_p = 2^(m_p - max m) over a row's pieces.  WAVES wavefronts share a row's pieces: 1, four rows to a
@@ -675,11 +696,12 @@ __global__ void __launch_bounds__(256) merge8_kernel(Merge8 a) {
   constexpr int E = D / 64, kJoin = WAVES == 1 ? 4 : 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x, share = WAVES == 1 ? 0 : wave;
-  if (row >= a.batch * a.H) return;
-  const int b = row / a.H, h = row - b * a.H;
+  if (row >= a.layers * a.batch * a.H) return;
+  const int seq = row / a.H, h = row - seq * a.H, layer = seq / a.batch, b = seq - layer * a.batch;
+  const int slot0 = layer * (a.main_slots + a.batch);
   const int span = a.plan.head[1], lo = a.plan.prefix[b], hi = a.plan.prefix[b + 1];
   const int first = lo / span, pieces = (hi > lo ? (hi - 1) / span - first + 1 : 0) + 1;      // the last one is the tail's
-  const auto at = [&](int p) { return (int64_t)(p == pieces - 1 ? a.main_slots + b : first + p + b) * a.H + h; };
+  const auto at = [&](int p) { return (int64_t)(slot0 + (p == pieces - 1 ? a.main_slots + b : first + p + b)) * a.H + h; };
   float top = -__builtin_inff(), sum = 0.f, o[E] = {};
   for (int p0 = share * 64; p0 < pieces; p0 += 64 * WAVES) {
     const int n = min(64, pieces - p0);
@@ -783,25 +805,35 @@ Cache8 cache_of(const okv8_cache *c, int32_t layer) {
   return k;
 }
 
-int max_stretches(const okv8_cache *c) { return std::max(1, kWaves / c->n_kv_heads); }
+// Stretches of a launch that covers this many layers: a wavefront for each (layer, stretch, KV head)
+int max_stretches(const okv8_cache *c, int layers) { return std::max(1, kWaves / (c->n_kv_heads * layers)); }
 
-// The workspace: plan (head, prefix, stretches), then the partial results of batch + stretches slots, then of batch tails.
+// The workspace: plan (head, prefix, stretches), then for every layer of a launch the partial results of batch + stretches slots and of batch tails.
 struct Workspace8 {
   int64_t prefix, stretch, ml, o, bytes;
-  int32_t slots;
+  int32_t slots, layers, stretches;
 };
-Workspace8 workspace_of(const okv8_cache *c, int32_t batch) {
+Workspace8 workspace_of(const okv8_cache *c, int32_t batch, int32_t layers) {
   const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
   Workspace8 w;
-  const int n = max_stretches(c);
-  w.slots = batch + n;
+  w.layers = layers;
+  w.stretches = max_stretches(c, layers);
+  w.slots = batch + w.stretches;
   w.prefix = 256;
   w.stretch = up(w.prefix + 4 * (int64_t)(batch + 1));
-  w.ml = up(w.stretch + 16 * (int64_t)n);
-  const int64_t rows = (int64_t)(w.slots + batch) * c->n_q_heads;
+  w.ml = up(w.stretch + 16 * (int64_t)w.stretches);
+  const int64_t rows = (int64_t)layers * (w.slots + batch) * c->n_q_heads;
   w.o = up(w.ml + 8 * rows);
   w.bytes = up(w.o + 4 * rows * c->head_dim);
   return w;
+}
+
+// Layers that okv8_decode_step attends in one launch: all of them, up to 32, where the workspace holds their partial results
+constexpr int kLayersAbreast = 32;
+Workspace8 workspace_for(const okv8_cache *c, const okv8_step *s) {
+  int layers = std::min(c->n_layers, kLayersAbreast);
+  while (layers > 1 && workspace_of(c, s->batch, layers).bytes > s->workspace_bytes) --layers;
+  return workspace_of(c, s->batch, layers);
 }
 
 Plan8 plan_of(const Workspace8 &w, void *base) {
@@ -819,8 +851,8 @@ int step_problem(const char *who, const okv8_cache *c, const okv8_step *s) {
   if (s->appends != 0 && s->appends != 1) return report(OKV_EINVAL, "%s: appends must be 0 or 1", who);
   if (!s->lens || !s->workspace) return report(OKV_EINVAL, "%s: NULL pointer", who);
   if (reinterpret_cast<uintptr_t>(s->workspace) & 255) return report(OKV_EINVAL, "%s: the workspace must be 256-byte aligned", who);
-  if (s->workspace_bytes < workspace_of(c, s->batch).bytes)
-    return report(OKV_ENOSPC, "%s: the workspace has %lld bytes, %lld are needed", who, (long long)s->workspace_bytes, (long long)workspace_of(c, s->batch).bytes);
+  if (s->workspace_bytes < workspace_of(c, s->batch, 1).bytes)
+    return report(OKV_ENOSPC, "%s: the workspace has %lld bytes, %lld are needed", who, (long long)s->workspace_bytes, (long long)workspace_of(c, s->batch, 1).bytes);
   return OKV_OK;
 }
 
@@ -877,9 +909,9 @@ int rows_call(const char *who, bool store, const okv8_cache *c, int32_t layer, i
 // Codes that do not fit the memory-side cache (256 MiB) are read past it, so that they do not push out what is used again.
 bool streamed(const okv8_cache *c) { return codes_layer_bytes(c) * c->n_layers > (int64_t)256 << 20; }
 
-int attend(const char *who, const okv8_cache *c, const okv8_step *s, int32_t layer, const void *q, int64_t q_stride, const void *k_new,
-           const void *v_new, int64_t kv_stride, void *out) {
-  const Workspace8 w = workspace_of(c, s->batch);
+// w.layers layers from `layer` on, as far as there are
+int attend(const char *who, const okv8_cache *c, const okv8_step *s, const Workspace8 &w, int32_t layer, int32_t layers, const void *q, int64_t q_stride,
+           const void *k_new, const void *v_new, int64_t kv_stride, void *out) {
   char *base = static_cast<char *>(s->workspace);
   const hipStream_t stream = static_cast<hipStream_t>(s->stream);
   Attn8 a;
@@ -889,30 +921,31 @@ int attend(const char *who, const okv8_cache *c, const okv8_step *s, int32_t lay
   a.q = static_cast<const _Float16 *>(q), a.k_new = static_cast<const _Float16 *>(k_new), a.v_new = static_cast<const _Float16 *>(v_new);
   a.part_ml = reinterpret_cast<float *>(base + w.ml), a.part_o = reinterpret_cast<float *>(base + w.o);
   a.q_stride = q_stride, a.kv_stride = kv_stride;
+  a.q_layer = q_stride * s->batch, a.kv_layer = k_new ? kv_stride * s->batch : 0;      // (several layers: okv8_decode_step, contiguous)
+  a.codes_layer = codes_layer_bytes(c), a.scales_layer = scales_layer_floats(c), a.tails_layer = tails_layer_halves(c);
   a.scale_log2e = (float)(1.4426950408889634 / (c->head_dim == 128 ? 11.313708498984761 : 8.0));
-  a.batch = s->batch, a.main_slots = w.slots, a.appends = s->appends;
-  a.main_blocks = (max_stretches(c) * c->n_kv_heads + 3) / 4;
-  const int tails = (s->batch * c->n_kv_heads + 3) / 4;
-  by_format<AttnLaunch8>(c, a, dim3((unsigned)(a.main_blocks + tails)), streamed(c), stream);
+  a.batch = s->batch, a.main_slots = w.slots, a.appends = s->appends, a.layers = layers, a.slot0 = 0;
+  a.main_blocks = (w.stretches * c->n_kv_heads + 3) / 4;
+  const int64_t blocks = (int64_t)layers * (a.main_blocks + (s->batch * c->n_kv_heads + 3) / 4);
+  by_format<AttnLaunch8>(c, a, dim3((unsigned)blocks), streamed(c), stream);
   Merge8 m;
   m.plan = a.plan, m.part_o = a.part_o, m.part_ml = a.part_ml, m.out = out;
-  m.batch = s->batch, m.H = c->n_q_heads, m.G = c->n_kv_heads, m.R = a.c.s.R, m.main_slots = w.slots, m.out_fp32 = c->out_dtype;
-  const int rows = s->batch * c->n_q_heads;
-  const bool wide = max_stretches(c) >= 16 * s->batch;
+  m.batch = s->batch, m.H = c->n_q_heads, m.main_slots = w.slots, m.layers = layers, m.out_fp32 = c->out_dtype;
+  const int64_t rows = (int64_t)layers * s->batch * c->n_q_heads;
+  const bool wide = w.stretches >= 16 * s->batch;
   if (c->head_dim == 128) {
-    if (wide) hipLaunchKernelGGL((merge8_kernel<128, 4>), dim3(rows), dim3(256), 0, stream, m);
-    else hipLaunchKernelGGL((merge8_kernel<128, 1>), dim3((rows + 3) / 4), dim3(256), 0, stream, m);
+    if (wide) hipLaunchKernelGGL((merge8_kernel<128, 4>), dim3((unsigned)rows), dim3(256), 0, stream, m);
+    else hipLaunchKernelGGL((merge8_kernel<128, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, m);
   } else {
-    if (wide) hipLaunchKernelGGL((merge8_kernel<64, 4>), dim3(rows), dim3(256), 0, stream, m);
-    else hipLaunchKernelGGL((merge8_kernel<64, 1>), dim3((rows + 3) / 4), dim3(256), 0, stream, m);
+    if (wide) hipLaunchKernelGGL((merge8_kernel<64, 4>), dim3((unsigned)rows), dim3(256), 0, stream, m);
+    else hipLaunchKernelGGL((merge8_kernel<64, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, m);
   }
   return hip_result(who, hipGetLastError());
 }
 
-int begin(const char *who, const okv8_cache *c, const okv8_step *s) {
-  const Workspace8 w = workspace_of(c, s->batch);
+int begin(const char *who, const okv8_cache *c, const okv8_step *s, const Workspace8 &w) {
   hipLaunchKernelGGL(plan8_kernel, dim3(1), dim3(kPlanThreads), 0, static_cast<hipStream_t>(s->stream), s->seqs, s->lens, s->batch, s->appends,
-                     cache_of(c, 0).s, max_stretches(c), plan_of(w, s->workspace));
+                     cache_of(c, 0).s, w.stretches, plan_of(w, s->workspace));
   return hip_result(who, hipGetLastError());
 }
 
@@ -939,7 +972,7 @@ int64_t okv8_tails_bytes(const okv8_cache *c) {
 int64_t okv8_workspace_bytes(const okv8_cache *c, int32_t max_batch) {
   if (const char *why = shape_problem(c)) return report(OKV_EINVAL, "okv8_workspace_bytes: %s", why);
   if (max_batch < 1 || max_batch > OKV8_MAX_BATCH) return report(OKV_EINVAL, "okv8_workspace_bytes: batch must be in [1, %d]", OKV8_MAX_BATCH);
-  return workspace_of(c, max_batch).bytes;
+  return workspace_of(c, max_batch, std::min(c->n_layers, kLayersAbreast)).bytes;
 }
 
 int okv8_store(const okv8_cache *c, int32_t layer, int32_t n_layers, int32_t batch, const int32_t *seqs, const int32_t *starts,
@@ -953,7 +986,7 @@ int okv8_load(const okv8_cache *c, int32_t layer, int32_t n_layers, int32_t batc
 
 int okv8_step_begin(const okv8_cache *c, const okv8_step *s) {
   if (const int rc = step_problem("okv8_step_begin", c, s)) return rc;
-  return begin("okv8_step_begin", c, s);
+  return begin("okv8_step_begin", c, s, workspace_of(c, s->batch, 1));
 }
 
 int okv8_decode_attn(const okv8_cache *c, const okv8_step *s, int32_t layer, const void *q, int64_t q_stride, const void *k_new,
@@ -967,7 +1000,7 @@ int okv8_decode_attn(const okv8_cache *c, const okv8_step *s, int32_t layer, con
   if (q_stride < (int64_t)c->n_q_heads * c->head_dim || q_stride % 8 ||
       (s->appends && (kv_stride < (int64_t)c->n_kv_heads * c->head_dim || kv_stride % 8)))
     return report(OKV_EINVAL, "okv8_decode_attn: strides must be multiples of 8 and at least a row");
-  return attend("okv8_decode_attn", c, s, layer, q, q_stride, k_new, v_new, kv_stride, out);
+  return attend("okv8_decode_attn", c, s, workspace_of(c, s->batch, 1), layer, 1, q, q_stride, k_new, v_new, kv_stride, out);
 }
 
 int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, const void *k_new, const void *v_new, void *out) {
@@ -976,11 +1009,12 @@ int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, con
     return report(OKV_EINVAL, "okv8_decode_step: NULL or misaligned pointer");
   if ((k_new != nullptr) != (s->appends == 1) || (v_new != nullptr) != (s->appends == 1))
     return report(OKV_EINVAL, "okv8_decode_step: k_new and v_new are given if, and only if, the step appends");
-  int rc = begin("okv8_decode_step", c, s);
+  const Workspace8 w = workspace_for(c, s);
+  int rc = begin("okv8_decode_step", c, s, w);
   const int64_t q_row = (int64_t)c->n_q_heads * c->head_dim, kv_row = (int64_t)c->n_kv_heads * c->head_dim;
-  for (int32_t l = 0; rc == OKV_OK && l < c->n_layers; ++l) {
+  for (int32_t l = 0; rc == OKV_OK && l < c->n_layers; l += w.layers) {
     const auto at = [&](const void *p, int64_t row, int64_t size) { return p ? static_cast<const char *>(p) + l * s->batch * row * size : nullptr; };
-    rc = attend("okv8_decode_step", c, s, l, at(q, q_row, 2), q_row, at(k_new, kv_row, 2), at(v_new, kv_row, 2), kv_row,
+    rc = attend("okv8_decode_step", c, s, w, l, std::min(w.layers, c->n_layers - l), at(q, q_row, 2), q_row, at(k_new, kv_row, 2), at(v_new, kv_row, 2), kv_row,
                 const_cast<char *>(at(out, q_row, c->out_dtype ? 4 : 2)));
   }
   return rc;
