@@ -128,7 +128,7 @@ int okv8_step_begin(const okv8_cache *c, const okv8_step *s);
 int okv8_decode_attn(const okv8_cache *c, const okv8_step *s, int32_t layer, const void *q, int64_t q_stride,
                      const void *k_new, const void *v_new, int64_t kv_stride, void *out);
 
-/* A step whose inputs are there for all layers, in three launches (okv8_step_begin and okv8_decode_attn for every layer
+/* A step whose inputs are there for all layers, in two launches, three beyond 64 sequences (okv8_step_begin and okv8_decode_attn for every layer
  * give the same up to the order in which partial results are added):
  * q [L][batch][H][d], k_new / v_new [L][batch][G][d] (or NULL), out [L][batch][H][d], all contiguous. */
 int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, const void *k_new,

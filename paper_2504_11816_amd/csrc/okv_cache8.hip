@@ -438,6 +438,7 @@ struct Attn8 {
   float scale_log2e;               // log2(e) / sqrt(d)
   int32_t batch, main_slots, main_blocks, layers, appends;      // main_blocks: of a layer
   int32_t slot0;                   // of the layer's partial results
+  int32_t max_stretches;           // > 0: no plan was made; up to 64 sequences, whose lengths the wavefronts share out themselves
 };
 
 // The launch covers `layers` layers; a wavefront works for one of them.
@@ -585,22 +586,72 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
   const Shape8 s = a.c.s;
   const int layer = block / a.main_blocks, unit = (block - layer * a.main_blocks) * 4 + wave, str = unit / s.G, g = unit - str * s.G;
   of_layer(a, layer);
-  const int total = a.plan.head[0], span = a.plan.head[1];
-  if (str * span >= total) return;
-  const int4 begin = a.plan.stretch[str];
+  // The plan, or, for a step of up to 64 sequences, what plan8_kernel does with a lane per sequence: `upto` tiles with that of the lane, `row_of` its
+  // row of the table, `there` the sequences that have tiles.  It costs a launch 1 us and saves one of 2.6 to 4.7; the launch that
+  // joins the results finds the plan where plan8_kernel leaves it.
+  const bool own_plan = a.max_stretches > 0;
+  int upto = 0, row_of = 0, total, span;
+  uint64_t there = 0;
+  int4 begin;
+  if (own_plan) {
+    row_of = min(max(a.seqs && lane < a.batch ? a.seqs[lane] : lane, 0), s.max_seqs - 1);
+    const int tiles = lane < a.batch ? max(min(a.lens[row_of], s.max_pages << s.log2_T) - a.appends, 0) / kTile : 0;
+    there = __ballot(tiles > 0);
+    upto = tiles;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int other = __shfl_up(upto, o);
+      if (lane >= o) upto += other;
+    }
+    total = __builtin_amdgcn_readlane(upto, 63);
+    span = max((total + a.max_stretches - 1) / a.max_stretches, kMinSpan);
+    if (blockIdx.x == 0 && wave == 0) {
+      if (lane < a.batch) a.plan.prefix[lane + 1] = upto;
+      if (lane == 0) a.plan.prefix[0] = 0, a.plan.head[1] = span;
+    }
+    if (str * span >= total) return;
+    const int first = __popcll(__ballot(upto <= str * span));
+    begin = make_int4(first, first ? __builtin_amdgcn_readlane(upto, first - 1) : 0, __builtin_amdgcn_readlane(upto, first),
+                      __builtin_amdgcn_readlane(row_of, first));
+  } else {
+    total = a.plan.head[0], span = a.plan.head[1];
+    if (str * span >= total) return;
+    begin = a.plan.stretch[str];
+  }
   const int log2_tpp = s.log2_T - 5;
   const int64_t head_at = tile_at<D>(s, 0, 0, g) + 16 * lane;
   const int64_t tile_bytes = (int64_t)s.G * 2 * kTile * D;
   const int v_step = s.gg * kTile * D;
 
-  // where the loads are: tile `next` of sequence fb (row frow of the table), `left` more of them in this stretch
-  int t = str * span, left = min(span, total - t);
-  int fb = begin.x, frow = begin.w, next = t - begin.y, in_seq = min(begin.z - t, left), pages = 0, page0 = 0;
+  // where the loads are: tile `next` of sequence fb (row frow of the table), `f_left` more of it in this stretch, `ahead` of all
+  const int t0 = str * span;
+  int left = min(span, total - t0), ahead = left;
+  int fb = begin.x, frow = begin.w, next = t0 - begin.y, in_seq = min(begin.z - t0, left), f_left = in_seq, pages, page0;
   const auto look_up = [&]() {
     page0 = next >> log2_tpp;
     pages = clamp_page(a.c.table[(int64_t)frow * s.max_pages + min(page0 + lane, s.max_pages - 1)], s.n_pages);
   };
   look_up();
+  // the sequence after it: where it is takes three dependent loads, which are under way while this one's tiles are
+  int then_b = 0, then_row = 0, then_tiles = 0, then_pages = 0;
+  const auto look_ahead = [&](const int more) {      // `more` tiles of the stretch behind fb's
+    if (more <= 0) return;
+    int lo, hi;
+    if (own_plan) {
+      then_b = __builtin_ctzll(there & (~0ull << fb << 1));
+      lo = __builtin_amdgcn_readlane(upto, then_b - 1), hi = __builtin_amdgcn_readlane(upto, then_b);
+      then_row = __builtin_amdgcn_readlane(row_of, then_b);
+    } else {
+      then_b = fb;
+      do {
+        ++then_b;
+        lo = a.plan.prefix[then_b], hi = a.plan.prefix[then_b + 1];
+      } while (lo == hi);
+      then_row = min(max(a.seqs ? a.seqs[then_b] : then_b, 0), s.max_seqs - 1);
+    }
+    then_tiles = min(hi - lo, more);
+    then_pages = clamp_page(a.c.table[(int64_t)then_row * s.max_pages + min(lane, s.max_pages - 1)], s.n_pages);
+  };
   const uint8_t *at;
   const float *scale_from;
   const auto place = [&]() {
@@ -614,34 +665,30 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
   struct Buffer {
     u32x4 k[D / 32], v[D / 32];
     float2 scale;
+    int b, tiles;                                // its sequence, and that one's tiles in this stretch
   };
-  // The loads have a cursor of their own, one tile ahead: `ahead` tiles of the stretch are still to be asked for.  A tile's K and V are asked for
-  // together, when the one before has been reduced: K as soon as its registers are free and V later is 9 % slower (ragged grouped heads 437 us
-  // a case against 397), a second tile in flight no faster (401).
-  int f_left = in_seq, ahead = left;
+  // A tile's K and V are asked for together, when the one before has been reduced: K as soon as its registers are free and V later is 9 % slower
+  // (ragged grouped heads 437 us a case against 397), a second tile in flight no faster (401).
   const auto fetch = [&](Buffer &t) {
     if (ahead == 0) return;
     place();
     load_codes<D, FMT, NT>(t.k, at);
     load_codes<D, FMT, NT>(t.v, at + v_step);
     t.scale = *reinterpret_cast<const float2 *>(scale_from);
+    t.b = fb, t.tiles = in_seq;
     --ahead;
     ++next;
     if (--f_left == 0 && ahead > 0) {            // the next tile is another sequence's
-      int lo, hi;
-      do {
-        ++fb;
-        lo = a.plan.prefix[fb], hi = a.plan.prefix[fb + 1];
-      } while (lo == hi);
-      frow = min(max(a.seqs ? a.seqs[fb] : fb, 0), s.max_seqs - 1);
-      next = 0;
-      f_left = min(hi - lo, ahead);
-      look_up();
+      fb = then_b, frow = then_row, pages = then_pages;
+      next = page0 = 0;
+      f_left = in_seq = then_tiles;
+      look_ahead(ahead - in_seq);
     }
   };
   Buffer tile;
+  look_ahead(ahead - in_seq);
   fetch(tile);
-  int b = begin.x, piece = in_seq;               // sequence at hand, tiles of it to go
+  int b = tile.b, piece = tile.tiles;            // sequence at hand, tiles of it to go
   half8 q[D / 32];
   Softmax8<D> acc;
   load_q<D>(q, a, b, g, lane);
@@ -668,12 +715,7 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
     if (--piece == 0) {
       acc.write(a, str + b, g, lane);
       if (left > 1) {
-        int first, end;
-        do {
-          ++b;
-          first = a.plan.prefix[b], end = a.plan.prefix[b + 1];
-        } while (first == end);
-        piece = min(end - first, left - 1);
+        b = tile.b, piece = tile.tiles;
         load_q<D>(q, a, b, g, lane);
         acc.clear();
       }
@@ -910,7 +952,7 @@ int rows_call(const char *who, bool store, const okv8_cache *c, int32_t layer, i
 bool streamed(const okv8_cache *c) { return codes_layer_bytes(c) * c->n_layers > (int64_t)256 << 20; }
 
 // w.layers layers from `layer` on, as far as there are
-int attend(const char *who, const okv8_cache *c, const okv8_step *s, const Workspace8 &w, int32_t layer, int32_t layers, const void *q, int64_t q_stride,
+int attend(const char *who, const okv8_cache *c, const okv8_step *s, const Workspace8 &w, bool planned, int32_t layer, int32_t layers, const void *q, int64_t q_stride,
            const void *k_new, const void *v_new, int64_t kv_stride, void *out) {
   char *base = static_cast<char *>(s->workspace);
   const hipStream_t stream = static_cast<hipStream_t>(s->stream);
@@ -925,6 +967,7 @@ int attend(const char *who, const okv8_cache *c, const okv8_step *s, const Works
   a.codes_layer = codes_layer_bytes(c), a.scales_layer = scales_layer_floats(c), a.tails_layer = tails_layer_halves(c);
   a.scale_log2e = (float)(1.4426950408889634 / (c->head_dim == 128 ? 11.313708498984761 : 8.0));
   a.batch = s->batch, a.main_slots = w.slots, a.appends = s->appends, a.layers = layers, a.slot0 = 0;
+  a.max_stretches = planned ? 0 : w.stretches;
   a.main_blocks = (w.stretches * c->n_kv_heads + 3) / 4;
   const int64_t blocks = (int64_t)layers * (a.main_blocks + (s->batch * c->n_kv_heads + 3) / 4);
   by_format<AttnLaunch8>(c, a, dim3((unsigned)blocks), streamed(c), stream);
@@ -972,7 +1015,8 @@ int64_t okv8_tails_bytes(const okv8_cache *c) {
 int64_t okv8_workspace_bytes(const okv8_cache *c, int32_t max_batch) {
   if (const char *why = shape_problem(c)) return report(OKV_EINVAL, "okv8_workspace_bytes: %s", why);
   if (max_batch < 1 || max_batch > OKV8_MAX_BATCH) return report(OKV_EINVAL, "okv8_workspace_bytes: batch must be in [1, %d]", OKV8_MAX_BATCH);
-  return workspace_of(c, max_batch, std::min(c->n_layers, kLayersAbreast)).bytes;
+  // (a launch of several layers cuts the sequences less often: with few of them it may need less than one of a single layer)
+  return std::max(workspace_of(c, max_batch, 1).bytes, workspace_of(c, max_batch, std::min(c->n_layers, kLayersAbreast)).bytes);
 }
 
 int okv8_store(const okv8_cache *c, int32_t layer, int32_t n_layers, int32_t batch, const int32_t *seqs, const int32_t *starts,
@@ -1000,7 +1044,7 @@ int okv8_decode_attn(const okv8_cache *c, const okv8_step *s, int32_t layer, con
   if (q_stride < (int64_t)c->n_q_heads * c->head_dim || q_stride % 8 ||
       (s->appends && (kv_stride < (int64_t)c->n_kv_heads * c->head_dim || kv_stride % 8)))
     return report(OKV_EINVAL, "okv8_decode_attn: strides must be multiples of 8 and at least a row");
-  return attend("okv8_decode_attn", c, s, workspace_of(c, s->batch, 1), layer, 1, q, q_stride, k_new, v_new, kv_stride, out);
+  return attend("okv8_decode_attn", c, s, workspace_of(c, s->batch, 1), true, layer, 1, q, q_stride, k_new, v_new, kv_stride, out);
 }
 
 int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, const void *k_new, const void *v_new, void *out) {
@@ -1010,11 +1054,12 @@ int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, con
   if ((k_new != nullptr) != (s->appends == 1) || (v_new != nullptr) != (s->appends == 1))
     return report(OKV_EINVAL, "okv8_decode_step: k_new and v_new are given if, and only if, the step appends");
   const Workspace8 w = workspace_for(c, s);
-  int rc = begin("okv8_decode_step", c, s, w);
+  const bool planned = s->batch > 64;
+  int rc = planned ? begin("okv8_decode_step", c, s, w) : OKV_OK;
   const int64_t q_row = (int64_t)c->n_q_heads * c->head_dim, kv_row = (int64_t)c->n_kv_heads * c->head_dim;
   for (int32_t l = 0; rc == OKV_OK && l < c->n_layers; l += w.layers) {
     const auto at = [&](const void *p, int64_t row, int64_t size) { return p ? static_cast<const char *>(p) + l * s->batch * row * size : nullptr; };
-    rc = attend("okv8_decode_step", c, s, w, l, std::min(w.layers, c->n_layers - l), at(q, q_row, 2), q_row, at(k_new, kv_row, 2), at(v_new, kv_row, 2), kv_row,
+    rc = attend("okv8_decode_step", c, s, w, planned, l, std::min(w.layers, c->n_layers - l), at(q, q_row, 2), q_row, at(k_new, kv_row, 2), at(v_new, kv_row, 2), kv_row,
                 const_cast<char *>(at(out, q_row, c->out_dtype ? 4 : 2)));
   }
   return rc;

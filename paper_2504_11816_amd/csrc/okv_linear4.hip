@@ -85,6 +85,15 @@ __device__ __forceinline__ half8 unpack4bit(const uint32_t w, const half2v near,
   return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The value N lanes before, around the row of 16 lanes
+template <int N>
+__device__ __forceinline__ half8 turn(const half8 x) {
+  u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[i], 0x120 + N, 0xf, 0xf, false);
+  return __builtin_bit_cast(half8, w);
+}
+
 template <class T, int N>
 struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Few {
   T v[N];
@@ -92,7 +101,10 @@ struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Few {
 
 // MF fragments of 16 rows and NT tiles of 16 features per workgroup, WAVES wavefronts that take the blocks of 128 inputs in turn, DEPTH blocks in
 // flight each; GROUPS groups in a block.  Workgroups (x, y, z): tiles, cuts of the inputs, rows.
-template <int MF, int NT, int WAVES, int DEPTH, int GROUPS, bool ZEROS>
+// FOUR: up to 4 rows.  What bounds few rows is the number of loads, and a fragment's four loads bring 4 rows' 16 bytes a lane four times over:
+// one load brings all of a block's 128 inputs, lane 4 j + i of a row of 16 lanes row i's part of product j, which turns into place by 4 j
+// lanes.  us, 1 row: 4096 x 16384 14.3 -> 11.9, 4096 x 4096 5.4 -> 5.0.
+template <int MF, int NT, int WAVES, int DEPTH, bool FOUR, int GROUPS, bool ZEROS>
 __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
   __shared__ floatx4 shares[WAVES][MF * NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -105,12 +117,12 @@ __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
   floatx4 sum[MF][NT] = {};
   const _Float16 *row[MF];               // rows that there are not are the last one: what they give is not stored
 #pragma unroll
-  for (int f = 0; f < MF; ++f) row[f] = a.x + (int64_t)min(row0 + 16 * f + r, a.m - 1) * a.n_in + 8 * quarter;
+  for (int f = 0; f < MF; ++f) row[f] = a.x + (int64_t)min(row0 + 16 * f + (FOUR ? r % 4 : r), a.m - 1) * a.n_in + (FOUR ? 32 * (r / 4) : 0) + 8 * quarter;
   struct Block {
     u32x4 w[NT];
     Few<u32x2, GROUPS> scale[NT];
     Few<uint8_t, GROUPS> zero[NT];
-    half8 x[MF][4];
+    half8 x[MF][FOUR ? 1 : 4];
   } in[DEPTH];
   const half8 none = {};
   const auto load = [&](Block &k, const int b) {
@@ -121,11 +133,16 @@ __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
       k.scale[t] = *reinterpret_cast<const Few<u32x2, GROUPS> *>(a.scales + (at * 4 + quarter) * 4 * GROUPS);
       if (ZEROS) k.zero[t] = *reinterpret_cast<const Few<uint8_t, GROUPS> *>(a.zeros + (at * 16 + r) * GROUPS);
     }
+    if constexpr (FOUR) {
+      const int i = b * kBlockIn;
+      k.x[0][0] = i + 32 * (r / 4) < a.n_in ? *reinterpret_cast<const half8 *>(row[0] + i) : none;
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = b * kBlockIn + 32 * j;
+      for (int j = 0; j < 4; ++j) {
+        const int i = b * kBlockIn + 32 * j;
 #pragma unroll
-      for (int f = 0; f < MF; ++f) k.x[f][j] = i < a.n_in ? *reinterpret_cast<const half8 *>(row[f] + i) : none;
+        for (int f = 0; f < MF; ++f) k.x[f][j] = i < a.n_in ? *reinterpret_cast<const half8 *>(row[f] + i) : none;
+      }
     }
   };
 #pragma unroll
@@ -137,6 +154,13 @@ __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
       const int b = b0 + i * WAVES;
       if (b >= last) break;
       const Block &k = in[i];
+      half8 turned[FOUR ? 4 : 1];
+      if constexpr (FOUR) {
+        turned[0] = k.x[0][0];
+        turned[1] = turn<12>(k.x[0][0]);
+        turned[2] = turn<8>(k.x[0][0]);
+        turned[3] = turn<4>(k.x[0][0]);
+      }
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -153,7 +177,7 @@ __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
             if (kApart) asm volatile("" : "+v"(w));
             const half8 v = unpack4bit(w, near, far);
 #pragma unroll
-            for (int f = 0; f < MF; ++f) part[f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, k.x[f][j], part[f], 0, 0, 0);
+            for (int f = 0; f < MF; ++f) part[f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, FOUR ? turned[FOUR ? j : 0] : k.x[f][FOUR ? 0 : j], part[f], 0, 0, 0);
           }
           const uint32_t s0 = k.scale[t].v[g][0], s1 = k.scale[t].v[g][1];
           const half2v lo = __builtin_bit_cast(half2v, s0), hi = __builtin_bit_cast(half2v, s1);
@@ -312,17 +336,17 @@ int hip_result(const char *who) {
   return e == hipSuccess ? OKV_OK : report(OKV_EHIP, "%s: %s", who, hipGetErrorString(e));
 }
 
-template <int MF, int NT, int WAVES, int DEPTH>
+template <int MF, int NT, int WAVES, int DEPTH, bool FOUR = false>
 void launch(const Linear4Args &a, int group, hipStream_t stream) {
   const dim3 grid((unsigned)((a.n_out / 16 + NT - 1) / NT), (unsigned)a.cuts, (unsigned)((a.m + 16 * MF - 1) / (16 * MF))), block(64 * WAVES);
   if (a.zeros) {
-    if (group == 128) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, 1, true>), grid, block, 0, stream, a);
-    else if (group == 64) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, 2, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, 4, true>), grid, block, 0, stream, a);
+    if (group == 128) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, FOUR, 1, true>), grid, block, 0, stream, a);
+    else if (group == 64) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, FOUR, 2, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, FOUR, 4, true>), grid, block, 0, stream, a);
   } else {
-    if (group == 128) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, 1, false>), grid, block, 0, stream, a);
-    else if (group == 64) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, 2, false>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, 4, false>), grid, block, 0, stream, a);
+    if (group == 128) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, FOUR, 1, false>), grid, block, 0, stream, a);
+    else if (group == 64) hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, FOUR, 2, false>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((linear4_kernel<MF, NT, WAVES, DEPTH, FOUR, 4, false>), grid, block, 0, stream, a);
   }
 }
 
@@ -430,7 +454,16 @@ int okv_linear4(const void *x, const void *packed, const void *bias, const void 
   const Choice c = choose(m, n_out, n_in, workspace && aligned16(workspace) ? workspace_bytes : 0);
   a.cuts = c.cuts, a.shares = static_cast<float *>(workspace);
   // wavefronts and blocks in flight of each: as measured for 16, 32 and 64 rows (registers bound both)
-  if (m <= 16) {
+  if (m <= 4) {
+    switch (c.tiles) {
+      case 1: launch<1, 1, 16, 2, true>(a, group, st); break;
+      case 2: launch<1, 2, 8, 2, true>(a, group, st); break;
+      case 3: launch<1, 3, 16, 1, true>(a, group, st); break;
+      case 4: launch<1, 4, 16, 1, true>(a, group, st); break;
+      case 6: launch<1, 6, 8, 1, true>(a, group, st); break;
+      default: launch<1, 8, 8, 1, true>(a, group, st); break;
+    }
+  } else if (m <= 16) {
     switch (c.tiles) {
       case 1: launch<1, 1, 16, 2>(a, group, st); break;
       case 2: launch<1, 2, 8, 2>(a, group, st); break;

@@ -309,3 +309,32 @@ def test_wrong_tensors_are_refused():
         Cache8(n_layers=1, n_q_heads=4, n_kv_heads=2, head_dim=64, page_tokens=32, n_pages=4, max_seqs=1, max_pages_per_seq=4, format="int4", device=DEV)
     with pytest.raises(binding.OkvError):
         Cache8(n_layers=1, n_q_heads=4, n_kv_heads=2, head_dim=80, page_tokens=32, n_pages=4, max_seqs=1, max_pages_per_seq=4, device=DEV)
+
+
+@pytest.mark.parametrize("lens", [[0, 0, 70, 0, 33, 1, 300, 0], [0], [5], [1000] * 3 + [0] * 4 + [64] * 57, [31] * 64, [32] * 64, [40, 0, 700] * 25], ids=lambda x: f"{len(x)}x{x[0]}")
+@pytest.mark.parametrize("H,G,d", [(8, 2, 64), (3, 3, 128)])
+def test_steps_of_all_layers(lens, H, G, d):
+    """okv8_decode_step: up to 64 sequences share their lengths out in the launch itself, more have them shared out by a launch before; sequences without
+    a tile among others; a workspace for one layer only."""
+    rng = np.random.default_rng(len(lens))
+    L, B = 3, len(lens)
+    c = make(rng, lens, L=L, H=H, G=G, d=d, T=32)
+    k, v = ([rows_of(rng, max(n, 1), G, d) for n in lens] for _ in range(2))
+    store(c, [x[:max(n - 1, 0)] for x, n in zip(k, lens)], [x[:max(n - 1, 0)] for x, n in zip(v, lens)], [max(n - 1, 0) for n in lens])
+    q = rng.standard_normal((L, B, H, d)).astype(np.float16)
+    kn, vn = (np.stack([x[max(n - 1, 0)] for x, n in zip(p, lens)])[None].repeat(L, 0) for p in (k, v))
+    out, now = torch.empty((L, B, H, d), device=DEV), dev(lens, torch.int32)
+    for appends, layers_abreast in ((True, L), (False, L), (False, 1)):
+        if layers_abreast == 1:
+            one = binding.Okv8Cache.from_buffer_copy(c.c)
+            one.n_layers = 1
+            c._step.workspace_bytes = binding.lib().okv8_workspace_bytes(one, B)
+        out.fill_(float("nan"))
+        c.step(dev(q), dev(kn) if appends else None, dev(vn) if appends else None, out, now)
+        got = out.double().cpu().numpy()
+        for b in sorted({0, 1, 2, B // 2, B - 2, B - 1} & set(range(B))):
+            for layer in range(L):
+                want = oracle.attend(q[layer, b], k[b], v[b], lens[b], "int8", appends)
+                err = np.linalg.norm(got[layer, b] - want, axis=1) / np.maximum(np.linalg.norm(want, axis=1), 1e-30) if lens[b] else np.abs(got[layer, b])
+                assert err.max() <= 7e-5, (b, layer, appends)
+        assert np.isfinite(got).all()
