@@ -22,17 +22,18 @@ TILE = 32
 
 
 def _address(t):
-    return 0 if t is None else t.data_ptr()
+    return None if t is None else t.data_ptr()
 
 
-def need(name, t, dtype, device, shape=None, dims=None):
-    """Raises unless t is a contiguous tensor of this type, on this device, of this shape."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor on {device}")
-    if (shape is not None and tuple(t.shape) != tuple(shape)) or (dims is not None and t.dim() != dims):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}" + (f", {tuple(shape)} is wanted" if shape is not None else ""))
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+def _fits(t, dtype, shape, device):
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.device == device
+
+
+def need(name, t, dtype, shape, device):
+    """Raises unless t is a contiguous tensor of this type and shape on this device."""
+    if not isinstance(t, torch.Tensor) or not _fits(t, dtype, shape, device):
+        what = f"{t.dtype} {list(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}, it is {what}")
 
 
 class Cache8:
@@ -63,7 +64,7 @@ class Cache8:
             n_layers, max_seqs, 2, n_kv_heads, TILE, head_dim)
         if table is None:
             table = torch.full((max_seqs, max_pages_per_seq), -1, dtype=torch.int32, device=self.device)
-        need("table", table, torch.int32, self.device, (max_seqs, max_pages_per_seq))
+        need("table", table, torch.int32, (max_seqs, max_pages_per_seq), self.device)
         self.table = table
         self.lens = torch.zeros(max_seqs, dtype=torch.int32, device=self.device)
         c.codes, c.scales, c.tails, c.page_table = (x.data_ptr() for x in (self.codes, self.scales, self.tails, self.table))
@@ -76,46 +77,56 @@ class Cache8:
         self.workspace = torch.empty(bytes_of("okv8_workspace_bytes", n), dtype=torch.uint8, device=self.device)
         self._step = binding.Okv8Step(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace.numel())
         self._step_ref = ctypes.byref(self._step)
-        self._decode_step = binding.lib().okv8_decode_step
+        lib = binding.lib()
+        self._store, self._load, self._decode_step = lib.okv8_store, lib.okv8_load, lib.okv8_decode_step
 
     # ---- prompts ----------------------------------------------------------------------------------
 
-    def _rows(self, fn, k, v, starts, lens, seqs, layer):
-        n_layers = k.shape[0] if k.dim() == 4 else 1
-        batch = starts.numel() - 1
-        shape = (*k.shape[:-2], self.G, self.d)
-        for name, t in (("k", k), ("v", v)):
-            if t.dtype != torch.float16 or t.device != self.device or tuple(t.shape) != shape or t.dim() not in (3, 4):
-                raise ValueError(f"{name} must be fp16 [layers][rows][{self.G}][{self.d}] (or one layer's) on {self.device}")
-            if t.numel() and (t[..., 0, :, :].stride()[-2:] != (self.d, 1) or any(a != b for a, b, n in zip(t.stride(), k.stride(), k.shape) if n > 1)):
+    # (A small call is as short on the GPU as on the host: checks are written so that tensors as they should be pass in a few tests.)
+    def _rows(self, call, k, v, starts, lens, seqs, layer):
+        shape, half, G, d, device = k.shape, torch.float16, self.G, self.d, self.device
+        if (k.dtype is not half or v.dtype is not half or v.shape != shape or len(shape) not in (3, 4) or shape[-1] != d or shape[-2] != G or k.device != device
+                or v.device != device):
+            raise ValueError(f"k and v must be fp16 [layers][rows][{G}][{d}] (or one layer's) on {device}, alike")
+        n_layers, rows = shape[0] if len(shape) == 4 else 1, shape[-3]
+        if k.is_contiguous() and v.is_contiguous():
+            row_stride, layer_stride = G * d, rows * G * d
+        else:
+            if rows and n_layers and (k[..., 0, :, :].stride()[-2:] != (d, 1) or any(x != y for x, y, n in zip(k.stride(), v.stride(), shape) if n > 1)):
                 raise ValueError("the heads of a row must be contiguous, k and v laid out alike")
-        self._seqs(seqs, batch)
-        need("starts", starts, torch.int32, self.device, dims=1)
-        need("lens", lens, torch.int32, self.device, dims=1)
-        if lens.numel() < (self.max_seqs if seqs is not None else batch):
-            raise ValueError("lens has an entry per row of the table (per sequence where seqs is None)")
-        binding._check(fn(self.ref, layer, n_layers, batch, _address(seqs), starts.data_ptr(), lens.data_ptr(), k.shape[-3], k.data_ptr(), v.data_ptr(),
-                          k.stride(-3) if k.shape[-3] > 1 else self.G * self.d, k.stride(0) if n_layers > 1 else 0, binding.current_stream(self.device)))
+            row_stride, layer_stride = k.stride(-3) if rows > 1 else G * d, k.stride(0) if n_layers > 1 else 0
+        batch = self._batch(starts, lens, seqs)
+        rc = call(self.ref, layer, n_layers, batch, _address(seqs), starts.data_ptr(), lens.data_ptr(), rows, k.data_ptr(), v.data_ptr(), row_stride, layer_stride,
+                  binding.current_stream(device))
+        if rc:
+            binding._check(rc)
 
-    def _seqs(self, seqs, batch):
+    def _batch(self, starts, lens, seqs):
+        batch = starts.shape[0] - 1 if starts.dim() == 1 else -1
+        if starts.dtype is not torch.int32 or batch < 0 or not starts.is_contiguous() or starts.device != self.device:
+            raise ValueError(f"starts must be an int32 vector of an entry more than there are sequences, on {self.device}")
+        self._lens(lens, seqs, batch)
+        return batch
+
+    def _lens(self, lens, seqs, batch):
+        if lens.dtype is not torch.int32 or lens.dim() != 1 or not lens.is_contiguous() or lens.device != self.device or lens.shape[0] < (batch if seqs is None else self.max_seqs):
+            raise ValueError(f"lens must be an int32 vector on {self.device} with an entry per row of the table (per sequence where seqs is None)")
         if seqs is not None:
-            need("seqs", seqs, torch.int32, self.device, (batch,))
+            need("seqs", seqs, torch.int32, (batch,), self.device)
 
     def store(self, k, v, starts, lens, seqs=None, layer=0):
         """Stores rows starts[b] .. starts[b + 1] - 1 of k, v (fp16 [layers][rows][G][d], from `layer` on; or one layer's [rows][G][d]) as the last tokens of
         sequence b, which then has lens[...] of them: lens is indexed by row of the table, seqs says which row each sequence is (None: b)."""
-        self._rows(binding.lib().okv8_store, k, v, starts, lens, seqs, layer)
+        self._rows(self._store, k, v, starts, lens, seqs, layer)
 
     def load(self, k, v, starts, lens, seqs=None, layer=0):
         """The reverse: the values that the cache holds, into k and v."""
-        self._rows(binding.lib().okv8_load, k, v, starts, lens, seqs, layer)
+        self._rows(self._load, k, v, starts, lens, seqs, layer)
 
     # ---- decode steps -----------------------------------------------------------------------------
 
     def _describe(self, batch, appends, lens, seqs):
-        if lens.dtype != torch.int32 or lens.device != self.device or lens.numel() < (self.max_seqs if seqs is not None else batch) or not lens.is_contiguous():
-            raise ValueError("lens must be int32 with an entry per row of the table (per sequence where seqs is None)")
-        self._seqs(seqs, batch)
+        self._lens(lens, seqs, batch)
         s = self._step
         s.batch, s.appends, s.seqs, s.lens, s.stream = batch, appends, _address(seqs), lens.data_ptr(), binding.current_stream(self.device)
 
@@ -130,7 +141,7 @@ class Cache8:
         batch = self._step.batch
         if q.dtype != torch.float16 or tuple(q.shape) != (batch, self.H, self.d) or q.stride(2) != 1 or q.stride(1) != self.d:
             raise ValueError(f"q must be fp16 [{batch}][{self.H}][{self.d}], rows may be strided")
-        need("out", out, self.out_dtype, self.device, (batch, self.H, self.d))
+        need("out", out, self.out_dtype, (batch, self.H, self.d), self.device)
         kv_stride = 0
         if k_new is not None:
             for t in (k_new, v_new):
@@ -143,13 +154,17 @@ class Cache8:
     def step(self, q, k_new, v_new, out, lens, seqs=None):
         """One step of all layers whose inputs are there: q [L][batch][H][d], k_new / v_new [L][batch][G][d] or None (nothing is appended),
         out [L][batch][H][d].  lens: keys attended, an appended one included."""
-        batch = q.shape[1]
-        need("q", q, torch.float16, self.device, (self.L, batch, self.H, self.d))
-        need("out", out, self.out_dtype, self.device, (self.L, batch, self.H, self.d))
+        L, H, d, device = self.L, self.H, self.d, self.device
+        batch = q.shape[1] if q.dim() == 4 else 0
+        if not _fits(q, torch.float16, (L, batch, H, d), device) or not _fits(out, self.out_dtype, (L, batch, H, d), device):
+            need("q", q, torch.float16, (L, batch, H, d), device)
+            need("out", out, self.out_dtype, (L, batch, H, d), device)
         if (k_new is None) != (v_new is None):
             raise ValueError("k_new and v_new come together")
-        if k_new is not None:
-            need("k_new", k_new, torch.float16, self.device, (self.L, batch, self.G, self.d))
-            need("v_new", v_new, torch.float16, self.device, (self.L, batch, self.G, self.d))
-        self._describe(batch, int(k_new is not None), lens, seqs)
-        binding._check(self._decode_step(self.ref, self._step_ref, q.data_ptr(), _address(k_new), _address(v_new), out.data_ptr()))
+        if k_new is not None and not (_fits(k_new, torch.float16, (L, batch, self.G, d), device) and _fits(v_new, torch.float16, (L, batch, self.G, d), device)):
+            need("k_new", k_new, torch.float16, (L, batch, self.G, d), device)
+            need("v_new", v_new, torch.float16, (L, batch, self.G, d), device)
+        self._describe(batch, 0 if k_new is None else 1, lens, seqs)
+        rc = self._decode_step(self.ref, self._step_ref, q.data_ptr(), _address(k_new), _address(v_new), out.data_ptr())
+        if rc:
+            binding._check(rc)

@@ -20,8 +20,9 @@ class PageArray:
         if tensor.dim() < 2 or not tensor[0].is_contiguous():
             raise ValueError("a page array is [layers][n_pages][...], every layer contiguous")
         self.tensor = tensor
-        page_bytes = tensor[0, 0].numel() * tensor.element_size()
-        self.c = binding.OkvPageArray(tensor.data_ptr(), page_bytes, tensor.stride(0) * tensor.element_size(), unit_tokens, int(whole_units))
+        self.layers, self.pages, self.device = tensor.shape[0], tensor.shape[1], tensor.device
+        self.page_bytes = tensor[0, 0].numel() * tensor.element_size()
+        self.c = binding.OkvPageArray(tensor.data_ptr(), self.page_bytes, tensor.stride(0) * tensor.element_size(), unit_tokens, int(whole_units))
 
 
 class RowArray:
@@ -41,7 +42,7 @@ class Pages:
     """table [max_seqs][max_pages_per_seq], lens [max_seqs], refs [n_pages]: int32 tensors that the calls read and write (new ones: -1, 0, 0)."""
 
     def __init__(self, *, table, lens, refs, page_tokens, arrays=(), rows=()):
-        self.device = table.device
+        self.device, self._lib = table.device, binding.lib()
         for name, t, dims in (("table", table, 2), ("lens", lens, 1), ("refs", refs, 1)):
             if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != self.device:
                 raise ValueError(f"{name} must be a contiguous int32 tensor of {dims} dimension(s) on {self.device}")
@@ -70,43 +71,48 @@ class Pages:
         self.ref = ctypes.byref(c)
 
     def _ids(self, name, t, n=None):
-        if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != self.device:
+        if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != self.device:
             raise ValueError(f"{name} must be a contiguous int32 vector on {self.device}")
-        if n is not None and t.numel() != n:
-            raise ValueError(f"{name} has {t.numel()} entries, {n} are wanted")
+        if n is not None and t.shape[0] != n:
+            raise ValueError(f"{name} has {t.shape[0]} entries, {n} are wanted")
         return t.data_ptr()
+
+    def _done(self, rc):
+        if rc:
+            binding._check(rc)
 
     def extend(self, seqs, n_new=None):
         """Sequence seqs[i] grows by n_new[i] tokens (None: one each) and takes the pages that it lacks."""
-        at = self._ids("seqs", seqs)
-        binding._check(binding.lib().okv_pages_extend(self.ref, seqs.numel(), at, None if n_new is None else self._ids("n_new", n_new, seqs.numel()),
-                                                      binding.current_stream(self.device)))
+        at, n = self._ids("seqs", seqs), seqs.shape[0]
+        self._done(self._lib.okv_pages_extend(self.ref, n, at, None if n_new is None else self._ids("n_new", n_new, n), binding.current_stream(self.device)))
 
     def fork(self, src, dst):
         """Sequence dst[i] (empty) becomes a fork of src[i]: shares its full pages, copies the rest."""
-        at = self._ids("src", src)
-        binding._check(binding.lib().okv_pages_fork(self.ref, src.numel(), at, self._ids("dst", dst, src.numel()), binding.current_stream(self.device)))
+        at, n = self._ids("src", src), src.shape[0]
+        self._done(self._lib.okv_pages_fork(self.ref, n, at, self._ids("dst", dst, n), binding.current_stream(self.device)))
 
     def free(self, seqs):
-        at = self._ids("seqs", seqs)
-        binding._check(binding.lib().okv_pages_free(self.ref, seqs.numel(), at, binding.current_stream(self.device)))
+        """The sequences become empty; pages that belong to no other are free."""
+        self._done(self._lib.okv_pages_free(self.ref, seqs.shape[0], self._ids("seqs", seqs), binding.current_stream(self.device)))
 
     def compact(self):
         """Pages in use become 0 .. n_used - 1 (status[1] says how many, status[2] how many were moved)."""
-        binding._check(binding.lib().okv_pages_compact(self.ref, binding.current_stream(self.device)))
+        self._done(self._lib.okv_pages_compact(self.ref, binding.current_stream(self.device)))
 
     def copy(self, src_ids, dst_ids, to=None):
         """Copies pages src_ids[i] to pages dst_ids[i] of the arrays `to` (PageArrays like this cache's; None: this cache's own)."""
         to = self.arrays if to is None else to
-        if len(to) != len(self.arrays) or any(t.c.page_bytes != a.c.page_bytes or t.tensor.shape[0] != a.tensor.shape[0] or t.tensor.device != self.device
-                                              for t, a in zip(to, self.arrays)):
-            raise ValueError("`to` has an array for each of the cache's, with the same layers and page sizes")
+        if len(to) != len(self.arrays):
+            raise ValueError("`to` has an array for each of the cache's")
         if not to:
             return
-        c = (binding.OkvPageArray * len(to))(*[t.c for t in to])
-        at = self._ids("src_ids", src_ids)
-        binding._check(binding.lib().okv_pages_copy(self.ref, src_ids.numel(), at, self._ids("dst_ids", dst_ids, src_ids.numel()), c,
-                                                    min(t.tensor.shape[1] for t in to), binding.current_stream(self.device)))
+        pages, c = 0x7fffffff, (binding.OkvPageArray * len(to))()
+        for i, (t, a) in enumerate(zip(to, self.arrays)):
+            if t.page_bytes != a.page_bytes or t.layers != a.layers or t.device != self.device:
+                raise ValueError("`to` has an array for each of the cache's, with the same layers and page sizes")
+            c[i], pages = t.c, min(pages, t.pages)
+        at, n = self._ids("src_ids", src_ids), src_ids.shape[0]
+        self._done(self._lib.okv_pages_copy(self.ref, n, at, self._ids("dst_ids", dst_ids, n), c, pages, binding.current_stream(self.device)))
 
     def check(self):
         """Waits for the GPU; raises if a call could not be carried out since the last check."""
