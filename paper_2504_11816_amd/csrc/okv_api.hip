@@ -205,7 +205,10 @@ int report(int code, const char *fmt, ...) {
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  g_error = buf;
+  try {
+    g_error = buf;
+  } catch (...) {                        // no memory for the message: the code alone
+  }
   return code;
 }
 }  // namespace okv

@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
   const int tile0 = blockIdx.x * NT, row0 = blockIdx.z * 16 * MF, n_tiles = a.n_out / 16;
   const int first = (int)((int64_t)a.blocks * blockIdx.y / a.cuts), last = (int)((int64_t)a.blocks * (blockIdx.y + 1) / a.cuts);
   const int r = lane % 16, quarter = lane / 16;
-  // Where there are many results, one tile and group after the other: the compiler would issue all their products first and spill.  (The empty
+  // Where there are many results, one tile after the other: the compiler would issue all their products first and spill.  (The empty
   // assembly statements keep their order.)
   constexpr bool kApart = GROUPS == 4 ? MF * NT > 2 : GROUPS == 2 && MF * NT >= 12;
   floatx4 sum[MF][NT] = {};
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
 #pragma unroll
           for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) {
             uint32_t w = k.w[t][j];
-            if (kApart) asm volatile("" : "+v"(w));
+            if (kApart && g == 0) asm volatile("" : "+v"(w));
             const half8 v = unpack4bit(w, near, far);
 #pragma unroll
             for (int f = 0; f < MF; ++f) part[f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, FOUR ? turned[FOUR ? j : 0] : k.x[f][FOUR ? 0 : j], part[f], 0, 0, 0);
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
           for (int f = 0; f < MF; ++f)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[f][t][e] = fmaf(part[f][e], (float)(e < 2 ? lo[e & 1] : hi[e & 1]), sum[f][t][e]);
-          if (kApart)
+          if (kApart && g == GROUPS - 1)
 #pragma unroll
             for (int f = 0; f < MF; ++f) asm volatile("" : "+v"(sum[f][t]));
         }
@@ -351,7 +351,7 @@ void launch(const Linear4Args &a, int group, hipStream_t stream) {
 }
 
 // Tiles of a workgroup and cuts of the inputs, by a model of the time (us, as measured with codes from HBM; the constants 2.6 us of every launch and
-// what is the same for all choices left out):  a block of 128 inputs takes a workgroup 0.057 for each tile (0.080 of more than four with few rows) and 0.022 + 0.0035 a row (0.0070 from
+// what is the same for all choices left out):  a block of 128 inputs takes a workgroup 0.057 for each tile (0.080 of more than four with few rows; up to 4 rows 0.0615, 0.1125, 0.181 and 0.256 for 1 to 4 of them) and 0.022 + 0.0035 a row (0.0070 from
 // the 17th on) for the rows, which it fetches through L2 whatever its tiles; one workgroup per compute unit at a time; cuts cost a
 // second launch, 2.2 (3.4 with few rows) and 1.0 for each MB of shares.  More tiles mean fewer fetches of the rows, cuts fill the compute units again.  us, tiles
 // x cuts: 1 row x 16384 x 4096 4 x 1 10.6, 8 x 1 14.5; 32 x 4096 x 4096 4 x 4 10.0, 1 x 1 11.5; 32 x 4096 x 16384 8 x 8 18.8, 1 x 1 34; 128 x 12288 x
@@ -371,7 +371,9 @@ Choice choose(int32_t m, int32_t n_out, int32_t n_in, int64_t workspace_bytes) {
       const double share_mb = 4e-6 * c * m * n_out;
       if (c > 1 && (blocks < 4 * c || (int64_t)c * m * n_out * 4 > workspace_bytes)) break;
       const int64_t groups = (int64_t)((n_tiles + t - 1) / t) * c * row_groups;
-      const double us = (double)((groups + kUnits - 1) / kUnits) * ((blocks + c - 1) / c) * ((t > 4 && m <= 16 ? 0.080 : 0.057) * t + per_rows) + (c > 1 ? (m <= 16 ? 3.4 : 2.2) + share_mb : 0.0);
+      const double per_block = m <= 4 ? (t == 1 ? 0.0615 : t == 2 ? 0.1125 : t == 3 ? 0.181 : t == 4 ? 0.256 : 0.090 * t)
+                                      : (t > 4 && m <= 16 ? 0.080 : 0.057) * t + per_rows;
+      const double us = (double)((groups + kUnits - 1) / kUnits) * ((blocks + c - 1) / c) * per_block + (c > 1 ? (m <= 16 ? 3.4 : 2.2) + share_mb : 0.0);
       if (us < best_us) best_us = us, best = {t, c};
     }
   return best;
@@ -457,7 +459,7 @@ int okv_linear4(const void *x, const void *packed, const void *bias, const void 
   if (m <= 4) {
     switch (c.tiles) {
       case 1: launch<1, 1, 16, 2, true>(a, group, st); break;
-      case 2: launch<1, 2, 8, 2, true>(a, group, st); break;
+      case 2: launch<1, 2, 8, 1, true>(a, group, st); break;
       case 3: launch<1, 3, 16, 1, true>(a, group, st); break;
       case 4: launch<1, 4, 16, 1, true>(a, group, st); break;
       case 6: launch<1, 6, 8, 1, true>(a, group, st); break;
