@@ -236,16 +236,17 @@ struct Packed {
   uint8_t *zeros;
 };
 
-// What a thread writes: one 32-bit word (8 inputs of a feature); code(n, k) is asked for inputs below n_in
-template <class Code>
-__device__ __forceinline__ uint32_t pack_word(const int64_t i, const int blocks, const int n_in, const Code &code) {
+// What a thread writes: one 32-bit word, 8 inputs of a feature; codes(n, k) are those of inputs k .. k + 7, a byte each
+template <class Codes>
+__device__ __forceinline__ uint32_t pack_word(const int64_t i, const int blocks, const int n_in, const Codes &codes) {
   const int64_t block = i >> 8;
   const int lane = (i >> 2) & 63, j = i & 3, n = (int)(block / blocks) * 16 + lane % 16;
   const int k = (int)(block % blocks) * kBlockIn + 32 * j + 8 * (lane / 16);
+  if (k >= n_in) return 0;
+  const uint64_t c = codes(n, k);
   uint32_t w = 0;
-  if (k < n_in)
 #pragma unroll
-    for (int p = 0; p < 4; ++p) w |= code(n, k + 2 * p) << (4 * p) | code(n, k + 2 * p + 1) << (16 + 4 * p);
+  for (int p = 0; p < 4; ++p) w |= (uint32_t)(c >> (16 * p) & 15u) << (4 * p) | (uint32_t)(c >> (16 * p + 8) & 15u) << (16 + 4 * p);
   return w;
 }
 
@@ -263,8 +264,14 @@ __global__ void __launch_bounds__(256) pack4_kernel(Packed to, const uint8_t *co
   const int64_t words = (int64_t)n_out / 16 * blocks * 256, all = (int64_t)n_out * padded;
   const int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   for (int64_t i = i0; i < words; i += step)
-    to.codes[i] = pack_word(i, blocks, n_in, [&](int n, int k) -> uint32_t {
-      return per_byte == 1 ? codes[(int64_t)n * n_in + k] & 15u : codes[((int64_t)n * n_in + k) >> 1] >> (4 * (k & 1)) & 15u;
+    to.codes[i] = pack_word(i, blocks, n_in, [&](int n, int k) -> uint64_t {
+      const int64_t at = (int64_t)n * n_in + k;
+      if (per_byte == 1) return *reinterpret_cast<const uint64_t *>(codes + at);
+      const uint32_t two = *reinterpret_cast<const uint32_t *>(codes + (at >> 1));
+      uint64_t c = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c |= (uint64_t)(two >> (4 * e) & 15u) << (8 * e);
+      return c;
     });
   for (int64_t i = i0; i < all; i += step) {
     const int n = (int)(i / padded), g = (int)(i % padded);
@@ -295,11 +302,17 @@ __global__ void __launch_bounds__(256) codes4_kernel(Packed to, const _Float16 *
   const int blocks = (n_in + kBlockIn - 1) / kBlockIn, padded = blocks * (kBlockIn / group);
   const int64_t words = (int64_t)n_out / 16 * blocks * 256;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256)
-    to.codes[i] = pack_word(i, blocks, n_in, [&](int n, int k) -> uint32_t {
+    to.codes[i] = pack_word(i, blocks, n_in, [&](int n, int k) -> uint64_t {
       const int g = k / group, per = kBlockIn / group;
       const float scale = (float)to.scales[scale_at(n, g, padded, per)], zero = to.zeros ? (float)to.zeros[zero_at(n, g, padded, per)] : 8.f;
-      const float q = scale > 0.f ? __builtin_rintf((float)src[(int64_t)n * n_in + k] / scale) : 0.f;
-      return (uint32_t)fminf(fmaxf(q + zero, 0.f), 15.f);
+      const half8 w = *reinterpret_cast<const half8 *>(src + (int64_t)n * n_in + k);
+      uint64_t c = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float q = scale > 0.f ? __builtin_rintf((float)w[e] / scale) : 0.f;
+        c |= (uint64_t)(uint32_t)fminf(fmaxf(q + zero, 0.f), 15.f) << (8 * e);
+      }
+      return c;
     });
 }
 
@@ -395,7 +408,7 @@ int64_t okv_linear4_packed_bytes(int32_t n_out, int32_t n_in, int32_t group, int
 int okv_linear4_pack(void *dst, const void *codes, int32_t per_byte, const void *scales, const void *zeros, int32_t n_out, int32_t n_in, int32_t group,
                      void *stream) {
   if (const char *why = shape_problem(n_out, n_in, group)) return report(OKV_EINVAL, "okv_linear4_pack: %s", why);
-  if (!dst || !codes || !scales || !aligned16(dst)) return report(OKV_EINVAL, "okv_linear4_pack: NULL or misaligned pointer");
+  if (!dst || !codes || !scales || !aligned16(dst) || !aligned16(codes)) return report(OKV_EINVAL, "okv_linear4_pack: NULL or misaligned pointer");
   if (per_byte != 1 && per_byte != 2) return report(OKV_EINVAL, "okv_linear4_pack: per_byte must be 1 or 2");
   const PackedLayout l = layout_of(n_out, n_in, group, zeros != nullptr);
   const int64_t words = (int64_t)n_out / 16 * l.blocks * 256;
