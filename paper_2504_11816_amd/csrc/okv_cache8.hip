@@ -42,7 +42,11 @@ constexpr int kTile = OKV8_TILE;
 #ifndef OKV8_WAVES
 #define OKV8_WAVES 1024
 #endif
-constexpr int kWaves = OKV8_WAVES;       // wavefronts of the part of a launch that reads codes: one per SIMD
+// Wavefronts of the part of a launch that reads codes: one per SIMD at d = 128, with 8 KiB in flight each, two at d = 64, where a tile is half that.  us of a
+// case of 4 layers x 2 of 32 x 1500 keys x 32 heads (d = 64) with 1024 / 2048 / 4096 of them 349 / 247 / 249; at d = 128 with 1024 / 1536 /
+// 2048: 32 x 768 keys x 32 heads 283 / 292 / 284, ragged grouped heads 388 / 402 / 399, two long documents 243 / 242 / 241, 16 x 100..400 keys x 12
+// heads 29 / - / 34.
+constexpr int kWaves = OKV8_WAVES;
 constexpr int kMinSpan = 2;              // tiles of a stretch at least
 
 struct Shape8 {
@@ -848,7 +852,7 @@ Cache8 cache_of(const okv8_cache *c, int32_t layer) {
 }
 
 // Stretches of a launch that covers this many layers: a wavefront for each (layer, stretch, KV head)
-int max_stretches(const okv8_cache *c, int layers) { return std::max(1, kWaves / (c->n_kv_heads * layers)); }
+int max_stretches(const okv8_cache *c, int layers) { return std::max(1, (c->head_dim == 64 ? 2 : 1) * kWaves / (c->n_kv_heads * layers)); }
 
 // The workspace: plan (head, prefix, stretches), then for every layer of a launch the partial results of batch + stretches slots and of batch tails.
 struct Workspace8 {
