@@ -16,6 +16,9 @@ Modules
   worklist      the tiling a split-K work list has to satisfy
   pipeline_sim  replay of a copy/attend op trace on a fake copy engine
   tail_sim      replay of "newest blocks stay in HBM" on sets of row positions
+  cache8        scales, codes and values of the 8-bit cache, and attention over them
+  pages         a model of extend, fork, free, compact and copy on page tables
+  linear4       packing and products of 4-bit weights with group scales
 
 Every function here is pinned by a CPU test (tests/test_oracle_*.py) to a
 closed form, an invariant, a library routine on a special case or brute

@@ -13,8 +13,8 @@
 //     the inputs; its wavefronts take blocks of 128 inputs in turn and add up through LDS.  (Rows staged in LDS for the whole workgroup,
 //     with a barrier per round of blocks, were 10 to 30 % slower from 16 to 256 rows.)
 //
-// Measured, codes from HBM, groups of 128: 1 row x 16384 x 4096 10.6 us (34.6 MB: 3.3 TB/s), x 12288 x 4096 8.6, x 4096 x 4096 5.2 (an empty launch
-// with its dependency is 2.6 of each); 32 rows 15.9, 14.0, 10.0; 256 rows x 16384 x 4096 62.9 (0.55 PFLOP/s).
+// Measured, codes from HBM, groups of 128, us: 1 row x 16384 x 4096 10.2 (34.6 MB: 3.4 TB/s), 12288 x 4096 8.7, 4096 x 4096 4.9, 4096 x 16384 11.5;
+// 32 rows 15.7, 13.9, 10.2, 18.9; 256 rows x 16384 x 4096 62.6 (0.55 PFLOP/s).
 #include "okv_linear4.h"
 #include "okv_report.h"
 
@@ -103,7 +103,7 @@ struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Few {
 // flight each; GROUPS groups in a block.  Workgroups (x, y, z): tiles, cuts of the inputs, rows.
 // FOUR: up to 4 rows.  What bounds few rows is the number of loads, and a fragment's four loads bring 4 rows' 16 bytes a lane four times over:
 // one load brings all of a block's 128 inputs, lane 4 j + i of a row of 16 lanes row i's part of product j, which turns into place by 4 j
-// lanes.  us, 1 row: 4096 x 16384 14.3 -> 11.9, 4096 x 4096 5.4 -> 5.0.
+// lanes.  us, 1 row, without it and with it: 4096 x 16384 14.3 and 11.8, 4096 x 4096 5.4 and 4.9.
 template <int MF, int NT, int WAVES, int DEPTH, bool FOUR, int GROUPS, bool ZEROS>
 __global__ void __launch_bounds__(64 * WAVES) linear4_kernel(Linear4Args a) {
   __shared__ floatx4 shares[WAVES][MF * NT][64];
@@ -363,12 +363,12 @@ void launch(const Linear4Args &a, int group, hipStream_t stream) {
   }
 }
 
-// Tiles of a workgroup and cuts of the inputs, by a model of the time (us, as measured with codes from HBM; the constants 2.6 us of every launch and
-// what is the same for all choices left out):  a block of 128 inputs takes a workgroup 0.057 for each tile (0.080 of more than four with few rows; up to 4 rows 0.0615, 0.1125, 0.181 and 0.256 for 1 to 4 of them) and 0.022 + 0.0035 a row (0.0070 from
-// the 17th on) for the rows, which it fetches through L2 whatever its tiles; one workgroup per compute unit at a time; cuts cost a
-// second launch, 2.2 (3.4 with few rows) and 1.0 for each MB of shares.  More tiles mean fewer fetches of the rows, cuts fill the compute units again.  us, tiles
-// x cuts: 1 row x 16384 x 4096 4 x 1 10.6, 8 x 1 14.5; 32 x 4096 x 4096 4 x 4 10.0, 1 x 1 11.5; 32 x 4096 x 16384 8 x 8 18.8, 1 x 1 34; 128 x 12288 x
-// 4096 6 x 1 26.7, 3 x 1 43.
+// Tiles of a workgroup and cuts of the inputs, by a model of the time (us, as measured with codes from HBM; what is the same for all choices
+// left out).  A block of 128 inputs takes a workgroup 0.057 for each tile (0.080 of more than four with 5 to 16 rows), and 0.022 + 0.0035 a row
+// (0.0070 from the 17th on) for the rows, which it fetches through L2 whatever its tiles; up to 4 rows, 0.0615, 0.1125, 0.181 and 0.256 in all
+// for 1 to 4 tiles and 0.090 each of more.  One workgroup per compute unit at a time.  Cuts cost a second launch, 2.2 (3.4 with up to 16 rows) and 1.0 for each MB of
+// shares.  More tiles mean fewer fetches of the rows, cuts fill the compute units again.  us, tiles x cuts: 32 rows x 4096 x 4096 4 x 4 10.0,
+// 1 x 1 11.5; 32 x 4096 x 16384 8 x 8 18.8, 1 x 1 34; 128 x 12288 x 4096 6 x 1 26.7, 3 x 1 43.
 struct Choice {
   int tiles, cuts;
 };

@@ -3,9 +3,9 @@
 // Two kinds of kernels.  What is decided -- which ids are free, who gets which, what moves where -- is prefix sums over a few thousand
 // integers: one workgroup of 1024 threads, a launch of 3 to 5 us.  What is moved is bound by HBM, twice its bytes: a workgroup takes 16 KiB,
 // four 16-byte loads of every thread in flight before the first store; loads through the caches (several forks read one page), stores past
-// them.  Measured, us: 48 forks of 256 KiB pages in 32 layers 118 (806 MB moved: 6.8 TB/s, a third of it read from HBM), 592 pages of 256 KiB
-// in 4 layers and 200 gathered 310 (5.3 TB/s); with 32 KiB a workgroup 200 and 471, with loads past the caches 158 and 314, stores through
-// them 144 and 337.
+// them.  Measured, us: 48 forks of 256 KiB pages in 32 layers 120 (403 MB written, 354 of the 403 MB read past L2), 592 pages of 256 KiB in 4
+// layers and 200 gathered 310 (5.4 TB/s, read and written); with 32 KiB a workgroup 200 and 471, with loads past the caches 158 and 314, stores
+// through them 144 and 337.
 #include "okv_pages.h"
 #include "okv_report.h"
 
