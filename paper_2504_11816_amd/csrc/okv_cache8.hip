@@ -704,7 +704,9 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
   acc.clear();
   for (;;) {
     float score[8];
-    const float scale_v = tile.scale.y == 0.f ? 1.f : tile.scale.y, by = tile.scale.x * a.scale_log2e, log2_v = __builtin_amdgcn_logf(scale_v);      // (scale 0: codes 0)
+    // A tile of zeros (scale 0, codes 0) has any scale, and takes one far below all others (at least 2^-33): m, which its scores may raise, would
+    // otherwise leave the other tiles' weights too few bits.  What it adds to l is at most 2^48 2^8 a key.
+    const float scale_v = tile.scale.y == 0.f ? 0x1p-48f : tile.scale.y, by = tile.scale.x * a.scale_log2e, log2_v = __builtin_amdgcn_logf(scale_v);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       floatx4 x = {0.f, 0.f, 0.f, 0.f};

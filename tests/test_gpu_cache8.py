@@ -338,3 +338,80 @@ def test_steps_of_all_layers(lens, H, G, d):
                 err = np.linalg.norm(got[layer, b] - want, axis=1) / np.maximum(np.linalg.norm(want, axis=1), 1e-30) if lens[b] else np.abs(got[layer, b])
                 assert err.max() <= 7e-5, (b, layer, appends)
         assert np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("H,G,d", [(4, 2, 64), (3, 3, 128)])
+@pytest.mark.parametrize("factors", [(0, 1, 0, 1, 0, 1), (1e4, 1e-4, 1, 0, 1e-4, 1e4), (1e-4, 1e4, 0, 1e-4, 1, 1e-4), (0, 0, 0, 0, 0, 0), (2e-6, 2e-6, 0, 2e-6, 0, 2e-6)])
+def test_tiles_of_zeros_and_of_magnitudes_far_apart(fmt, H, G, d, factors):
+    """A tile's V scale goes through the softmax's exponent and out of the sum again: tiles whose values are all zero count in the sum, and tiles of
+    large and of small values add up.  Weights below 2^-14 of the largest scaled one lose at most 2^-24 of it, with each of 203 keys: 203 2^-24 = 1.3e-5
+    of a vector on top of the 7e-5."""
+    rng = np.random.default_rng(d)
+    n = 32 * len(factors) + 11
+    k, v = rows_of(rng, n, G, d), rows_of(rng, n, G, d) / 8
+    for t, f in enumerate(factors):
+        v[32 * t:32 * t + 32] = (v[32 * t:32 * t + 32].astype(np.float64) * f).astype(np.float16)
+    if not any(factors):
+        v[:] = 0
+    assert np.isfinite(v).all()
+    c = make(rng, [n], H=H, G=G, d=d, fmt=fmt)
+    store(c, [k[:-1]], [v[:-1]], [n - 1])
+    q, out = rng.standard_normal((1, 1, H, d)).astype(np.float16), torch.full((1, 1, H, d), float("nan"), device=DEV)
+    c.step(dev(q), dev(k[None, -1:]), dev(v[None, -1:]), out, dev([n], torch.int32))
+    got, want = out[0, 0].double().cpu().numpy(), oracle.attend(q[0, 0], k, v, n, fmt, True)
+    err, size = np.linalg.norm(got - want, axis=1), np.linalg.norm(want, axis=1)
+    assert (err <= 8.5e-5 * size).all(), (err / np.maximum(size, 1e-30)).max()
+
+
+def test_numbers_that_are_none_stay_where_they_are():
+    """A NaN in one tile of one KV head makes that sequence's results of that head NaN, though other pieces of it are joined with the one that has it;
+    a query head that has one makes its own NaN; nothing else changes by a bit."""
+    rng = np.random.default_rng(21)
+    lens, H, G, d = [3000, 500, 40], 4, 2, 64
+    k, v = ([rows_of(rng, n, G, d) for n in lens] for _ in range(2))
+    q = rng.standard_normal((1, 3, H, d)).astype(np.float16)
+
+    def results(k, v, q):
+        c = make(np.random.default_rng(1), lens, H=H, G=G, d=d)
+        store(c, k, v, lens)
+        out = torch.full((1, 3, H, d), 7.0, device=DEV)
+        c.step(dev(q), None, None, out, dev(lens, torch.int32))
+        return out[0].cpu().numpy()
+
+    plain = results(k, v, q)
+    assert np.isfinite(plain).all()
+    for what in ("k", "v", "tail", "q nan", "q inf"):
+        kk, vv, qq = [x.copy() for x in k], [x.copy() for x in v], q.copy()
+        bad = np.zeros((3, H), bool)
+        if what == "k":
+            kk[0][1000, 1, 5], bad[0, 2:] = np.nan, True
+        elif what == "v":
+            vv[1][37, 0, 9], bad[1, :2] = np.inf, True
+        elif what == "tail":
+            kk[2][39, 0, 3], bad[2, :2] = np.nan, True
+        else:
+            qq[0, 1, 3, 7], bad[1, 3] = np.nan if what == "q nan" else np.inf, True
+        got = results(kk, vv, qq)
+        assert np.isnan(got[bad]).all(), what
+        assert np.array_equal(got[~bad], plain[~bad]), what
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("size", [1.0, 1e-3, 1e-5])
+@pytest.mark.parametrize("zeros", [(0,), (0, 2, 4), (3,), (5,), (0, 1, 2, 3, 4)])
+def test_small_values_beside_tiles_of_zeros(fmt, size, zeros):
+    """Keys of zero values count in the sum and take nothing from the others' accuracy, however small those are; every key in a whole tile, so that no
+    fp16 tail is a part of the result.  The weights have their 22 bits: 7e-5 as elsewhere."""
+    rng = np.random.default_rng(17)
+    n, H, G, d = 192, 4, 2, 64
+    k, v = rows_of(rng, n, G, d), (rows_of(rng, n, G, d).astype(np.float64) * size).astype(np.float16)
+    for t in zeros:
+        v[32 * t:32 * t + 32] = 0
+    c = make(rng, [n, n], H=H, G=G, d=d, fmt=fmt)
+    store(c, [k, k], [v, v], [n, n])
+    q, out = rng.standard_normal((1, 2, H, d)).astype(np.float16), torch.full((1, 2, H, d), float("nan"), device=DEV)
+    c.step(dev(q), None, None, out, dev([n, n], torch.int32))
+    for b in range(2):
+        got, want = out[0, b].double().cpu().numpy(), oracle.attend(q[0, b], k, v, n, fmt, False)
+        assert (np.linalg.norm(got - want, axis=1) <= 7e-5 * np.linalg.norm(want, axis=1)).all()
