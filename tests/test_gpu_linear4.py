@@ -165,3 +165,19 @@ def test_wrong_tensors_are_refused():
     with pytest.raises(RuntimeError):                        # an OkvError: widths that do not add up
         w(x, [out[:, :16].contiguous()])
     assert w(x[:0], out[:0]) is not None
+
+
+@pytest.mark.parametrize("m,n_in", [(1, 256), (3, 4096), (4, 4096), (17, 1024), (40, 4096), (70, 512)])
+def test_rows_that_hold_nan_keep_it_to_themselves(m, n_in):
+    """Infinities and NaN in a row of x reach that row's results and no other's; cuts of the inputs among the sizes."""
+    rng = np.random.default_rng(m)
+    codes, scales, _ = weights(rng, 256, n_in, 64, False)
+    w = Linear4(dev(codes), dev(scales), None, None, n_in=n_in)
+    x, out = rng.standard_normal((m, n_in)).astype(np.float16), [torch.full((m, 256), 7.0, dtype=torch.float16, device=DEV) for _ in range(2)]
+    w(dev(x), out[0])
+    row = m // 2
+    x[row, [0, n_in - 1]] = np.nan, np.inf
+    w(dev(x), out[1])
+    others = torch.arange(m, device=DEV) != row
+    assert torch.isnan(out[1][row]).all() and torch.isfinite(out[0]).all()
+    assert torch.equal(out[0][others], out[1][others])

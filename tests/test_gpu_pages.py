@@ -294,3 +294,23 @@ def test_wrong_tensors_are_refused():
         Pages(table=p.table, lens=p.lens, refs=p.refs, page_tokens=16, arrays=[PageArray(p.a[:, :20].contiguous(), 4)])
     with pytest.raises(binding.OkvError):
         Pages(table=p.table, lens=p.lens, refs=p.refs, page_tokens=24, arrays=[PageArray(p.a, 4)]).compact()
+
+
+def test_arrays_beyond_4_gib():
+    """Pages whose bytes begin past 2^32, within a layer and from a layer to the next."""
+    T, n_pages, words = 16, 2200, 1 << 14                    # 1 MiB a page, 2.3e9 bytes a layer: the second layer's pages pass 2^32
+    x = torch.zeros((2, n_pages, T, words), dtype=torch.int32, device=DEV)
+    last = n_pages - 1
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for p in (last, last - 7):
+        x[:, p] = torch.randint(0, 1 << 30, (2, T, words), generator=g, dtype=torch.int32, device=DEV)
+    table, lens, refs = torch.full((2, 2), -1, dtype=torch.int32, device=DEV), ids([T + 5, 0]), ids([1] * (n_pages - 1) + [1])
+    table[0, :2] = ids([last - 7, last])
+    refs[last - 3] = 0                                       # the only free page
+    pages = Pages(table=table, lens=lens, refs=refs, page_tokens=T, arrays=[PageArray(x, 1)])
+    pages.fork(ids([0]), ids([1]))
+    assert pages.status.tolist()[0] == 0 and table[1].tolist() == [last - 7, last - 3]
+    assert torch.equal(x[:, last - 3, :5], x[:, last, :5]) and not x[:, last - 3, 5:].any()
+    pages.copy(ids([last, last - 7]), ids([2, last - 1]))
+    assert torch.equal(x[:, 2], x[:, last]) and torch.equal(x[:, last - 1], x[:, last - 7])
+    assert not x[:, 0].any() and not x[:, 3:last - 7].any()
