@@ -15,8 +15,8 @@
 //     by wavefronts of their own in the same launch, which also store the appended row and quantise a tail that is full.
 //
 // The keys of a launch are cut into equal stretches of tiles over the sequences laid end to end, a wavefront per (stretch, KV head);
-// partial results (max, sum, weighted sum) are joined by a second launch.  A step whose layers' inputs are all there attends up to 32 layers in one
-// launch, the stretches that much longer.
+// partial results (max, sum, weighted sum) are joined by a second launch (short sequences are not cut and need none).  A step whose layers'
+// inputs are all there attends up to 32 layers in one launch, the stretches that much longer.
 //
 // Measured, us a launch: attention over 810 MB (4 layers of 32 x 768 keys x 32 heads, d = 128) 131 (6.2 TB/s), 158 where every tail is full and is
 // quantised; over 1.20 GB (2 layers of 128 x 512..4096 keys, 8 KV heads of 4) 180 (6.7 TB/s), its plan 5, joining 5.5; over 713 MB (2 layers of 2
@@ -38,6 +38,7 @@ namespace okv {
 namespace {
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -448,6 +449,8 @@ struct Attn8 {
   int32_t batch, main_slots, main_blocks, layers, appends;      // main_blocks: of a layer
   int32_t slot0;                   // of the layer's partial results
   int32_t max_stretches;           // > 0: no plan was made; up to 64 sequences, whose lengths the wavefronts share out themselves
+  void *out;                       // attn8_whole_kernel: [layers][batch][H][d]
+  int32_t out_fp32;
 };
 
 // The launch covers `layers` layers; a wavefront works for one of them.
@@ -524,20 +527,27 @@ __device__ __forceinline__ void load_q(half8 (&q)[D / 32], const Attn8 &a, const
   for (int c = 0; c < D / 32; ++c) q[c] = r < a.c.s.R ? *reinterpret_cast<const half8 *>(from + 32 * c) : zero;
 }
 
+// What a step reads of a sequence: `held` keys in codes, `rows` in the tail
+struct Keys8 {
+  int row, held, rows;
+};
+__device__ __forceinline__ Keys8 keys_of(const Attn8 &a, const int b) {
+  const Shape8 &s = a.c.s;
+  Keys8 k;
+  k.row = min(max(a.seqs ? a.seqs[b] : b, 0), s.max_seqs - 1);
+  const int n = min(max(a.lens[k.row], 0), s.max_pages << s.log2_T);
+  k.held = max(n - a.appends, 0) / kTile * kTile;
+  k.rows = n - k.held;
+  return k;
+}
+
 // A sequence's fp16 tail: the appended row goes there, its keys are attended, and it is quantised when it is full.
 template <int D, int FMT>
-__device__ __forceinline__ void attend_tail(const Attn8 &a, const int unit, _Float16 *lds, const int lane) {
+__device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D / 32], const Attn8 &a, const Keys8 &keys, const int b, const int g,
+                                            _Float16 *lds, const int lane) {
   const Shape8 &s = a.c.s;
-  const int b = unit / s.G, g = unit - b * s.G;
-  if (b >= a.batch) return;
-  const int row = min(max(a.seqs ? a.seqs[b] : b, 0), s.max_seqs - 1);
-  const int n = min(max(a.lens[row], 0), s.max_pages << s.log2_T);
-  const int held = max(n - a.appends, 0) / kTile * kTile, rows = n - held;
-  Softmax8<D> acc;
-  acc.clear();
+  const int row = keys.row, held = keys.held, rows = keys.rows;
   if (rows > 0) {
-    half8 q[D / 32];
-    load_q<D>(q, a, b, g, lane);
     _Float16 *const tail[2] = {a.c.tails + tail_at<D>(s, row, 0, g), a.c.tails + tail_at<D>(s, row, 1, g)};
     const _Float16 *const fresh[2] = {a.k_new + b * a.kv_stride + g * D, a.v_new + b * a.kv_stride + g * D};
     Rows32<D> x;
@@ -566,7 +576,6 @@ __device__ __forceinline__ void attend_tail(const Attn8 &a, const int unit, _Flo
       x.template quantise_to<FMT>(a.c, page, (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
     }
   }
-  acc.write(a, a.main_slots + b, g, lane);
 }
 
 template <int D, int FMT, bool NT>
@@ -576,6 +585,35 @@ __device__ __forceinline__ void load_codes(u32x4 (&w)[D / 32], const uint8_t *fr
     const u32x4 *p = reinterpret_cast<const u32x4 *>(from) + 64 * j;
     w[j] = NT ? __builtin_nontemporal_load(p) : *p;
   }
+}
+
+// A tile's codes and scales
+template <int D>
+struct Tile8 {
+  u32x4 k[D / 32], v[D / 32];
+  float2 scale;
+};
+template <int D, int FMT>
+__device__ __forceinline__ void reduce_tile(Softmax8<D> &acc, const half8 (&q)[D / 32], const Tile8<D> &tile, const float scale_log2e) {
+  float score[8];
+  // A tile of zeros (scale 0, codes 0) has any scale, and takes one far below all others (at least 2^-33): m, which its scores may raise, would
+  // otherwise leave the other tiles' weights too few bits.  What it adds to l is at most 2^48 2^8 a key.
+  const float scale_v = tile.scale.y == 0.f ? 0x1p-48f : tile.scale.y, by = tile.scale.x * scale_log2e, log2_v = __builtin_amdgcn_logf(scale_v);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const u32x4 w = tile.k[h * (D / 64) + c / 2];
+      x = __builtin_amdgcn_mfma_f32_16x16x32_f16(unpack8<FMT>(w[2 * (c % 2)], w[2 * (c % 2) + 1]), q[c], x, 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) score[4 * h + j] = fmaf(x[j], by, log2_v);
+  }
+  half8 hi, lo;
+  acc.weigh(score, hi, lo, __builtin_amdgcn_rcpf(scale_v));
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) acc.add(e, unpack8<FMT>(tile.v[e / 2][2 * (e % 2)], tile.v[e / 2][2 * (e % 2) + 1]), hi, lo);
 }
 
 template <int D, int FMT, bool NT>
@@ -589,7 +627,14 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
     block -= a.main_blocks * a.layers;
     const int per_layer = (a.batch * a.c.s.G + 3) >> 2, layer = block / per_layer;
     of_layer(a, layer);
-    attend_tail<D, FMT>(a, (block - layer * per_layer) * 4 + wave, lds_all[wave], lane);
+    const int unit = (block - layer * per_layer) * 4 + wave, b = unit / a.c.s.G, g = unit - b * a.c.s.G;
+    if (b >= a.batch) return;
+    half8 q[D / 32];
+    Softmax8<D> acc;
+    load_q<D>(q, a, b, g, lane);
+    acc.clear();
+    attend_tail<D, FMT>(acc, q, a, keys_of(a, b), b, g, lds_all[wave], lane);
+    acc.write(a, a.main_slots + b, g, lane);
     return;
   }
   const Shape8 s = a.c.s;
@@ -671,9 +716,7 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
     scale_from = a.c.scales + (tile * s.G + g) * 2;
   };
 
-  struct Buffer {
-    u32x4 k[D / 32], v[D / 32];
-    float2 scale;
+  struct Buffer : Tile8<D> {
     int b, tiles;                                // its sequence, and that one's tiles in this stretch
   };
   // A tile's K and V are asked for together, when the one before has been reduced: K as soon as its registers are free and V later is 9 % slower
@@ -703,25 +746,7 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
   load_q<D>(q, a, b, g, lane);
   acc.clear();
   for (;;) {
-    float score[8];
-    // A tile of zeros (scale 0, codes 0) has any scale, and takes one far below all others (at least 2^-33): m, which its scores may raise, would
-    // otherwise leave the other tiles' weights too few bits.  What it adds to l is at most 2^48 2^8 a key.
-    const float scale_v = tile.scale.y == 0.f ? 0x1p-48f : tile.scale.y, by = tile.scale.x * a.scale_log2e, log2_v = __builtin_amdgcn_logf(scale_v);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        const u32x4 w = tile.k[h * (D / 64) + c / 2];
-        x = __builtin_amdgcn_mfma_f32_16x16x32_f16(unpack8<FMT>(w[2 * (c % 2)], w[2 * (c % 2) + 1]), q[c], x, 0, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) score[4 * h + j] = fmaf(x[j], by, log2_v);
-    }
-    half8 hi, lo;
-    acc.weigh(score, hi, lo, __builtin_amdgcn_rcpf(scale_v));
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e) acc.add(e, unpack8<FMT>(tile.v[e / 2][2 * (e % 2)], tile.v[e / 2][2 * (e % 2) + 1]), hi, lo);
+    reduce_tile<D, FMT>(acc, q, tile, a.scale_log2e);
     fetch(tile);
     if (--piece == 0) {
       acc.write(a, str + b, g, lane);
@@ -732,6 +757,67 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
       }
     }
     if (--left == 0) break;
+  }
+}
+
+// A launch over sequences that are short, without a second one that joins: a workgroup has a whole (layer, sequence, KV head), its wavefronts take the
+// tiles in turn, the one with the fewest also the tail, and join through LDS.  Bound by its chain of dependent loads (length and table, codes, LDS).
+// When: see whole_waves().
+template <int D, int FMT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) attn8_whole_kernel(const Attn8 launch) {
+  __shared__ floatx4 o_all[WAVES][D / 16][64];
+  __shared__ float ml_all[WAVES][2][16];
+  __shared__ _Float16 lds[kTile * lds_row(D)];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Attn8 a = launch;
+  const Shape8 s = a.c.s;
+  const int item = blockIdx.x / s.G, g = blockIdx.x - item * s.G, layer = item / a.batch, b = item - layer * a.batch;
+  of_layer(a, layer);
+  const Keys8 keys = keys_of(a, b);
+  const int tiles = keys.held / kTile, log2_tpp = s.log2_T - 5;
+  const int pages = clamp_page(a.c.table[(int64_t)keys.row * s.max_pages + min(lane, s.max_pages - 1)], s.n_pages);      // (at most 64 of them)
+  Tile8<D> tile;
+  const auto fetch = [&](const int t) {
+    const int64_t at = ((int64_t)__builtin_amdgcn_readlane(pages, t >> log2_tpp) << log2_tpp) + (t & ((1 << log2_tpp) - 1));
+    const uint8_t *from = a.c.codes + at * s.G * 2 * kTile * D + tile_at<D>(s, 0, 0, g) + 16 * lane;
+    load_codes<D, FMT, false>(tile.k, from);
+    load_codes<D, FMT, false>(tile.v, from + s.gg * kTile * D);
+    tile.scale = *reinterpret_cast<const float2 *>(a.c.scales + (at * s.G + g) * 2);
+  };
+  half8 q[D / 32];
+  Softmax8<D> acc;
+  acc.clear();
+  load_q<D>(q, a, b, g, lane);
+  if (wave < tiles) fetch(wave);
+  if (wave == tiles % WAVES) attend_tail<D, FMT>(acc, q, a, keys, b, g, lds, lane);
+  for (int t = wave; t < tiles; t += WAVES) {
+    reduce_tile<D, FMT>(acc, q, tile, a.scale_log2e);
+    if (t + WAVES < tiles) fetch(t + WAVES);
+  }
+  const float sum = sum_with_lane_xor<16>(sum_with_lane_xor<32>(acc.l));
+  if (lane < 16) ml_all[wave][0][lane] = acc.m, ml_all[wave][1][lane] = sum;
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) o_all[wave][e][lane] = acc.o[e];
+  __syncthreads();
+  // 4 consecutive elements of a query head per thread
+  for (int i = threadIdx.x; i < D / 16 * 64; i += 64 * WAVES) {
+    const int e = i >> 6, l = i & 63, r = l % 16;
+    if (r >= s.R) continue;
+    float top = ml_all[0][0][r], all = 0.f;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml_all[w][0][r]);
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float by = __builtin_amdgcn_exp2f(ml_all[w][0][r] - base);
+      all = fmaf(by, ml_all[w][1][r], all);
+      o += by * o_all[w][e][l];
+    }
+    o *= all == 0.f ? 0.f : 1.f / all;      // no key at all: 0
+    const int64_t to = ((int64_t)item * s.G * s.R + g * s.R + r) * D + 16 * e + 4 * (l / 16);
+    if (a.out_fp32) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + to) = o;
+    else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + to) = half4{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
   }
 }
 
@@ -932,6 +1018,14 @@ struct AttnLaunch8 {
   }
 };
 
+template <int D, int FMT>
+struct WholeLaunch8 {
+  static void go(const Attn8 &a, dim3 grid, int waves, hipStream_t stream) {
+    if (waves == 8) hipLaunchKernelGGL((attn8_whole_kernel<D, FMT, 8>), grid, dim3(512), 0, stream, a);
+    else hipLaunchKernelGGL((attn8_whole_kernel<D, FMT, 4>), grid, dim3(256), 0, stream, a);
+  }
+};
+
 int rows_call(const char *who, bool store, const okv8_cache *c, int32_t layer, int32_t n_layers, int32_t batch, const int32_t *seqs,
               const int32_t *starts, const int32_t *lens, int64_t n_rows, const void *k, const void *v, int64_t row_stride,
               int64_t layer_stride, void *stream) {
@@ -962,6 +1056,17 @@ int rows_call(const char *who, bool store, const okv8_cache *c, int32_t layer, i
 // Codes that do not fit the memory-side cache (256 MiB) are read past it, so that they do not push out what is used again.
 bool streamed(const okv8_cache *c) { return codes_layer_bytes(c) * c->n_layers > (int64_t)256 << 20; }
 
+// Wavefronts of the workgroups that attend a whole sequence and KV head each, 0: the sequences are cut.  Lengths are on the GPU, so the rule goes by
+// what a row of the page table can hold: at most 1024 keys (a lane has a page), so that a long sequence among short ones costs little.
+// us a step cut / 4 / 8 wavefronts: 4 x 250..256 keys x 8 KV heads, d = 64, 7.9 / 4.7 / 4.9; 16 x 100..400 x 12, d = 128, 9.6 / 7.1 / 6.4;
+// 4 x 1000..1024 x 32, d = 128, 12.6 / 13.1 / 10.5; 100 x 10..200 x 8, d = 64, 12.0 / 5.9 / 8.1; 64 x 400..512 x 8, d = 128, 17.9 / 15.6 /
+// 18.3; and where it is not taken: 32 x 700..768 x 32, d = 128, 34.4 / 36.2 / 40.5; 1 x 2000 x 4, d = 64, 8.7 / 11.4 / 9.5.
+int whole_waves(const okv8_cache *c, int32_t batch, int32_t layers) {
+  const int64_t keys = (int64_t)c->max_pages_per_seq * c->page_tokens, groups = (int64_t)layers * batch * c->n_kv_heads;
+  if (keys > 1024) return 0;
+  return groups <= 256 ? 8 : groups <= 1024 && groups * keys <= 1 << 19 ? 4 : 0;
+}
+
 // w.layers layers from `layer` on, as far as there are
 int attend(const char *who, const okv8_cache *c, const okv8_step *s, const Workspace8 &w, bool planned, int32_t layer, int32_t layers, const void *q, int64_t q_stride,
            const void *k_new, const void *v_new, int64_t kv_stride, void *out) {
@@ -979,6 +1084,11 @@ int attend(const char *who, const okv8_cache *c, const okv8_step *s, const Works
   a.scale_log2e = (float)(1.4426950408889634 / (c->head_dim == 128 ? 11.313708498984761 : 8.0));
   a.batch = s->batch, a.main_slots = w.slots, a.appends = s->appends, a.layers = layers, a.slot0 = 0;
   a.max_stretches = planned ? 0 : w.stretches;
+  a.out = out, a.out_fp32 = c->out_dtype;
+  if (const int waves = whole_waves(c, s->batch, layers)) {
+    by_format<WholeLaunch8>(c, a, dim3((unsigned)(layers * s->batch * c->n_kv_heads)), waves, stream);
+    return hip_result(who, hipGetLastError());
+  }
   a.main_blocks = (w.stretches * c->n_kv_heads + 3) / 4;
   const int64_t blocks = (int64_t)layers * (a.main_blocks + (s->batch * c->n_kv_heads + 3) / 4);
   by_format<AttnLaunch8>(c, a, dim3((unsigned)blocks), streamed(c), stream);
@@ -1065,7 +1175,7 @@ int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, con
   if ((k_new != nullptr) != (s->appends == 1) || (v_new != nullptr) != (s->appends == 1))
     return report(OKV_EINVAL, "okv8_decode_step: k_new and v_new are given if, and only if, the step appends");
   const Workspace8 w = workspace_for(c, s);
-  const bool planned = s->batch > 64;
+  const bool planned = s->batch > 64 && !whole_waves(c, s->batch, w.layers);
   int rc = planned ? begin("okv8_decode_step", c, s, w) : OKV_OK;
   const int64_t q_row = (int64_t)c->n_q_heads * c->head_dim, kv_row = (int64_t)c->n_kv_heads * c->head_dim;
   for (int32_t l = 0; rc == OKV_OK && l < c->n_layers; l += w.layers) {

@@ -415,3 +415,39 @@ def test_small_values_beside_tiles_of_zeros(fmt, size, zeros):
     for b in range(2):
         got, want = out[0, b].double().cpu().numpy(), oracle.attend(q[0, b], k, v, n, fmt, False)
         assert (np.linalg.norm(got - want, axis=1) <= 7e-5 * np.linalg.norm(want, axis=1)).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("B,H,G,d,hi", [(3, 8, 2, 128, 960), (40, 16, 8, 64, 450), (1, 16, 1, 64, 900), (70, 6, 3, 64, 900), (30, 30, 30, 128, 500), (33, 8, 8, 128, 900)])
+def test_short_sequences_by_table_width(fmt, B, H, G, d, hi):
+    """Tables that hold up to 1024 keys, with few and with many (sequence, KV head) pairs, a layer at a time and two at once; the same sequences under
+    a wider table, which are cut.  Both are within the tolerance of the definition, as the head of the file derives it."""
+    rng = np.random.default_rng(B + hi)
+    lens = [int(x) for x in rng.integers(0, hi + 1, B)]
+    lens[0] = hi // 32 * 32
+    k, v = ([rows_of(rng, max(n, 1), G, d) for n in lens] for _ in range(2))
+    q = rng.standard_normal((2, B, H, d)).astype(np.float16)
+    kn, vn = (np.stack([x[max(n - 1, 0)] for x, n in zip(p, lens)])[None].repeat(2, 0) for p in (k, v))
+    now = dev(lens, torch.int32)
+    picked = sorted({0, 1 % B, B // 2, B - 1})
+    want = {(layer, b, appends): oracle.attend(q[layer, b], k[b], v[b], lens[b], fmt, appends) for layer in range(2) for b in picked for appends in (True, False)}
+    for width in (None, 2200):
+        c = make(np.random.default_rng(3), lens + ([0] if width is None else [width]), L=2, H=H, G=G, d=d, T=32, fmt=fmt)
+        store(c, [x[:max(n - 1, 0)] for x, n in zip(k, lens)], [x[:max(n - 1, 0)] for x, n in zip(v, lens)], [max(n - 1, 0) for n in lens], seqs=list(range(B)))
+        out = torch.empty((2, B, H, d), device=DEV)
+        for appends in (True, False):
+            out.fill_(float("nan"))
+            c.step(dev(q), dev(kn) if appends else None, dev(vn) if appends else None, out, now)
+            got = [out.double().cpu().numpy()]
+            if not appends:
+                out.fill_(float("nan"))
+                c.begin(B, now, appends=False)
+                for layer in range(2):
+                    c.attend(layer, dev(q[layer]), None, None, out[layer])
+                got.append(out.double().cpu().numpy())
+            for x in got:
+                assert np.isfinite(x).all()
+                for layer in range(2):
+                    for b in picked:
+                        w = want[layer, b, appends]
+                        assert (np.linalg.norm(x[layer, b] - w, axis=1) <= 7e-5 * np.linalg.norm(w, axis=1)).all(), (width, layer, b, appends)
