@@ -548,6 +548,9 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
   const Shape8 &s = a.c.s;
   const int row = keys.row, held = keys.held, rows = keys.rows;
   if (rows > 0) {
+    // (where a full tail goes: asked for before the rows, so that it is there when they are attended)
+    const bool full = a.appends && rows == kTile;
+    const int to_page = full ? a.c.table[(int64_t)row * s.max_pages + (held >> s.log2_T)] : 0;
     _Float16 *const tail[2] = {a.c.tails + tail_at<D>(s, row, 0, g), a.c.tails + tail_at<D>(s, row, 1, g)};
     const _Float16 *const fresh[2] = {a.k_new + b * a.kv_stride + g * D, a.v_new + b * a.kv_stride + g * D};
     Rows32<D> x;
@@ -571,10 +574,7 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
     acc.weigh(score, hi, lo, 1.f);
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) acc.add(e, x.v[e], hi, lo);
-    if (a.appends && rows == kTile) {
-      const int page = clamp_page(a.c.table[(int64_t)row * s.max_pages + (held >> s.log2_T)], s.n_pages);
-      x.template quantise_to<FMT>(a.c, page, (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
-    }
+    if (full) x.template quantise_to<FMT>(a.c, clamp_page(to_page, s.n_pages), (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
   }
 }
 
