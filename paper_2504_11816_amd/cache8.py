@@ -46,7 +46,7 @@ class Cache8:
             raise ValueError(f"format must be one of {sorted(FORMATS)}")
         if out_dtype not in (torch.float16, torch.float32):
             raise ValueError("out_dtype must be torch.float16 or torch.float32")
-        self.device = torch.device(device)
+        self.device = torch.empty(0, device=device).device      # "cuda" is the current device's "cuda:n", as its tensors say
         self.L, self.H, self.G, self.d, self.T = n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens
         self.max_seqs, self.out_dtype = max_seqs, out_dtype
         c = self.c = binding.Okv8Cache(n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, FORMATS[format], int(out_dtype == torch.float32),

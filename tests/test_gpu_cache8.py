@@ -451,3 +451,10 @@ def test_short_sequences_by_table_width(fmt, B, H, G, d, hi):
                     for b in picked:
                         w = want[layer, b, appends]
                         assert (np.linalg.norm(x[layer, b] - w, axis=1) <= 7e-5 * np.linalg.norm(w, axis=1)).all(), (width, layer, b, appends)
+
+
+def test_the_current_device_by_its_short_name():
+    c = Cache8(n_layers=1, n_q_heads=2, n_kv_heads=2, head_dim=64, page_tokens=32, n_pages=3, max_seqs=1, max_pages_per_seq=3, device="cuda")
+    assert c.device == c.codes.device == c.table.device
+    c.pages.extend(dev([0], torch.int32), dev([40], torch.int32))
+    assert c.lens.tolist() == [40]
