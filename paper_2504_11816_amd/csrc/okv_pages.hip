@@ -194,12 +194,12 @@ struct Moved {
 struct MovedRows {
   char *base;
   int64_t layer_stride;
-  int32_t groups, rows, row_bytes, wide;
+  int32_t groups, rows, row_bytes, wide, pieces;
 };
 struct Moves {
   Moved arrays[OKV_PAGES_MAX_ARRAYS];
   MovedRows rows[OKV_PAGES_MAX_ROWS];
-  int32_t n_arrays, n_rows, pieces;      // pieces of a page over all arrays
+  int32_t n_arrays, n_rows, pieces, row_pieces;      // pieces of a page over all arrays, of a sequence's rows over all row arrays
 };
 
 // The first `bytes` bytes of what begins at piece `piece` of a page
@@ -234,16 +234,25 @@ __device__ __forceinline__ void move_page(const Moves &m, int piece, const int l
     piece -= a.pieces;
   }
 }
+// Piece `piece` of the first n rows of every group
 template <class T>
-__device__ __forceinline__ void move_rows(char *to, const char *from, const MovedRows &r, const int n) {
+__device__ __forceinline__ void move_rows(char *to, const char *from, const MovedRows &r, const int n, const int piece) {
   const int per_row = r.row_bytes / (int)sizeof(T), per_group = n * per_row, all = r.groups * per_group, stride = r.rows * per_row;
-  for (int i = threadIdx.x; i < all; i += kMoveThreads) {
-    const int g = i / per_group, at = g * stride + i - g * per_group;
-    reinterpret_cast<T *>(to)[at] = reinterpret_cast<const T *>(from)[at];
+  const int first = piece * kMoveThreads * kInFlight + threadIdx.x;
+  int at[kInFlight];
+  T x[kInFlight];
+#pragma unroll
+  for (int i = 0; i < kInFlight; ++i) {
+    const int j = first + i * kMoveThreads, g = j / per_group;
+    at[i] = g * stride + j - g * per_group;
+    if (j < all) x[i] = reinterpret_cast<const T *>(from)[at[i]];
   }
+#pragma unroll
+  for (int i = 0; i < kInFlight; ++i)
+    if (first + i * kMoveThreads < all) reinterpret_cast<T *>(to)[at[i]] = x[i];
 }
 
-// Block (piece, layer, fork): a piece of the fork's last page; the last piece is its row of the table (layer 0) and the row arrays
+// Block (piece, layer, fork): a piece of the fork's last page, behind these a piece of its rows, and behind those its row of the table (layer 0)
 __global__ void __launch_bounds__(kMoveThreads) fork_move_kernel(State s, const int32_t *src, const int32_t *dst, Lists l, Moves m) {
   const int i = blockIdx.z, layer = blockIdx.y, piece = blockIdx.x;
   if (!l.count[0]) return;
@@ -252,16 +261,21 @@ __global__ void __launch_bounds__(kMoveThreads) fork_move_kernel(State s, const 
     if (to >= 0 && from >= 0 && from < s.n_pages) move_page(m, piece, layer, from, to, len & ((1 << s.log2_T) - 1));
     return;
   }
+  int of_rows = piece - m.pieces;
 #pragma unroll
   for (int k = 0; k < OKV_PAGES_MAX_ROWS; ++k) {
     if (k >= m.n_rows) break;
     const MovedRows &r = m.rows[k];
-    const int64_t bytes = (int64_t)r.groups * r.rows * r.row_bytes;
-    const int n = len % r.rows;
-    if (n == 0) continue;
-    char *base = r.base + layer * r.layer_stride;
-    if (r.wide) move_rows<u32x4>(base + b * bytes, base + a * bytes, r, n);
-    else move_rows<uint32_t>(base + b * bytes, base + a * bytes, r, n);
+    if (of_rows >= 0 && of_rows < r.pieces) {
+      const int64_t bytes = (int64_t)r.groups * r.rows * r.row_bytes;
+      const int n = len % r.rows;
+      if (n == 0) return;
+      char *base = r.base + layer * r.layer_stride;
+      if (r.wide) move_rows<u32x4>(base + b * bytes, base + a * bytes, r, n, of_rows);
+      else move_rows<uint32_t>(base + b * bytes, base + a * bytes, r, n, of_rows);
+      return;
+    }
+    of_rows -= r.pieces;
   }
   if (layer) return;
   const int full = len >> s.log2_T;
@@ -383,7 +397,7 @@ Lists lists_of(const okv_pages *p) {
 }
 Moves moves_of(const okv_pages *p, const okv_page_array *to) {
   Moves m;
-  m.n_arrays = p->n_arrays, m.n_rows = p->n_rows, m.pieces = 0;
+  m.n_arrays = p->n_arrays, m.n_rows = p->n_rows, m.pieces = m.row_pieces = 0;
   for (int i = 0; i < p->n_arrays; ++i) {
     const okv_page_array &a = p->arrays[i], &t = to ? to[i] : a;
     Moved &k = m.arrays[i];
@@ -399,8 +413,10 @@ Moves moves_of(const okv_pages *p, const okv_page_array *to) {
   if (p->n_arrays && m.pieces == 0) m.pieces = 1;
   for (int i = 0; i < p->n_rows; ++i) {
     const okv_row_array &r = p->rows[i];
-    m.rows[i] = {static_cast<char *>(r.base), r.layer_stride, r.groups, r.rows, r.row_bytes,
-                 multiple(r.base, 16) && multiple(r.row_bytes, 16) && multiple(r.layer_stride, 16)};
+    const bool wide = multiple(r.base, 16) && multiple(r.row_bytes, 16) && multiple(r.layer_stride, 16);
+    const int64_t piece = (int64_t)kMoveThreads * kInFlight * (wide ? 16 : 4), bytes = (int64_t)r.groups * r.rows * r.row_bytes;
+    m.rows[i] = {static_cast<char *>(r.base), r.layer_stride, r.groups, r.rows, r.row_bytes, wide, (int32_t)((bytes + piece - 1) / piece)};
+    m.row_pieces += m.rows[i].pieces;
   }
   return m;
 }
@@ -444,7 +460,7 @@ int okv_pages_fork(const okv_pages *p, int32_t n, const int32_t *src, const int3
   const Moves m = moves_of(p, nullptr);
   const State s = state_of(p);
   hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), s, src, dst, n, l);
-  hipLaunchKernelGGL(fork_move_kernel, dim3((unsigned)(m.pieces + 1), (unsigned)p->n_layers, (unsigned)n), dim3(kMoveThreads), 0,
+  hipLaunchKernelGGL(fork_move_kernel, dim3((unsigned)(m.pieces + m.row_pieces + 1), (unsigned)p->n_layers, (unsigned)n), dim3(kMoveThreads), 0,
                      static_cast<hipStream_t>(stream), s, src, dst, l, m);
   return hip_result("okv_pages_fork");
 }

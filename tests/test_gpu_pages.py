@@ -314,3 +314,20 @@ def test_arrays_beyond_4_gib():
     pages.copy(ids([last, last - 7]), ids([2, last - 1]))
     assert torch.equal(x[:, 2], x[:, last]) and torch.equal(x[:, last - 1], x[:, last - 7])
     assert not x[:, 0].any() and not x[:, 3:last - 7].any()
+
+
+@pytest.mark.parametrize("groups,rows,words", [(3, 7, 5), (1, 32, 1), (40, 32, 32), (5, 16, 200), (300, 3, 4)])
+def test_rows_of_many_sizes_are_forked(groups, rows, words):
+    """Row arrays of less and of more than a workgroup's piece, moved by 4 bytes and by 16, with every number of rows in use."""
+    x = torch.randint(0, 1 << 30, (2, 4, groups, rows, words), dtype=torch.int32).to(DEV)
+    for n in sorted({1, 2, rows // 2, rows - 1, rows}):
+        table, lens, refs = torch.full((4, 2), -1, dtype=torch.int32, device=DEV), ids([n, 0, 0, 0]), torch.zeros(8, dtype=torch.int32, device=DEV)
+        table[0, 0], refs[0] = 0, 1
+        y = x.clone()
+        pages = Pages(table=table, lens=lens, refs=refs, page_tokens=64, arrays=[], rows=[RowArray(y, groups, rows)])
+        pages.fork(ids([0, 0]), ids([1, 3]))
+        want = x.clone()
+        for to in (1, 3):
+            want[:, to, :, :n % rows] = x[:, 0, :, :n % rows]
+        assert pages.status.tolist()[0] == 0 and lens.tolist() == [n, n, 0, n]
+        assert torch.equal(y, want)
