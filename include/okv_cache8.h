@@ -69,6 +69,9 @@ typedef struct okv8_cache {
   int64_t n_pages;             /* pages of every layer, at most 2^31 - 1                     */
   void *codes, *scales, *tails;
   const int32_t *page_table;
+  const int32_t *refused;      /* NULL, or a word: while it is not 0, storing writes nothing, and a step that
+                                  appends writes nothing to the cache (its results then mean nothing).
+                                  status + 3 of okv_pages.h: pages could not be taken        */
 } okv8_cache;
 
 /* Bytes of the three buffers (all layers); < 0 on a bad shape. */

@@ -11,13 +11,17 @@
  *   lens   [max_seqs] int32: tokens of every sequence; its first ceil(lens / T) entries are its pages
  *   refs   [n_pages] int32: sequences that a page belongs to; 0: free.  Start with table -1, lens and refs 0.
  *   status [4] int32: 0 or the code of the first call that could not be carried out (the caller clears
- *          it); [1] pages in use after the last okv_pages_compact; [2] pages that it moved; [3] unused
+ *          it); [1] pages in use after the last okv_pages_compact; [2] pages that it moved; [3] 0 or the
+ *          code of the last okv_pages_extend (the caller may clear it)
  *
  * A page that several sequences share is full and is never written: a fork copies the last, partly
  * filled page.  Free pages are taken lowest id first, in the order of the arguments.  Whether there are
  * enough is known on the GPU only: a call that lacks pages, or room in a row of the table, changes
  * nothing and leaves OKV_ENOSPC in status[0], one whose arguments do not fit the state OKV_ESTATE; a
- * program that cannot rule this out reads status[0] when it next synchronises.
+ * program that cannot rule this out reads status[0] when it next synchronises.  A step that follows an
+ * okv_pages_extend which changed nothing must not append: the row would go where the last token is, which
+ * may be in a shared page.  A step over the 8-bit cache sees to that itself (okv8_cache.refused), and so does storing rows; a program
+ * that appends to an fp16 pool reads status[3] first, unless it knows that there are pages.
  *
  * Conventions as in okv.h: C ABI, every pointer DEVICE unless labelled, the caller owns all memory,
  * calls enqueue on `stream` and return at once without allocating; OKV_OK or a negative OKV_E* code;

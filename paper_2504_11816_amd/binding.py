@@ -41,7 +41,7 @@ class Okv8Cache(ctypes.Structure):
     """okv8_cache of include/okv_cache8.h."""
     _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "page_tokens", "format", "out_dtype", "max_seqs",
                                               "max_pages_per_seq")] + [("n_pages", ctypes.c_int64)] + [
-        (n, ctypes.c_void_p) for n in ("codes", "scales", "tails", "page_table")]
+        (n, ctypes.c_void_p) for n in ("codes", "scales", "tails", "page_table", "refused")]
 
 
 class Okv8Step(ctypes.Structure):

@@ -44,7 +44,7 @@ class Scratch:
 def decoder_step(cache, layers, scratch, x, seqs, eps=1e-5):
     """One token for each of the sequences `seqs` (int32 rows of the cache's table): their lengths grow by one, and every layer appends its key and value
     and attends.  x fp16 [batch][h1], overwritten with the last layer's output.  Nothing waits or allocates on the GPU's side; a cache that is out of pages
-    says so in cache.pages.check()."""
+    says so in cache.pages.check(): it is then as it was before the step, and x means nothing."""
     B, stream = x.shape[0], binding.current_stream(x.device)
     a, q, k, v, t, y, z, u = scratch.rows(B)
     h1 = x.shape[1]

@@ -63,9 +63,11 @@ struct Cache8 {
   uint8_t *codes;          // of the (first) layer
   float *scales;
   _Float16 *tails;
-  const int32_t *table;
+  const int32_t *table, *refused;
   Shape8 s;
 };
+// Whether nothing may be written: the pages for it could not be taken, and the last token is not the new one
+__device__ __forceinline__ bool refused(const Cache8 &c) { return c.refused && *c.refused; }
 
 // ---- codes ------------------------------------------------------------------------------------------
 
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(256) store8_kernel(RowsArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = (a.c.s.G + 3) >> 2;
   const int item = blockIdx.x / groups, g = (blockIdx.x - item * groups) * 4 + wave;
-  if (g >= a.c.s.G) return;
+  if (g >= a.c.s.G || refused(a.c)) return;
   const int b = sequence_of(a.starts, a.batch, item, lane);
   const RowsOf r = rows_of(a, b);
   const int u = item - (a.starts[b] / kTile + 2 * b), t = r.before / kTile + u;
@@ -549,7 +551,7 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
   const int row = keys.row, held = keys.held, rows = keys.rows;
   if (rows > 0) {
     // (where a full tail goes: asked for before the rows, so that it is there when they are attended)
-    const bool full = a.appends && rows == kTile;
+    const bool full = a.appends && rows == kTile, writes = a.appends && !refused(a.c);
     const int to_page = full ? a.c.table[(int64_t)row * s.max_pages + (held >> s.log2_T)] : 0;
     _Float16 *const tail[2] = {a.c.tails + tail_at<D>(s, row, 0, g), a.c.tails + tail_at<D>(s, row, 1, g)};
     const _Float16 *const fresh[2] = {a.k_new + b * a.kv_stride + g * D, a.v_new + b * a.kv_stride + g * D};
@@ -557,7 +559,7 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
     x.load([&](int kv, int key) -> const _Float16 * {
       return key >= rows ? nullptr : a.appends && key == rows - 1 ? fresh[kv] : tail[kv] + key * D;
     }, lds, lane);
-    if (a.appends && lane < 2 * (D / 8)) {
+    if (writes && lane < 2 * (D / 8)) {
       const int kv = lane / (D / 8), col = lane % (D / 8) * 8;
       *reinterpret_cast<half8 *>(tail[kv] + (rows - 1) * D + col) = *reinterpret_cast<const half8 *>(fresh[kv] + col);
     }
@@ -574,7 +576,7 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
     acc.weigh(score, hi, lo, 1.f);
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) acc.add(e, x.v[e], hi, lo);
-    if (full) x.template quantise_to<FMT>(a.c, clamp_page(to_page, s.n_pages), (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
+    if (full && writes) x.template quantise_to<FMT>(a.c, clamp_page(to_page, s.n_pages), (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
   }
 }
 
@@ -938,7 +940,7 @@ Cache8 cache_of(const okv8_cache *c, int32_t layer) {
   k.codes = static_cast<uint8_t *>(c->codes) + layer * codes_layer_bytes(c);
   k.scales = static_cast<float *>(c->scales) + layer * scales_layer_floats(c);
   k.tails = static_cast<_Float16 *>(c->tails) + layer * tails_layer_halves(c);
-  k.table = c->page_table;
+  k.table = c->page_table, k.refused = c->refused;
   k.s = {c->n_kv_heads, c->n_q_heads / c->n_kv_heads, kv_head_group(c->n_kv_heads, c->head_dim), log2_of(c->page_tokens),
          c->max_seqs, c->max_pages_per_seq, (int32_t)c->n_pages};
   return k;

@@ -111,11 +111,9 @@ __global__ void __launch_bounds__(kThreads) extend_kernel(State s, const int32_t
   }
   if (threadIdx.x == kThreads - 1) first[kThreads * each] = at;
   __syncthreads();
-  if (bad || total > s.n_pages) {
-    if (threadIdx.x == 0) blame(s, OKV_ENOSPC);
-    return;
-  }
-  if (take_free(s, total, sums, [&](int rank, int page) { fresh[rank] = page; }) < total) {
+  const bool lacks = bad || total > s.n_pages || take_free(s, total, sums, [&](int rank, int page) { fresh[rank] = page; }) < total;
+  if (threadIdx.x == 0) s.status[3] = lacks ? OKV_ENOSPC : 0;
+  if (lacks) {
     if (threadIdx.x == 0) blame(s, OKV_ENOSPC);
     return;
   }

@@ -115,9 +115,10 @@ class Pages:
         self._done(self._lib.okv_pages_copy(self.ref, n, at, self._ids("dst_ids", dst_ids, n), c, pages, binding.current_stream(self.device)))
 
     def check(self):
-        """Waits for the GPU; raises if a call could not be carried out since the last check."""
+        """Waits for the GPU; raises if a call could not be carried out since the last check.  After an extend() that could not be, a Cache8 is not
+        written to until one is carried out or check() has raised."""
         code = int(self.status[0])
         if code:
-            self.status[0] = 0
+            self.status[::3] = 0
             raise binding.OkvError(code, "no room: too few free pages, or a row of the table is full" if code == binding.OKV_ENOSPC
                                    else "the sequences that were named do not fit the state of the cache")

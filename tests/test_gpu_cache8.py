@@ -458,3 +458,60 @@ def test_the_current_device_by_its_short_name():
     assert c.device == c.codes.device == c.table.device
     c.pages.extend(dev([0], torch.int32), dev([40], torch.int32))
     assert c.lens.tolist() == [40]
+
+
+@pytest.mark.parametrize("layerwise", [False, True])
+@pytest.mark.parametrize("width", [4, 60])
+def test_a_step_that_lacks_pages_writes_nothing(layerwise, width):
+    """Two sequences share a full page and both need another, of which there is one: the call that takes pages changes nothing, and neither does the
+    step behind it, in any page, tail or length.  When a page has been freed, the same step goes as if it were the first."""
+    rng = np.random.default_rng(8)
+    H, G, d, T, L = 4, 2, 64, 32, 2
+
+    def start(n_pages):
+        c = Cache8(n_layers=L, n_q_heads=H, n_kv_heads=G, head_dim=d, page_tokens=T, n_pages=n_pages, max_seqs=4, max_pages_per_seq=width, out_dtype=torch.float32, device=DEV)
+        c.pages.extend(dev([0, 3], torch.int32), dev([T, 5], torch.int32))
+        c.pages.fork(dev([0], torch.int32), dev([1], torch.int32))
+        c.codes.copy_(codes[:, :n_pages])
+        c.scales.copy_(scales[:, :n_pages])
+        c.tails.copy_(tails)
+        c.pages.check()
+        return c
+
+    codes = dev(rng.integers(1, 255, (L, 6, T // 32, 2 * G * 32 * d)), torch.uint8)
+    scales, tails = dev(rng.random((L, 6, T // 32, 2 * G)), torch.float32), dev(rng.standard_normal((L, 4, 2, G, 32, d)).astype(np.float16))
+    seqs = dev([0, 1], torch.int32)
+    q, kn, vn = (dev(rng.standard_normal((L, 2, h, d)).astype(np.float16)) for h in (H, G, G))
+
+    def step(c):
+        out = torch.full((L, 2, H, d), float("nan"), device=DEV)
+        c.pages.extend(seqs)
+        if layerwise:
+            c.begin(2, c.lens, seqs)
+            for layer in range(L):
+                c.attend(layer, q[layer], kn[layer], vn[layer], out[layer])
+        else:
+            c.step(q, kn, vn, out, c.lens, seqs)
+        return out
+
+    c = start(3)                                             # page 0 shared, page 1 of sequence 3, page 2 free
+    before = [x.clone() for x in (c.codes, c.scales, c.tails, c.table, c.lens, c.refs)]
+    step(c)
+    with pytest.raises(binding.OkvError):
+        c.pages.check()
+    for x, y in zip(before, (c.codes, c.scales, c.tails, c.table, c.lens, c.refs)):
+        assert torch.equal(x, y)
+    # a prompt's chunk that finds no room, and is stored all the same
+    more = dev(rng.standard_normal((L, 100, G, d)).astype(np.float16))
+    c.pages.extend(dev([0], torch.int32), dev([100], torch.int32))
+    c.store(more, more, dev([0, 100], torch.int32), c.lens, dev([0], torch.int32))
+    with pytest.raises(binding.OkvError):
+        c.pages.check()
+    for x, y in zip(before, (c.codes, c.scales, c.tails, c.table, c.lens, c.refs)):
+        assert torch.equal(x, y)
+    c.pages.free(dev([3], torch.int32))
+    roomy = start(6)
+    assert torch.equal(step(c), step(roomy))
+    c.pages.check()
+    roomy.pages.check()
+    assert c.lens.tolist()[:2] == [T + 1, T + 1] and torch.equal(c.tails[:, :2], roomy.tails[:, :2])
