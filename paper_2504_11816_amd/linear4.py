@@ -52,7 +52,7 @@ class Linear4:
             raise ValueError(f"bias must be a contiguous fp16 vector of {self.n_out} on {self.device}")
         self.bias = bias
         self.packed = torch.empty(n, dtype=torch.uint8, device=self.device)
-        self.workspace, self._workspace_bytes, self._wants = None, 0, {}
+        self.workspace, self._workspace_bytes, self._wants, self._outgrown = None, 0, {}, []
         self._call, self._packed_at, self._bias_at = binding.lib().okv_linear4, self.packed.data_ptr(), bias.data_ptr() if bias is not None else None
 
     @classmethod
@@ -99,6 +99,8 @@ class Linear4:
             want = self._wants[m] = max(0, int(binding.lib().okv_linear4_workspace_bytes(m, self.n_out, self.n_in)))
         ws = self.workspace
         if want and (ws is None or self._workspace_bytes < want):
+            if ws is not None:
+                self._outgrown.append(ws)                    # captured graphs may write to it for as long as this matrix is there
             ws = self.workspace = torch.empty(want, dtype=torch.uint8, device=device)
             self._workspace_bytes = want
         rc = self._call(x.data_ptr(), self._packed_at, self._bias_at, None if residual is None else residual.data_ptr(), arr, cols, n, m, self.n_out, self.n_in,

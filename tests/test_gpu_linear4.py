@@ -181,3 +181,31 @@ def test_rows_that_hold_nan_keep_it_to_themselves(m, n_in):
     others = torch.arange(m, device=DEV) != row
     assert torch.isnan(out[1][row]).all() and torch.isfinite(out[0]).all()
     assert torch.equal(out[0][others], out[1][others])
+
+
+def test_a_graph_keeps_its_workspace():
+    """A larger batch that wants more workspace does not take the one that a captured graph writes to: what is allocated afterwards stays as it is,
+    replay after replay, and so do the graph's results."""
+    rng = np.random.default_rng(4)
+    codes, scales, _ = weights(rng, 4096, 16384, 128, False)
+    w = Linear4(dev(codes), dev(scales), None, None, n_in=16384)
+    x = dev(rng.standard_normal((64, 16384)).astype(np.float16))
+    want, out, large = (torch.empty((n, 4096), dtype=torch.float16, device=DEV) for n in (32, 32, 64))
+    w(x[:32], want)
+    assert w.workspace is not None
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w(x[:32], out)
+    size = w.workspace.numel()
+    w(x, large)
+    assert w.workspace.numel() > size                        # (the case that this is about)
+    first = large.clone()
+    others = [torch.full((size // 4,), 3.0, device=DEV) for _ in range(4)]
+    for _ in range(3):
+        out.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all((t == 3).all() for t in others)
+        w(x, large)
+        assert torch.equal(large, first)
