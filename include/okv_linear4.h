@@ -46,13 +46,13 @@ int okv_linear4_pack(void *dst, const void *codes, int32_t per_byte, const void 
 int okv_linear4_quantize(void *dst, const void *src, int32_t n_out, int32_t n_in, int32_t group, int32_t zeros, void *stream);
 
 /* out = act(x W^T + bias) + residual, as okv_linear.
- *   x         fp16 [m][n_in], m <= OKV_LINEAR4_MAX_BATCH
+ *   x         fp16 [m][n_in], m <= OKV_LINEAR4_MAX_BATCH; must not overlap out
  *   packed    as the calls above leave it, with the same n_out, n_in, group and zeros
  *   bias      fp16 [n_out] or NULL;  residual  fp16 [m][n_out] or NULL (n_seg must be 1; may be out[0])
  *   out       HOST array of n_seg (1 to 3) DEVICE pointers: run s of the output features is written as fp16
  *             [m][cols[s]] to out[s]
  *   cols      HOST [n_seg] multiples of 16 that add up to n_out, or NULL: equal runs
- *   relu      1: act = max(., 0)
+ *   relu      1: act = max(., 0), NaN where the argument is (okv_linear gives 0 there)
  *   workspace okv_linear4_workspace_bytes bytes of scratch, 16-byte aligned; with less (or NULL) a form that needs none runs.
  *             Calls that may run at the same time need workspaces of their own. */
 int okv_linear4(const void *x, const void *packed, const void *bias, const void *residual, void *const *out,

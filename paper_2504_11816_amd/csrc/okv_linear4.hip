@@ -59,7 +59,7 @@ __device__ __forceinline__ void finish(const Linear4Args &a, floatx4 y, const in
   }
   if (a.relu)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fmaxf(y[e], 0.f);
+    for (int e = 0; e < 4; ++e) y[e] = y[e] < 0.f ? 0.f : y[e];      // (NaN stays)
   if (a.residual) {
     const half4v more = *reinterpret_cast<const half4v *>(a.residual + (int64_t)row * a.n_out + n);
 #pragma unroll

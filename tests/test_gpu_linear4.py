@@ -209,3 +209,14 @@ def test_a_graph_keeps_its_workspace():
         assert torch.equal(out, want) and all((t == 3).all() for t in others)
         w(x, large)
         assert torch.equal(large, first)
+
+
+@pytest.mark.parametrize("m,n_in", [(1, 256), (20, 4096)])
+def test_relu_keeps_nan(m, n_in):
+    rng = np.random.default_rng(6)
+    codes, scales, _ = weights(rng, 256, n_in, 64, False)
+    w = Linear4(dev(codes), dev(scales), None, None, n_in=n_in)
+    x, out = rng.standard_normal((m, n_in)).astype(np.float16), torch.empty((m, 256), dtype=torch.float16, device=DEV)
+    x[m - 1, 3] = np.nan
+    w(dev(x), out, relu=True)
+    assert torch.isnan(out[m - 1]).all() and (out[:m - 1] >= 0).all()
