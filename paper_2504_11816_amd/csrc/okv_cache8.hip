@@ -9,8 +9,9 @@
 //     with V's keys stored in that order, the operand layout of the second product, V^T (rows: elements) times the weights;
 //   * codes become fp16 numbers exactly (int8: a byte shuffle that makes 1024 + u, and a subtraction; e4m3: the conversion instruction), the
 //     scale of K multiplies the scores in fp32, that of V goes into the weights' exponent;
-//   * weights go into the second product as two fp16 numbers, w = hi + lo, w - hi - lo below 2^-22: one rounded to 11 bits would leave
-//     errors of 1e-4 of the result, which an fp32 output would show;
+//   * weights go into the second product as two fp16 numbers, hi and lo, whose products are added up apart: each is off by 2^-22 of itself or by 2^-42 of
+//     the largest, whichever is more (see Softmax8).  One rounded to 11 bits would leave errors of 1e-4 of the result, which an fp32 output
+//     would show;
 //   * only whole tiles are in codes, so the loop over them has no masks; the up to 32 keys in a sequence's fp16 tail are attended
 //     by wavefronts of their own in the same launch, which also store the appended row and quantise a tail that is full.
 //
@@ -466,30 +467,36 @@ __device__ __forceinline__ void of_layer(Attn8 &a, const int layer) {
   a.slot0 = layer * (a.main_slots + a.batch);
 }
 
+// The weights that count may be far below the largest: a key that takes most of the softmax and has small values leaves the result to all the others.
+// So weights use fp16's whole range (up to 2^15, and at least 2^7 for the largest score when m is raised), and lo, what hi leaves of one, is 2^10
+// times larger than it and rounded to nearest: a weight is off by 2^-22 of itself or by 2^-35, whichever is more, and 2^-35 is at most 2^-42 of
+// the largest.  (With lo in hi's sums its grid is fp16's, 2^-24, and cutting off there, one way, took 7e-3 off the result of 16384 keys
+// whose scores are 12 below one key's of small values; now 1.1e-6.)
 template <int D>
 struct Softmax8 {
-  floatx4 o[D / 16];
+  static constexpr float kTop = 15.f, kRaised = 7.f, kLo = 1024.f;
+  floatx4 o[D / 16], o_lo[D / 16];         // of hi; of lo, kLo times too large
   float m, l;
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) o[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < D / 16; ++e) o[e] = o_lo[e] = floatx4{0.f, 0.f, 0.f, 0.f};
     m = -__builtin_inff(), l = 0.f;
   }
 
-  // The lane's 8 scores of 32 keys, in log2 units and with log2 of the tile's V scale added -> weights w = 2^(s - m) as two fp16 numbers each,
-  // w = hi + lo to 22 bits.  The scale is in the weights, so that the products add up in the accumulators of the matrix cores;
-  // l counts the weights without it.  m is raised, and what is there multiplied down, only when a score is 8 or more above it
-  // (weights stay below 2^8): hardly ever after a piece's first tile.
+  // The lane's 8 scores of 32 keys, in log2 units and with log2 of the tile's V scale added -> weights w = 2^(s - m) as two fp16 numbers each.
+  // The scale is in the weights, so that the products add up in the accumulators of the matrix cores;
+  // l counts the weights without it.  m is raised, and what is there multiplied down, only when a weight would pass 2^15, 8 above
+  // the largest score that m was raised for: hardly ever after a piece's first tile.
   __device__ __forceinline__ void weigh(const float (&s)[8], half8 &hi, half8 &lo, const float scale) {
     const float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    if (__any(top > m + 8.f)) {
-      const float now = fmaxf(m, max_with_lane_xor<16>(max_with_lane_xor<32>(top)));
+    if (__any(top > m + kTop)) {
+      const float now = fmaxf(m, max_with_lane_xor<16>(max_with_lane_xor<32>(top)) - kRaised);
       const float alpha = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
       m = now;
       l *= alpha;
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) o[e] *= alpha;
+      for (int e = 0; e < D / 16; ++e) o[e] *= alpha, o_lo[e] *= alpha;
     }
     float w[8], sum = 0.f;
 #pragma unroll
@@ -500,15 +507,16 @@ struct Softmax8 {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const half2v h = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[i], w[i + 1]));
-      const half2v r = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[i] - (float)h[0], w[i + 1] - (float)h[1]));
-      hi[i] = h[0], hi[i + 1] = h[1], lo[i] = r[0], lo[i + 1] = r[1];
+      hi[i] = h[0], hi[i + 1] = h[1];
+      lo[i] = (_Float16)((w[i] - (float)h[0]) * kLo), lo[i + 1] = (_Float16)((w[i + 1] - (float)h[1]) * kLo);
     }
     l = fmaf(sum, scale, l);
   }
   __device__ __forceinline__ void add(const int e, const half8 v, const half8 hi, const half8 lo) {
     o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, o[e], 0, 0, 0);
-    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo, o[e], 0, 0, 0);
+    o_lo[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo, o_lo[e], 0, 0, 0);
   }
+  __device__ __forceinline__ floatx4 sum_of(const int e) const { return o[e] + o_lo[e] * (1.f / kLo); }
   __device__ __forceinline__ void write(const Attn8 &a, const int64_t slot, const int g, const int lane) const {
     const float sum = sum_with_lane_xor<16>(sum_with_lane_xor<32>(l));
     const int R = a.c.s.R, r = lane % 16;
@@ -516,7 +524,7 @@ struct Softmax8 {
     const int64_t at = ((a.slot0 + slot) * a.c.s.G + g) * R + r;
     if (lane < 16) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, sum);
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) *reinterpret_cast<floatx4 *>(a.part_o + at * D + 16 * e + 4 * (lane / 16)) = o[e];
+    for (int e = 0; e < D / 16; ++e) *reinterpret_cast<floatx4 *>(a.part_o + at * D + 16 * e + 4 * (lane / 16)) = sum_of(e);
   }
 };
 
@@ -599,7 +607,7 @@ template <int D, int FMT>
 __device__ __forceinline__ void reduce_tile(Softmax8<D> &acc, const half8 (&q)[D / 32], const Tile8<D> &tile, const float scale_log2e) {
   float score[8];
   // A tile of zeros (scale 0, codes 0) has any scale, and takes one far below all others (at least 2^-33): m, which its scores may raise, would
-  // otherwise leave the other tiles' weights too few bits.  What it adds to l is at most 2^48 2^8 a key.
+  // otherwise leave the other tiles' weights too few bits.  What it adds to l is at most 2^48 2^15 a key.
   const float scale_v = tile.scale.y == 0.f ? 0x1p-48f : tile.scale.y, by = tile.scale.x * scale_log2e, log2_v = __builtin_amdgcn_logf(scale_v);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -799,7 +807,7 @@ __global__ void __launch_bounds__(64 * WAVES) attn8_whole_kernel(const Attn8 lau
   const float sum = sum_with_lane_xor<16>(sum_with_lane_xor<32>(acc.l));
   if (lane < 16) ml_all[wave][0][lane] = acc.m, ml_all[wave][1][lane] = sum;
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) o_all[wave][e][lane] = acc.o[e];
+  for (int e = 0; e < D / 16; ++e) o_all[wave][e][lane] = acc.sum_of(e);
   __syncthreads();
   // 4 consecutive elements of a query head per thread
   for (int i = threadIdx.x; i < D / 16 * 64; i += 64 * WAVES) {
