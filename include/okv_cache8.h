@@ -71,7 +71,8 @@ typedef struct okv8_cache {
   const int32_t *page_table;
   const int32_t *refused;      /* NULL, or a word: while it is not 0, storing writes nothing, and a step that
                                   appends writes nothing to the cache (its results then mean nothing).
-                                  status + 3 of okv_pages.h: pages could not be taken        */
+                                  status + 3 of okv_pages.h: pages could not be taken, and the caller has
+                                  not seen it yet                                            */
 } okv8_cache;
 
 /* Bytes of the three buffers (all layers); < 0 on a bad shape. */

@@ -12,13 +12,16 @@
  *   refs   [n_pages] int32: sequences that a page belongs to; 0: free.  Start with table -1, lens and refs 0.
  *   status [4] int32: 0 or the code of the first call that could not be carried out (the caller clears
  *          it); [1] pages in use after the last okv_pages_compact; [2] pages that it moved; [3] 0 or the
- *          code of the last okv_pages_extend (the caller may clear it)
+ *          code of the last okv_pages_extend (the caller may clear it), which stays as long as status[0]
+ *          is not cleared
  *
  * A page that several sequences share is full and is never written: a fork copies the last, partly
  * filled page.  Free pages are taken lowest id first, in the order of the arguments.  Whether there are
  * enough is known on the GPU only: a call that lacks pages, or room in a row of the table, changes
  * nothing and leaves OKV_ENOSPC in status[0], one whose arguments do not fit the state OKV_ESTATE; a
- * program that cannot rule this out reads status[0] when it next synchronises.  A step that follows an
+ * program that cannot rule this out reads status[0] when it next synchronises.  After an okv_pages_extend that was
+ * refused, later ones change nothing either, whatever their sequences, until the caller has cleared
+ * status[0]: no sequence has tokens that no step has written.  A step that follows an
  * okv_pages_extend which changed nothing must not append: the row would go where the last token is, which
  * may be in a shared page.  A step over the 8-bit cache sees to that itself (okv8_cache.refused), and so does storing rows; a program
  * that appends to an fp16 pool reads status[3] first, unless it knows that there are pages.
@@ -75,7 +78,8 @@ typedef struct okv_pages {
 
 int64_t okv_pages_workspace_bytes(int32_t n_pages);
 
-/* Sequence seqs[i] grows by n_new[i] >= 0 tokens: takes the pages that it lacks and raises lens.
+/* Sequence seqs[i] grows by n_new[i] >= 0 tokens: takes the pages that it lacks and raises lens.  Nothing is done
+ * while status[0] and status[3] both hold a code.
  *   seqs [n] distinct, or NULL: i;  n_new [n], or NULL: 1 each */
 int okv_pages_extend(const okv_pages *p, int32_t n, const int32_t *seqs, const int32_t *n_new, void *stream);
 

@@ -10,7 +10,8 @@ class Model:
         self.refs = [0] * n_pages
         self.table = [[-1] * width for _ in range(max_seqs)]
         self.lens = [0] * max_seqs
-        self.status = 0
+        self.status = 0                                          # the caller clears it
+        self.refused = False
 
     def _free(self):
         return [p for p, r in enumerate(self.refs) if r == 0]
@@ -19,7 +20,9 @@ class Model:
         self.status = self.status or code
 
     def extend(self, seqs, n_new):
-        free, takes = self._free(), []
+        if self.refused and self.status:
+            return
+        self.refused, free, takes = True, self._free(), []
         for s, n in zip(seqs, n_new):
             if not 0 <= s < len(self.lens):
                 continue
@@ -28,6 +31,7 @@ class Model:
             takes += [(s, p) for p in range(-(-self.lens[s] // self.T), -(-(self.lens[s] + n) // self.T))]
         if len(takes) > len(free):
             return self._blame(-2)
+        self.refused = False
         for (s, at), page in zip(takes, free):
             self.table[s][at], self.refs[page] = page, 1
         for s, n in zip(seqs, n_new):

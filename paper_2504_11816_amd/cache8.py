@@ -72,7 +72,7 @@ class Cache8:
         self.pages = Pages(table=self.table, lens=self.lens, refs=self.refs, page_tokens=page_tokens,
                            arrays=[PageArray(self.codes, TILE, whole_units=True), PageArray(self.scales, TILE, whole_units=True)],
                            rows=[RowArray(self.tails, 2 * n_kv_heads, TILE)])
-        c.refused = self.pages.status.data_ptr() + 12        # what the last extend() could not take is not written to
+        c.refused = self.pages.status.data_ptr() + 12        # after an extend() that could not take its pages nothing is written until check()
         # the workspace of a whole batch; steps of one cache follow one another on one stream
         n = min(max_seqs, 4096)
         self.workspace = torch.empty(bytes_of("okv8_workspace_bytes", n), dtype=torch.uint8, device=self.device)

@@ -89,6 +89,9 @@ constexpr int kEachSeq = OKV_PAGES_MAX_SEQS / kThreads;
 
 __global__ void __launch_bounds__(kThreads) extend_kernel(State s, const int32_t *seqs, const int32_t *n_new, int n, int32_t *fresh) {
   __shared__ int sums[kThreads / 64], first[OKV_PAGES_MAX_SEQS + 1], bad;
+  // After one that was refused nothing grows until the caller has seen it: with this one's outcome in its place, the steps over the other's
+  // sequences would write.  (Nobody writes status before the barriers of `scan`.)
+  if (s.status[0] != 0 && s.status[3] != 0) return;
   if (threadIdx.x == 0) bad = 0;
   __syncthreads();
   const int each = (n + kThreads - 1) / kThreads;

@@ -82,7 +82,8 @@ class Pages:
             binding._check(rc)
 
     def extend(self, seqs, n_new=None):
-        """Sequence seqs[i] grows by n_new[i] tokens (None: one each) and takes the pages that it lacks."""
+        """Sequence seqs[i] grows by n_new[i] tokens (None: one each) and takes the pages that it lacks.  Changes nothing where there are too few, and
+        nothing from then on until check() has raised."""
         at, n = self._ids("seqs", seqs), seqs.shape[0]
         self._done(self._lib.okv_pages_extend(self.ref, n, at, None if n_new is None else self._ids("n_new", n_new, n), binding.current_stream(self.device)))
 
@@ -115,8 +116,8 @@ class Pages:
         self._done(self._lib.okv_pages_copy(self.ref, n, at, self._ids("dst_ids", dst_ids, n), c, pages, binding.current_stream(self.device)))
 
     def check(self):
-        """Waits for the GPU; raises if a call could not be carried out since the last check.  After an extend() that could not be, a Cache8 is not
-        written to until one is carried out or check() has raised."""
+        """Waits for the GPU; raises if a call could not be carried out since the last check.  After an extend() that could not be, no
+        sequence grows and a Cache8 is not written to until check() has raised."""
         code = int(self.status[0])
         if code:
             self.status[::3] = 0
