@@ -78,6 +78,7 @@ class Cache8:
         self.workspace = torch.empty(bytes_of("okv8_workspace_bytes", n), dtype=torch.uint8, device=self.device)
         self._step = binding.Okv8Step(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace.numel())
         self._step_ref = ctypes.byref(self._step)
+        self._reads = ()                                     # lens and seqs of the step that begin() described
         lib = binding.lib()
         self._store, self._load, self._decode_step = lib.okv8_store, lib.okv8_load, lib.okv8_decode_step
 
@@ -132,8 +133,10 @@ class Cache8:
         s.batch, s.appends, s.seqs, s.lens, s.stream = batch, appends, _address(seqs), lens.data_ptr(), binding.current_stream(self.device)
 
     def begin(self, batch, lens, seqs=None, appends=True):
-        """Describes a step whose layers come one by one (attend)."""
+        """Describes a step whose layers come one by one (attend).  Every layer reads lens and seqs: they are kept until the next begin(), and must not change
+        before the last layer."""
         self._describe(batch, int(appends), lens, seqs)
+        self._reads = lens, seqs
         binding._check(binding.lib().okv8_step_begin(self.ref, self._step_ref))
 
     def attend(self, layer, q, k_new, v_new, out):

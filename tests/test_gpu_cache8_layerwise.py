@@ -1,0 +1,56 @@
+"""Steps over the 8-bit cache whose layers come one by one: what begin() is given, the calls between it and the layers, the streams that they come on, and
+what attend() refuses."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2504_11816_amd.cache8 import Cache8
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+L, H, G, D, T = 2, 4, 2, 64, 32
+
+
+def ids(x):
+    return torch.tensor(list(x), dtype=torch.int32, device=DEV)
+
+
+def filled(lens, width=40, seed=1):
+    """A cache with these sequences, one token of room in each; width: of the page table, above 32 sequences are cut among wavefronts."""
+    rng = np.random.default_rng(seed)
+    c = Cache8(n_layers=L, n_q_heads=H, n_kv_heads=G, head_dim=D, page_tokens=T, n_pages=sum(n // T + 1 for n in lens), max_seqs=len(lens), max_pages_per_seq=width,
+               out_dtype=torch.float32, device=DEV)
+    every = ids(range(len(lens)))
+    c.pages.extend(every, ids(lens))
+    k, v = (torch.tensor(rng.standard_normal((L, sum(lens), G, D)), dtype=torch.float16, device=DEV) for _ in range(2))
+    c.store(k, v, ids(np.concatenate([[0], np.cumsum(lens)])), c.lens)
+    c.pages.extend(every)
+    c.pages.check()
+    return c
+
+
+def inputs(B, seed=2):
+    rng = np.random.default_rng(seed)
+    return [torch.tensor(rng.standard_normal((L, B, h, D)), dtype=torch.float16, device=DEV) for h in (H, G, G)]
+
+
+def layers(c, q, k, v, out):
+    for layer in range(L):
+        c.attend(layer, q[layer], k[layer], v[layer], out[layer])
+
+
+@pytest.mark.parametrize("width", [32, 40])
+def test_lengths_and_rows_that_nobody_else_keeps(width):
+    """begin() with temporaries: what is allocated and filled after it is not what the layers read."""
+    lens = [40, 100, 7, 64]
+    a, b = filled(lens, width), filled(lens, width)
+    q, k, v = inputs(3)
+    outs = [torch.empty((L, 3, H, D), device=DEV) for _ in range(2)]
+    seqs, now = ids([2, 0, 3]), a.lens.clone()
+    a.begin(3, now, seqs)
+    layers(a, q, k, v, outs[0])
+    b.begin(3, b.lens + 0, ids([2, 0, 3]))
+    others = [torch.ones(n, dtype=torch.int32, device=DEV) for n in (3, 4) for _ in range(50)]
+    layers(b, q, k, v, outs[1])
+    assert torch.equal(*outs) and torch.equal(a.tails, b.tails) and torch.equal(a.codes, b.codes)
+    assert all((x == 1).all() for x in others)
