@@ -78,7 +78,9 @@ class Cache8:
         self.workspace = torch.empty(bytes_of("okv8_workspace_bytes", n), dtype=torch.uint8, device=self.device)
         self._step = binding.Okv8Step(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace.numel())
         self._step_ref = ctypes.byref(self._step)
-        self._reads = ()                                     # lens and seqs of the step that begin() described
+        # the step that begin() described, and the lens and seqs that its layers read; None: there is none
+        self._layers = binding.Okv8Step(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace.numel())
+        self._layers_ref, self._reads = ctypes.byref(self._layers), None
         lib = binding.lib()
         self._store, self._load, self._decode_step = lib.okv8_store, lib.okv8_load, lib.okv8_decode_step
 
@@ -127,22 +129,24 @@ class Cache8:
 
     # ---- decode steps -----------------------------------------------------------------------------
 
-    def _describe(self, batch, appends, lens, seqs):
+    def _describe(self, s, batch, appends, lens, seqs):
+        self._reads = None                                   # (the workspace is this step's from here on)
         self._lens(lens, seqs, batch)
-        s = self._step
         s.batch, s.appends, s.seqs, s.lens, s.stream = batch, appends, _address(seqs), lens.data_ptr(), binding.current_stream(self.device)
 
     def begin(self, batch, lens, seqs=None, appends=True):
-        """Describes a step whose layers come one by one (attend).  Every layer reads lens and seqs: they are kept until the next begin(), and must not change
-        before the last layer."""
-        self._describe(batch, int(appends), lens, seqs)
+        """Describes a step whose layers come one by one (attend).  Every layer reads lens and seqs: they are kept until the next begin() or step(), and
+        must not change before the last layer."""
+        self._describe(self._layers, batch, int(appends), lens, seqs)
+        binding._check(binding.lib().okv8_step_begin(self.ref, self._layers_ref))
         self._reads = lens, seqs
-        binding._check(binding.lib().okv8_step_begin(self.ref, self._step_ref))
 
     def attend(self, layer, q, k_new, v_new, out):
         """One layer of the step that begin() described: q [batch][H][d], k_new / v_new [batch][G][d] (rows may be strided, k_new and v_new alike)
-        or None, out [batch][H][d]."""
-        batch = self._step.batch
+        or None, out [batch][H][d].  A step() of all layers, or a begin() that is refused, ends the step."""
+        if self._reads is None:
+            raise ValueError("begin() describes the step first (a step() of all layers in between ends it)")
+        batch = self._layers.batch
         if q.dtype != torch.float16 or tuple(q.shape) != (batch, self.H, self.d) or q.stride(2) != 1 or q.stride(1) != self.d:
             raise ValueError(f"q must be fp16 [{batch}][{self.H}][{self.d}], rows may be strided")
         need("out", out, self.out_dtype, (batch, self.H, self.d), self.device)
@@ -152,7 +156,7 @@ class Cache8:
                 if t.dtype != torch.float16 or tuple(t.shape) != (batch, self.G, self.d) or t.stride(2) != 1 or t.stride(1) != self.d or t.stride(0) != k_new.stride(0):
                     raise ValueError(f"k_new and v_new must be fp16 [{batch}][{self.G}][{self.d}], rows strided alike")
             kv_stride = k_new.stride(0) if batch > 1 else self.G * self.d
-        binding._check(binding.lib().okv8_decode_attn(self.ref, self._step_ref, layer, q.data_ptr(), q.stride(0) if batch > 1 else self.H * self.d,
+        binding._check(binding.lib().okv8_decode_attn(self.ref, self._layers_ref, layer, q.data_ptr(), q.stride(0) if batch > 1 else self.H * self.d,
                                                       _address(k_new), _address(v_new), kv_stride, out.data_ptr()))
 
     def step(self, q, k_new, v_new, out, lens, seqs=None):
@@ -168,7 +172,7 @@ class Cache8:
         if k_new is not None and not (_fits(k_new, torch.float16, (L, batch, self.G, d), device) and _fits(v_new, torch.float16, (L, batch, self.G, d), device)):
             need("k_new", k_new, torch.float16, (L, batch, self.G, d), device)
             need("v_new", v_new, torch.float16, (L, batch, self.G, d), device)
-        self._describe(batch, 0 if k_new is None else 1, lens, seqs)
+        self._describe(self._step, batch, 0 if k_new is None else 1, lens, seqs)
         rc = self._decode_step(self.ref, self._step_ref, q.data_ptr(), _address(k_new), _address(v_new), out.data_ptr())
         if rc:
             binding._check(rc)

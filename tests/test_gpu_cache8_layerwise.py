@@ -54,3 +54,40 @@ def test_lengths_and_rows_that_nobody_else_keeps(width):
     layers(b, q, k, v, outs[1])
     assert torch.equal(*outs) and torch.equal(a.tails, b.tails) and torch.equal(a.codes, b.codes)
     assert all((x == 1).all() for x in others)
+
+
+@pytest.mark.parametrize("width", [32, 40])
+def test_a_step_of_all_layers_ends_a_layerwise_one(width):
+    """A step() between two layers has lengths, rows and a plan of its own: the other layers are refused, and change nothing."""
+    c = filled([40, 100, 7], width)
+    q, k, v = inputs(3)
+    out = torch.empty((L, 3, H, D), device=DEV)
+    c.begin(3, c.lens)
+    c.attend(0, q[0], k[0], v[0], out[0])
+    c.step(q[:, :2].contiguous(), None, None, torch.empty((L, 2, H, D), device=DEV), c.lens, ids([1, 2]))
+    before = [x.clone() for x in (c.codes, c.scales, c.tails, out)]
+    for n in (2, 3):
+        with pytest.raises(ValueError):
+            c.attend(1, q[1, :n], k[1, :n], v[1, :n], out[1, :n])
+    with pytest.raises(ValueError):
+        c.attend(1, q[1, :2], None, None, out[1, :2])
+    assert all(torch.equal(x, y) for x, y in zip(before, (c.codes, c.scales, c.tails, out)))
+    c.begin(3, c.lens)                                       # again, from its first layer
+    layers(c, q, k, v, out)
+    other, want = filled([40, 100, 7], width), torch.empty_like(out)
+    other.begin(3, other.lens)
+    layers(other, q, k, v, want)
+    assert torch.equal(out, want) and torch.equal(c.tails, other.tails)
+
+
+def test_a_layer_without_a_step():
+    c = filled([40, 7])
+    q, k, v = inputs(2)
+    out = torch.empty((2, H, D), device=DEV)
+    with pytest.raises(ValueError):
+        c.attend(0, q[0], k[0], v[0], out)
+    c.begin(2, c.lens)
+    with pytest.raises(ValueError):
+        c.begin(2, c.lens.long())                            # refused: there is no step any more
+    with pytest.raises(ValueError):
+        c.attend(0, q[0], k[0], v[0], out)
