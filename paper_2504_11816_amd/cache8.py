@@ -156,6 +156,7 @@ class Cache8:
                 if t.dtype != torch.float16 or tuple(t.shape) != (batch, self.G, self.d) or t.stride(2) != 1 or t.stride(1) != self.d or t.stride(0) != k_new.stride(0):
                     raise ValueError(f"k_new and v_new must be fp16 [{batch}][{self.G}][{self.d}], rows strided alike")
             kv_stride = k_new.stride(0) if batch > 1 else self.G * self.d
+        self._layers.stream = binding.current_stream(self.device)
         binding._check(binding.lib().okv8_decode_attn(self.ref, self._layers_ref, layer, q.data_ptr(), q.stride(0) if batch > 1 else self.H * self.d,
                                                       _address(k_new), _address(v_new), kv_stride, out.data_ptr()))
 

@@ -91,3 +91,51 @@ def test_a_layer_without_a_step():
         c.begin(2, c.lens.long())                            # refused: there is no step any more
     with pytest.raises(ValueError):
         c.attend(0, q[0], k[0], v[0], out)
+
+
+def test_layers_run_on_the_current_stream():
+    """A layer's call on another stream than begin()'s comes after what that stream had to do before: here a long product, then q, k and v."""
+    c, other_c = filled([40, 100, 7]), filled([40, 100, 7])
+    q, k, v = inputs(3)
+    want, out = (torch.empty((L, 3, H, D), device=DEV) for _ in range(2))
+    other_c.begin(3, other_c.lens)
+    layers(other_c, q, k, v, want)
+    late = [torch.zeros_like(x) for x in (q, k, v)]
+    a = torch.randn((8192, 8192), device=DEV)
+    torch.cuda.synchronize()
+    c.begin(3, c.lens)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(4):
+            a = a @ a
+            a = a / a.abs().max()
+        for to, x in zip(late, (q, k, v)):
+            to.copy_(x)
+        layers(c, *late, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(c.tails, other_c.tails)
+
+
+def test_captured_layers():
+    """begin() and the layers in a graph, replayed with eager work in between, against eager steps."""
+    c, other = filled([40, 31, 7]), filled([40, 31, 7])
+    q, k, v = inputs(3)
+    out, want = (torch.empty((L, 3, H, D), device=DEV) for _ in range(2))
+    every, lens, n = ids(range(3)), c.lens.clone(), other.lens.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.begin(3, lens, every)
+        layers(c, q, k, v, out)
+        lens.add_(1)
+    for i in range(5):
+        for x in (q, k, v):
+            x.normal_()
+        graph.replay()
+        torch.randn(1 << 14, device=DEV).sum().item()
+        other.begin(3, n, every)
+        layers(other, q, k, v, want)
+        n.add_(1)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(c.tails, other.tails), i
