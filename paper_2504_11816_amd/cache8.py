@@ -147,14 +147,17 @@ class Cache8:
         if self._reads is None:
             raise ValueError("begin() describes the step first (a step() of all layers in between ends it)")
         batch = self._layers.batch
-        if q.dtype != torch.float16 or tuple(q.shape) != (batch, self.H, self.d) or q.stride(2) != 1 or q.stride(1) != self.d:
-            raise ValueError(f"q must be fp16 [{batch}][{self.H}][{self.d}], rows may be strided")
+        if q.dtype != torch.float16 or tuple(q.shape) != (batch, self.H, self.d) or q.stride(2) != 1 or q.stride(1) != self.d or q.device != self.device:
+            raise ValueError(f"q must be fp16 [{batch}][{self.H}][{self.d}] on {self.device}, rows may be strided")
         need("out", out, self.out_dtype, (batch, self.H, self.d), self.device)
         kv_stride = 0
+        if (k_new is None) != (v_new is None) or (k_new is None) != (self._layers.appends == 0):
+            raise ValueError("k_new and v_new come together, if the step appends")
         if k_new is not None:
             for t in (k_new, v_new):
-                if t.dtype != torch.float16 or tuple(t.shape) != (batch, self.G, self.d) or t.stride(2) != 1 or t.stride(1) != self.d or t.stride(0) != k_new.stride(0):
-                    raise ValueError(f"k_new and v_new must be fp16 [{batch}][{self.G}][{self.d}], rows strided alike")
+                if (t.dtype != torch.float16 or tuple(t.shape) != (batch, self.G, self.d) or t.stride(2) != 1 or t.stride(1) != self.d
+                        or t.stride(0) != k_new.stride(0) or t.device != self.device):
+                    raise ValueError(f"k_new and v_new must be fp16 [{batch}][{self.G}][{self.d}] on {self.device}, rows strided alike")
             kv_stride = k_new.stride(0) if batch > 1 else self.G * self.d
         self._layers.stream = binding.current_stream(self.device)
         binding._check(binding.lib().okv8_decode_attn(self.ref, self._layers_ref, layer, q.data_ptr(), q.stride(0) if batch > 1 else self.H * self.d,

@@ -139,3 +139,22 @@ def test_captured_layers():
         n.add_(1)
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(c.tails, other.tails), i
+
+
+def test_wrong_tensors_are_refused():
+    """On the host, before anything is launched."""
+    c = filled([40, 100, 7])
+    q, k, v = (x[0] for x in inputs(3))
+    out = torch.empty((3, H, D), device=DEV)
+    before = [x.clone() for x in (c.codes, c.scales, c.tails)]
+    good = dict(q=q, k_new=k, v_new=v, out=out)
+    c.begin(3, c.lens)
+    for bad in (dict(q=q.cpu()), dict(k_new=k.cpu()), dict(v_new=v.cpu()), dict(out=out.cpu()), dict(k_new=None), dict(v_new=None), dict(k_new=None, v_new=None),
+                dict(q=q.float()), dict(q=q[:2]), dict(k_new=k[:, :1]), dict(v_new=v.float()), dict(v_new=v.transpose(0, 1)), dict(out=out.half()), dict(out=out[:2])):
+        with pytest.raises(ValueError):
+            c.attend(0, **{**good, **bad})
+    c.begin(3, c.lens, appends=False)
+    for bad in (dict(), dict(k_new=None), dict(v_new=None)):
+        with pytest.raises(ValueError):
+            c.attend(0, **{**good, **bad})
+    assert all(torch.equal(x, y) for x, y in zip(before, (c.codes, c.scales, c.tails)))
