@@ -42,7 +42,8 @@ int okv_linear4_pack(void *dst, const void *codes, int32_t per_byte, const void 
  *   zeros 0:  scale = max |w| / 7,                           code = clamp(rne(w / scale) + 8, 0, 15)
  *   zeros 1:  scale = (max(w, 0) - min(w, 0)) / 15,  zero = rne(-min(w, 0) / scale),
  *             code = clamp(rne(w / scale) + zero, 0, 15)
- * with the scale rounded to fp16 before it is divided by (a group whose scale is 0 in fp16 has scale 0). */
+ * with the scale rounded to fp16 before it is divided by (a group whose scale is 0 in fp16 has scale 0).
+ * A group with a weight that is infinite or NaN has scale NaN, so that every result of its feature is NaN. */
 int okv_linear4_quantize(void *dst, const void *src, int32_t n_out, int32_t n_in, int32_t group, int32_t zeros, void *stream);
 
 /* out = act(x W^T + bias) + residual, as okv_linear.

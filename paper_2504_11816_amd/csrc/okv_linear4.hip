@@ -287,13 +287,14 @@ __global__ void __launch_bounds__(256) scales4_kernel(Packed to, const _Float16 
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int n = (int)(i / padded), g = (int)(i % padded);
     float lo = 0.f, hi = 0.f;
+    bool finite = true;                  // (the minimum and the maximum pass over NaN)
     if (g < groups)
       for (int k = 0; k < group; k += 8) {
         const half8 w = *reinterpret_cast<const half8 *>(src + (int64_t)n * n_in + (int64_t)g * group + k);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) lo = fminf(lo, (float)w[e]), hi = fmaxf(hi, (float)w[e]);
+        for (int e = 0; e < 8; ++e) lo = fminf(lo, (float)w[e]), hi = fmaxf(hi, (float)w[e]), finite = finite && __builtin_isfinite((float)w[e]);
       }
-    const _Float16 scale = (_Float16)(to.zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f);
+    const _Float16 scale = (_Float16)(!finite ? __builtin_nanf("") : to.zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f);
     to.scales[scale_at(n, g, padded, kBlockIn / group)] = scale;
     if (to.zeros) to.zeros[zero_at(n, g, padded, kBlockIn / group)] = (float)scale > 0.f ? (uint8_t)fminf(__builtin_rintf(-lo / (float)scale), 15.f) : 8;
   }

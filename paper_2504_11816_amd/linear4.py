@@ -57,7 +57,8 @@ class Linear4:
 
     @classmethod
     def quantize(cls, weight, group=128, zeros=False, bias=None):
-        """Quantises fp16 [n_out][n_in] weights, every group by itself (see the header)."""
+        """Quantises fp16 [n_out][n_in] weights, every group by itself (see the header).  A group with a weight that is infinite or NaN is
+        NaN throughout."""
         if weight.dtype != torch.float16 or weight.dim() != 2:
             raise ValueError("weight must be an fp16 matrix")
         w = cls.__new__(cls)
