@@ -516,6 +516,13 @@ struct Softmax8 {
     o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, o[e], 0, 0, 0);
     o_lo[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo, o_lo[e], 0, 0, 0);
   }
+  // The same for values that may be infinite: a weight that hi has whole leaves lo 0, whose product with an infinity would be NaN.  (Infinities and NaN
+  // reach the sums by hi, and are the largest finite number in lo's.)
+  __device__ __forceinline__ void add_any(const int e, const half8 v, const half8 hi, const half8 lo) {
+    const half8 most = (half8)(_Float16)65504.f;
+    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, o[e], 0, 0, 0);
+    o_lo[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_elementwise_max(__builtin_elementwise_min(v, most), -most), lo, o_lo[e], 0, 0, 0);
+  }
   __device__ __forceinline__ floatx4 sum_of(const int e) const { return o[e] + o_lo[e] * (1.f / kLo); }
   __device__ __forceinline__ void write(const Attn8 &a, const int64_t slot, const int g, const int lane) const {
     const float sum = sum_with_lane_xor<16>(sum_with_lane_xor<32>(l));
@@ -583,7 +590,7 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
     half8 hi, lo;
     acc.weigh(score, hi, lo, 1.f);
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) acc.add(e, x.v[e], hi, lo);
+    for (int e = 0; e < D / 16; ++e) acc.add_any(e, x.v[e], hi, lo);
     if (full && writes) x.template quantise_to<FMT>(a.c, clamp_page(to_page, s.n_pages), (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
   }
 }
@@ -875,9 +882,10 @@ __global__ void __launch_bounds__(256) merge8_kernel(Merge8 a) {
       if (i) ask(i);
 #pragma unroll
       for (int j = 0; j < kJoin; ++j) {
-        const float wi = i + j < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(i + j, n - 1))) : 0.f;
+        const bool there = i + j < n;                      // (beyond them x is the last one again, which may be infinite)
+        const float wi = there ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(i + j, n - 1))) : 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(wi, x[j][e], o[e]);
+        for (int e = 0; e < E; ++e) o[e] = fmaf(wi, there ? x[j][e] : 0.f, o[e]);
       }
     }
   }
