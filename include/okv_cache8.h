@@ -125,8 +125,9 @@ int okv8_step_begin(const okv8_cache *c, const okv8_step *s);
  *     out[b][h] = sum_i softmax_i(q[b][h] . k_i / sqrt(d)) v_i,   i < lens,  KV head h / (H / G)
  * An appending step reads the tokens before 32 floor((lens - 1) / 32) as their codes say and the others, the
  * appended one included, in fp16 from the tail, and then quantises a tail that is full; a step that appends
- * nothing reads the tokens before 32 floor(lens / 32) as their codes say.  An infinite value in the tail makes the result infinite
- * (NaN if its weight is below 2^-31 of the largest, or if the same element has the other infinity or a NaN).
+ * nothing reads the tokens before 32 floor(lens / 32) as their codes say.  Infinite numbers in the tail are taken for what they
+ * are: a score of -infinity leaves its key out (NaN if no key is left), an infinite value makes the result infinite (NaN if its weight is
+ * below 2^-31 of the largest, if the same element has the other infinity, or a NaN).
  *   q     fp16 [batch][H][d], q_stride elements from a sequence to the next (a multiple of 8)
  *   k_new, v_new  fp16 [batch][G][d], kv_stride likewise; both NULL if the step does not append
  *   out   [batch][H][d] in out_dtype */

@@ -588,6 +588,9 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
       for (int i = 0; i < 4; ++i) score[4 * h + i] = 16 * h + 4 * (lane / 16) + i < rows ? t[i] * a.scale_log2e : -__builtin_inff();
     }
     half8 hi, lo;
+    // Keys may be infinite as well: where all scores are -infinity, weights are 0 and not NaN, since other pieces of the sequence may have more, and m
+    // says that there were keys.
+    acc.m = fmaxf(acc.m, -__FLT_MAX__);
     acc.weigh(score, hi, lo, 1.f);
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) acc.add_any(e, x.v[e], hi, lo);
@@ -831,7 +834,7 @@ __global__ void __launch_bounds__(64 * WAVES) attn8_whole_kernel(const Attn8 lau
       all = fmaf(by, ml_all[w][1][r], all);
       o += by * o_all[w][e][l];
     }
-    o *= all == 0.f ? 0.f : 1.f / all;      // no key at all: 0
+    o *= all == 0.f && top == -__builtin_inff() ? 0.f : 1.f / all;      // no key at all: 0
     const int64_t to = ((int64_t)item * s.G * s.R + g * s.R + r) * D + 16 * e + 4 * (l / 16);
     if (a.out_fp32) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + to) = o;
     else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + to) = half4{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
@@ -896,11 +899,11 @@ __global__ void __launch_bounds__(256) merge8_kernel(Merge8 a) {
     for (int e = 0; e < E; ++e) all[wave][2 + E * lane + e] = o[e];
     __syncthreads();
     if (wave) return;
-    float m = top;
+    const float own = top;
 #pragma unroll
-    for (int i = 1; i < WAVES; ++i) m = fmaxf(m, all[i][0]);
-    const float base = m == -__builtin_inff() ? 0.f : m;
-    const float w0 = __builtin_amdgcn_exp2f(top - base);
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, all[i][0]);
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    const float w0 = __builtin_amdgcn_exp2f(own - base);
     sum *= w0;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= w0;
@@ -912,7 +915,7 @@ __global__ void __launch_bounds__(256) merge8_kernel(Merge8 a) {
       for (int e = 0; e < E; ++e) o[e] = fmaf(w, all[i][2 + E * lane + e], o[e]);
     }
   }
-  const float by = sum == 0.f ? 0.f : 1.f / sum;      // no key at all: 0
+  const float by = sum == 0.f && top == -__builtin_inff() ? 0.f : 1.f / sum;      // no key at all: 0
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int64_t to = (int64_t)row * D + E * lane + e;

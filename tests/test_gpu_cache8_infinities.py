@@ -69,3 +69,11 @@ def test_infinite_values(fmt, d, width, n, appends):
     check(fmt, d, width, n, appends, lambda tail: [
         [], [("v", tail[-1], 3, INF)], [("v", tail[len(tail) // 2], 3, -INF), ("v", tail[-1], d - 1, INF)], [("v", i, 9, INF) for i in tail],
         [("v", tail[0], 7, INF), ("v", tail[-1], 7, -INF)]])
+
+
+@every_case
+def test_infinite_scores(fmt, d, width, n, appends):
+    """A score of -infinity leaves its key out: one of the tail's, all of them (NaN, if there are no others), all but one; one of +infinity makes NaN."""
+    check(fmt, d, width, n, appends, lambda tail: [
+        [], [("k", tail[-1], 5, -INF)], [("k", i, 5, -INF) for i in tail], [("k", tail[len(tail) // 2], 5, INF)],
+        [("k", i, 5, -INF) for i in tail[1:]] + [("v", tail[0], 0, INF)]])
