@@ -41,14 +41,17 @@ __device__ __forceinline__ int length_of(const State &s, int r) { return min(max
 __device__ __forceinline__ int pages_of(const State &s, int n) { return (n + (1 << s.log2_T) - 1) >> s.log2_T; }
 __device__ __forceinline__ void blame(const State &s, int code) { if (s.status[0] == 0) s.status[0] = code; }
 
-// Exclusive prefix sum over the workgroup; `total` is everybody's
+// x + y, numbers that are not negative, at most 2^31 - 1
+__device__ __forceinline__ int add_up(const int x, const int y) { return (int)min((uint32_t)x + (uint32_t)y, 0x7fffffffu); }
+
+// Exclusive prefix sum over the workgroup; `total` is everybody's.  Sums that pass 2^31 - 1 stay there (and the prefixes mean nothing)
 __device__ __forceinline__ int scan(const int x, int &total, int *sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int upto = x;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int other = __shfl_up(upto, o);
-    if (lane >= o) upto += other;
+    if (lane >= o) upto = add_up(upto, other);
   }
   __syncthreads();                       // sums may still be read from the last time
   if (lane == 63) sums[wave] = upto;
@@ -57,8 +60,8 @@ __device__ __forceinline__ int scan(const int x, int &total, int *sums) {
   total = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < wave) before += sums[w];
-    total += sums[w];
+    if (w < wave) before = add_up(before, sums[w]);
+    total = add_up(total, sums[w]);
   }
   return before;
 }
@@ -104,13 +107,13 @@ __global__ void __launch_bounds__(kThreads) extend_kernel(State s, const int32_t
     const int len = length_of(s, row), add = n_new ? max(n_new[j], 0) : 1;
     if (add > (s.width << s.log2_T) - len) bad = 1;
     else more[i] = pages_of(s, len + add) - pages_of(s, len);
-    need += more[i];
+    need = add_up(need, more[i]);
   }
   int total, at = scan(need, total, sums);
 #pragma unroll
   for (int i = 0; i < kEachSeq; ++i) {
     if (i < each) first[threadIdx.x * each + i] = at;
-    at += more[i];
+    at = add_up(at, more[i]);
   }
   if (threadIdx.x == kThreads - 1) first[kThreads * each] = at;
   __syncthreads();

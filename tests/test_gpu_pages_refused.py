@@ -85,3 +85,17 @@ def test_later_extensions_wait_until_the_status_is_cleared():
     m.status = 0
     do("extend", [0], [1])
     assert lens.tolist() == [7, 6, 1]
+
+
+@pytest.mark.parametrize("rows,width", [(2, 1 << 30), (8, 1 << 28), (3, 1 << 30)])
+def test_more_pages_than_are_counted_in_32_bits(rows, width):
+    """A call whose sequences lack 2^31 pages and more together, each of them less: refused like any other that lacks some."""
+    table = torch.full((rows, width), -1, dtype=torch.int32, device=DEV)
+    lens, refs = torch.zeros(rows, dtype=torch.int32, device=DEV), torch.zeros(100, dtype=torch.int32, device=DEV)
+    p = Pages(table=table, lens=lens, refs=refs, page_tokens=1)
+    p.extend(ids(range(rows)), ids([width] * rows))
+    assert p.status.tolist()[::3] == [binding.OKV_ENOSPC] * 2 and not lens.any() and not refs.any()
+    p.status.zero_()
+    p.extend(ids(range(rows)), ids(range(rows)))
+    assert p.status.tolist()[0] == 0 and lens.tolist() == list(range(rows)) and int(refs.sum()) == sum(range(rows))
+    assert [int(table[r, i]) for r in range(rows) for i in range(r + 1)] == [x for r in range(rows) for x in [*range(r * (r - 1) // 2, r * (r + 1) // 2), -1]]
