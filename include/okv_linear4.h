@@ -9,6 +9,10 @@
  * code in 0 .. 15; scale fp16; zero in 0 .. 15, or 8 everywhere.  The products take code - zero exactly in
  * fp16 on the matrix cores and multiply the fp32 sums of a group by its scale: weights are not rounded again.
  *
+ * Faster than the fp16 products of okv_layer.h for few rows; for many they save memory and cost time.  us, codes and weights from HBM, groups of
+ * 128 / of 32 / fp16, 16384 x 4096: 16 rows 11.3 / 12.2 / 25.0, 64 rows 23.4 / 28.4 / 25.1, 128 rows 32 / 50 / 33, 256 rows 62 / 96 / 47, 1024
+ * rows 239 / 370 / 115, 4096 rows 945 / 1453 / 461; 4096 x 4096: 32 rows 9.8 / 10.1 / 9.7, 256 rows 23.8 / 27.5 / 19.1, 1024 rows 63 / 95 / 39.
+ *
  * Conventions as in okv_layer.h.
  */
 #ifndef OKV_LINEAR4_H
