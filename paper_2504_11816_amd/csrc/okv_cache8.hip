@@ -46,14 +46,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = OKV8_TILE;
-#ifndef OKV8_WAVES
-#define OKV8_WAVES 1024
-#endif
 // Wavefronts of the part of a launch that reads codes: one per SIMD at d = 128, with 8 KiB in flight each, two at d = 64, where a tile is half that.  us of a
 // case of 4 layers x 2 of 32 x 1500 keys x 32 heads (d = 64) with 1024 / 2048 / 4096 of them 349 / 247 / 249; at d = 128 with 1024 / 1536 /
 // 2048: 32 x 768 keys x 32 heads 283 / 292 / 284, ragged grouped heads 388 / 402 / 399, two long documents 243 / 242 / 241, 16 x 100..400 keys x 12
 // heads 29 / - / 34.
-constexpr int kWaves = OKV8_WAVES;
+constexpr int kWaves = 1024;
 constexpr int kMinSpan = 2;              // tiles of a stretch at least
 
 struct Shape8 {
@@ -251,7 +248,6 @@ __device__ __forceinline__ int sequence_of(const int32_t *starts, const int batc
 
 struct RowsOf {          // the rows of a call that belong to one sequence
   int row, first, n, after, before;      // row of the page table; first row of k / v; rows; tokens after and before
-  int64_t limit;
 };
 __device__ __forceinline__ RowsOf rows_of(const RowsArgs &a, const int b) {
   RowsOf r;
@@ -598,7 +594,7 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
   }
 }
 
-template <int D, int FMT, bool NT>
+template <int D, bool NT>
 __device__ __forceinline__ void load_codes(u32x4 (&w)[D / 32], const uint8_t *from) {
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) {
@@ -744,8 +740,8 @@ __global__ void __launch_bounds__(256) attn8_kernel(const Attn8 launch) {
   const auto fetch = [&](Buffer &t) {
     if (ahead == 0) return;
     place();
-    load_codes<D, FMT, NT>(t.k, at);
-    load_codes<D, FMT, NT>(t.v, at + v_step);
+    load_codes<D, NT>(t.k, at);
+    load_codes<D, NT>(t.v, at + v_step);
     t.scale = *reinterpret_cast<const float2 *>(scale_from);
     t.b = fb, t.tiles = in_seq;
     --ahead;
@@ -800,8 +796,8 @@ __global__ void __launch_bounds__(64 * WAVES) attn8_whole_kernel(const Attn8 lau
   const auto fetch = [&](const int t) {
     const int64_t at = ((int64_t)__builtin_amdgcn_readlane(pages, t >> log2_tpp) << log2_tpp) + (t & ((1 << log2_tpp) - 1));
     const uint8_t *from = a.c.codes + at * s.G * 2 * kTile * D + tile_at<D>(s, 0, 0, g) + 16 * lane;
-    load_codes<D, FMT, false>(tile.k, from);
-    load_codes<D, FMT, false>(tile.v, from + s.gg * kTile * D);
+    load_codes<D, false>(tile.k, from);
+    load_codes<D, false>(tile.v, from + s.gg * kTile * D);
     tile.scale = *reinterpret_cast<const float2 *>(a.c.scales + (at * s.G + g) * 2);
   };
   half8 q[D / 32];
