@@ -484,9 +484,14 @@ struct Softmax8 {
   // The scale is in the weights, so that the products add up in the accumulators of the matrix cores;
   // l counts the weights without it.  m is raised, and what is there multiplied down, only when a weight would pass 2^15, 8 above
   // the largest score that m was raised for: hardly ever after a piece's first tile.
+  // FIRST: nothing is there yet.  Then m tells even from scores that are all -infinity that there were keys (their weights are 0 and not NaN: other
+  // pieces of the sequence may have more).
+  template <bool FIRST = false>
   __device__ __forceinline__ void weigh(const float (&s)[8], half8 &hi, half8 &lo, const float scale) {
     const float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    if (__any(top > m + kTop)) {
+    if constexpr (FIRST) {
+      m = fmaxf(max_with_lane_xor<16>(max_with_lane_xor<32>(top)) - kRaised, -__FLT_MAX__);
+    } else if (__any(top > m + kTop)) {
       const float now = fmaxf(m, max_with_lane_xor<16>(max_with_lane_xor<32>(top)) - kRaised);
       const float alpha = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
       m = now;
@@ -508,18 +513,21 @@ struct Softmax8 {
     }
     l = fmaf(sum, scale, l);
   }
+  __device__ __forceinline__ floatx4 sum_of(const int e) const { return o[e] + o_lo[e] * (1.f / kLo); }
   __device__ __forceinline__ void add(const int e, const half8 v, const half8 hi, const half8 lo) {
     o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, o[e], 0, 0, 0);
     o_lo[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, lo, o_lo[e], 0, 0, 0);
   }
-  // The same for values that may be infinite: a weight that hi has whole leaves lo 0, whose product with an infinity would be NaN.  (Infinities and NaN
+  // The same of the first keys, whose values may be infinite: a weight that hi has whole leaves lo 0, whose product with an infinity would be NaN.  (Infinities and NaN
   // reach the sums by hi, and are the largest finite number in lo's.)
-  __device__ __forceinline__ void add_any(const int e, const half8 v, const half8 hi, const half8 lo) {
+  __device__ __forceinline__ void first(const int e, const half8 v, const half8 hi, const half8 lo) {
     const half8 most = (half8)(_Float16)65504.f;
-    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, o[e], 0, 0, 0);
-    o_lo[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_elementwise_max(__builtin_elementwise_min(v, most), -most), lo, o_lo[e], 0, 0, 0);
+    const floatx4 none = {0.f, 0.f, 0.f, 0.f};
+    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, hi, none, 0, 0, 0);
+    o_lo[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_elementwise_max(__builtin_elementwise_min(v, most), -most), lo, none, 0, 0, 0);
+    // (one sum leaves registers to the tile that is under way beside a tail: at d = 64 four wavefronts a SIMD and not three; at 128 it is slower)
+    if constexpr (D == 64) o[e] = sum_of(e), o_lo[e] = none;
   }
-  __device__ __forceinline__ floatx4 sum_of(const int e) const { return o[e] + o_lo[e] * (1.f / kLo); }
   __device__ __forceinline__ void write(const Attn8 &a, const int64_t slot, const int g, const int lane) const {
     const float sum = sum_with_lane_xor<16>(sum_with_lane_xor<32>(l));
     const int R = a.c.s.R, r = lane % 16;
@@ -554,7 +562,7 @@ __device__ __forceinline__ Keys8 keys_of(const Attn8 &a, const int b) {
   return k;
 }
 
-// A sequence's fp16 tail: the appended row goes there, its keys are attended, and it is quantised when it is full.
+// A sequence's fp16 tail: the appended row goes there, its keys are attended (the first ones of `acc`), and it is quantised when it is full.
 template <int D, int FMT>
 __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D / 32], const Attn8 &a, const Keys8 &keys, const int b, const int g,
                                             _Float16 *lds, const int lane) {
@@ -584,12 +592,9 @@ __device__ __forceinline__ void attend_tail(Softmax8<D> &acc, const half8 (&q)[D
       for (int i = 0; i < 4; ++i) score[4 * h + i] = 16 * h + 4 * (lane / 16) + i < rows ? t[i] * a.scale_log2e : -__builtin_inff();
     }
     half8 hi, lo;
-    // Keys may be infinite as well: where all scores are -infinity, weights are 0 and not NaN, since other pieces of the sequence may have more, and m
-    // says that there were keys.
-    acc.m = fmaxf(acc.m, -__FLT_MAX__);
-    acc.weigh(score, hi, lo, 1.f);
+    acc.template weigh<true>(score, hi, lo, 1.f);
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) acc.add_any(e, x.v[e], hi, lo);
+    for (int e = 0; e < D / 16; ++e) acc.first(e, x.v[e], hi, lo);
     if (full && writes) x.template quantise_to<FMT>(a.c, clamp_page(to_page, s.n_pages), (held / kTile) & ((1 << (s.log2_T - 5)) - 1), g, lane);
   }
 }
@@ -864,7 +869,8 @@ __global__ void __launch_bounds__(256) merge8_kernel(Merge8 a) {
     const auto ask = [&](const int i) {
 #pragma unroll
       for (int j = 0; j < kJoin; ++j) {
-        const float *from = a.part_o + at(p0 + min(i + j, n - 1)) * D + E * lane;
+        // (beyond the last piece the first one: if that is no tail, it is finite, or NaN as the result will be, and its weight here, 0, adds nothing)
+        const float *from = a.part_o + at(p0 + (i + j < n ? i + j : 0)) * D + E * lane;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[j][e] = from[e];
       }
@@ -877,14 +883,19 @@ __global__ void __launch_bounds__(256) merge8_kernel(Merge8 a) {
     sum = sum * old + wave_sum(w * ml.y);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= old;
+    if (n == 1) {                                          // a tail, which may be infinite
+      const float w0 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), 0));
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(w0, x[0][e], o[e]);
+      continue;
+    }
     for (int i = 0; i < n; i += kJoin) {
       if (i) ask(i);
 #pragma unroll
       for (int j = 0; j < kJoin; ++j) {
-        const bool there = i + j < n;                      // (beyond them x is the last one again, which may be infinite)
-        const float wi = there ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(i + j, n - 1))) : 0.f;
+        const float wi = i + j < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(i + j, n - 1))) : 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(wi, there ? x[j][e] : 0.f, o[e]);
+        for (int e = 0; e < E; ++e) o[e] = fmaf(wi, x[j][e], o[e]);
       }
     }
   }
