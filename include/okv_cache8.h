@@ -94,7 +94,8 @@ int okv8_store(const okv8_cache *c, int32_t layer, int32_t n_layers, int32_t bat
                int64_t row_stride, int64_t layer_stride, void *stream);
 
 /* The reverse: the last starts[b + 1] - starts[b] of lens[] tokens of every sequence as the cache holds
- * them (code * scale rounded to fp16, or the tail's rows), into k and v, shaped as for okv8_store. */
+ * them (code * scale rounded to fp16, or the tail's rows), into k and v, shaped as for okv8_store.  (A tile's largest number may be held up to
+ * 2^-11 of it too large: fp16's largest, 65504, comes out as an infinity.) */
 int okv8_load(const okv8_cache *c, int32_t layer, int32_t n_layers, int32_t batch, const int32_t *seqs,
               const int32_t *starts, const int32_t *lens, int64_t n_rows, void *k, void *v,
               int64_t row_stride, int64_t layer_stride, void *stream);
@@ -134,7 +135,8 @@ int okv8_step_begin(const okv8_cache *c, const okv8_step *s);
 int okv8_decode_attn(const okv8_cache *c, const okv8_step *s, int32_t layer, const void *q, int64_t q_stride,
                      const void *k_new, const void *v_new, int64_t kv_stride, void *out);
 
-/* A step whose inputs are there for all layers, in two launches, three beyond 64 sequences (okv8_step_begin and okv8_decode_attn for every layer
+/* A step whose inputs are there for all layers, in one launch where a row of the page table holds at most 1024 keys and there are few of (layer, sequence,
+ * KV head), otherwise in two, three beyond 64 sequences (okv8_step_begin and okv8_decode_attn for every layer
  * give the same up to the order in which partial results are added):
  * q [L][batch][H][d], k_new / v_new [L][batch][G][d] (or NULL), out [L][batch][H][d], all contiguous. */
 int okv8_decode_step(const okv8_cache *c, const okv8_step *s, const void *q, const void *k_new,

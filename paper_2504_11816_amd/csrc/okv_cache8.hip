@@ -19,10 +19,10 @@
 // partial results (max, sum, weighted sum) are joined by a second launch (short sequences are not cut and need none).  A step whose layers'
 // inputs are all there attends up to 32 layers in one launch, the stretches that much longer.
 //
-// Measured, us a launch: attention over 810 MB (4 layers of 32 x 768 keys x 32 heads, d = 128) 131 (6.2 TB/s), 158 where every tail is full and is
-// quantised; over 1.20 GB (2 layers of 128 x 512..4096 keys, 8 KV heads of 4) 180 (6.7 TB/s), its plan 5, joining 5.5; over 713 MB (2 layers of 2
-// documents of up to 131072 keys) 112 (6.3 TB/s), joining 6.  Storing 24 prompts of 100..2000 x 32 heads x 4 layers 495 (2.44 GB, 4.9 TB/s:
-// bound by HBM), reading them back 442 (5.5 TB/s).  What is counted as read past L2 is within 1 % of the bytes of codes, scales and tails.
+// Measured, us a launch: attention over 810 MB (4 layers of 32 x 768 keys x 32 heads, d = 128) 132 (6.1 TB/s), 159 where every tail is full and is
+// quantised; over 1.20 GB (2 layers of 128 x 512..4096 keys, 8 KV heads of 4) 184 (6.5 TB/s), its plan 5, joining 5.6; over 713 MB (2 layers of 2
+// documents of up to 131072 keys) 115 (6.2 TB/s), joining 6.  Storing 24 prompts of 100..2000 x 32 heads x 4 layers 500 (2.44 GB, 4.9 TB/s:
+// bound by HBM), reading them back 443 (5.5 TB/s).  What is counted as read past L2 is within 1 % of the bytes of codes, scales and tails.
 #include "okv_cache8.h"
 #include "okv_host.h"
 #include "okv_lanes.h"
@@ -47,9 +47,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = OKV8_TILE;
 // Wavefronts of the part of a launch that reads codes: one per SIMD at d = 128, with 8 KiB in flight each, two at d = 64, where a tile is half that.  us of a
-// case of 4 layers x 2 of 32 x 1500 keys x 32 heads (d = 64) with 1024 / 2048 / 4096 of them 349 / 247 / 249; at d = 128 with 1024 / 1536 /
-// 2048: 32 x 768 keys x 32 heads 283 / 292 / 284, ragged grouped heads 388 / 402 / 399, two long documents 243 / 242 / 241, 16 x 100..400 keys x 12
-// heads 29 / - / 34.
+// case of 4 layers x 2 of 32 x 1500 keys x 32 heads (d = 64) with 1024 / 2048 / 4096 of them 367 / 250 / 252; at d = 128 with 1024 / 1536 /
+// 2048: 32 x 768 keys x 32 heads 281 / 288 / 280, ragged grouped heads 381 / 399 / 396, two long documents 236 / 235 / 234.
 constexpr int kWaves = 1024;
 constexpr int kMinSpan = 2;              // tiles of a stretch at least
 
@@ -1086,9 +1085,9 @@ bool streamed(const okv8_cache *c) { return codes_layer_bytes(c) * c->n_layers >
 
 // Wavefronts of the workgroups that attend a whole sequence and KV head each, 0: the sequences are cut.  Lengths are on the GPU, so the rule goes by
 // what a row of the page table can hold: at most 1024 keys (a lane has a page), so that a long sequence among short ones costs little.
-// us a step cut / 4 / 8 wavefronts: 4 x 250..256 keys x 8 KV heads, d = 64, 7.9 / 4.7 / 4.9; 16 x 100..400 x 12, d = 128, 9.6 / 7.1 / 6.4;
-// 4 x 1000..1024 x 32, d = 128, 12.6 / 13.1 / 10.5; 100 x 10..200 x 8, d = 64, 12.0 / 5.9 / 8.1; 64 x 400..512 x 8, d = 128, 17.9 / 15.6 /
-// 18.3; and where it is not taken: 32 x 700..768 x 32, d = 128, 34.4 / 36.2 / 40.5; 1 x 2000 x 4, d = 64, 8.7 / 11.4 / 9.5.
+// us a step cut / 4 / 8 wavefronts: 4 x 250..256 keys x 8 KV heads, d = 64, 8.0 / 5.0 / 5.0; 16 x 100..400 x 12, d = 128, 10.0 / 7.2 / 6.7;
+// 4 x 1000..1024 x 32, d = 128, 13.3 / 13.4 / 10.9; 100 x 10..200 x 8, d = 64, 11.9 / 6.2 / 8.6; 64 x 400..512 x 8, d = 128, 17.8 / 15.8 /
+// 19.1; and where it is not taken: 32 x 700..768 x 32, d = 128, 34.9 / 36.6 / 41.8; 1 x 2000 x 4, d = 64, 8.9 / 11.6 / 9.9.
 int whole_waves(const okv8_cache *c, int32_t batch, int32_t layers) {
   const int64_t keys = (int64_t)c->max_pages_per_seq * c->page_tokens, groups = (int64_t)layers * batch * c->n_kv_heads;
   if (keys > 1024) return 0;

@@ -4,7 +4,7 @@
 //
 //   * one 16-byte load per lane brings a wavefront a block of 16 features x 128 inputs, in operand order for four 16x16x32
 //     matrix-core instructions: nothing moves between lanes;
-//   * a code becomes an fp16 number with one and-or (0x6400 | code is 1024 + code; four bits further up it is 1024 + 16 code) and one packed
+//   * a code becomes an fp16 number with one and-or (0x6400 | code is 1024 + code, a method that is widely published; four bits further up it is 1024 + 16 code) and one packed
 //     subtraction or fused multiply-add that also takes the zero point off: code - zero, exactly, at about one instruction a weight;
 //   * the sums of a group stay apart from the others' in fp32 and are multiplied by its scale there: one fma per result and group
 //     instead of one rounding per weight;

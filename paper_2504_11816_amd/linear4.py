@@ -6,7 +6,7 @@
     qkv(x, [q, k, v])                                 # the output features in up to three tensors
     w(x, y, residual=y)                               # y += x W^T + bias
 
-For a decode batch's rows: from 64 to 128 rows on, by group size and matrix, fp16 weights are faster (figures in the header).
+For a decode batch's rows: from 32 (4096 x 4096) to 128 rows on, by group size and matrix, fp16 weights are faster (figures in the header).
 """
 import ctypes
 
