@@ -115,7 +115,8 @@ typedef struct okv8_step {
 
 /* Workspace of a step of up to max_batch sequences; < 0 on a bad shape.  okv8_decode_step attends up to 32 layers in one launch
  * with it; what this returns for a cache of one layer is enough for okv8_decode_attn, and okv8_decode_step then takes fewer
- * layers at a time.  Its contents mean nothing between steps.  Steps that may run at the same time need
+ * layers at a time.  Its contents mean nothing between steps; from okv8_step_begin to the step's last okv8_decode_attn nothing else may use it
+ * (okv8_decode_step included), and seqs and lens must stay as they are.  Steps that may run at the same time need
  * workspaces of their own. */
 int64_t okv8_workspace_bytes(const okv8_cache *c, int32_t max_batch);
 
