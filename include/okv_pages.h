@@ -1,5 +1,5 @@
 /*
- * okv_pages -- pages of a paged KV cache: taking, forking, freeing, compacting and copying them, on one
+ * okv_pages -- pages of a paged KV cache: taking, forking, shortening, freeing, compacting and copying them, on one
  * MI355X.
  *
  * A cache whose pages are runs of bytes, the same number for every page, can be managed here: the fp16
@@ -90,6 +90,13 @@ int okv_pages_fork(const okv_pages *p, int32_t n, const int32_t *src, const int3
 
 /* The sequences become empty; pages that belong to no other are free.  seqs [n] (twice the same: once). */
 int okv_pages_free(const okv_pages *p, int32_t n, const int32_t *seqs, void *stream);
+
+/* Sequence seqs[i] loses its last n_drop[i] >= 0 tokens (drafted ones that were rejected); pages that no token of it is in any longer
+ * belong to it no more.  OKV_ESTATE, and nothing changes, where a sequence has fewer tokens, where the page that its new last token leaves partly
+ * filled is shared (a shared page is full), and where a row array no longer holds the rows of a group that becomes partly filled (with rows = 32: the
+ * new length is no multiple of 32 and lies below the last one that the old length has passed).
+ *   seqs [n] distinct, or NULL: i;  n_drop [n] */
+int okv_pages_shrink(const okv_pages *p, int32_t n, const int32_t *seqs, const int32_t *n_drop, void *stream);
 
 /* Moves pages so that the pages in use are 0 .. n_used - 1: the m-th of those with ids from n_used on goes
  * to the m-th free id below.  Table and refs follow.  Pages keep what they hold until they are taken

@@ -17,8 +17,10 @@ Modules
   pipeline_sim  replay of a copy/attend op trace on a fake copy engine
   tail_sim      replay of "newest blocks stay in HBM" on sets of row positions
   cache8        scales, codes and values of the 8-bit cache, and attention over them
-  pages         a model of extend, fork, free, compact and copy on page tables
+  pages         a model of extend, fork, shrink, free, compact and copy on page tables
   linear4       packing and products of 4-bit weights with group scales
+  chunk         rotation by positions, attention of several new rows of a sequence,
+                probabilities of logits, verification of drafted tokens
 
 Every function here is pinned by a CPU test (tests/test_oracle_*.py) to a
 closed form, an invariant, a library routine on a special case or brute

@@ -1,4 +1,4 @@
-"""Pages of a paged cache: extend, fork, free and compact on plain lists (oracle side).
+"""Pages of a paged cache: extend, fork, shrink, free and compact on plain lists (oracle side).
 
 TEST INFRASTRUCTURE ONLY; shares no code with the HIP library.
 """
@@ -70,6 +70,24 @@ class Model:
                 if p >= 0:
                     self.refs[p] -= 1
             self.table[s], self.lens[s] = [-1] * self.width, 0
+
+    def shrink(self, seqs, n_drop, row_counts=()):
+        """row_counts: the rows of a group of each row array."""
+        for s, n in zip(seqs, n_drop):
+            if not 0 <= s < len(self.lens) or n <= 0:
+                continue
+            left = self.lens[s] - n
+            if left < 0 or (left % self.T and self.refs[self.table[s][left // self.T]] != 1):
+                return self._blame(-3)
+            if any(left % r and left // r != self.lens[s] // r for r in row_counts):
+                return self._blame(-3)
+        for s, n in zip(seqs, n_drop):
+            if not 0 <= s < len(self.lens) or n <= 0:
+                continue
+            for p in range(-(-(self.lens[s] - n) // self.T), -(-self.lens[s] // self.T)):
+                self.refs[self.table[s][p]] -= 1
+                self.table[s][p] = -1
+            self.lens[s] -= n
 
     def compact(self):
         """-> [(page, where it went)]"""

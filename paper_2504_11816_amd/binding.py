@@ -51,7 +51,15 @@ class Okv8Step(ctypes.Structure):
 
 
 # every symbol include/okv_pages.h declares (same library)
-PAGES_EXPORTS = ["okv_pages_workspace_bytes", "okv_pages_extend", "okv_pages_fork", "okv_pages_free", "okv_pages_compact", "okv_pages_copy"]
+PAGES_EXPORTS = ["okv_pages_workspace_bytes", "okv_pages_extend", "okv_pages_fork", "okv_pages_free", "okv_pages_compact", "okv_pages_copy", "okv_pages_shrink"]
+
+
+# every symbol include/okv_chunk.h declares (same library)
+CHUNK_EXPORTS = ["okv_rope_append", "okv_chunk_attn", "okv_chunk_workspace_bytes"]
+
+
+# every symbol include/okv_sample.h declares (same library)
+SAMPLE_EXPORTS = ["okv_token_probs", "okv_token_probs_workspace_bytes", "okv_verify", "okv_verify_workspace_bytes"]
 
 
 # every symbol include/okv_linear4.h declares (same library)
@@ -74,6 +82,28 @@ class OkvPages(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "page_tokens", "max_seqs", "max_pages_per_seq", "n_pages", "n_arrays", "n_rows")] + [
         ("arrays", OkvPageArray * 4), ("rows", OkvRowArray * 2)] + [(n, ctypes.c_void_p) for n in ("table", "lens", "refs", "status", "workspace")] + [
         ("workspace_bytes", ctypes.c_int64)]
+
+
+class OkvLayerPool(ctypes.Structure):
+    """okv_layer_pool of include/okv_chunk.h."""
+    _fields_ = [(x, ctypes.c_int32) for x in ("n_q_heads", "n_kv_heads", "head_dim", "block_tokens", "max_blocks_per_seq", "max_ctx", "max_seqs")]
+    _fields_ += [("n_blocks", ctypes.c_int64), ("pool", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("refused", ctypes.c_void_p)]
+
+
+class OkvRows(ctypes.Structure):
+    """okv_rows of include/okv_chunk.h."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("seqs", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
+
+
+class OkvRope(ctypes.Structure):
+    """okv_rope of include/okv_chunk.h."""
+    _fields_ = [("turns", ctypes.c_void_p), ("rotated", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("positions", ctypes.c_void_p)]
+
+
+class OkvChunk(ctypes.Structure):
+    """okv_chunk of include/okv_chunk.h."""
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p), ("prefix", ctypes.c_void_p),
+                ("out_dtype", ctypes.c_int32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
 
 
 class OkvDecoderLayer(ctypes.Structure):
@@ -199,6 +229,14 @@ def lib():
             "okv_pages_free": (ctypes.c_int, [ctypes.POINTER(OkvPages), I32, P, P]),
             "okv_pages_compact": (ctypes.c_int, [ctypes.POINTER(OkvPages), P]),
             "okv_pages_copy": (ctypes.c_int, [ctypes.POINTER(OkvPages), I32, P, P, ctypes.POINTER(OkvPageArray), I32, P]),
+            "okv_pages_shrink": (ctypes.c_int, [ctypes.POINTER(OkvPages), I32, P, P, P]),
+            "okv_rope_append": (ctypes.c_int, [ctypes.POINTER(OkvLayerPool), ctypes.POINTER(OkvRows), ctypes.POINTER(OkvRope), P, P, I64, P, I64, P, I64, P]),
+            "okv_chunk_workspace_bytes": (I64, [ctypes.POINTER(OkvLayerPool)]),
+            "okv_chunk_attn": (ctypes.c_int, [ctypes.POINTER(OkvLayerPool), ctypes.POINTER(OkvRows), ctypes.POINTER(OkvChunk), P, I64, P, P]),
+            "okv_token_probs_workspace_bytes": (I64, [I32, I32]),
+            "okv_token_probs": (ctypes.c_int, [P, I32, I64, P, P, I64, I32, I32, P, I64, P]),
+            "okv_verify_workspace_bytes": (I64, [I32, I32]),
+            "okv_verify": (ctypes.c_int, [P, I64, P, I64, P, P, P, P, P, P, I32, I32, I32, P, I64, P]),
             "okv8_codes_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),
             "okv8_scales_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),
             "okv8_tails_bytes": (I64, [ctypes.POINTER(Okv8Cache)]),

@@ -36,6 +36,10 @@ struct State {
   int32_t max_seqs, width, log2_T, n_pages;
 };
 
+struct RowCounts {
+  int32_t rows[OKV_PAGES_MAX_ROWS];      // of the row arrays; 0: there is none
+};
+
 __device__ __forceinline__ bool is_row(const State &s, int r) { return r >= 0 && r < s.max_seqs; }
 __device__ __forceinline__ int length_of(const State &s, int r) { return min(max(s.lens[r], 0), s.width << s.log2_T); }
 __device__ __forceinline__ int pages_of(const State &s, int n) { return (n + (1 << s.log2_T) - 1) >> s.log2_T; }
@@ -306,6 +310,42 @@ __global__ void __launch_bounds__(kMoveThreads) free_kernel(State s, const int32
   if (threadIdx.x == 0) s.lens[row] = 0;
 }
 
+// Whether the call fits the state, a thread per sequence; then the pages, a wavefront per sequence
+__global__ void __launch_bounds__(kThreads) shrink_kernel(State s, const int32_t *seqs, const int32_t *n_drop, int n, RowCounts tails) {
+  __shared__ int bad;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  for (int j = threadIdx.x; j < n; j += kThreads) {
+    const int row = seqs ? seqs[j] : j, drop = max(n_drop[j], 0);
+    if (!is_row(s, row) || drop == 0) continue;
+    const int len = length_of(s, row), left = len - drop;
+    bool fits = left >= 0;
+    if (fits && left & ((1 << s.log2_T) - 1)) {          // a page that is no longer full belongs to this sequence alone
+      const int page = s.table[(int64_t)row * s.width + (left >> s.log2_T)];
+      fits = page >= 0 && page < s.n_pages && s.refs[page] == 1;
+    }
+#pragma unroll
+    for (int i = 0; i < OKV_PAGES_MAX_ROWS; ++i)         // rows that the array holds for later tokens now
+      if (fits && tails.rows[i] > 0) fits = left % tails.rows[i] == 0 || left / tails.rows[i] == len / tails.rows[i];
+    if (!fits) bad = 1;
+  }
+  __syncthreads();
+  if (bad) {
+    if (threadIdx.x == 0) blame(s, OKV_ESTATE);
+    return;
+  }
+  for (int j = threadIdx.x >> 6; j < n; j += kThreads / 64) {
+    const int row = seqs ? seqs[j] : j, drop = max(n_drop[j], 0);
+    if (!is_row(s, row) || drop == 0) continue;
+    const int len = length_of(s, row), left = len - drop;
+    for (int p = pages_of(s, left) + (threadIdx.x & 63); p < pages_of(s, len); p += 64) {
+      const int page = atomicExch(s.table + (int64_t)row * s.width + p, -1);
+      if (page >= 0 && page < s.n_pages) atomicSub(s.refs + page, 1);
+    }
+    if ((threadIdx.x & 63) == 0) s.lens[row] = max(left, 0);
+  }
+}
+
 __global__ void __launch_bounds__(kThreads) compact_plan_kernel(State s, Lists l) {
   __shared__ int sums[kThreads / 64];
   const int each = (s.n_pages + kThreads - 1) / kThreads, p0 = min((int)threadIdx.x * each, s.n_pages), p1 = min(p0 + each, s.n_pages);
@@ -475,6 +515,17 @@ int okv_pages_free(const okv_pages *p, int32_t n, const int32_t *seqs, void *str
   if (!seqs) return report(OKV_EINVAL, "okv_pages_free: NULL pointer");
   hipLaunchKernelGGL(free_kernel, dim3((unsigned)n), dim3(kMoveThreads), 0, static_cast<hipStream_t>(stream), state_of(p), seqs);
   return hip_result("okv_pages_free");
+}
+
+int okv_pages_shrink(const okv_pages *p, int32_t n, const int32_t *seqs, const int32_t *n_drop, void *stream) {
+  if (const int rc = check("okv_pages_shrink", p, n, OKV_PAGES_MAX_SEQS)) return rc;
+  if (n == 0) return OKV_OK;
+  if (!n_drop) return report(OKV_EINVAL, "okv_pages_shrink: NULL pointer");
+  if (!seqs && n > p->max_seqs) return report(OKV_EINVAL, "okv_pages_shrink: more sequences than the table has rows");
+  RowCounts tails = {};
+  for (int i = 0; i < p->n_rows; ++i) tails.rows[i] = p->rows[i].rows;
+  hipLaunchKernelGGL(shrink_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), state_of(p), seqs, n_drop, n, tails);
+  return hip_result("okv_pages_shrink");
 }
 
 int okv_pages_compact(const okv_pages *p, void *stream) {

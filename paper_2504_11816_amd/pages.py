@@ -1,7 +1,7 @@
 """Pages of a paged KV cache (include/okv_pages.h) over torch-owned memory.
 
     pages = Pages(table=table, lens=lens, refs=refs, page_tokens=T, arrays=[PageArray(pool, unit_tokens=16)])
-    pages.extend(seqs, n_new); pages.fork(src, dst); pages.free(seqs); pages.compact(); pages.copy(src_ids, dst_ids, to=[PageArray(staging)])
+    pages.extend(seqs, n_new); pages.fork(src, dst); pages.shrink(seqs, n_drop); pages.free(seqs); pages.compact(); pages.copy(src_ids, dst_ids, to=[PageArray(staging)])
 
 The state is on the GPU and every call runs on the current stream without waiting; check() reads the status and raises.
 """
@@ -95,6 +95,12 @@ class Pages:
     def free(self, seqs):
         """The sequences become empty; pages that belong to no other are free."""
         self._done(self._lib.okv_pages_free(self.ref, seqs.shape[0], self._ids("seqs", seqs), binding.current_stream(self.device)))
+
+    def shrink(self, seqs, n_drop):
+        """Sequence seqs[i] loses its last n_drop[i] tokens; pages that it needs no longer are free, if they belong to no other.  Changes nothing where
+        that does not fit the state (see the header)."""
+        at, n = self._ids("seqs", seqs), seqs.shape[0]
+        self._done(self._lib.okv_pages_shrink(self.ref, n, at, self._ids("n_drop", n_drop, n), binding.current_stream(self.device)))
 
     def compact(self):
         """Pages in use become 0 .. n_used - 1 (status[1] says how many, status[2] how many were moved)."""
