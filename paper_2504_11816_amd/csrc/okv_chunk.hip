@@ -7,7 +7,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "okv.h"
 
@@ -21,6 +23,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 
 // ---- the pool -------------------------------------------------------------------------------------
 
@@ -156,6 +159,7 @@ struct Attend {
   int32_t window;                        // 0: none
   const float *slopes;
   const int32_t *prefix;
+  float *parts;                          // results of pieces of rows' keys: kRows x D sums, and behind them kRows maxima and kRows sums of weights
 };
 
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -163,191 +167,391 @@ constexpr float kRaise = 8.f;            // the maximum is raised when a score i
 // Weights are 2^(s - m + kLift): at most 2^15, and normal numbers in fp16 down to 2^-21 of the largest
 constexpr float kLift = 7.f;
 constexpr int kKeys = 64;                // of a block
-constexpr int kWaves = 4, kTileRows = 32 * kWaves;
+constexpr int kTarget = 512;             // pieces that a call's keys are cut into, where it has fewer tiles of rows
+constexpr int kMinSpan = 4;              // blocks of a piece at least
 
-// Where 16-byte piece p of row r sits in a block in LDS, in pieces: sixteen rows' same piece, and the four pieces of 32 elements of four rows, are in different banks
-template <int D>
-__device__ __forceinline__ int piece_at(const int r, const int p) {
-  if constexpr (D == 128) return 16 * r + (p ^ (4 * (r & 3) | ((r >> 2) & 3)));
-  else return 8 * r + (p ^ (4 * ((r >> 1) & 1) | ((r >> 2) & 3)));
-}
+// A workgroup of W wavefronts has 32 W of the n R rows (tokens, and for each its R query heads) of a sequence and KV head, a wavefront 32 of them.
+template <int D, int W>
+struct Form {
+  static constexpr int kThreads = 64 * W, kRows = 32 * W;
+  static constexpr int kRing = W == 8 ? 3 : 2;                // blocks of keys, and of values, in LDS
+  static constexpr int kBlockBytes = kKeys * D * 2, kLoads = kBlockBytes / 1024 / W;      // loads of a wavefront per block of keys (or values)
+  static constexpr int kPartFloats = kRows * (D + 2);
+};
 
-__device__ __forceinline__ half8 transposed(const char *lds, const int first, const int second) {
+__device__ __forceinline__ half8 transposed(const char *first, const char *second) {
   typedef __attribute__((address_space(3))) short4v *at;
-  const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(lds + first)), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(lds + second));
+  const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)first), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)second);
   const half4 x = __builtin_bit_cast(half4, a), y = __builtin_bit_cast(half4, b);
   return half8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
 }
 
-// Rows of a workgroup: kTileRows of the n R rows (tokens, and for each its R query heads) of a sequence and KV head.
-struct Item {
-  int first, n, len, s, tile, g;         // the sequence's first row, its rows, its tokens, its row of the table; s < 0: nothing to do
-};
-__device__ __forceinline__ Item item_of(const Pool &c, const Rows &r, int piece) {
-  const int lane = threadIdx.x & 63;
-  Item it;
-  it.s = -1;
-  for (int b0 = 0; b0 < r.batch; b0 += 64) {
-    const int b = b0 + lane;
-    int first = 0, last = 0;
-    if (b < r.batch) rows_of(r, b, first, last);
-    const int tiles = (int)(((int64_t)(last - first) * c.R + kTileRows - 1) / kTileRows);
-    int upto = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int other = __shfl_up(upto, o);
-      if (lane >= o) upto += other;
-    }
-    const int all = __shfl(upto, 63) * c.G;
-    if (piece >= all) {
-      piece -= all;
-      continue;
-    }
-    const int rank = piece / c.G, at = __popcll(__ballot(upto <= rank));
-    it.g = piece % c.G;
-    it.tile = __shfl(tiles, at) - 1 - (rank - __shfl(upto - tiles, at));      // the last rows, which see the most keys, first
-    it.first = __shfl(first, at), it.n = __shfl(last, at) - it.first;
-    const int s = r.seqs ? r.seqs[b0 + at] : b0 + at;
-    it.s = s >= 0 && s < c.max_seqs ? s : -2;
-    it.len = it.s < 0 ? 0 : min(max(r.lens[s], 0), c.capacity);
-    break;
-  }
-  return it;
+// One 16-byte-per-lane load from `base` + off straight into LDS: lane l's bytes land at lds + 16 l.  Written as assembly because the compiler, which cannot tell the block being
+// written from the one being read, waits for all such loads in front of every LDS read otherwise.  m0 is left as it was found.
+__device__ __forceinline__ const char *uniform(const char *p) {      // all lanes have the same: in scalar registers
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const char *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+__device__ __forceinline__ void load_to_lds(const char *base, const uint32_t off, const uint32_t lds) {
+  base = uniform(base);
+  uint32_t found;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0" : "=&s"(found) : "s"(lds), "v"(off), "s"(base) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_for_loads() {      // until N are outstanding
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void barrier_leaving_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
-template <int D, bool WIDE, bool SHAPED>
-__global__ void __launch_bounds__(kWaves * 64) chunk_kernel(Pool c, Rows r, Attend a) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kKeys * D * 2];
-  char *const lds_k = lds, *const lds_v = lds + kKeys * D * 2;
-  const Item it = item_of(c, r, blockIdx.x);
-  if (it.s == -1) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
-  const int row = it.tile * kTileRows + wave * 32 + col;                    // of the sequence's n R rows
-  const int token = row / c.R, head = it.g * c.R + row % c.R;
-  const bool mine = token < it.n;
-  const int base = it.len - it.n, pos = base + token;
-  const int prefix = a.prefix && it.s >= 0 ? min(max(a.prefix[it.s], 0), it.len) : 0;
+// The blocks of keys that some row of a tile sees, in order: `ahead` blocks of the prefix, and those from `first` on
+struct Keys {
+  int ahead, first, total;
+};
+template <int ROWS>
+__device__ __forceinline__ Keys keys_of(const int n, const int len, const int prefix, const int window, const int R, const int tile) {
+  const int pos0 = len - n + tile * ROWS / R, pos1 = len - n + min((tile * ROWS + ROWS - 1) / R, n - 1);
+  Keys k;
+  k.first = window == 0 || pos0 < window ? 0 : (pos0 - window + 1) / kKeys;
+  k.ahead = min((prefix + kKeys - 1) / kKeys, k.first);
+  k.total = k.ahead + max((max(pos1 + 1, prefix) + kKeys - 1) / kKeys - k.first, 0);
+  return k;
+}
+
+// What a workgroup does.  The rows of every sequence and KV head are cut into tiles, and where these are too few to fill the chip the keys of each tile of a sequence
+// into as many cuts: all of them by the same rule, from lengths that are on the device, by every workgroup for itself.
+struct Piece {
+  int first, n, len, s, prefix;          // the sequence: its first row, its rows, its tokens, its row of the table (below 0: there is none)
+  int tile, g, cut, cuts, slot;          // slot: of the piece's results among those that are cut
+  bool there;
+};
+struct Sequence {
+  int first, n, s, len, prefix, tiles, blocks;
+};
+template <int ROWS>
+__device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, const int32_t *prefix, const int window, const int b) {
+  Sequence q{0, 0, -1, 0, 0, 0, 0};
+  if (b >= r.batch) return q;
+  int last;
+  rows_of(r, b, q.first, last);
+  q.n = last - q.first;
+  const int s = r.seqs ? r.seqs[b] : b;
+  if (s >= 0 && s < c.max_seqs) {
+    q.s = s;
+    q.len = min(max(r.lens[s], 0), c.capacity);
+    if (prefix) q.prefix = min(max(prefix[s], 0), q.len);
+  }
+  q.tiles = (int)(((int64_t)q.n * c.R + ROWS - 1) / ROWS);
+  if (q.tiles) q.blocks = keys_of<ROWS>(q.n, q.len, q.prefix, window, c.R, q.tiles - 1).total;
+  return q;
+}
+__device__ __forceinline__ int wave_scan(int x) {         // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int other = __shfl_up(x, o);
+    if (lane >= o) x += other;
+  }
+  return x;
+}
+__device__ __forceinline__ double wave_total(double x) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+// take(sequences of 64 lanes, cuts, pieces and cut pieces up to and with each, those before all of them) until it returns true
+template <int ROWS, class Take>
+__device__ __forceinline__ void with_plan(const Pool &c, const Rows &r, const int32_t *prefix, const int window, const Take &take) {
+  const int lane = threadIdx.x & 63;
+  Sequence q = sequence_at<ROWS>(c, r, prefix, window, lane);
+  double work = (double)q.tiles * q.blocks;
+  for (int b0 = 64; b0 < r.batch; b0 += 64) {
+    const Sequence more = sequence_at<ROWS>(c, r, prefix, window, b0 + lane);
+    work += (double)more.tiles * more.blocks;
+  }
+  const double share = ceil(wave_total(work) * c.G / kTarget);
+  const int span = max(kMinSpan, (int)fmin(share, 1e9));
+  int pieces = 0, cut_pieces = 0;
+  for (int b0 = 0; b0 < r.batch; b0 += 64) {
+    if (b0) q = sequence_at<ROWS>(c, r, prefix, window, b0 + lane);
+    const int cuts = max((q.blocks + span - 1) / span, 1), mine = q.tiles * c.G * cuts;
+    const int upto = wave_scan(mine), cut_upto = wave_scan(cuts > 1 ? mine : 0);
+    if (take(q, cuts, upto, cut_upto, pieces, cut_pieces)) return;
+    pieces += __shfl(upto, 63), cut_pieces += __shfl(cut_upto, 63);
+  }
+}
+template <int ROWS>
+__device__ __forceinline__ Piece piece_of(const Pool &c, const Rows &r, const int32_t *prefix, const int window, const int index) {
+  Piece p;
+  p.there = false;
+  with_plan<ROWS>(c, r, prefix, window, [&](const Sequence &q, const int cuts, const int upto, const int cut_upto, const int before, const int cut_before) {
+    const uint64_t ended = __ballot(before + upto <= index);
+    if (ended == ~0ull) return false;
+    const int at = __popcll(ended);
+    auto of = [&](const int x) { return __builtin_amdgcn_readlane(x, at); };
+    p.there = true;
+    p.first = of(q.first), p.n = of(q.n), p.s = of(q.s), p.len = of(q.len), p.prefix = of(q.prefix), p.cuts = of(cuts);
+    const int tiles = of(q.tiles), within = index - before - (of(upto) - tiles * c.G * p.cuts);
+    // The heads of a tile next to each other, so that those of a head are on the same XCD where they are a multiple of eight; then the tiles, which read the same
+    // keys; those that see the most keys first
+    p.g = within % c.G;
+    p.tile = tiles - 1 - within / c.G % tiles;
+    p.cut = within / c.G / tiles;
+    p.slot = cut_before + of(cut_upto) - tiles * c.G * p.cuts + within;
+    return true;
+  });
+  return p;
+}
+
+template <int D, int W, bool WIDE, bool SHAPED>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
+  using F = Form<D, W>;
+  constexpr int kRing = F::kRing, kLoads = F::kLoads, kRowBytes = 2 * D;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kRing * F::kBlockBytes];
+  __shared__ int odd_first, odd_last;                    // blocks with values that are not finite, of those that not every row sees
+  const Piece p = piece_of<F::kRows>(c, r, a.prefix, a.window, blockIdx.x);
+  if (!p.there) return;
+  if (threadIdx.x == 0) odd_first = INT_MAX, odd_last = -1;      // (a barrier comes before their use)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  const int row0 = p.tile * F::kRows + wave * 32, row = row0 + col;         // of the sequence's n R rows
+  const int token = row / c.R, head = p.g * c.R + row % c.R;
+  const int base = p.len - p.n, pos = base + token;
   const int from = a.window == 0 || pos < a.window ? 0 : pos - a.window + 1;
-  // keys that some row of the tile sees
-  const int token0 = it.tile * kTileRows / c.R, token1 = min((it.tile * kTileRows + kTileRows - 1) / c.R, it.n - 1);
-  const int pos0 = base + token0, pos1 = base + token1;
-  const int from0 = a.window == 0 || pos0 < a.window ? 0 : pos0 - a.window + 1;
-  const int end = max(pos1 + 1, prefix);
+  // of this wavefront's rows
+  const bool idle = row0 / c.R >= p.n;
+  const int pos0 = base + row0 / c.R, pos1 = base + min((row0 + 31) / c.R, p.n - 1);
+  const int from0 = a.window == 0 || pos0 < a.window ? 0 : pos0 - a.window + 1, from1 = a.window == 0 || pos1 < a.window ? 0 : pos1 - a.window + 1;
+
+  // this piece's blocks of the tile's
+  const Keys keys = keys_of<F::kRows>(p.n, p.len, p.prefix, a.window, c.R, p.tile);
+  const int i0 = (int)((int64_t)keys.total * p.cut / p.cuts), total = (int)((int64_t)keys.total * (p.cut + 1) / p.cuts) - i0;
+  auto block_at = [&](const int i) {                   // past the end: the last again
+    const int j = i0 + min(i, total - 1);
+    return j < keys.ahead ? j : keys.first + j - keys.ahead;
+  };
 
   half8 qf[D / 16];
   {
-    const _Float16 *q = a.q + (it.first + min(token, it.n - 1)) * a.q_stride + head * D + 8 * half;
+    const _Float16 *q = a.q + (p.first + min(token, p.n - 1)) * a.q_stride + head * D + 8 * half;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) qf[k] = *reinterpret_cast<const half8 *>(q + 16 * k);
   }
   const float slope = SHAPED && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+
+  // Loads.  Row r of a block has its 16-byte pieces in units (D / 8) r .. of LDS, piece k in unit (D / 8) r + (k ^ turn(r)): sixteen rows' same piece, and the four pieces
+  // of 32 elements of four rows, are in different banks.  A load brings 1 KiB, 512 / D rows of a tile of 16; load j of a block is wavefront j % W's.
+  constexpr int kTileLoads = 16 * kRowBytes / 1024, kLoadRows = 1024 / kRowBytes, kUnits = D / 8;
+  static_assert(W % kTileLoads == 0, "a wavefront's loads are of the same rows of their tiles");
+  uint32_t lane_offset;
+  {
+    const int rr = wave % kTileLoads * kLoadRows + lane / kUnits, turn = D == 128 ? 4 * (rr & 3) | ((rr >> 2) & 3) : 4 * ((rr >> 1) & 1) | ((rr >> 2) & 3);
+    lane_offset = (uint32_t)(rr * kRowBytes + ((lane % kUnits) ^ turn) * 16);
+  }
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds) + wave * 1024;
+  const int32_t *table_row = c.table + (int64_t)max(p.s, 0) * c.width;
+  const char *pool = reinterpret_cast<const char *>(c.kv + head_offset<D>(c, p.g));
+  const int64_t slab = (int64_t)2 * c.G * D << (4 + c.st_log2);
+  const int last_tile = (p.len - 1) >> 4;
+  int held_from = INT_MIN / 2, held = p.s;              // lane l: the block in entry held_from + l of the sequence's row of the table
+  const char *value_base[kLoads];
+  auto load_keys = [&](const int i, const int slot, const char *(&bases)[kLoads]) {
+    const int t0 = __builtin_amdgcn_readfirstlane(block_at(i)) * (kKeys / 16) + wave / kTileLoads;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int t = min(t0 + j * (W / kTileLoads), last_tile), e = t >> c.log2_tiles, tb = t & ((1 << c.log2_tiles) - 1);
+      if (c.table && (unsigned)(e - held_from) >= 64u) {
+        held_from = e;
+        held = min(max(table_row[min(e + lane, c.width - 1)], 0), c.n_blocks - 1);
+      }
+      const int block = __builtin_amdgcn_readlane(held, c.table ? e - held_from : 0);
+      bases[j] = uniform(pool + 2 * (block * c.block_elems + (tb >> c.st_log2) * slab + (int64_t)(tb & ((1 << c.st_log2) - 1)) * (c.gg * 16 * D)));
+      load_to_lds(bases[j], lane_offset, __builtin_amdgcn_readfirstlane(lds0 + slot * F::kBlockBytes + j * W * 1024));
+    }
+  };
+  const uint32_t behind = 2 * v_offset<D>(c);
+  auto load_values = [&](const int slot) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(value_base[j] + behind, lane_offset, __builtin_amdgcn_readfirstlane(lds0 + (kRing + slot) * F::kBlockBytes + j * W * 1024));
+  };
+
+  // where this lane's operands begin in a block; xor 32 k (keys' k-th 16 elements) or 64 e (values' e-th 32 elements)
+  const int x4 = (lane >> 2) & 3;
+  uint32_t key_at, value_at0, value_at1;
+  if constexpr (D == 128) {
+    key_at = col * kRowBytes + 16 * (half ^ (4 * (col & 3) | ((col >> 2) & 3)));
+    value_at0 = (4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * x4 | half)) + 8 * (lane & 1);
+    value_at1 = (8 + 4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * x4 | (half + 2))) + 8 * (lane & 1);
+  } else {
+    key_at = col * kRowBytes + 16 * (half ^ (4 * ((col >> 1) & 1) | ((col >> 2) & 3)));
+    value_at0 = (4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * (x4 >> 1) | half)) + 8 * (lane & 1);
+    value_at1 = (8 + 4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * (x4 >> 1) | (half + 2))) + 8 * (lane & 1);
+  }
+
   floatx16 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = floatx16{};
   float m = -1e30f, l = 0.f;
 
-  const int32_t *table_row = c.table + (int64_t)max(it.s, 0) * c.width;
-  const int64_t my_head = head_offset<D>(c, it.g);
-  const int behind = v_offset<D>(c);
-  const int prefix_blocks = (prefix + kKeys - 1) / kKeys, first_block = from0 / kKeys, last_block = (end + kKeys - 1) / kKeys;
-  for (int block = 0; block < last_block; ++block) {
-    if (block < first_block && block >= prefix_blocks) {
-      block = first_block - 1;
-      continue;
-    }
-    const int key0 = block * kKeys;
-    __syncthreads();
-    constexpr int kPieces = D / 8;
-#pragma unroll
-    for (int i = 0; i < kKeys * kPieces / (kWaves * 64); ++i) {
-      const int u = i * kWaves * 64 + threadIdx.x, key = u / kPieces, piece = u % kPieces;
-      const int t = min((key0 + key) >> 4, (it.len - 1) >> 4);
-      const _Float16 *k = c.kv + tile_at<D>(c, table_row, it.s, t) + my_head + (key & 15) * D + 8 * piece;
-      *reinterpret_cast<u32x4 *>(lds_k + 16 * piece_at<D>(key, piece)) = *reinterpret_cast<const u32x4 *>(k);
-      *reinterpret_cast<u32x4 *>(lds_v + 16 * piece_at<D>(key, piece)) = *reinterpret_cast<const u32x4 *>(k + behind);
-    }
-    __syncthreads();
-    // scores: keys 32 b + 8 (i / 4) + 4 half + i % 4 of this lane's row
-    floatx16 x[2];
+  // scores: keys 32 b + 8 (i / 4) + 4 half + i % 4 of this lane's row
+  auto score = [&](floatx16 (&x)[2], const int slot) {
+    const char *k0 = lds + slot * F::kBlockBytes;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       x[b] = floatx16{};
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const half8 kf = *reinterpret_cast<const half8 *>(lds_k + 16 * piece_at<D>(32 * b + col, 2 * k + half));
-        x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[k], x[b], 0, 0, 0);
+      for (int k = 0; k < D / 16; ++k)
+        x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8 *>(k0 + (key_at ^ (32 * k)) + b * 32 * kRowBytes), qf[k], x[b], 0, 0, 0);
+    }
+  };
+  const int tile_token0 = p.tile * F::kRows / c.R, tile_pos0 = base + tile_token0, tile_pos1 = base + min((p.tile * F::kRows + F::kRows - 1) / c.R, p.n - 1);
+  const int tile_from1 = a.window == 0 || tile_pos1 < a.window ? 0 : tile_pos1 - a.window + 1;
+  auto all_see = [&](const int key0) { return (key0 + kKeys - 1 <= tile_pos0 && key0 >= tile_from1) || key0 + kKeys <= p.prefix; };      // rows of the tile
+  auto in_sight = [&](const int key0) { return !idle && ((key0 <= pos1 && key0 + kKeys > from0) || key0 < p.prefix); };
+
+  int slot = 0;
+  auto step = [&](const int i, floatx16 (&x)[2], floatx16 (&next)[2]) {
+    const int after = slot + 1 == kRing ? 0 : slot + 1, before = slot == 0 ? kRing - 1 : slot - 1;
+    wait_for_loads<(kRing - 2) * 2 * kLoads>();
+    barrier_leaving_loads();                             // the next block of keys and this one of values are there, those before free
+    load_values(before);
+    load_keys(i + kRing, slot, value_base);
+    __builtin_amdgcn_sched_barrier(0);
+    const int key0 = block_at(i) * kKeys;
+    if (!all_see(key0)) {
+      // A number that is not finite may be of a key that some row does not see, and 0 times it is not 0: it is taken out here, and added at the end where it is seen
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        u32x4 *at = reinterpret_cast<u32x4 *>(lds + (kRing + slot) * F::kBlockBytes + (j * W + wave) * 1024 + 16 * lane), w = *at;
+        uint32_t any = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t bad = ((w[k] & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+          w[k] &= ~(bad - (bad >> 15));
+          any |= bad;
+        }
+        if (any) {
+          *at = w;
+          odd = true;
+        }
+      }
+      if (odd) atomicMin(&odd_first, i), atomicMax(&odd_last, i);
+      __syncthreads();
+    }
+    const bool seen = in_sight(key0), whole = (key0 + kKeys - 1 <= pos0 && key0 >= from1) || key0 + kKeys <= p.prefix;
+    float by = a.scale;
+    if (seen) {
+      float top = -INFINITY;
+      if (SHAPED || !whole) {
+        // (shaped, masked: in units of log 2 from here on)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int key = key0 + 32 * b + 8 * (j / 4) + 4 * half + j % 4;
+            float s = x[b][j] * a.scale;
+            if constexpr (SHAPED) {
+              if (a.cap != 0.f) s = a.cap * tanhf(s);
+              s = fmaf(-slope, (float)abs(pos - key), s);
+            }
+            if (!whole && !((key <= pos && key >= from) || key < p.prefix)) s = -INFINITY;
+            x[b][j] = s;
+          }
+        by = 1.f;
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) top = fmaxf(fmaxf(top, x[b][j]), x[b][j + 1]);
+      top = max_with_lane_xor<32>(top) * by;
+      if (__ballot(top > m + kRaise)) {
+        const float to = top > m + kRaise ? top : m, scale = __builtin_amdgcn_exp2f(m - to);
+        l *= scale;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] *= scale;
+        m = to;
       }
     }
-    const bool whole = (key0 + kKeys - 1 <= pos0 && key0 >= (a.window == 0 || pos1 < a.window ? 0 : pos1 - a.window + 1)) || key0 + kKeys <= prefix;
-    float top = -INFINITY;
+    if (i + 1 < total && in_sight(block_at(i + 1) * kKeys)) score(next, after);
+    if (seen) {
+      half8 hi[4], lo[WIDE ? 4 : 1];
+      const float less = kLift - m;
+      float sums[4] = {};
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = key0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4;
-        float s = x[b][i] * a.scale;
-        if constexpr (SHAPED) {
-          if (a.cap != 0.f) s = a.cap * tanhf(s);
-          s = fmaf(-slope, (float)abs(pos - key), s);
+        for (int j = 0; j < 16; ++j) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(x[b][j], by, less));
+          sums[j % 4] += w;
+          hi[2 * b + j / 8][j % 8] = (_Float16)w;
+          if constexpr (WIDE) lo[2 * b + j / 8][j % 8] = (_Float16)(w - (float)(_Float16)w);
         }
-        if (!whole && !((key <= pos && key >= from) || key < prefix)) s = -INFINITY;
-        x[b][i] = s;
-        top = fmaxf(top, s);
-      }
-    top = max_with_lane_xor<32>(top);
-    if (__ballot(top > m + kRaise)) {
-      const float to = top > m + kRaise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
-      l *= by;
+      l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+      // results: elements 32 e + 8 (i / 4) + 4 half + i % 4 of this lane's row
+      const char *v0 = lds + (kRing + slot) * F::kBlockBytes;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) o[i] *= by;
-      m = to;
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          const half8 vf = transposed(v0 + (value_at0 ^ (64 * e)) + t * 16 * kRowBytes, v0 + (value_at1 ^ (64 * e)) + t * 16 * kRowBytes);
+          o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, hi[t], o[e], 0, 0, 0);
+          if constexpr (WIDE) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo[t], o[e], 0, 0, 0);
+        }
     }
-    half8 hi[4], lo[4];
+    slot = after;
+  };
+
+  if (total > 0) {
+    load_keys(0, 0, value_base);
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int g = 1; g < kRing; ++g) {
+      load_values(g - 1);
+      load_keys(g, g, value_base);
+    }
+    wait_for_loads<(kRing - 1) * 2 * kLoads>();
+    barrier_leaving_loads();
+    floatx16 x[2], y[2];
+    if (in_sight(block_at(0) * kKeys)) score(x, 0);
+    for (int i = 0;; i += 2) {
+      step(i, x, y);
+      if (i + 1 >= total) break;
+      step(i + 1, y, x);
+      if (i + 2 >= total) break;
+    }
+    wait_for_loads<0>();                                 // nothing may still be on its way into LDS
+    __syncthreads();
+#pragma unroll 1
+    for (int i = odd_first; i <= odd_last; ++i) {
+      const int key0 = block_at(i) * kKeys;
+      if (all_see(key0)) continue;
+#pragma unroll 1
+      for (int key = key0; key < min(key0 + kKeys, p.len); ++key) {
+        const bool mine = (key <= pos && key >= from) || key < p.prefix;
+        const _Float16 *v = c.kv + tile_at<D>(c, table_row, p.s, key >> 4) + head_offset<D>(c, p.g) + v_offset<D>(c) + (key & 15) * D + 4 * half;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(x[b][i] - m + kLift);
-        l += p;
-        hi[2 * b + i / 8][i % 8] = (_Float16)p;
-        if constexpr (WIDE) lo[2 * b + i / 8][i % 8] = (_Float16)(p - (float)(_Float16)p);
-      }
-    // results: elements 32 e + 8 (i / 4) + 4 half + i % 4 of this lane's row
+        for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e)
+          for (int j = 0; j < 4; ++j) {
+            const half4 x = *reinterpret_cast<const half4 *>(v + 32 * e + 8 * j);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int key = 16 * t + 4 * half + (lane & 15) / 4, piece = 4 * e + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-        half8 vf = transposed(lds_v, 16 * piece_at<D>(key, piece) + 8 * (lane & 1), 16 * piece_at<D>(key + 8, piece) + 8 * (lane & 1));
-        if (!whole) {
-          // numbers that are not finite may be of keys that a row does not see, and 0 times them is not 0: they go in apart, by whether a row sees them
-          half8 above, below, rest;
-          bool odd = false;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float v = (float)vf[j];
-            const bool fine = fabsf(v) < INFINITY;
-            above[j] = fine || v < 0.f ? (_Float16)0.f : (_Float16)1.f;
-            below[j] = fine || v > 0.f ? (_Float16)0.f : (_Float16)1.f;
-            rest[j] = fine ? vf[j] : (_Float16)0.f;
-            odd |= !fine;
+            for (int q = 0; q < 4; ++q)
+              if (mine && !(fabsf((float)x[q]) < INFINITY)) o[e][4 * j + q] += (float)x[q];
           }
-          vf = rest;
-          if (__ballot(odd)) {
-            const floatx16 up = __builtin_amdgcn_mfma_f32_32x32x16_f16(above, hi[t], floatx16{}, 0, 0, 0);
-            const floatx16 down = __builtin_amdgcn_mfma_f32_32x32x16_f16(below, hi[t], floatx16{}, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[e][i] += (up[i] != 0.f ? INFINITY : 0.f) - (down[i] != 0.f ? INFINITY : 0.f);
-          }
-        }
-        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, hi[t], o[e], 0, 0, 0);
-        if constexpr (WIDE) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo[t], o[e], 0, 0, 0);
       }
+    }
   }
-  if (!mine) return;
+  if (token >= p.n) return;
   l = sum_with_lane_xor<32>(l);
-  const float over = l == 0.f ? 0.f : 1.f / l;
-  const int64_t to = ((int64_t)(it.first + token) * (c.G * c.R) + head) * D;
+  float *parts = a.parts + (int64_t)p.slot * F::kPartFloats;
+  const int of_tile = wave * 32 + col;
+  const float over = p.cuts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+  const int64_t to = p.cuts > 1 ? of_tile * D : ((int64_t)(p.first + token) * (c.G * c.R) + head) * D;
+  if (p.cuts > 1 && half == 0) parts[F::kRows * D + of_tile] = m, parts[F::kRows * (D + 1) + of_tile] = l;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -356,9 +560,64 @@ __global__ void __launch_bounds__(kWaves * 64) chunk_kernel(Pool c, Rows r, Atte
 #pragma unroll
       for (int j = 0; j < 4; ++j) y[j] = o[e][4 * i + j] * over;
       const int64_t at = to + 32 * e + 8 * i + 4 * half;
-      if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
+      if (p.cuts > 1) *reinterpret_cast<floatx4 *>(parts + at) = y;
+      else if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
       else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
     }
+}
+
+// Joins the cuts of a tile's rows: a workgroup per 32 rows of a tile that is cut, a wavefront per 8
+constexpr int kJoinRows = 32, kJoinWaves = 4;
+
+template <int D, int W, bool WIDE>
+__global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(Pool c, Rows r, Attend a) {
+  using F = Form<D, W>;
+  const int tile_index = blockIdx.x / (F::kRows / kJoinRows);
+  Piece p;
+  p.there = false;
+  int tiles_before = 0;
+  with_plan<F::kRows>(c, r, a.prefix, a.window, [&](const Sequence &q, const int cuts, const int, const int cut_upto, const int, const int cut_before) {
+    const int mine = cuts > 1 ? q.tiles * c.G : 0, upto = wave_scan(mine);
+    const uint64_t ended = __ballot(tiles_before + upto <= tile_index);
+    if (ended == ~0ull) {
+      tiles_before += __shfl(upto, 63);
+      return false;
+    }
+    const int at = __popcll(ended);
+    auto of = [&](const int x) { return __builtin_amdgcn_readlane(x, at); };
+    p.there = true;
+    p.first = of(q.first), p.n = of(q.n), p.cuts = of(cuts);
+    const int tiles = of(q.tiles), within = tile_index - tiles_before - (of(upto) - tiles * c.G);
+    p.g = within % c.G;
+    p.tile = tiles - 1 - within / c.G;
+    p.cut = tiles * c.G;                                 // slots from a cut of the tile to the next
+    p.slot = cut_before + of(cut_upto) - tiles * c.G * p.cuts + within;
+    return true;
+  });
+  if (!p.there) return;
+  constexpr int kEach = D / 64;
+  const int lane = threadIdx.x & 63, of_tile0 = blockIdx.x % (F::kRows / kJoinRows) * kJoinRows + (threadIdx.x >> 6) * (kJoinRows / kJoinWaves);
+  for (int k = 0; k < kJoinRows / kJoinWaves; ++k) {
+    const int of_tile = of_tile0 + k, row = p.tile * F::kRows + of_tile, token = row / c.R, head = p.g * c.R + row % c.R;
+    if (token >= p.n) return;
+    float m = -1e30f, l = 0.f, o[kEach] = {};
+    for (int cut = 0; cut < p.cuts; ++cut) {
+      const float *part = a.parts + (int64_t)(p.slot + cut * p.cut) * F::kPartFloats;
+      const float theirs = part[F::kRows * D + of_tile], weight = part[F::kRows * (D + 1) + of_tile], to = fmaxf(m, theirs);
+      const float mine = __builtin_amdgcn_exp2f(m - to), other = __builtin_amdgcn_exp2f(theirs - to);
+      l = l * mine + weight * other;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) o[i] = o[i] * mine + part[of_tile * D + kEach * lane + i] * other;
+      m = to;
+    }
+    const float over = l == 0.f ? 0.f : 1.f / l;
+    const int64_t at = ((int64_t)(p.first + token) * (c.G * c.R) + head) * D + kEach * lane;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if constexpr (WIDE) static_cast<float *>(a.out)[at + i] = o[i] * over;
+      else static_cast<_Float16 *>(a.out)[at + i] = (_Float16)(o[i] * over);
+    }
+  }
 }
 
 // ---- host -------------------------------------------------------------------------------------------
@@ -404,6 +663,9 @@ Pool pool_of(const okv_layer_pool *c) {
   p.block_elems = (int64_t)2 * p.G * c->head_dim * slice;
   return p;
 }
+// Whether a sequence can have more blocks of keys than a piece has at least
+bool may_cut(const Pool &p) { return (p.capacity + kKeys - 1) / kKeys > kMinSpan; }
+
 int hip_result(const char *who) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? OKV_OK : report(OKV_EHIP, "%s: %s", who, hipGetErrorString(e));
@@ -449,7 +711,10 @@ int okv_rope_append(const okv_layer_pool *c, const okv_rows *r, const okv_rope *
 
 int64_t okv_chunk_workspace_bytes(const okv_layer_pool *c) {
   if (const char *why = shape_problem(c)) return report(OKV_EINVAL, "okv_chunk_workspace_bytes: %s", why);
-  return 0;
+  if (!may_cut(pool_of(c))) return 0;
+  // A sequence that is cut is cut into less than twice its keys' shares of a span, and these are at most kTarget
+  const int64_t of_piece = c->head_dim == 128 ? Form<128, 8>::kPartFloats : Form<64, 8>::kPartFloats;
+  return 2 * kTarget * of_piece * 4;
 }
 
 int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *a, const void *q, int64_t q_stride, void *out, void *stream) {
@@ -469,20 +734,33 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
     return report(OKV_ENOSPC, "%s: the workspace must be %lld bytes, 256-byte aligned", who, (long long)need);
   const Pool pool = pool_of(c);
   const Rows rows{r->seqs, r->starts, r->lens, r->batch, r->n_rows};
-  // a tile of rows begins at a sequence's first row
-  const int64_t tiles = ((int64_t)r->n_rows * pool.R + kTileRows - 1) / kTileRows + std::min(r->batch, r->n_rows), pieces = tiles * pool.G;
-  if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
   Attend x;
   x.q = static_cast<const _Float16 *>(q), x.out = out, x.q_stride = q_stride;
   const float scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)d);
   x.scale = a->cap != 0.f ? scale / a->cap : scale * kLog2e, x.cap = a->cap * kLog2e;
   x.window = a->window, x.slopes = a->slopes, x.prefix = a->prefix;
-  const bool wide = a->out_dtype == 1, shaped = a->cap != 0.f || a->slopes;
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)pieces), dim3(kWaves * 64), 0, static_cast<hipStream_t>(stream), pool, rows, x); };
+  x.parts = static_cast<float *>(a->workspace);
+  const bool wide = a->out_dtype == 1, shaped = a->cap != 0.f || a->slopes, cuts = may_cut(pool);
+  // a tile of rows begins at a sequence's first row; cutting adds less than kTarget pieces
+  const int64_t all_rows = (int64_t)r->n_rows * pool.R;
+  const bool eight = all_rows * pool.G >= 256 * 256;
+  const int64_t rows_of_tile = eight ? 256 : 128;
+  const int64_t tiles = (all_rows + rows_of_tile - 1) / rows_of_tile + std::min(r->batch, r->n_rows), pieces = tiles * pool.G + (cuts ? kTarget : 0);
+  if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto run = [&](auto d_, auto w_, auto wide_) {
+    constexpr int D = decltype(d_)::value, W = decltype(w_)::value;
+    constexpr bool WIDE = decltype(wide_)::value;
+    if (shaped) hipLaunchKernelGGL((chunk_kernel<D, W, WIDE, true>), dim3((unsigned)pieces), dim3(64 * W), 0, s, pool, rows, x);
+    else hipLaunchKernelGGL((chunk_kernel<D, W, WIDE, false>), dim3((unsigned)pieces), dim3(64 * W), 0, s, pool, rows, x);
+    // (a tile that is cut has two cuts at least, and all of them are less than 2 kTarget)
+    if (cuts) hipLaunchKernelGGL((join_kernel<D, W, WIDE>), dim3((unsigned)(std::min<int64_t>(kTarget, tiles * pool.G) * (Form<D, W>::kRows / kJoinRows))), dim3(64 * kJoinWaves), 0, s, pool, rows, x);
+  };
   auto typed = [&](auto d_) {
-    constexpr int D = decltype(d_)::value;
-    if (wide) shaped ? launch(chunk_kernel<D, true, true>) : launch(chunk_kernel<D, true, false>);
-    else shaped ? launch(chunk_kernel<D, false, true>) : launch(chunk_kernel<D, false, false>);
+    const std::integral_constant<int, 8> w8{};
+    const std::integral_constant<int, 4> w4{};
+    if (wide) eight ? run(d_, w8, std::true_type{}) : run(d_, w4, std::true_type{});
+    else eight ? run(d_, w8, std::false_type{}) : run(d_, w4, std::false_type{});
   };
   if (d == 128) typed(std::integral_constant<int, 128>{});
   else typed(std::integral_constant<int, 64>{});
