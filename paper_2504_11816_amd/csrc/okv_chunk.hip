@@ -155,8 +155,9 @@ struct Attend {
   const _Float16 *q;
   void *out;
   int64_t q_stride;
-  float scale, cap;                      // of scores in units of log 2: scale log2(e), or with a cap scale / cap and cap log2(e)
+  float scale, cap;                      // of scores in units of log 2: scale log2(e), or with a cap 2 log2(e) scale / cap and cap log2(e)
   int32_t window;                        // 0: none
+  int32_t may_cut;                       // whether keys may be cut among workgroups (a second launch joins them)
   const float *slopes;
   const int32_t *prefix;
   float *parts;                          // results of pieces of rows' keys: kRows x D sums, and behind them kRows maxima and kRows sums of weights
@@ -166,17 +167,19 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kRaise = 8.f;            // the maximum is raised when a score is this far above it
 // Weights are 2^(s - m + kLift): at most 2^15, and normal numbers in fp16 down to 2^-21 of the largest
 constexpr float kLift = 7.f;
-constexpr int kKeys = 64;                // of a block
-constexpr int kTarget = 512;             // pieces that a call's keys are cut into, where it has fewer tiles of rows
-constexpr int kMinSpan = 4;              // blocks of a piece at least
+constexpr int kWaves = 4, kRing = 2;     // blocks of keys, and of values, in LDS
 
-// A workgroup of W wavefronts has 32 W of the n R rows (tokens, and for each its R query heads) of a sequence and KV head, a wavefront 32 of them.
-template <int D, int W>
+// Rows are the n R rows (tokens, and for each its R query heads) of a sequence and KV head; a wavefront has 32 of them, whose blocks of keys go by.
+// Few rows: a workgroup has 32, each wavefront every fourth block of 32 keys, and joins them.  Many: a workgroup has 128, a wavefront 32, and all share blocks of 64 keys.
+template <int D, bool FEW>
 struct Form {
-  static constexpr int kThreads = 64 * W, kRows = 32 * W;
-  static constexpr int kRing = W == 8 ? 3 : 2;                // blocks of keys, and of values, in LDS
-  static constexpr int kBlockBytes = kKeys * D * 2, kLoads = kBlockBytes / 1024 / W;      // loads of a wavefront per block of keys (or values)
+  static constexpr int kRows = FEW ? 32 : 32 * kWaves, kKeys = FEW ? 32 : 64, kStep = FEW ? kWaves * kKeys : kKeys;      // keys of a step of the workgroup
+  static constexpr int kBlockBytes = kKeys * D * 2, kLoads = kBlockBytes / 1024 / (FEW ? 1 : kWaves);                   // loads of a wavefront per block of keys (or values)
+  static constexpr int kLds = (FEW ? kWaves : 1) * 2 * kRing * kBlockBytes;
   static constexpr int kPartFloats = kRows * (D + 2);
+  // How keys are cut (see with_plan): workgroups that run at a time, pieces at most, and in steps what a piece costs beside its own and what joining does
+  static constexpr int kSlots = FEW && D == 128 ? 256 : 512, kPieces = FEW ? 2048 : 1024, kUncut = 512 / kStep;
+  static constexpr float kPerPiece = FEW ? 1.f : 4.f, kPerJoin = FEW ? 3.f : 10.f;
 };
 
 __device__ __forceinline__ half8 transposed(const char *first, const char *second) {
@@ -186,16 +189,20 @@ __device__ __forceinline__ half8 transposed(const char *first, const char *secon
   return half8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
 }
 
+// What all lanes have the same, in scalar registers
+__device__ __forceinline__ int uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const char *uniform(const char *p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const char *>((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
 // One 16-byte-per-lane load from `base` + off straight into LDS: lane l's bytes land at lds + 16 l.  Written as assembly because the compiler, which cannot tell the block being
 // written from the one being read, waits for all such loads in front of every LDS read otherwise.  m0 is left as it was found.
-__device__ __forceinline__ const char *uniform(const char *p) {      // all lanes have the same: in scalar registers
-  const uint64_t x = reinterpret_cast<uint64_t>(p);
-  return reinterpret_cast<const char *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
-}
 __device__ __forceinline__ void load_to_lds(const char *base, const uint32_t off, const uint32_t lds) {
-  base = uniform(base);
   uint32_t found;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0" : "=&s"(found) : "s"(lds), "v"(off), "s"(base) : "memory");
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(found)
+               : "s"(uniform((int)lds)), "v"(off), "s"(uniform(base))
+               : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_for_loads() {      // until N are outstanding
@@ -209,17 +216,17 @@ __device__ __forceinline__ void barrier_leaving_loads() {
   asm volatile("" ::: "memory");
 }
 
-// The blocks of keys that some row of a tile sees, in order: `ahead` blocks of the prefix, and those from `first` on
+// The steps of keys that some row of a tile sees, in order: `ahead` of the prefix, and those from `first` on
 struct Keys {
   int ahead, first, total;
 };
-template <int ROWS>
+template <class F>
 __device__ __forceinline__ Keys keys_of(const int n, const int len, const int prefix, const int window, const int R, const int tile) {
-  const int pos0 = len - n + tile * ROWS / R, pos1 = len - n + min((tile * ROWS + ROWS - 1) / R, n - 1);
+  const int pos0 = len - n + tile * F::kRows / R, pos1 = len - n + min((tile * F::kRows + F::kRows - 1) / R, n - 1);
   Keys k;
-  k.first = window == 0 || pos0 < window ? 0 : (pos0 - window + 1) / kKeys;
-  k.ahead = min((prefix + kKeys - 1) / kKeys, k.first);
-  k.total = k.ahead + max((max(pos1 + 1, prefix) + kKeys - 1) / kKeys - k.first, 0);
+  k.first = window == 0 || pos0 < window ? 0 : (pos0 - window + 1) / F::kStep;
+  k.ahead = min((prefix + F::kStep - 1) / F::kStep, k.first);
+  k.total = k.ahead + max((max(pos1 + 1, prefix) + F::kStep - 1) / F::kStep - k.first, 0);
   return k;
 }
 
@@ -227,13 +234,13 @@ __device__ __forceinline__ Keys keys_of(const int n, const int len, const int pr
 // into as many cuts: all of them by the same rule, from lengths that are on the device, by every workgroup for itself.
 struct Piece {
   int first, n, len, s, prefix;          // the sequence: its first row, its rows, its tokens, its row of the table (below 0: there is none)
-  int tile, g, cut, cuts, slot;          // slot: of the piece's results among those that are cut
+  int tile, g, cut, cuts, slot, apart;   // slot: of the piece's results among those that are cut; from a cut of the tile to the next
   bool there;
 };
 struct Sequence {
-  int first, n, s, len, prefix, tiles, blocks;
+  int first, n, s, len, prefix, tiles, steps;
 };
-template <int ROWS>
+template <class F>
 __device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, const int32_t *prefix, const int window, const int b) {
   Sequence q{0, 0, -1, 0, 0, 0, 0};
   if (b >= r.batch) return q;
@@ -246,8 +253,8 @@ __device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, co
     q.len = min(max(r.lens[s], 0), c.capacity);
     if (prefix) q.prefix = min(max(prefix[s], 0), q.len);
   }
-  q.tiles = (int)(((int64_t)q.n * c.R + ROWS - 1) / ROWS);
-  if (q.tiles) q.blocks = keys_of<ROWS>(q.n, q.len, q.prefix, window, c.R, q.tiles - 1).total;
+  q.tiles = (int)(((int64_t)q.n * c.R + F::kRows - 1) / F::kRows);
+  if (q.tiles) q.steps = keys_of<F>(q.n, q.len, q.prefix, window, c.R, q.tiles - 1).total;
   return q;
 }
 __device__ __forceinline__ int wave_scan(int x) {         // inclusive
@@ -259,37 +266,61 @@ __device__ __forceinline__ int wave_scan(int x) {         // inclusive
   }
   return x;
 }
-__device__ __forceinline__ double wave_total(double x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
-}
-// take(sequences of 64 lanes, cuts, pieces and cut pieces up to and with each, those before all of them) until it returns true
-template <int ROWS, class Take>
-__device__ __forceinline__ void with_plan(const Pool &c, const Rows &r, const int32_t *prefix, const int window, const Take &take) {
+__device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { return max((int)(((unsigned)q.steps + (unsigned)span - 1) / (unsigned)span), 1); }
+
+// The longest piece, in steps: what is expected to take the least time.  With P pieces of up to s steps (W in all) on kSlots workgroups at a time that is s + kPerPiece where
+// P <= kSlots, else (W + P kPerPiece) / kSlots and half a piece until the last one has ended; kPerJoin is added where any are cut.
+template <class F>
+__device__ __forceinline__ int span_of(const Pool &c, const Rows &r, const Attend &a, const Sequence &mine) {
   const int lane = threadIdx.x & 63;
-  Sequence q = sequence_at<ROWS>(c, r, prefix, window, lane);
-  double work = (double)q.tiles * q.blocks;
+  constexpr int kNone = 0x3fffffff;
+  if (!a.may_cut) return kNone;
+  float work = (float)mine.tiles * mine.steps, tiles = (float)mine.tiles, most = (float)mine.steps;
   for (int b0 = 64; b0 < r.batch; b0 += 64) {
-    const Sequence more = sequence_at<ROWS>(c, r, prefix, window, b0 + lane);
-    work += (double)more.tiles * more.blocks;
+    const Sequence q = sequence_at<F>(c, r, a.prefix, a.window, b0 + lane);
+    work += (float)q.tiles * q.steps, tiles += (float)q.tiles, most = fmaxf(most, (float)q.steps);
   }
-  const double share = ceil(wave_total(work) * c.G / kTarget);
-  const int span = max(kMinSpan, (int)fmin(share, 1e9));
+  work = wave_sum(work) * c.G, tiles = wave_sum(tiles) * c.G, most = wave_max(most);
+  auto time = [&](const float pieces, const float longest) {
+    return pieces <= F::kSlots ? longest + F::kPerPiece : (work + pieces * F::kPerPiece) * (1.f / F::kSlots) + .5f * (longest + F::kPerPiece);
+  };
+  float best = time(tiles, most);
+  int span = kNone;
+  const int least = max(1, (int)fminf(ceilf(work * (1.0001f / F::kPieces)), 1e9f));
+  if (best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return span;
+  for (int i = 0; i < 12; ++i) {
+    const float of_most = i < 8 ? most / (float)(i + 2) : work * (i == 8 ? .5f : i == 9 ? 1.f / 1.5f : i == 10 ? 1.f / 3.f : 1.f) * (1.f / F::kSlots);
+    const int s = uniform(max(least, (int)ceilf(of_most)));
+    float pieces = (float)mine.tiles * (float)cuts_of(mine, s);
+    for (int b0 = 64; b0 < r.batch; b0 += 64) {
+      const Sequence q = sequence_at<F>(c, r, a.prefix, a.window, b0 + lane);
+      pieces += (float)q.tiles * (float)cuts_of(q, s);
+    }
+    const float t = time(wave_sum(pieces) * c.G, fminf(most, (float)s)) + F::kPerJoin;
+    if (t < best) best = t, span = s;
+  }
+  return uniform(span);
+}
+// take(sequences of 64 lanes, their cuts, pieces and cut pieces up to and with each, those before all of them) until it returns true
+template <class F, class Take>
+__device__ __forceinline__ void with_plan(const Pool &c, const Rows &r, const Attend &a, const Take &take) {
+  const int lane = threadIdx.x & 63;
+  Sequence q = sequence_at<F>(c, r, a.prefix, a.window, lane);
+  const int span = span_of<F>(c, r, a, q);
   int pieces = 0, cut_pieces = 0;
   for (int b0 = 0; b0 < r.batch; b0 += 64) {
-    if (b0) q = sequence_at<ROWS>(c, r, prefix, window, b0 + lane);
-    const int cuts = max((q.blocks + span - 1) / span, 1), mine = q.tiles * c.G * cuts;
+    if (b0) q = sequence_at<F>(c, r, a.prefix, a.window, b0 + lane);
+    const int cuts = cuts_of(q, span), mine = q.tiles * c.G * cuts;
     const int upto = wave_scan(mine), cut_upto = wave_scan(cuts > 1 ? mine : 0);
     if (take(q, cuts, upto, cut_upto, pieces, cut_pieces)) return;
-    pieces += __shfl(upto, 63), cut_pieces += __shfl(cut_upto, 63);
+    pieces += uniform(__shfl(upto, 63)), cut_pieces += uniform(__shfl(cut_upto, 63));
   }
 }
-template <int ROWS>
-__device__ __forceinline__ Piece piece_of(const Pool &c, const Rows &r, const int32_t *prefix, const int window, const int index) {
+template <class F>
+__device__ __forceinline__ Piece piece_of(const Pool &c, const Rows &r, const Attend &a, const int index) {
   Piece p;
   p.there = false;
-  with_plan<ROWS>(c, r, prefix, window, [&](const Sequence &q, const int cuts, const int upto, const int cut_upto, const int before, const int cut_before) {
+  with_plan<F>(c, r, a, [&](const Sequence &q, const int cuts, const int upto, const int cut_upto, const int before, const int cut_before) {
     const uint64_t ended = __ballot(before + upto <= index);
     if (ended == ~0ull) return false;
     const int at = __popcll(ended);
@@ -299,40 +330,48 @@ __device__ __forceinline__ Piece piece_of(const Pool &c, const Rows &r, const in
     const int tiles = of(q.tiles), within = index - before - (of(upto) - tiles * c.G * p.cuts);
     // The heads of a tile next to each other, so that those of a head are on the same XCD where they are a multiple of eight; then the tiles, which read the same
     // keys; those that see the most keys first
-    p.g = within % c.G;
-    p.tile = tiles - 1 - within / c.G % tiles;
-    p.cut = within / c.G / tiles;
+    const int rank = uniform(within / c.G);
+    p.g = within - rank * c.G;
+    p.cut = uniform(rank / tiles);
+    p.tile = tiles - 1 - (rank - p.cut * tiles);
     p.slot = cut_before + of(cut_upto) - tiles * c.G * p.cuts + within;
     return true;
   });
   return p;
 }
 
-template <int D, int W, bool WIDE, bool SHAPED>
-__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
-  using F = Form<D, W>;
-  constexpr int kRing = F::kRing, kLoads = F::kLoads, kRowBytes = 2 * D;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kRing * F::kBlockBytes];
-  __shared__ int odd_first, odd_last;                    // blocks with values that are not finite, of those that not every row sees
-  const Piece p = piece_of<F::kRows>(c, r, a.prefix, a.window, blockIdx.x);
+template <int D, bool FEW, bool WIDE, bool SHAPED>
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
+  using F = Form<D, FEW>;
+  constexpr int kLoads = F::kLoads, kKeys = F::kKeys, kRowBytes = 2 * D, kParts = kKeys / 32;
+  __shared__ __attribute__((aligned(1024))) char lds[F::kLds];
+  __shared__ int odd_first, odd_last;                    // steps with values that are not finite, of those that not every row sees
+  const Piece p = piece_of<F>(c, r, a, blockIdx.x);
   if (!p.there) return;
   if (threadIdx.x == 0) odd_first = INT_MAX, odd_last = -1;      // (a barrier comes before their use)
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int row0 = p.tile * F::kRows + wave * 32, row = row0 + col;         // of the sequence's n R rows
-  const int token = row / c.R, head = p.g * c.R + row % c.R;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  const int row0 = p.tile * F::kRows + (FEW ? 0 : wave * 32), row = row0 + col;         // of the sequence's n R rows
+  const int token = row / c.R, head = p.g * c.R + row - token * c.R;
   const int base = p.len - p.n, pos = base + token;
-  const int from = a.window == 0 || pos < a.window ? 0 : pos - a.window + 1;
-  // of this wavefront's rows
-  const bool idle = row0 / c.R >= p.n;
-  const int pos0 = base + row0 / c.R, pos1 = base + min((row0 + 31) / c.R, p.n - 1);
-  const int from0 = a.window == 0 || pos0 < a.window ? 0 : pos0 - a.window + 1, from1 = a.window == 0 || pos1 < a.window ? 0 : pos1 - a.window + 1;
+  auto first_seen = [&](const int pos) { return a.window == 0 || pos < a.window ? 0 : pos - a.window + 1; };      // (but for the prefix)
+  const int from = first_seen(pos);
+  // of this wavefront's rows, and of the tile's
+  const int token0 = uniform(row0 / c.R), token1 = min(uniform((row0 + 31) / c.R), p.n - 1);
+  const bool idle = token0 >= p.n;
+  const int pos0 = base + token0, pos1 = base + token1, from0 = first_seen(pos0), from1 = first_seen(pos1);
+  const int tile_pos0 = base + uniform(p.tile * F::kRows / c.R), tile_pos1 = base + min(uniform((p.tile * F::kRows + F::kRows - 1) / c.R), p.n - 1);
+  const int tile_from1 = first_seen(tile_pos1);
+  auto all_see = [&](const int key0) { return (key0 + kKeys - 1 <= tile_pos0 && key0 >= tile_from1) || key0 + kKeys <= p.prefix; };      // rows of the tile
+  auto in_sight = [&](const int key0) { return !idle && ((key0 <= pos1 && key0 + kKeys > from0) || key0 < p.prefix); };                  // of some row of the wavefront
 
-  // this piece's blocks of the tile's
-  const Keys keys = keys_of<F::kRows>(p.n, p.len, p.prefix, a.window, c.R, p.tile);
-  const int i0 = (int)((int64_t)keys.total * p.cut / p.cuts), total = (int)((int64_t)keys.total * (p.cut + 1) / p.cuts) - i0;
-  auto block_at = [&](const int i) {                   // past the end: the last again
+  // this piece's steps of the tile's
+  Keys keys = keys_of<F>(p.n, p.len, p.prefix, a.window, c.R, p.tile);
+  keys.ahead = uniform(keys.ahead), keys.first = uniform(keys.first), keys.total = uniform(keys.total);
+  const int i0 = uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)p.cut / (unsigned)p.cuts));
+  const int total = uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)(p.cut + 1) / (unsigned)p.cuts)) - i0;
+  auto key_at_step = [&](const int i) {                // this wavefront's first key of a step; past the end: the last again
     const int j = i0 + min(i, total - 1);
-    return j < keys.ahead ? j : keys.first + j - keys.ahead;
+    return (j < keys.ahead ? j : keys.first + j - keys.ahead) * F::kStep + (FEW ? wave * kKeys : 0);
   };
 
   half8 qf[D / 16];
@@ -343,91 +382,89 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
   }
   const float slope = SHAPED && a.slopes ? a.slopes[head] * kLog2e : 0.f;
 
-  // Loads.  Row r of a block has its 16-byte pieces in units (D / 8) r .. of LDS, piece k in unit (D / 8) r + (k ^ turn(r)): sixteen rows' same piece, and the four pieces
-  // of 32 elements of four rows, are in different banks.  A load brings 1 KiB, 512 / D rows of a tile of 16; load j of a block is wavefront j % W's.
-  constexpr int kTileLoads = 16 * kRowBytes / 1024, kLoadRows = 1024 / kRowBytes, kUnits = D / 8;
-  static_assert(W % kTileLoads == 0, "a wavefront's loads are of the same rows of their tiles");
-  uint32_t lane_offset;
-  {
-    const int rr = wave % kTileLoads * kLoadRows + lane / kUnits, turn = D == 128 ? 4 * (rr & 3) | ((rr >> 2) & 3) : 4 * ((rr >> 1) & 1) | ((rr >> 2) & 3);
-    lane_offset = (uint32_t)(rr * kRowBytes + ((lane % kUnits) ^ turn) * 16);
-  }
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds) + wave * 1024;
+  // Loads.  Row r of a block has its 16-byte pieces in units (D / 8) r .. of LDS, piece k in unit (D / 8) r + (k ^ turn(r)), turn 4 (r & 3) + ((r >> 2) & 3) (D = 64: of r / 2, one bit each):
+  // sixteen rows' same piece, and the four pieces of 32 elements of four rows, are in different banks.  A load brings 1 KiB, 512 / D rows of a tile of 16.  FEW: a
+  // wavefront has rings of its own and loads all of its blocks; else load j of a block is wavefront j % 4's.
+  constexpr int kTileLoads = 16 * kRowBytes / 1024, kUnits = D / 8, kBases = FEW ? kLoads / kTileLoads : kLoads;
+  static_assert(kWaves % kTileLoads == 0, "a wavefront's loads of a shared block are of the same rows of their tiles");
+  const int lane_row = lane / kUnits;
+  const uint32_t lane_base = lane_row * kRowBytes + 16 * ((lane % kUnits) ^ (D == 128 ? 4 * lane_row : 4 * ((lane_row >> 1) & 1) | (lane_row >> 2)));
+  auto lane_offset = [&](const int j) { return (lane_base ^ (j * (D == 128 ? 16 : 32))) + j * 1024; };         // of load j of a tile
+  const uint32_t shared_offset = lane_offset(wave % kTileLoads);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (FEW ? wave * (F::kLds / kWaves) : 0);
+  char *const mine = lds + (FEW ? wave * (F::kLds / kWaves) : 0);
   const int32_t *table_row = c.table + (int64_t)max(p.s, 0) * c.width;
-  const char *pool = reinterpret_cast<const char *>(c.kv + head_offset<D>(c, p.g));
+  const char *pool = uniform(reinterpret_cast<const char *>(c.kv + head_offset<D>(c, p.g)));
   const int64_t slab = (int64_t)2 * c.G * D << (4 + c.st_log2);
   const int last_tile = (p.len - 1) >> 4;
   int held_from = INT_MIN / 2, held = p.s;              // lane l: the block in entry held_from + l of the sequence's row of the table
-  const char *value_base[kLoads];
-  auto load_keys = [&](const int i, const int slot, const char *(&bases)[kLoads]) {
-    const int t0 = __builtin_amdgcn_readfirstlane(block_at(i)) * (kKeys / 16) + wave / kTileLoads;
+  const char *value_base[kBases];
+  auto load = [&](const char *(&bases)[kBases], const uint32_t more, const int slot) {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int t = min(t0 + j * (W / kTileLoads), last_tile), e = t >> c.log2_tiles, tb = t & ((1 << c.log2_tiles) - 1);
+    for (int j = 0; j < kLoads; ++j)
+      if constexpr (FEW) load_to_lds(bases[j / kTileLoads] + more, lane_offset(j % kTileLoads), lds0 + slot * F::kBlockBytes + j * 1024);
+      else load_to_lds(bases[j] + more, shared_offset, lds0 + slot * F::kBlockBytes + (j * kWaves + wave) * 1024);
+  };
+  auto load_keys = [&](const int i, const int slot) {
+    const int t0 = uniform(key_at_step(i)) / 16 + (FEW ? 0 : wave / kTileLoads);
+#pragma unroll
+    for (int j = 0; j < kBases; ++j) {
+      const int t = min(t0 + (FEW ? j : j * (kWaves / kTileLoads)), last_tile), e = t >> c.log2_tiles, tb = t & ((1 << c.log2_tiles) - 1);
       if (c.table && (unsigned)(e - held_from) >= 64u) {
         held_from = e;
         held = min(max(table_row[min(e + lane, c.width - 1)], 0), c.n_blocks - 1);
       }
       const int block = __builtin_amdgcn_readlane(held, c.table ? e - held_from : 0);
-      bases[j] = uniform(pool + 2 * (block * c.block_elems + (tb >> c.st_log2) * slab + (int64_t)(tb & ((1 << c.st_log2) - 1)) * (c.gg * 16 * D)));
-      load_to_lds(bases[j], lane_offset, __builtin_amdgcn_readfirstlane(lds0 + slot * F::kBlockBytes + j * W * 1024));
+      value_base[j] = uniform(pool + 2 * (block * c.block_elems + (tb >> c.st_log2) * slab + (int64_t)(tb & ((1 << c.st_log2) - 1)) * (c.gg * 16 * D)));
     }
+    load(value_base, 0, slot);
   };
   const uint32_t behind = 2 * v_offset<D>(c);
-  auto load_values = [&](const int slot) {
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) load_to_lds(value_base[j] + behind, lane_offset, __builtin_amdgcn_readfirstlane(lds0 + (kRing + slot) * F::kBlockBytes + j * W * 1024));
-  };
+  auto load_values = [&](const int slot) { load(value_base, behind, kRing + slot); };      // of the keys that were loaded last
 
   // where this lane's operands begin in a block; xor 32 k (keys' k-th 16 elements) or 64 e (values' e-th 32 elements)
-  const int x4 = (lane >> 2) & 3;
+  const int x4 = (lane >> 2) & 3, p4 = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
   uint32_t key_at, value_at0, value_at1;
   if constexpr (D == 128) {
     key_at = col * kRowBytes + 16 * (half ^ (4 * (col & 3) | ((col >> 2) & 3)));
-    value_at0 = (4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * x4 | half)) + 8 * (lane & 1);
-    value_at1 = (8 + 4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * x4 | (half + 2))) + 8 * (lane & 1);
+    value_at0 = (4 * half + x4) * kRowBytes + 16 * (p4 ^ (4 * x4 | half)) + 8 * (lane & 1);
+    value_at1 = (8 + 4 * half + x4) * kRowBytes + 16 * (p4 ^ (4 * x4 | (half + 2))) + 8 * (lane & 1);
   } else {
     key_at = col * kRowBytes + 16 * (half ^ (4 * ((col >> 1) & 1) | ((col >> 2) & 3)));
-    value_at0 = (4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * (x4 >> 1) | half)) + 8 * (lane & 1);
-    value_at1 = (8 + 4 * half + x4) * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ (4 * (x4 >> 1) | (half + 2))) + 8 * (lane & 1);
+    value_at0 = (4 * half + x4) * kRowBytes + 16 * (p4 ^ (4 * (x4 >> 1) | half)) + 8 * (lane & 1);
+    value_at1 = (8 + 4 * half + x4) * kRowBytes + 16 * (p4 ^ (4 * (x4 >> 1) | (half + 2))) + 8 * (lane & 1);
   }
 
   floatx16 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = floatx16{};
   float m = -1e30f, l = 0.f;
-
   // scores: keys 32 b + 8 (i / 4) + 4 half + i % 4 of this lane's row
-  auto score = [&](floatx16 (&x)[2], const int slot) {
-    const char *k0 = lds + slot * F::kBlockBytes;
+  auto score = [&](floatx16 (&x)[kParts], const int slot) {
+    const char *k0 = mine + slot * F::kBlockBytes;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kParts; ++b) {
       x[b] = floatx16{};
 #pragma unroll
       for (int k = 0; k < D / 16; ++k)
         x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8 *>(k0 + (key_at ^ (32 * k)) + b * 32 * kRowBytes), qf[k], x[b], 0, 0, 0);
     }
   };
-  const int tile_token0 = p.tile * F::kRows / c.R, tile_pos0 = base + tile_token0, tile_pos1 = base + min((p.tile * F::kRows + F::kRows - 1) / c.R, p.n - 1);
-  const int tile_from1 = a.window == 0 || tile_pos1 < a.window ? 0 : tile_pos1 - a.window + 1;
-  auto all_see = [&](const int key0) { return (key0 + kKeys - 1 <= tile_pos0 && key0 >= tile_from1) || key0 + kKeys <= p.prefix; };      // rows of the tile
-  auto in_sight = [&](const int key0) { return !idle && ((key0 <= pos1 && key0 + kKeys > from0) || key0 < p.prefix); };
 
-  int slot = 0;
-  auto step = [&](const int i, floatx16 (&x)[2], floatx16 (&next)[2]) {
-    const int after = slot + 1 == kRing ? 0 : slot + 1, before = slot == 0 ? kRing - 1 : slot - 1;
-    wait_for_loads<(kRing - 2) * 2 * kLoads>();
-    barrier_leaving_loads();                             // the next block of keys and this one of values are there, those before free
-    load_values(before);
-    load_keys(i + kRing, slot, value_base);
+  auto step = [&](const int i, const int slot, floatx16 (&x)[kParts], floatx16 (&next)[kParts]) {
+    wait_for_loads<0>();
+    if constexpr (!FEW) barrier_leaving_loads();         // the next block of keys and this one of values are there, those before free
+    load_values(slot ^ 1);
+    load_keys(i + 2, slot);
     __builtin_amdgcn_sched_barrier(0);
-    const int key0 = block_at(i) * kKeys;
+    const int key0 = uniform(key_at_step(i));
+    char *const v0 = mine + (kRing + slot) * F::kBlockBytes;
     if (!all_see(key0)) {
       // A number that is not finite may be of a key that some row does not see, and 0 times it is not 0: it is taken out here, and added at the end where it is seen
       bool odd = false;
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
-        u32x4 *at = reinterpret_cast<u32x4 *>(lds + (kRing + slot) * F::kBlockBytes + (j * W + wave) * 1024 + 16 * lane), w = *at;
+        u32x4 *at = reinterpret_cast<u32x4 *>(v0 + (FEW ? j : j * kWaves + wave) * 1024 + 16 * lane), w = *at;
         uint32_t any = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -441,182 +478,230 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 
         }
       }
       if (odd) atomicMin(&odd_first, i), atomicMax(&odd_last, i);
-      __syncthreads();
+      if constexpr (!FEW) __syncthreads();
     }
-    const bool seen = in_sight(key0), whole = (key0 + kKeys - 1 <= pos0 && key0 >= from1) || key0 + kKeys <= p.prefix;
+    if (!in_sight(key0)) {
+      if (i + 1 < total && in_sight(uniform(key_at_step(i + 1)))) score(next, slot ^ 1);
+      return;
+    }
+    const bool whole = (key0 + kKeys - 1 <= pos0 && key0 >= from1) || key0 + kKeys <= p.prefix;
+    const int apart = pos - key0 - 4 * half;             // from the lane's first key to its row
     float by = a.scale;
-    if (seen) {
-      float top = -INFINITY;
-      if (SHAPED || !whole) {
-        // (shaped, masked: in units of log 2 from here on)
+    if constexpr (SHAPED) {
+      // (in units of log 2 from here on)  tanh(y) = 1 - 2 / (e^2y + 1): off by 3 2^-24 of 1, whatever y
+      if (a.cap != 0.f) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < kParts; ++b)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int key = key0 + 32 * b + 8 * (j / 4) + 4 * half + j % 4;
-            float s = x[b][j] * a.scale;
-            if constexpr (SHAPED) {
-              if (a.cap != 0.f) s = a.cap * tanhf(s);
-              s = fmaf(-slope, (float)abs(pos - key), s);
-            }
-            if (!whole && !((key <= pos && key >= from) || key < p.prefix)) s = -INFINITY;
-            x[b][j] = s;
-          }
-        by = 1.f;
+          for (int j = 0; j < 16; ++j) x[b][j] = fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[b][j] * a.scale) + 1.f), a.cap);
+      } else {
+#pragma unroll
+        for (int b = 0; b < kParts; ++b) x[b] *= a.scale;
       }
+      if (a.slopes) {
+        const float far = (float)apart;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < kParts; ++b)
 #pragma unroll
-        for (int j = 0; j < 16; j += 2) top = fmaxf(fmaxf(top, x[b][j]), x[b][j + 1]);
-      top = max_with_lane_xor<32>(top) * by;
-      if (__ballot(top > m + kRaise)) {
-        const float to = top > m + kRaise ? top : m, scale = __builtin_amdgcn_exp2f(m - to);
-        l *= scale;
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] *= scale;
-        m = to;
+          for (int j = 0; j < 16; ++j) x[b][j] = fmaf(-slope, fabsf(far - (float)(32 * b + 8 * (j / 4) + j % 4)), x[b][j]);
       }
+      by = 1.f;
     }
-    if (i + 1 < total && in_sight(block_at(i + 1) * kKeys)) score(next, after);
-    if (seen) {
-      half8 hi[4], lo[WIDE ? 4 : 1];
-      const float less = kLift - m;
-      float sums[4] = {};
+    if (!whole) {
+      const int fixed = p.prefix - key0 - 4 * half, upto = max(apart, fixed - 1), below = from - key0 - 4 * half;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < kParts; ++b)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(x[b][j], by, less));
-          sums[j % 4] += w;
-          hi[2 * b + j / 8][j % 8] = (_Float16)w;
-          if constexpr (WIDE) lo[2 * b + j / 8][j % 8] = (_Float16)(w - (float)(_Float16)w);
-        }
-      l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-      // results: elements 32 e + 8 (i / 4) + 4 half + i % 4 of this lane's row
-      const char *v0 = lds + (kRing + slot) * F::kBlockBytes;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) {
-          const half8 vf = transposed(v0 + (value_at0 ^ (64 * e)) + t * 16 * kRowBytes, v0 + (value_at1 ^ (64 * e)) + t * 16 * kRowBytes);
-          o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, hi[t], o[e], 0, 0, 0);
-          if constexpr (WIDE) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo[t], o[e], 0, 0, 0);
+          const int key = 32 * b + 8 * (j / 4) + j % 4;
+          const bool hidden = (key > upto) | ((key < below) & (key >= fixed));
+          x[b][j] = hidden ? -INFINITY : x[b][j];
         }
     }
-    slot = after;
+    float top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < kParts; ++b)
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) top = fmaxf(fmaxf(top, x[b][j]), x[b][j + 1]);
+    top = max_with_lane_xor<32>(top) * by;
+    if (__ballot(top > m + kRaise)) {
+      const float to = top > m + kRaise ? top : m, scale = __builtin_amdgcn_exp2f(m - to);
+      l *= scale;
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) o[e] *= scale;
+      m = to;
+    }
+    // The next block's scores under this one's weights (past the end, or out of sight: for nothing)
+    score(next, slot ^ 1);
+    half8 hi[2 * kParts], lo[WIDE ? 2 * kParts : 1];
+    const float less = kLift - m;
+    float sums[4] = {};
+#pragma unroll
+    for (int b = 0; b < kParts; ++b)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(x[b][j], by, less));
+        sums[j % 4] += w;
+        hi[2 * b + j / 8][j % 8] = (_Float16)w;
+        if constexpr (WIDE) lo[2 * b + j / 8][j % 8] = (_Float16)(w - (float)(_Float16)w);
+      }
+    l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    // results: elements 32 e + 8 (i / 4) + 4 half + i % 4 of this lane's row
+#pragma unroll
+    for (int t = 0; t < 2 * kParts; ++t)
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) {
+        const half8 vf = transposed(v0 + (value_at0 ^ (64 * e)) + t * 16 * kRowBytes, v0 + (value_at1 ^ (64 * e)) + t * 16 * kRowBytes);
+        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, hi[t], o[e], 0, 0, 0);
+        if constexpr (WIDE) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo[t], o[e], 0, 0, 0);
+      }
   };
 
   if (total > 0) {
-    load_keys(0, 0, value_base);
-#pragma unroll
-    for (int g = 1; g < kRing; ++g) {
-      load_values(g - 1);
-      load_keys(g, g, value_base);
-    }
-    wait_for_loads<(kRing - 1) * 2 * kLoads>();
+    load_keys(0, 0);
+    load_values(0);
+    load_keys(1, 1);
+    wait_for_loads<2 * kLoads>();
     barrier_leaving_loads();
-    floatx16 x[2], y[2];
-    if (in_sight(block_at(0) * kKeys)) score(x, 0);
+    floatx16 x[kParts], y[kParts];
+    if (in_sight(uniform(key_at_step(0)))) score(x, 0);
     for (int i = 0;; i += 2) {
-      step(i, x, y);
+      step(i, 0, x, y);
       if (i + 1 >= total) break;
-      step(i + 1, y, x);
+      step(i + 1, 1, y, x);
       if (i + 2 >= total) break;
     }
     wait_for_loads<0>();                                 // nothing may still be on its way into LDS
     __syncthreads();
 #pragma unroll 1
     for (int i = odd_first; i <= odd_last; ++i) {
-      const int key0 = block_at(i) * kKeys;
+      const int key0 = uniform(key_at_step(i));
       if (all_see(key0)) continue;
 #pragma unroll 1
       for (int key = key0; key < min(key0 + kKeys, p.len); ++key) {
-        const bool mine = (key <= pos && key >= from) || key < p.prefix;
+        const bool seen = (key <= pos && key >= from) || key < p.prefix;
         const _Float16 *v = c.kv + tile_at<D>(c, table_row, p.s, key >> 4) + head_offset<D>(c, p.g) + v_offset<D>(c) + (key & 15) * D + 4 * half;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const half4 x = *reinterpret_cast<const half4 *>(v + 32 * e + 8 * j);
+            const half4 w = *reinterpret_cast<const half4 *>(v + 32 * e + 8 * j);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              if (mine && !(fabsf((float)x[q]) < INFINITY)) o[e][4 * j + q] += (float)x[q];
+              if (seen && !(fabsf((float)w[q]) < INFINITY)) o[e][4 * j + q] += (float)w[q];
           }
       }
     }
   }
-  if (token >= p.n) return;
   l = sum_with_lane_xor<32>(l);
   float *parts = a.parts + (int64_t)p.slot * F::kPartFloats;
-  const int of_tile = wave * 32 + col;
-  const float over = p.cuts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-  const int64_t to = p.cuts > 1 ? of_tile * D : ((int64_t)(p.first + token) * (c.G * c.R) + head) * D;
-  if (p.cuts > 1 && half == 0) parts[F::kRows * D + of_tile] = m, parts[F::kRows * (D + 1) + of_tile] = l;
+  if constexpr (!FEW) {
+    if (token >= p.n) return;
+    const int of_tile = wave * 32 + col;
+    const float over = p.cuts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const int64_t to = p.cuts > 1 ? of_tile * D : ((int64_t)(p.first + token) * (c.G * c.R) + head) * D;
+    if (p.cuts > 1 && half == 0) parts[F::kRows * D + of_tile] = m, parts[F::kRows * (D + 1) + of_tile] = l;
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e)
+    for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      floatx4 y;
+      for (int i = 0; i < 4; ++i) {
+        floatx4 y;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = o[e][4 * i + j] * over;
-      const int64_t at = to + 32 * e + 8 * i + 4 * half;
+        for (int j = 0; j < 4; ++j) y[j] = o[e][4 * i + j] * over;
+        const int64_t at = to + 32 * e + 8 * i + 4 * half;
+        if (p.cuts > 1) *reinterpret_cast<floatx4 *>(parts + at) = y;
+        else if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
+        else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
+      }
+  } else {
+    // The wavefronts' results through LDS (each has written to rings of its own only): a row's D sums, then the maxima and the sums of weights
+    constexpr int kStride = D + 4, kEach = F::kLds / kWaves / 4;
+    static_assert(32 * kStride + 64 <= kEach, "a wavefront's results fit its rings");
+    float *const all = reinterpret_cast<float *>(lds), *const own = all + wave * kEach;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<floatx4 *>(own + col * kStride + 32 * e + 8 * i + 4 * half) = floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
+    if (half == 0) own[32 * kStride + col] = m, own[32 * kStride + 32 + col] = l;
+    __syncthreads();
+    const int of_tile = wave * 8 + lane / 8, joined_row = p.tile * 32 + of_tile, joined_token = joined_row / c.R;
+    if (joined_token >= p.n) return;
+    float most = -1e30f, sum = 0.f, factor[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, all[w * kEach + 32 * kStride + of_tile]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      factor[w] = __builtin_amdgcn_exp2f(all[w * kEach + 32 * kStride + of_tile] - most);
+      sum += all[w * kEach + 32 * kStride + 32 + of_tile] * factor[w];
+    }
+    const float over = p.cuts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t to = p.cuts > 1 ? of_tile * D : ((int64_t)(p.first + joined_token) * (c.G * c.R) + p.g * c.R + joined_row - joined_token * c.R) * D;
+    if (p.cuts > 1 && lane % 8 == 0) parts[F::kRows * D + of_tile] = most, parts[F::kRows * (D + 1) + of_tile] = sum;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+      floatx4 y = {};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) y += *reinterpret_cast<const floatx4 *>(all + w * kEach + of_tile * kStride + 32 * e + 4 * (lane % 8)) * factor[w];
+      y *= over;
+      const int64_t at = to + 32 * e + 4 * (lane % 8);
       if (p.cuts > 1) *reinterpret_cast<floatx4 *>(parts + at) = y;
       else if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
       else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
     }
+  }
 }
 
-// Joins the cuts of a tile's rows: a workgroup per 32 rows of a tile that is cut, a wavefront per 8
-constexpr int kJoinRows = 32, kJoinWaves = 4;
+// Joins the cuts of a tile's rows: a workgroup per 32 rows of a tile that is cut
+constexpr int kJoinRows = 32, kJoinThreads = 256;
 
-template <int D, int W, bool WIDE>
-__global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(Pool c, Rows r, Attend a) {
-  using F = Form<D, W>;
+template <int D, bool FEW, bool WIDE>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(Pool c, Rows r, Attend a) {
+  using F = Form<D, FEW>;
   const int tile_index = blockIdx.x / (F::kRows / kJoinRows);
   Piece p;
   p.there = false;
   int tiles_before = 0;
-  with_plan<F::kRows>(c, r, a.prefix, a.window, [&](const Sequence &q, const int cuts, const int, const int cut_upto, const int, const int cut_before) {
+  with_plan<F>(c, r, a, [&](const Sequence &q, const int cuts, const int, const int cut_upto, const int, const int cut_before) {
     const int mine = cuts > 1 ? q.tiles * c.G : 0, upto = wave_scan(mine);
     const uint64_t ended = __ballot(tiles_before + upto <= tile_index);
     if (ended == ~0ull) {
-      tiles_before += __shfl(upto, 63);
+      tiles_before += uniform(__shfl(upto, 63));
       return false;
     }
     const int at = __popcll(ended);
     auto of = [&](const int x) { return __builtin_amdgcn_readlane(x, at); };
     p.there = true;
     p.first = of(q.first), p.n = of(q.n), p.cuts = of(cuts);
-    const int tiles = of(q.tiles), within = tile_index - tiles_before - (of(upto) - tiles * c.G);
-    p.g = within % c.G;
-    p.tile = tiles - 1 - within / c.G;
-    p.cut = tiles * c.G;                                 // slots from a cut of the tile to the next
+    const int tiles = of(q.tiles), within = tile_index - tiles_before - (of(upto) - tiles * c.G), rank = uniform(within / c.G);
+    p.g = within - rank * c.G;
+    p.tile = tiles - 1 - rank;
+    p.apart = tiles * c.G;
     p.slot = cut_before + of(cut_upto) - tiles * c.G * p.cuts + within;
     return true;
   });
   if (!p.there) return;
-  constexpr int kEach = D / 64;
-  const int lane = threadIdx.x & 63, of_tile0 = blockIdx.x % (F::kRows / kJoinRows) * kJoinRows + (threadIdx.x >> 6) * (kJoinRows / kJoinWaves);
-  for (int k = 0; k < kJoinRows / kJoinWaves; ++k) {
-    const int of_tile = of_tile0 + k, row = p.tile * F::kRows + of_tile, token = row / c.R, head = p.g * c.R + row % c.R;
+  constexpr int kLanes = D / 4, kTogether = kJoinThreads / kLanes;      // a row's lanes, four elements each; rows at a time
+#pragma unroll 1
+  for (int k = 0; k < kJoinRows; k += kTogether) {
+    const int of_tile = blockIdx.x % (F::kRows / kJoinRows) * kJoinRows + k + threadIdx.x / kLanes, row = p.tile * F::kRows + of_tile, token = row / c.R, head = p.g * c.R + row - token * c.R;
     if (token >= p.n) return;
-    float m = -1e30f, l = 0.f, o[kEach] = {};
+    const float *part = a.parts + (int64_t)p.slot * F::kPartFloats;
+    const int64_t apart = (int64_t)p.apart * F::kPartFloats;
+    float m = -1e30f, l = 0.f;
+#pragma unroll 4
+    for (int cut = 0; cut < p.cuts; ++cut) m = fmaxf(m, part[cut * apart + F::kRows * D + of_tile]);
+    floatx4 o = {};
+#pragma unroll 4
     for (int cut = 0; cut < p.cuts; ++cut) {
-      const float *part = a.parts + (int64_t)(p.slot + cut * p.cut) * F::kPartFloats;
-      const float theirs = part[F::kRows * D + of_tile], weight = part[F::kRows * (D + 1) + of_tile], to = fmaxf(m, theirs);
-      const float mine = __builtin_amdgcn_exp2f(m - to), other = __builtin_amdgcn_exp2f(theirs - to);
-      l = l * mine + weight * other;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) o[i] = o[i] * mine + part[of_tile * D + kEach * lane + i] * other;
-      m = to;
+      const float *one = part + cut * apart;
+      const float factor = __builtin_amdgcn_exp2f(one[F::kRows * D + of_tile] - m);
+      l += one[F::kRows * (D + 1) + of_tile] * factor;
+      o += *reinterpret_cast<const floatx4 *>(one + of_tile * D + 4 * (threadIdx.x % kLanes)) * factor;
     }
-    const float over = l == 0.f ? 0.f : 1.f / l;
-    const int64_t at = ((int64_t)(p.first + token) * (c.G * c.R) + head) * D + kEach * lane;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      if constexpr (WIDE) static_cast<float *>(a.out)[at + i] = o[i] * over;
-      else static_cast<_Float16 *>(a.out)[at + i] = (_Float16)(o[i] * over);
-    }
+    o *= l == 0.f ? 0.f : 1.f / l;
+    const int64_t at = ((int64_t)(p.first + token) * (c.G * c.R) + head) * D + 4 * (threadIdx.x % kLanes);
+    if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = o;
+    else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
   }
 }
 
@@ -663,9 +748,6 @@ Pool pool_of(const okv_layer_pool *c) {
   p.block_elems = (int64_t)2 * p.G * c->head_dim * slice;
   return p;
 }
-// Whether a sequence can have more blocks of keys than a piece has at least
-bool may_cut(const Pool &p) { return (p.capacity + kKeys - 1) / kKeys > kMinSpan; }
-
 int hip_result(const char *who) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? OKV_OK : report(OKV_EHIP, "%s: %s", who, hipGetErrorString(e));
@@ -711,10 +793,12 @@ int okv_rope_append(const okv_layer_pool *c, const okv_rows *r, const okv_rope *
 
 int64_t okv_chunk_workspace_bytes(const okv_layer_pool *c) {
   if (const char *why = shape_problem(c)) return report(OKV_EINVAL, "okv_chunk_workspace_bytes: %s", why);
-  if (!may_cut(pool_of(c))) return 0;
-  // A sequence that is cut is cut into less than twice its keys' shares of a span, and these are at most kTarget
-  const int64_t of_piece = c->head_dim == 128 ? Form<128, 8>::kPartFloats : Form<64, 8>::kPartFloats;
-  return 2 * kTarget * of_piece * 4;
+  // A tile that is cut has less than twice as many cuts as its steps are spans, which are kPieces at most
+  auto of = [&](auto form) {
+    using F = decltype(form);
+    return pool_of(c).capacity <= F::kUncut * F::kStep ? (int64_t)0 : (int64_t)2 * F::kPieces * F::kPartFloats * 4;
+  };
+  return c->head_dim == 128 ? std::max(of(Form<128, true>{}), of(Form<128, false>{})) : std::max(of(Form<64, true>{}), of(Form<64, false>{}));
 }
 
 int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *a, const void *q, int64_t q_stride, void *out, void *stream) {
@@ -737,34 +821,35 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
   Attend x;
   x.q = static_cast<const _Float16 *>(q), x.out = out, x.q_stride = q_stride;
   const float scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)d);
-  x.scale = a->cap != 0.f ? scale / a->cap : scale * kLog2e, x.cap = a->cap * kLog2e;
+  x.scale = a->cap != 0.f ? 2.f * kLog2e * (scale / a->cap) : scale * kLog2e, x.cap = a->cap * kLog2e;
   x.window = a->window, x.slopes = a->slopes, x.prefix = a->prefix;
   x.parts = static_cast<float *>(a->workspace);
-  const bool wide = a->out_dtype == 1, shaped = a->cap != 0.f || a->slopes, cuts = may_cut(pool);
-  // a tile of rows begins at a sequence's first row; cutting adds less than kTarget pieces
+  x.parts = static_cast<float *>(a->workspace);
+  const bool wide = a->out_dtype == 1, shaped = a->cap != 0.f || a->slopes;
+  // How many rows a sequence brings is on the device: by the mean
   const int64_t all_rows = (int64_t)r->n_rows * pool.R;
-  const bool eight = all_rows * pool.G >= 256 * 256;
-  const int64_t rows_of_tile = eight ? 256 : 128;
-  const int64_t tiles = (all_rows + rows_of_tile - 1) / rows_of_tile + std::min(r->batch, r->n_rows), pieces = tiles * pool.G + (cuts ? kTarget : 0);
-  if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
+  const bool few = all_rows <= 32 * (int64_t)r->batch;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto run = [&](auto d_, auto w_, auto wide_) {
-    constexpr int D = decltype(d_)::value, W = decltype(w_)::value;
-    constexpr bool WIDE = decltype(wide_)::value;
-    if (shaped) hipLaunchKernelGGL((chunk_kernel<D, W, WIDE, true>), dim3((unsigned)pieces), dim3(64 * W), 0, s, pool, rows, x);
-    else hipLaunchKernelGGL((chunk_kernel<D, W, WIDE, false>), dim3((unsigned)pieces), dim3(64 * W), 0, s, pool, rows, x);
-    // (a tile that is cut has two cuts at least, and all of them are less than 2 kTarget)
-    if (cuts) hipLaunchKernelGGL((join_kernel<D, W, WIDE>), dim3((unsigned)(std::min<int64_t>(kTarget, tiles * pool.G) * (Form<D, W>::kRows / kJoinRows))), dim3(64 * kJoinWaves), 0, s, pool, rows, x);
+  auto run = [&](auto d_, auto few_, auto wide_) {
+    constexpr int D = decltype(d_)::value;
+    constexpr bool FEW = decltype(few_)::value, WIDE = decltype(wide_)::value;
+    using F = Form<D, FEW>;
+    x.may_cut = pool.capacity > F::kUncut * F::kStep;
+    // a tile of rows begins at a sequence's first row; cutting adds at most kPieces
+    const int64_t tiles = (all_rows + F::kRows - 1) / F::kRows + std::min(r->batch, r->n_rows), pieces = tiles * pool.G + (x.may_cut ? F::kPieces : 0);
+    if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
+    if (shaped) hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, true>), dim3((unsigned)pieces), dim3(64 * kWaves), 0, s, pool, rows, x);
+    else hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, false>), dim3((unsigned)pieces), dim3(64 * kWaves), 0, s, pool, rows, x);
+    // (tiles that are cut have more steps than a span)
+    if (x.may_cut)
+      hipLaunchKernelGGL((join_kernel<D, FEW, WIDE>), dim3((unsigned)(std::min<int64_t>(F::kPieces, tiles * pool.G) * (F::kRows / kJoinRows))), dim3(kJoinThreads), 0, s, pool, rows, x);
+    return hip_result(who);
   };
   auto typed = [&](auto d_) {
-    const std::integral_constant<int, 8> w8{};
-    const std::integral_constant<int, 4> w4{};
-    if (wide) eight ? run(d_, w8, std::true_type{}) : run(d_, w4, std::true_type{});
-    else eight ? run(d_, w8, std::false_type{}) : run(d_, w4, std::false_type{});
+    if (few) return wide ? run(d_, std::true_type{}, std::true_type{}) : run(d_, std::true_type{}, std::false_type{});
+    return wide ? run(d_, std::false_type{}, std::true_type{}) : run(d_, std::false_type{}, std::false_type{});
   };
-  if (d == 128) typed(std::integral_constant<int, 128>{});
-  else typed(std::integral_constant<int, 64>{});
-  return hip_result(who);
+  return d == 128 ? typed(std::integral_constant<int, 128>{}) : typed(std::integral_constant<int, 64>{});
 }
 
 }  // extern "C"

@@ -16,58 +16,174 @@ namespace okv {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+
+// Rows begin anywhere: vectors of elements that are aligned as one of them is
+typedef _Float16 half8 __attribute__((ext_vector_type(8), aligned(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---- probabilities --------------------------------------------------------------------------------
+//
+// Every logit is read and every probability written once where a row fits the registers of a workgroup: one launch.  Longer rows are cut into pieces of as many workgroups, in two launches: the
+// largest number and the sum of every piece, then the quotients, whose logits come from the memory-side cache.
 
-// The largest number of a row so far, the sum of 2^((x - largest) by) over it, and where it was first
+constexpr int kRowThreads = 1024, kPieceThreads = 256;
+constexpr int kEach = 32;                // logits of a thread, eight in a row at a time
+constexpr int kOneLaunch = kRowThreads * kEach;
+constexpr int kPieceLogits = kPieceThreads * kEach;
+
+// The largest number of a piece, where it was first, and the sum of 2^((x - largest) by) over it
 struct Seen {
   float top, sum;
-  int at;
+  int at, unused;
 };
-__device__ __forceinline__ Seen joined(const Seen &a, const Seen &b, const float by) {
-  Seen r;
-  r.top = fmaxf(a.top, b.top);
-  // (-infinity alone has nothing to add)
-  r.sum = (a.top == -INFINITY ? a.sum : a.sum * __builtin_amdgcn_exp2f((a.top - r.top) * by)) + (b.top == -INFINITY ? b.sum : b.sum * __builtin_amdgcn_exp2f((b.top - r.top) * by));
-  r.at = a.top > b.top || (a.top == b.top && a.at < b.at) ? a.at : b.at;
-  return r;
+
+template <class T>
+__device__ __forceinline__ void load8(const T *x, const int n, float (&to)[8]) {      // n of them are there, -infinity for the others
+  if (n >= 8) {
+    if constexpr (sizeof(T) == 2) {
+      const half8 v = *reinterpret_cast<const half8 *>(x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) to[i] = (float)v[i];
+    } else {
+      const floatx4 u = reinterpret_cast<const floatx4 *>(x)[0], v = reinterpret_cast<const floatx4 *>(x)[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[i] = u[i], to[4 + i] = v[i];
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) to[i] = i < n ? (float)x[i] : -INFINITY;
 }
-__device__ __forceinline__ Seen of_workgroup(Seen x, const float by, Seen *waves) {
+__device__ __forceinline__ void store8(float *y, const int n, const float (&x)[8]) {
+  if (n >= 8) {
+    reinterpret_cast<floatx4 *>(y)[0] = floatx4{x[0], x[1], x[2], x[3]};
+    reinterpret_cast<floatx4 *>(y)[1] = floatx4{x[4], x[5], x[6], x[7]};
+    return;
+  }
 #pragma unroll
-  for (int o = 32; o; o >>= 1) x = joined(x, Seen{__shfl_xor(x.top, o), __shfl_xor(x.sum, o), __shfl_xor(x.at, o)}, by);
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = x;
+  for (int i = 0; i < 8; ++i)
+    if (i < n) y[i] = x[i];
+}
+
+// THREADS threads' numbers of a piece of a row, eight from 8 (i THREADS + thread) on each: their largest, first place (at temperature 0), exponentials in their stead, and the sum
+template <int THREADS>
+__device__ __forceinline__ Seen seen_by_all(float (&x)[kEach / 8][8], const float t, const float by, float *shared) {
+  constexpr int kWaves = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Seen s{-INFINITY, 0.f, 0x7fffffff, 0};
+#pragma unroll
+  for (int i = 0; i < kEach / 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s.top = fmaxf(s.top, x[i][j]);
+  s.top = wave_max(s.top);
+  if (lane == 0) shared[wave] = s.top;
   __syncthreads();
-  x = waves[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) x = joined(x, waves[w], by);
-  return x;
+  for (int w = 0; w < kWaves; ++w) s.top = fmaxf(s.top, shared[w]);
+  __syncthreads();
+  if (t == 0.f) {
+#pragma unroll
+    for (int i = kEach / 8 - 1; i >= 0; --i)
+#pragma unroll
+      for (int j = 7; j >= 0; --j)
+        if (x[i][j] == s.top) s.at = 8 * (i * THREADS + (int)threadIdx.x) + j;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s.at = min(s.at, __shfl_xor(s.at, o));
+    if (lane == 0) shared[wave] = __builtin_bit_cast(float, s.at);
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s.at = min(s.at, __builtin_bit_cast(int, shared[w]));
+    if (s.top == -INFINITY) s.at = 0x7fffffff;           // (nothing is the largest)
+    return s;
+  }
+  const float less = s.top == -INFINITY ? 0.f : s.top;
+#pragma unroll
+  for (int i = 0; i < kEach / 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s.sum += x[i][j] = __builtin_amdgcn_exp2f((x[i][j] - less) * by);
+  s.sum = wave_sum(s.sum);
+  if (lane == 0) shared[wave] = s.sum;
+  __syncthreads();
+  s.sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) s.sum += shared[w];
+  return s;
+}
+// (x - top) / t in units of log 2.  A temperature below 1e-30 is as good as that: the largest take all
+__device__ __forceinline__ float per_temperature(const float t) { return t >= 0.f ? kLog2e / fmaxf(t, 1e-30f) : NAN; }
+
+template <class T>
+__global__ void __launch_bounds__(kRowThreads) row_probs_kernel(const T *logits, const int64_t stride, const float *temperature, float *out, const int64_t out_stride, const int vocab) {
+  __shared__ float shared[kRowThreads / 64];
+  const T *x = logits + blockIdx.x * stride;
+  float *y = out + blockIdx.x * out_stride;
+  float v[kEach / 8][8];
+#pragma unroll
+  for (int i = 0; i < kEach / 8; ++i) {
+    const int at = 8 * (i * kRowThreads + (int)threadIdx.x);
+    load8(x + at, vocab - at, v[i]);
+  }
+  const float t = temperature ? temperature[blockIdx.x] : 1.f;
+  const Seen s = seen_by_all<kRowThreads>(v, t, per_temperature(t), shared);
+  const float over = s.sum == 0.f ? 0.f : 1.f / s.sum;
+#pragma unroll
+  for (int i = 0; i < kEach / 8; ++i) {
+    const int at = 8 * (i * kRowThreads + (int)threadIdx.x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = t == 0.f ? (at + j == s.at ? 1.f : 0.f) : v[i][j] * over;
+    store8(y + at, vocab - at, v[i]);
+  }
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) probs_kernel(const T *logits, const int64_t stride, const float *temperature, float *out, const int64_t out_stride,
-                                                         const int vocab) {
-  __shared__ Seen waves[kWaves];
-  const T *x = logits + blockIdx.x * stride;
-  float *y = out + blockIdx.x * out_stride;
-  const float t = temperature ? temperature[blockIdx.x] : 1.f;
-  // (x - top) / t in units of log 2.  A temperature below 1e-30 is as good as none: the largest take all
-  const float by = t >= 0.f ? kLog2e / fmaxf(t, 1e-30f) : NAN;
-  Seen s{-INFINITY, 0.f, 0x7fffffff};
-  for (int i = threadIdx.x; i < vocab; i += kThreads) {
-    const float v = (float)x[i];
-    if (v > s.top) s = Seen{v, s.top == -INFINITY ? s.sum + 1.f : s.sum * __builtin_amdgcn_exp2f((s.top - v) * by) + 1.f, i};
-    else if (v != -INFINITY) s.sum += __builtin_amdgcn_exp2f((v - s.top) * by);
+__global__ void __launch_bounds__(kPieceThreads) piece_seen_kernel(const T *logits, const int64_t stride, const float *temperature, const int vocab, Seen *seen) {
+  __shared__ float shared[kPieceThreads / 64];
+  const int first = blockIdx.x * kPieceLogits, row = blockIdx.y;
+  const T *x = logits + row * stride;
+  float v[kEach / 8][8];
+#pragma unroll
+  for (int i = 0; i < kEach / 8; ++i) {
+    const int at = first + 8 * (i * kPieceThreads + (int)threadIdx.x);
+    load8(x + at, vocab - at, v[i]);
   }
-  s = of_workgroup(s, by, waves);
-  if (t == 0.f) {
-    for (int i = threadIdx.x; i < vocab; i += kThreads) y[i] = i == s.at ? 1.f : 0.f;
-    return;
+  const float t = temperature ? temperature[row] : 1.f;
+  Seen s = seen_by_all<kPieceThreads>(v, t, per_temperature(t), shared);
+  if (s.at != 0x7fffffff) s.at += first;
+  if (threadIdx.x == 0) seen[(int64_t)row * gridDim.x + blockIdx.x] = s;
+}
+template <class T>
+__global__ void __launch_bounds__(kPieceThreads) piece_probs_kernel(const T *logits, const int64_t stride, const float *temperature, float *out, const int64_t out_stride, const int vocab,
+                                                                    const Seen *seen) {
+  const int first = blockIdx.x * kPieceLogits, row = blockIdx.y, lane = threadIdx.x & 63, pieces = gridDim.x;
+  const T *x = logits + row * stride;
+  float *y = out + row * out_stride;
+  float v[kEach / 8][8];
+#pragma unroll
+  for (int i = 0; i < kEach / 8; ++i) {
+    const int at = first + 8 * (i * kPieceThreads + (int)threadIdx.x);
+    load8(x + at, vocab - at, v[i]);
   }
-  const float over = s.sum == 0.f ? 0.f : 1.f / s.sum;
-  for (int i = threadIdx.x; i < vocab; i += kThreads) {
-    const float v = (float)x[i];
-    y[i] = v == -INFINITY && s.sum == s.sum ? 0.f : __builtin_amdgcn_exp2f((v - s.top) * by) * over;
+  const float t = temperature ? temperature[row] : 1.f, by = per_temperature(t);
+  float top = -INFINITY, sum = 0.f;
+  int at_top = 0x7fffffff;
+  for (int i = lane; i < pieces; i += 64) top = fmaxf(top, seen[(int64_t)row * pieces + i].top);
+  top = wave_max(top);
+  const float less = top == -INFINITY ? 0.f : top;
+  for (int i = lane; i < pieces; i += 64) {
+    const Seen s = seen[(int64_t)row * pieces + i];
+    if (s.top == top) at_top = min(at_top, s.at);
+    sum += s.top == -INFINITY ? s.sum : s.sum * __builtin_amdgcn_exp2f((s.top - less) * by);
+  }
+  sum = wave_sum(sum);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) at_top = min(at_top, __shfl_xor(at_top, o));
+  const float over = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int i = 0; i < kEach / 8; ++i) {
+    const int at = first + 8 * (i * kPieceThreads + (int)threadIdx.x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = t == 0.f ? (at + j == at_top ? 1.f : 0.f) : __builtin_amdgcn_exp2f((v[i][j] - less) * by) * over;
+    store8(y + at, vocab - at, v[i]);
   }
 }
 
@@ -82,18 +198,20 @@ struct Verify {
   int32_t batch, n_rows, vocab;
 };
 
-__device__ __forceinline__ bool counts(const double w) { return w > 0. && w < INFINITY; }
-
-// A sequence's rows, how many of its drafts are accepted, and where its next token is drawn from: what a wavefront finds out
+// A sequence's rows, and how many of its drafts are accepted: by a wavefront
 struct Turn {
   int first, n, accepted;
 };
-__device__ __forceinline__ Turn turn_of(const Verify &a, const int b) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ Turn rows_of(const Verify &a, const int b) {
   Turn t;
   t.first = min(max(a.starts[b], 0), a.n_rows);
   t.n = min(max(a.starts[b + 1], t.first), a.n_rows) - t.first;
   t.accepted = t.n;
+  return t;
+}
+__device__ __forceinline__ Turn turn_of(const Verify &a, const int b) {
+  const int lane = threadIdx.x & 63;
+  Turn t = rows_of(a, b);
   for (int i0 = 0; i0 < t.n; i0 += 64) {
     const int i = i0 + lane;
     bool bad = false;
@@ -115,32 +233,114 @@ __device__ __forceinline__ Turn turn_of(const Verify &a, const int b) {
   return t;
 }
 
-// The weights of the row that the next token is drawn from
+// Weights of the row that the next token is drawn from, kPart tokens at a time: a wavefront has kPart / 64 = 32 consecutive ones in each lane
+constexpr int kPart = 2048, kOfLane = kPart / 64;
 struct Weights {
-  const float *p, *q;                    // q NULL: nothing is taken off, but the whole of `without`
-  int without;
-  __device__ __forceinline__ Weights(const Verify &a, const int b, const Turn &t) {
+  float p[kOfLane], q[kOfLane];
+  int without;                           // place in the lane of the token that a certain draft takes off, -1: none
+  __device__ __forceinline__ Weights(const Verify &a, const int b, const Turn &t, const int part) {
     const int64_t at = t.first + t.accepted;
-    p = a.target + (at + b) * a.target_stride;
-    q = t.accepted < t.n && a.draft ? a.draft + at * a.draft_stride : nullptr;
-    without = t.accepted < t.n && !a.draft ? a.drafts[at] : -1;
+    const int i0 = part * kPart + (threadIdx.x & 63) * kOfLane, n = a.vocab - i0;
+    const bool rejected = t.accepted < t.n;
+    read(p, a.target + (at + b) * a.target_stride + i0, n);
+    if (rejected && a.draft) read(q, a.draft + at * a.draft_stride + i0, n);
+    else
+#pragma unroll
+      for (int i = 0; i < kOfLane; ++i) q[i] = 0.f;
+    without = rejected && !a.draft ? a.drafts[at] - i0 : -1;
   }
-  __device__ __forceinline__ double rest(const int i) const {
-    const double w = i == without ? 0. : q ? (double)p[i] - (double)q[i] : (double)p[i];
-    return counts(w) ? w : 0.;
+  __device__ __forceinline__ static void read(float (&to)[kOfLane], const float *from, const int n) {
+    if (n >= kOfLane) {
+#pragma unroll
+      for (int i = 0; i < kOfLane / 4; ++i) {
+        const floatx4 v = reinterpret_cast<const floatx4 *>(from)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[4 * i + j] = v[j];
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kOfLane; ++i) to[i] = i < n ? from[i] : 0.f;
   }
-  __device__ __forceinline__ double all(const int i) const { return counts(p[i]) ? (double)p[i] : 0.; }
+  __device__ __forceinline__ static double counted(const double w) { return w > 0. && w < INFINITY ? w : 0.; }
+  __device__ __forceinline__ double one(const int i, const bool all) const { return counted(all ? p[i] : i == without ? 0. : (double)p[i] - (double)q[i]); }
 };
-
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-
-// Tokens kPart at a time: sums over these in 64 bits, then the part in which u times the sum lies, then the token
-constexpr int kPart = 2048;
-
+// A part's sum over rest(), or over all()
+__device__ __forceinline__ double sum_of(const Weights &w, const bool all) {
+  double sum = 0.;
+#pragma unroll
+  for (int i = 0; i < kOfLane; ++i) sum += w.one(i, all);
+  return wave_sum64(sum);
+}
+// The first lane whose `mine` and those before it come to more than x less `before`, and the sum before it; should rounding leave none, the last that is not 0 (-1: all are)
+__device__ __forceinline__ int lane_of(const double mine, const double x, double &before) {
+  const int lane = threadIdx.x & 63;
+  double upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double other = __shfl_up(upto, o);
+    if (lane >= o) upto += other;
+  }
+  const uint64_t above = __ballot(mine > 0. && before + upto > x), some = __ballot(mine > 0.);
+  const int at = above ? __ffsll((unsigned long long)above) - 1 : 63 - __clzll((long long)some);
+  if (above) before += __shfl(upto - mine, at);
+  else before += __shfl(upto, 63);
+  return above ? at : some ? at | 64 : -1;             // (| 64: of those so far)
+}
+// Where u lies among the parts' sums, by a wavefront: the part (-1: all sums are 0), the sum before it (below 0: rounding has left none, it is the last part with a weight and its last token),
+// and u times the sum of them
+struct Place {
+  int part;
+  double before, x;
+};
+__device__ __forceinline__ Place place_of(const double *sums, const int parts, const float u) {
+  const int lane = threadIdx.x & 63;
+  double total = 0.;
+  for (int i = lane; i < parts; i += 64) total += sums[i];
+  Place p{-1, 0., (double)u * wave_sum64(total)};
+  for (int i0 = 0; i0 < parts; i0 += 64) {
+    const int at = lane_of(i0 + lane < parts ? sums[i0 + lane] : 0., p.x, p.before);
+    if (at < 0) continue;
+    p.part = i0 + (at & 63);
+    if (at < 64) return p;
+  }
+  p.before = -1.;
+  return p;
+}
+// The token in its part, by a wavefront that has the part's weights
+__device__ __forceinline__ int token_in(const Weights &w, const Place &p, const bool all) {
+  double mine = 0.;
+#pragma unroll
+  for (int i = 0; i < kOfLane; ++i) mine += w.one(i, all);
+  const bool last = p.before < 0.;
+  double before = last ? 0. : p.before;
+  const double x = last ? INFINITY : p.x;
+  const int at = lane_of(mine, x, before);
+  // (lane `at` goes through its weights)
+  int token = 0;
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < kOfLane; ++i) {
+    const double v = w.one(i, all);
+    before += v;
+    if (v > 0. && !found) token = i, found = at < 64 && before > x;
+  }
+  return p.part * kPart + (at & 63) * kOfLane + __shfl(token, at & 63);
+}
+// The token that u draws, by a wavefront: rest and all are the parts' sums
+__device__ __forceinline__ int next_token(const Verify &a, const int b, const Turn &t, const double *rest, const double *all, const int parts, const float u) {
+  Place p = place_of(rest, parts, u);
+  const bool fallback = p.part < 0;
+  if (fallback) p = place_of(all, parts, u);
+  if (p.part < 0) return -1;
+  const Weights w(a, b, t, p.part);
+  return token_in(w, p, fallback);
+}
 __device__ __forceinline__ void write_tokens(const Verify &a, const int b, const Turn &t, const int token) {
   const int lane = threadIdx.x & 63;
   for (int i = lane; i <= t.n; i += 64) a.tokens[t.first + b + i] = i < t.accepted ? a.drafts[t.first + i] : i == t.accepted ? token : -1;
@@ -150,69 +350,42 @@ __device__ __forceinline__ void write_tokens(const Verify &a, const int b, const
   }
 }
 
-// The token, by one wavefront: sums[part] are over rest(), sums[parts + part] over all()
-__device__ __forceinline__ int token_of(const Verify &a, const Weights &w, const double *sums, const int parts, const float u) {
-  const int lane = threadIdx.x & 63;
-  double total = 0.;
-  for (int i = lane; i < parts; i += 64) total += sums[i];
-  total = wave_sum64(total);
-  const bool fallback = !(total > 0.);
-  if (fallback) {
-    total = 0.;
-    sums += parts;
-    for (int i = lane; i < parts; i += 64) total += sums[i];
-    total = wave_sum64(total);
-    if (!(total > 0.)) return -1;
+// A workgroup per sequence, a wavefront per part: few tokens, in one launch
+constexpr int kOneWaves = 16;
+__global__ void __launch_bounds__(64 * kOneWaves) verify_kernel(Verify a) {
+  __shared__ double sums[2][kOneWaves];
+  const int b = blockIdx.x, wave = threadIdx.x >> 6, parts = (a.vocab + kPart - 1) / kPart;
+  const Turn t = turn_of(a, b);
+  const float u = a.uniforms[t.first + b + t.n];
+  if (wave < parts) {
+    const Weights w(a, b, t, wave);
+    const double rest = sum_of(w, false), all = sum_of(w, true);
+    if ((threadIdx.x & 63) == 0) sums[0][wave] = rest, sums[1][wave] = all;
   }
-  const double x = (double)u * total;
-  // the first place whose sum up to it is above x; should rounding leave none, the last whose weight is not 0
-  auto find = [&](const int n, const auto &weight, double &before) {
-    int last = -1;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-      const double v = i0 + lane < n ? weight(i0 + lane) : 0.;
-      double upto = v;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double other = __shfl_up(upto, o);
-        if (lane >= o) upto += other;
-      }
-      const uint64_t there = __ballot(v > 0.), above = __ballot(v > 0. && before + upto > x);
-      if (above) {
-        const int at = __ffsll((unsigned long long)above) - 1;
-        before += __shfl(upto - v, at);
-        return i0 + at;
-      }
-      if (there) last = i0 + 63 - __clzll((long long)there);
-      before += __shfl(upto, 63);
-    }
-    return last;
-  };
-  double before = 0.;
-  const int part = find(parts, [&](int i) { return sums[i]; }, before);
-  if (part < 0) return -1;
-  const int i0 = part * kPart, n = min(kPart, a.vocab - i0);
-  if (before > x) before = x;
-  return i0 + find(n, [&](int i) { return fallback ? w.all(i0 + i) : w.rest(i0 + i); }, before);
+  __syncthreads();
+  if (wave == 0) write_tokens(a, b, t, next_token(a, b, t, sums[0], sums[1], parts, u));
 }
 
-// A workgroup per sequence
-__global__ void __launch_bounds__(kThreads) verify_kernel(Verify a, double *sums) {
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int parts = (a.vocab + kPart - 1) / kPart;
-  double *mine = sums + (int64_t)b * 2 * parts;
+// Many tokens: a wavefront per part of every sequence, then one per sequence.  sums [batch][2][parts]
+constexpr int kPartWaves = 4;
+__global__ void __launch_bounds__(64 * kPartWaves) parts_kernel(Verify a, double *sums) {
+  const int b = blockIdx.y, part = blockIdx.x * kPartWaves + (threadIdx.x >> 6), parts = (a.vocab + kPart - 1) / kPart;
+  if (part >= parts) return;
   const Turn t = turn_of(a, b);
-  const Weights w(a, b, t);
-  for (int part = wave; part < parts; part += kWaves) {
-    double rest = 0., all = 0.;
-#pragma unroll 4
-    for (int i = part * kPart + lane; i < min((part + 1) * kPart, a.vocab); i += 64) rest += w.rest(i), all += w.all(i);
-    rest = wave_sum64(rest), all = wave_sum64(all);
-    if (lane == 0) mine[part] = rest, mine[parts + part] = all;
+  const Weights w(a, b, t, part);
+  const double rest = sum_of(w, false), all = sum_of(w, true);
+  if ((threadIdx.x & 63) == 0) {
+    sums[((int64_t)b * 2) * parts + part] = rest, sums[((int64_t)b * 2 + 1) * parts + part] = all;
+    if (part == 0) a.accepted[b] = t.accepted;
   }
-  __threadfence_block();
-  __syncthreads();
-  if (wave) return;
-  write_tokens(a, b, t, token_of(a, w, mine, parts, a.uniforms[t.first + b + t.n]));
+}
+__global__ void __launch_bounds__(64) token_kernel(Verify a, const double *sums) {
+  const int b = blockIdx.x, parts = (a.vocab + kPart - 1) / kPart;
+  Turn t = rows_of(a, b);
+  t.accepted = min(max(a.accepted[b], 0), t.n);
+  const float u = a.uniforms[t.first + b + t.n];
+  sums += (int64_t)b * 2 * parts;
+  write_tokens(a, b, t, next_token(a, b, t, sums, sums + parts, parts, u));
 }
 
 bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -232,7 +405,7 @@ extern "C" {
 int64_t okv_token_probs_workspace_bytes(int32_t max_rows, int32_t vocab) {
   if (max_rows < 0 || max_rows > OKV_SAMPLE_MAX_ROWS || vocab < 1 || vocab > OKV_SAMPLE_MAX_VOCAB)
     return report(OKV_EINVAL, "okv_token_probs_workspace_bytes: rows must be in [0, 2^20] and vocab in [1, 2^24]");
-  return 0;
+  return vocab <= kOneLaunch ? 0 : (int64_t)max_rows * ((vocab + kPieceLogits - 1) / kPieceLogits) * (int64_t)sizeof(Seen);
 }
 
 int okv_token_probs(const void *logits, int32_t dtype, int64_t stride, const float *temperature, float *out, int64_t out_stride, int32_t rows, int32_t vocab,
@@ -245,18 +418,31 @@ int okv_token_probs(const void *logits, int32_t dtype, int64_t stride, const flo
   if (rows == 0) return OKV_OK;
   if (!logits || !out || !aligned(logits, dtype ? 4 : 2) || !aligned(out, 4) || !aligned(temperature, 4)) return report(OKV_EINVAL, "%s: NULL or misaligned pointer", who);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return report(OKV_ENOSPC, "%s: the workspace must be %lld bytes, 16-byte aligned", who, (long long)need);
-  const dim3 grid((unsigned)rows), block(kThreads);
-  if (dtype == 0)
-    hipLaunchKernelGGL(probs_kernel<_Float16>, grid, block, 0, static_cast<hipStream_t>(stream), static_cast<const _Float16 *>(logits), stride, temperature, out, out_stride, vocab);
-  else
-    hipLaunchKernelGGL(probs_kernel<float>, grid, block, 0, static_cast<hipStream_t>(stream), static_cast<const float *>(logits), stride, temperature, out, out_stride, vocab);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto run = [&](auto *x) {
+    if (vocab <= kOneLaunch) {
+      hipLaunchKernelGGL(row_probs_kernel, dim3((unsigned)rows), dim3(kRowThreads), 0, s, x, stride, temperature, out, out_stride, vocab);
+      return;
+    }
+    Seen *const seen = static_cast<Seen *>(workspace);
+    const int32_t pieces = (vocab + kPieceLogits - 1) / kPieceLogits;
+    for (int32_t first = 0; first < rows; first += 32768) {      // (rows of a grid's second dimension)
+      const dim3 grid((unsigned)pieces, (unsigned)std::min(rows - first, 32768));
+      const float *const t = temperature ? temperature + first : nullptr;
+      Seen *const at = seen + (int64_t)first * pieces;
+      hipLaunchKernelGGL(piece_seen_kernel, grid, dim3(kPieceThreads), 0, s, x + first * stride, stride, t, vocab, at);
+      hipLaunchKernelGGL(piece_probs_kernel, grid, dim3(kPieceThreads), 0, s, x + first * stride, stride, t, out + first * out_stride, out_stride, vocab, static_cast<const Seen *>(at));
+    }
+  };
+  if (dtype == 0) run(static_cast<const _Float16 *>(logits));
+  else run(static_cast<const float *>(logits));
   return hip_result(who);
 }
 
 int64_t okv_verify_workspace_bytes(int32_t max_batch, int32_t vocab) {
   if (max_batch < 0 || max_batch > OKV_VERIFY_MAX_BATCH || vocab < 1 || vocab > OKV_SAMPLE_MAX_VOCAB)
     return report(OKV_EINVAL, "okv_verify_workspace_bytes: batch must be in [0, 4096] and vocab in [1, 2^24]");
-  return (int64_t)max_batch * 2 * ((vocab + kPart - 1) / kPart) * 8;
+  return (int64_t)max_batch * ((vocab + kPart - 1) / kPart) * 2 * 8;
 }
 
 int okv_verify(const float *target, int64_t target_stride, const float *draft_probs, int64_t draft_stride, const int32_t *drafts, const int32_t *starts,
@@ -274,7 +460,14 @@ int okv_verify(const float *target, int64_t target_stride, const float *draft_pr
     if (!aligned(p, 4)) return report(OKV_EINVAL, "%s: misaligned pointer", who);
   if (!workspace || workspace_bytes < need || !aligned(workspace, 16)) return report(OKV_ENOSPC, "%s: the workspace must be %lld bytes, 16-byte aligned", who, (long long)need);
   Verify a{target, draft_probs, target_stride, draft_stride, drafts, starts, uniforms, tokens, accepted, rejected, batch, n_rows, vocab};
-  hipLaunchKernelGGL(verify_kernel, dim3((unsigned)batch), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a, static_cast<double *>(workspace));
+  const int32_t parts = (vocab + kPart - 1) / kPart;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (parts <= kOneWaves) {
+    hipLaunchKernelGGL(verify_kernel, dim3((unsigned)batch), dim3(64 * kOneWaves), 0, s, a);
+  } else {
+    hipLaunchKernelGGL(parts_kernel, dim3((unsigned)((parts + kPartWaves - 1) / kPartWaves), (unsigned)batch), dim3(64 * kPartWaves), 0, s, a, static_cast<double *>(workspace));
+    hipLaunchKernelGGL(token_kernel, dim3((unsigned)batch), dim3(64), 0, s, a, static_cast<const double *>(workspace));
+  }
   return hip_result(who);
 }
 
