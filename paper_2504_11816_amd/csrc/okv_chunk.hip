@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(kAppendWaves * 64) append_kernel(Pool c, Rows 
 
 // ---- attention ------------------------------------------------------------------------------------
 
+struct Plan;
 struct Attend {
   const _Float16 *q;
   void *out;
@@ -160,6 +161,7 @@ struct Attend {
   int32_t may_cut;                       // whether keys may be cut among workgroups (a second launch joins them)
   const float *slopes;
   const int32_t *prefix;
+  Plan *plan;                            // in the workspace
   float *parts;                          // results of pieces of rows' keys: kRows x D sums, and behind them kRows maxima and kRows sums of weights
 };
 
@@ -177,9 +179,11 @@ struct Form {
   static constexpr int kBlockBytes = kKeys * D * 2, kLoads = kBlockBytes / 1024 / (FEW ? 1 : kWaves);                   // loads of a wavefront per block of keys (or values)
   static constexpr int kLds = (FEW ? kWaves : 1) * 2 * kRing * kBlockBytes;
   static constexpr int kPartFloats = kRows * (D + 2);
-  // How keys are cut (see with_plan): workgroups that run at a time, pieces at most, and in steps what a piece costs beside its own and what joining does
-  static constexpr int kSlots = FEW && D == 128 ? 256 : 512, kPieces = FEW ? 2048 : 1024, kUncut = 512 / kStep;
+  // How keys are cut (see Plan): workgroups that run at a time, and in steps what a piece costs beside its own, what joining does, and what is never cut
+  static constexpr int kSlots = FEW && D == 128 ? 256 : 512, kUncut = 512 / kStep;
   static constexpr float kPerPiece = FEW ? 1.f : 4.f, kPerJoin = FEW ? 3.f : 10.f;
+  static constexpr int kPieces = 1024;                  // that steps come to at most, where tiles are cut into equal pieces
+  static constexpr int kParts = 2 * (FEW ? kSlots : kPieces);                  // results of pieces
 };
 
 __device__ __forceinline__ half8 transposed(const char *first, const char *second) {
@@ -230,18 +234,26 @@ __device__ __forceinline__ Keys keys_of(const int n, const int len, const int pr
   return k;
 }
 
-// What a workgroup does.  The rows of every sequence and KV head are cut into tiles, and where these are too few to fill the chip the keys of each tile of a sequence
-// into as many cuts: all of them by the same rule, from lengths that are on the device, by every workgroup for itself.
-struct Piece {
-  int first, n, len, s, prefix;          // the sequence: its first row, its rows, its tokens, its row of the table (below 0: there is none)
-  int tile, g, cut, cuts, slot, apart;   // slot: of the piece's results among those that are cut; from a cut of the tile to the next
-  bool there;
-};
+// What workgroups do.  The rows of every sequence and KV head are cut into tiles (`tiles` of a sequence, each for G heads: its items), whose keys are walked in steps.  Where workgroups that take an item
+// each would leave much of the chip idle, keys are cut among them, and a second launch joins the results.
+//   many rows   every tile of a sequence is cut into as many pieces (`cuts`), of `span` steps at most
+//   few rows    all items' steps, one item after the other, are shared out in stretches of `span`: a workgroup takes a stretch, which ends some items, holds some and begins one
+// Lengths are on the device: every wavefront finds this out for itself, a lane per sequence; beyond 64 sequences a launch of one workgroup adds up chunks of 64 first.
+constexpr int kNone = 0x3fffffff;
 struct Sequence {
-  int first, n, s, len, prefix, tiles, steps;
+  int first, n, s, len, prefix;          // its first row, its rows, its row of the table (below 0: there is none), its tokens, those of its prefix
+  int tiles, steps;                      // steps: of its last tile, which sees the most keys; others' are taken to be as many
 };
+struct Plan {                            // in the workspace, for more than 64 sequences; before each chunk of 64, and behind the last
+  int span, unused;
+  int pieces[OKV_CHUNK_MAX_BATCH / 64 + 1], cut_pieces[OKV_CHUNK_MAX_BATCH / 64 + 1], cut_tiles[OKV_CHUNK_MAX_BATCH / 64 + 1];
+  unsigned long long steps[OKV_CHUNK_MAX_BATCH / 64 + 1];
+};
+constexpr int64_t kPlanBytes = 2048;
+static_assert(sizeof(Plan) <= kPlanBytes, "");
+
 template <class F>
-__device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, const int32_t *prefix, const int window, const int b) {
+__device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, const Attend &a, const int b) {
   Sequence q{0, 0, -1, 0, 0, 0, 0};
   if (b >= r.batch) return q;
   int last;
@@ -251,107 +263,192 @@ __device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, co
   if (s >= 0 && s < c.max_seqs) {
     q.s = s;
     q.len = min(max(r.lens[s], 0), c.capacity);
-    if (prefix) q.prefix = min(max(prefix[s], 0), q.len);
+    if (a.prefix) q.prefix = min(max(a.prefix[s], 0), q.len);
   }
   q.tiles = (int)(((int64_t)q.n * c.R + F::kRows - 1) / F::kRows);
-  if (q.tiles) q.steps = keys_of<F>(q.n, q.len, q.prefix, window, c.R, q.tiles - 1).total;
+  if (q.tiles) q.steps = max(keys_of<F>(q.n, q.len, q.prefix, a.window, c.R, q.tiles - 1).total, 1);      // (an item without keys is a step, too: its rows are 0)
   return q;
 }
-__device__ __forceinline__ int wave_scan(int x) {         // inclusive
+template <class T>
+__device__ __forceinline__ T wave_scan(T x) {             // inclusive
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int other = __shfl_up(x, o);
+    const T other = __shfl_up(x, o);
     if (lane >= o) x += other;
   }
   return x;
 }
-__device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { return max((int)(((unsigned)q.steps + (unsigned)span - 1) / (unsigned)span), 1); }
+__device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { return (int)(((unsigned)q.steps + (unsigned)span - 1) / (unsigned)span); }
 
-// The longest piece, in steps: what is expected to take the least time.  With P pieces of up to s steps (W in all) on kSlots workgroups at a time that is s + kPerPiece where
-// P <= kSlots, else (W + P kPerPiece) / kSlots and half a piece until the last one has ended; kPerJoin is added where any are cut.
-template <class F>
-__device__ __forceinline__ int span_of(const Pool &c, const Rows &r, const Attend &a, const Sequence &mine) {
-  const int lane = threadIdx.x & 63;
-  constexpr int kNone = 0x3fffffff;
+// The span that is expected to take the least time, kNone: nothing is cut.  P pieces of up to s steps (W in all) on kSlots workgroups at a time take s + kPerPiece where P <= kSlots, else
+// (W + P kPerPiece) / kSlots and half a piece until the last one has ended; kPerJoin is added where any are cut.  sum(f) and most(f): over all sequences.
+template <class F, bool FEW, class Sum, class Most>
+__device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum &sum, const Most &most) {
   if (!a.may_cut) return kNone;
-  float work = (float)mine.tiles * mine.steps, tiles = (float)mine.tiles, most = (float)mine.steps;
-  for (int b0 = 64; b0 < r.batch; b0 += 64) {
-    const Sequence q = sequence_at<F>(c, r, a.prefix, a.window, b0 + lane);
-    work += (float)q.tiles * q.steps, tiles += (float)q.tiles, most = fmaxf(most, (float)q.steps);
-  }
-  work = wave_sum(work) * c.G, tiles = wave_sum(tiles) * c.G, most = wave_max(most);
-  auto time = [&](const float pieces, const float longest) {
-    return pieces <= F::kSlots ? longest + F::kPerPiece : (work + pieces * F::kPerPiece) * (1.f / F::kSlots) + .5f * (longest + F::kPerPiece);
+  const float work = sum([](const Sequence &q) { return (float)q.tiles * (float)q.steps; }) * c.G, items = sum([](const Sequence &q) { return (float)q.tiles; }) * c.G;
+  const float longest = most([](const Sequence &q) { return (float)q.steps; });
+  auto time = [&](const float pieces, const float s) {
+    return pieces <= F::kSlots ? s + F::kPerPiece : (work + pieces * F::kPerPiece) * (1.f / F::kSlots) + .5f * (s + F::kPerPiece);
   };
-  float best = time(tiles, most);
+  float best = time(items, longest);
   int span = kNone;
-  const int least = max(1, (int)fminf(ceilf(work * (1.0001f / F::kPieces)), 1e9f));
-  if (best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return span;
-  for (int i = 0; i < 12; ++i) {
-    const float of_most = i < 8 ? most / (float)(i + 2) : work * (i == 8 ? .5f : i == 9 ? 1.f / 1.5f : i == 10 ? 1.f / 3.f : 1.f) * (1.f / F::kSlots);
-    const int s = uniform(max(least, (int)ceilf(of_most)));
-    float pieces = (float)mine.tiles * (float)cuts_of(mine, s);
-    for (int b0 = 64; b0 < r.batch; b0 += 64) {
-      const Sequence q = sequence_at<F>(c, r, a.prefix, a.window, b0 + lane);
-      pieces += (float)q.tiles * (float)cuts_of(q, s);
+  if constexpr (FEW) {
+    const float even = ceilf(work * (1.0001f / F::kSlots));
+    if (longest > F::kUncut && even + (items * (1.f / F::kSlots) + 1.f) * F::kPerPiece + F::kPerJoin < best) span = (int)fminf(even, 1e9f);
+  } else {
+    const int least = max(1, (int)fminf(ceilf(work * (1.0001f / F::kPieces)), 1e9f));
+    if (best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return span;
+    for (int i = 0; i < 12; ++i) {
+      const float of_all = i == 8 ? .5f : i == 9 ? 1.f / 1.5f : i == 10 ? 1.f / 3.f : 1.f;
+      const int s = uniform(max(least, (int)ceilf(i < 8 ? longest / (float)(i + 2) : work * (of_all / F::kSlots))));
+      const float pieces = sum([&](const Sequence &q) { return (float)q.tiles * (float)cuts_of(q, s); }) * c.G;
+      const float t = time(pieces, fminf(longest, (float)s)) + F::kPerJoin;
+      if (t < best) best = t, span = s;
     }
-    const float t = time(wave_sum(pieces) * c.G, fminf(most, (float)s)) + F::kPerJoin;
-    if (t < best) best = t, span = s;
   }
   return uniform(span);
 }
-// take(sequences of 64 lanes, their cuts, pieces and cut pieces up to and with each, those before all of them) until it returns true
-template <class F, class Take>
-__device__ __forceinline__ void with_plan(const Pool &c, const Rows &r, const Attend &a, const Take &take) {
-  const int lane = threadIdx.x & 63;
-  Sequence q = sequence_at<F>(c, r, a.prefix, a.window, lane);
-  const int span = span_of<F>(c, r, a, q);
-  int pieces = 0, cut_pieces = 0;
-  for (int b0 = 0; b0 < r.batch; b0 += 64) {
-    if (b0) q = sequence_at<F>(c, r, a.prefix, a.window, b0 + lane);
-    const int cuts = cuts_of(q, span), mine = q.tiles * c.G * cuts;
-    const int upto = wave_scan(mine), cut_upto = wave_scan(cuts > 1 ? mine : 0);
-    if (take(q, cuts, upto, cut_upto, pieces, cut_pieces)) return;
-    pieces += uniform(__shfl(upto, 63)), cut_pieces += uniform(__shfl(cut_upto, 63));
+
+// The chunk of 64 sequences with the index-th of what `before` counts, a lane a sequence
+template <class F, bool FEW>
+struct Chunk {
+  Sequence q;                            // this lane's
+  int b0, span, at;                      // the chunk's first sequence; its number
+  const Plan *plan;                      // NULL: the only chunk
+  __device__ __forceinline__ Chunk(const Pool &c, const Rows &r, const Attend &a) : b0(0), at(0), plan(nullptr) {
+    if (r.batch > 64) {
+      plan = a.plan;
+      span = uniform(plan->span);
+      return;
+    }
+    q = sequence_at<F>(c, r, a, threadIdx.x & 63);
+    span = span_of<F, FEW>(c, a, [&](const auto &f) { return wave_sum(f(q)); }, [&](const auto &f) { return wave_max(f(q)); });
   }
-}
-template <class F>
-__device__ __forceinline__ Piece piece_of(const Pool &c, const Rows &r, const Attend &a, const int index) {
-  Piece p;
-  p.there = false;
-  with_plan<F>(c, r, a, [&](const Sequence &q, const int cuts, const int upto, const int cut_upto, const int before, const int cut_before) {
-    const uint64_t ended = __ballot(before + upto <= index);
-    if (ended == ~0ull) return false;
-    const int at = __popcll(ended);
-    auto of = [&](const int x) { return __builtin_amdgcn_readlane(x, at); };
-    p.there = true;
-    p.first = of(q.first), p.n = of(q.n), p.s = of(q.s), p.len = of(q.len), p.prefix = of(q.prefix), p.cuts = of(cuts);
-    const int tiles = of(q.tiles), within = index - before - (of(upto) - tiles * c.G * p.cuts);
-    // The heads of a tile next to each other, so that those of a head are on the same XCD where they are a multiple of eight; then the tiles, which read the same
-    // keys; those that see the most keys first
-    const int rank = uniform(within / c.G);
-    p.g = within - rank * c.G;
-    p.cut = uniform(rank / tiles);
-    p.tile = tiles - 1 - (rank - p.cut * tiles);
-    p.slot = cut_before + of(cut_upto) - tiles * c.G * p.cuts + within;
+  template <class T>
+  __device__ __forceinline__ bool find(const Pool &c, const Rows &r, const Attend &a, const T (Plan::*before)[OKV_CHUNK_MAX_BATCH / 64 + 1], const T index) {
+    if (!plan) return true;
+    const int lane = threadIdx.x & 63, chunks = (r.batch + 63) / 64;
+    at = __popcll(__ballot(lane < chunks && (plan->*before)[min(lane + 1, chunks)] <= index));
+    if (at >= chunks) return false;
+    b0 = 64 * at;
+    q = sequence_at<F>(c, r, a, b0 + lane);
     return true;
-  });
-  return p;
+  }
+  template <class T>
+  __device__ __forceinline__ T first(const T (Plan::*before)[OKV_CHUNK_MAX_BATCH / 64 + 1]) const { return plan ? (plan->*before)[at] : 0; }
+};
+
+struct Piece {
+  Sequence q;
+  int tile, g, begin, end;               // steps of its tile's q.steps
+  int slot;                              // of its results in the workspace, below 0: it is whole
+  int cuts, apart;                       // (joining) slots of the tile's, and from one to the next
+};
+__device__ __forceinline__ int of_lane(const int x, const int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ Sequence of_lane(const Sequence &q, const int lane) {
+  return {of_lane(q.first, lane), of_lane(q.n, lane), of_lane(q.s, lane), of_lane(q.len, lane), of_lane(q.prefix, lane), of_lane(q.tiles, lane), of_lane(q.steps, lane)};
+}
+// Items of a sequence: the heads of a tile next to each other, so that those of a head are on the same XCD where they are a multiple of eight; tiles that see the most keys first
+__device__ __forceinline__ void set_item(Piece &p, const Pool &c, const int item) {
+  const int rank = uniform(item / c.G);
+  p.g = item - rank * c.G;
+  p.tile = p.q.tiles - 1 - rank;
+}
+// The index-th piece, where items are whole or cut into equal pieces.  A sequence's first cuts come first: tiles read the same keys together
+template <class F, bool FEW>
+__device__ __forceinline__ bool piece_of(Piece &p, Chunk<F, FEW> &k, const Pool &c, const Rows &r, const Attend &a, const int index) {
+  if (!k.find(c, r, a, &Plan::pieces, index)) return false;
+  const int cuts = cuts_of(k.q, k.span), mine = k.q.tiles * c.G * cuts, within_chunk = index - k.first(&Plan::pieces);
+  const int upto = wave_scan(mine);
+  const uint64_t ended = __ballot(upto <= within_chunk);
+  if (ended == ~0ull) return false;
+  const int at = __popcll(ended);
+  p.q = of_lane(k.q, at);
+  p.cuts = of_lane(cuts, at);
+  const int within = within_chunk - of_lane(upto - mine, at), items = p.q.tiles * c.G, cut = uniform(within / items);
+  set_item(p, c, within - cut * items);
+  p.begin = uniform((int)((uint64_t)(unsigned)p.q.steps * (unsigned)cut / (unsigned)p.cuts));
+  p.end = uniform((int)((uint64_t)(unsigned)p.q.steps * (unsigned)(cut + 1) / (unsigned)p.cuts));
+  p.slot = -1;
+  if (p.cuts > 1) {
+    const int cut_mine = cuts > 1 ? mine : 0, cut_upto = wave_scan(cut_mine);
+    p.slot = k.first(&Plan::cut_pieces) + of_lane(cut_upto - cut_mine, at) + within;
+  }
+  return true;
+}
+// Where step `step` of all items' lies: its sequence (its number: b), the item and the step of the item
+template <class F, bool FEW>
+__device__ __forceinline__ bool step_of(Sequence &q, int &b, int &item, int &within, Chunk<F, FEW> &k, const Pool &c, const Rows &r, const Attend &a, const unsigned long long step) {
+  if (!k.find(c, r, a, &Plan::steps, step)) return false;
+  const unsigned long long mine = (unsigned long long)((unsigned)k.q.tiles * (unsigned)c.G) * (unsigned)k.q.steps, within_chunk = step - k.first(&Plan::steps);
+  const unsigned long long upto = wave_scan(mine);
+  const uint64_t ended = __ballot(upto <= within_chunk);
+  if (ended == ~0ull) return false;
+  const int at = __popcll(ended);
+  const unsigned long long before = upto - mine;
+  const unsigned long long rest = within_chunk - ((unsigned long long)(unsigned)of_lane((int)(before >> 32), at) << 32 | (unsigned)of_lane((int)before, at));
+  q = of_lane(k.q, at);
+  b = k.b0 + at;
+  item = uniform((int)(rest / (unsigned)q.steps));
+  within = uniform((int)(rest - (unsigned long long)(unsigned)item * (unsigned)q.steps));
+  return true;
+}
+
+// One workgroup: what more than 64 sequences come to
+constexpr int kPlanThreads = 1024, kPlanEach = OKV_CHUNK_MAX_BATCH / kPlanThreads;
+template <class F, bool FEW>
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pool c, Rows r, Attend a) {
+  constexpr int kPlanWaves = kPlanThreads / 64;
+  __shared__ float shared[kPlanWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunks = (r.batch + 63) / 64;
+  Sequence q[kPlanEach];
+#pragma unroll
+  for (int i = 0; i < kPlanEach; ++i) q[i] = sequence_at<F>(c, r, a, i * kPlanThreads + (int)threadIdx.x);
+  auto all = [&](float x, const bool largest) {
+    x = largest ? wave_max(x) : wave_sum(x);
+    __syncthreads();
+    if (lane == 0) shared[wave] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPlanWaves; ++w) x = largest ? fmaxf(x, shared[w]) : x + shared[w];
+    return x;
+  };
+  auto each = [&](const auto &f, const bool largest) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i) x = largest ? fmaxf(x, f(q[i])) : x + f(q[i]);
+    return all(x, largest);
+  };
+  const int span = span_of<F, FEW>(c, a, [&](const auto &f) { return each(f, false); }, [&](const auto &f) { return each(f, true); });
+  Plan &plan = *a.plan;
+#pragma unroll
+  for (int i = 0; i < kPlanEach; ++i) {                  // chunk 16 i + wave
+    const int cuts = cuts_of(q[i], span), items = q[i].tiles * c.G, chunk = i * kPlanWaves + wave;
+    const int pieces = wave_scan(items * cuts), cut_pieces = wave_scan(cuts > 1 ? items * cuts : 0), cut_tiles = wave_scan(cuts > 1 ? items : 0);
+    const unsigned long long steps = wave_scan((unsigned long long)(unsigned)items * (unsigned)q[i].steps);
+    if (lane == 63 && chunk < chunks) plan.pieces[chunk + 1] = pieces, plan.cut_pieces[chunk + 1] = cut_pieces, plan.cut_tiles[chunk + 1] = cut_tiles, plan.steps[chunk + 1] = steps;
+  }
+  __threadfence_block();
+  __syncthreads();
+  if (wave) return;
+  const bool there = lane < chunks;
+  const int pieces = wave_scan(there ? plan.pieces[lane + 1] : 0), cut_pieces = wave_scan(there ? plan.cut_pieces[lane + 1] : 0), cut_tiles = wave_scan(there ? plan.cut_tiles[lane + 1] : 0);
+  const unsigned long long steps = wave_scan(there ? plan.steps[lane + 1] : 0ull);
+  if (there) plan.pieces[lane + 1] = pieces, plan.cut_pieces[lane + 1] = cut_pieces, plan.cut_tiles[lane + 1] = cut_tiles, plan.steps[lane + 1] = steps;
+  if (lane == 0) plan.span = span, plan.pieces[0] = plan.cut_pieces[0] = plan.cut_tiles[0] = 0, plan.steps[0] = 0;
 }
 
 template <int D, bool FEW, bool WIDE, bool SHAPED>
-__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
+__device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, const Piece &piece, char *const lds, int &odd_first, int &odd_last) {
   using F = Form<D, FEW>;
   constexpr int kLoads = F::kLoads, kKeys = F::kKeys, kRowBytes = 2 * D, kParts = kKeys / 32;
-  __shared__ __attribute__((aligned(1024))) char lds[F::kLds];
-  __shared__ int odd_first, odd_last;                    // steps with values that are not finite, of those that not every row sees
-  const Piece p = piece_of<F>(c, r, a, blockIdx.x);
-  if (!p.there) return;
+  const Sequence &p = piece.q;
   if (threadIdx.x == 0) odd_first = INT_MAX, odd_last = -1;      // (a barrier comes before their use)
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int row0 = p.tile * F::kRows + (FEW ? 0 : wave * 32), row = row0 + col;         // of the sequence's n R rows
-  const int token = row / c.R, head = p.g * c.R + row - token * c.R;
+  const int row0 = piece.tile * F::kRows + (FEW ? 0 : wave * 32), row = row0 + col;         // of the sequence's n R rows
+  const int token = row / c.R, head = piece.g * c.R + row - token * c.R;
   const int base = p.len - p.n, pos = base + token;
   auto first_seen = [&](const int pos) { return a.window == 0 || pos < a.window ? 0 : pos - a.window + 1; };      // (but for the prefix)
   const int from = first_seen(pos);
@@ -359,16 +456,17 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   const int token0 = uniform(row0 / c.R), token1 = min(uniform((row0 + 31) / c.R), p.n - 1);
   const bool idle = token0 >= p.n;
   const int pos0 = base + token0, pos1 = base + token1, from0 = first_seen(pos0), from1 = first_seen(pos1);
-  const int tile_pos0 = base + uniform(p.tile * F::kRows / c.R), tile_pos1 = base + min(uniform((p.tile * F::kRows + F::kRows - 1) / c.R), p.n - 1);
+  const int tile_pos0 = base + uniform(piece.tile * F::kRows / c.R), tile_pos1 = base + min(uniform((piece.tile * F::kRows + F::kRows - 1) / c.R), p.n - 1);
   const int tile_from1 = first_seen(tile_pos1);
   auto all_see = [&](const int key0) { return (key0 + kKeys - 1 <= tile_pos0 && key0 >= tile_from1) || key0 + kKeys <= p.prefix; };      // rows of the tile
   auto in_sight = [&](const int key0) { return !idle && ((key0 <= pos1 && key0 + kKeys > from0) || key0 < p.prefix); };                  // of some row of the wavefront
 
   // this piece's steps of the tile's
-  Keys keys = keys_of<F>(p.n, p.len, p.prefix, a.window, c.R, p.tile);
+  Keys keys = keys_of<F>(p.n, p.len, p.prefix, a.window, c.R, piece.tile);
   keys.ahead = uniform(keys.ahead), keys.first = uniform(keys.first), keys.total = uniform(keys.total);
-  const int i0 = uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)p.cut / (unsigned)p.cuts));
-  const int total = uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)(p.cut + 1) / (unsigned)p.cuts)) - i0;
+  const bool whole_tile = piece.slot < 0;
+  const int i0 = whole_tile ? 0 : uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)piece.begin / (unsigned)p.steps));
+  const int total = whole_tile ? keys.total : uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)piece.end / (unsigned)p.steps)) - i0;
   auto key_at_step = [&](const int i) {                // this wavefront's first key of a step; past the end: the last again
     const int j = i0 + min(i, total - 1);
     return (j < keys.ahead ? j : keys.first + j - keys.ahead) * F::kStep + (FEW ? wave * kKeys : 0);
@@ -394,7 +492,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + (FEW ? wave * (F::kLds / kWaves) : 0);
   char *const mine = lds + (FEW ? wave * (F::kLds / kWaves) : 0);
   const int32_t *table_row = c.table + (int64_t)max(p.s, 0) * c.width;
-  const char *pool = uniform(reinterpret_cast<const char *>(c.kv + head_offset<D>(c, p.g)));
+  const char *pool = uniform(reinterpret_cast<const char *>(c.kv + head_offset<D>(c, piece.g)));
   const int64_t slab = (int64_t)2 * c.G * D << (4 + c.st_log2);
   const int last_tile = (p.len - 1) >> 4;
   int held_from = INT_MIN / 2, held = p.s;              // lane l: the block in entry held_from + l of the sequence's row of the table
@@ -580,7 +678,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll 1
       for (int key = key0; key < min(key0 + kKeys, p.len); ++key) {
         const bool seen = (key <= pos && key >= from) || key < p.prefix;
-        const _Float16 *v = c.kv + tile_at<D>(c, table_row, p.s, key >> 4) + head_offset<D>(c, p.g) + v_offset<D>(c) + (key & 15) * D + 4 * half;
+        const _Float16 *v = c.kv + tile_at<D>(c, table_row, p.s, key >> 4) + head_offset<D>(c, piece.g) + v_offset<D>(c) + (key & 15) * D + 4 * half;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -594,13 +692,13 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
     }
   }
   l = sum_with_lane_xor<32>(l);
-  float *parts = a.parts + (int64_t)p.slot * F::kPartFloats;
+  float *parts = a.parts + (int64_t)max(piece.slot, 0) * F::kPartFloats;
   if constexpr (!FEW) {
     if (token >= p.n) return;
     const int of_tile = wave * 32 + col;
-    const float over = p.cuts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-    const int64_t to = p.cuts > 1 ? of_tile * D : ((int64_t)(p.first + token) * (c.G * c.R) + head) * D;
-    if (p.cuts > 1 && half == 0) parts[F::kRows * D + of_tile] = m, parts[F::kRows * (D + 1) + of_tile] = l;
+    const float over = !whole_tile ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    const int64_t to = !whole_tile ? of_tile * D : ((int64_t)(p.first + token) * (c.G * c.R) + head) * D;
+    if (!whole_tile && half == 0) parts[F::kRows * D + of_tile] = m, parts[F::kRows * (D + 1) + of_tile] = l;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -609,7 +707,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = o[e][4 * i + j] * over;
         const int64_t at = to + 32 * e + 8 * i + 4 * half;
-        if (p.cuts > 1) *reinterpret_cast<floatx4 *>(parts + at) = y;
+        if (!whole_tile) *reinterpret_cast<floatx4 *>(parts + at) = y;
         else if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
         else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
       }
@@ -624,7 +722,7 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
       for (int i = 0; i < 4; ++i) *reinterpret_cast<floatx4 *>(own + col * kStride + 32 * e + 8 * i + 4 * half) = floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
     if (half == 0) own[32 * kStride + col] = m, own[32 * kStride + 32 + col] = l;
     __syncthreads();
-    const int of_tile = wave * 8 + lane / 8, joined_row = p.tile * 32 + of_tile, joined_token = joined_row / c.R;
+    const int of_tile = wave * 8 + lane / 8, joined_row = piece.tile * 32 + of_tile, joined_token = joined_row / c.R;
     if (joined_token >= p.n) return;
     float most = -1e30f, sum = 0.f, factor[kWaves];
 #pragma unroll
@@ -634,9 +732,9 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
       factor[w] = __builtin_amdgcn_exp2f(all[w * kEach + 32 * kStride + of_tile] - most);
       sum += all[w * kEach + 32 * kStride + 32 + of_tile] * factor[w];
     }
-    const float over = p.cuts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-    const int64_t to = p.cuts > 1 ? of_tile * D : ((int64_t)(p.first + joined_token) * (c.G * c.R) + p.g * c.R + joined_row - joined_token * c.R) * D;
-    if (p.cuts > 1 && lane % 8 == 0) parts[F::kRows * D + of_tile] = most, parts[F::kRows * (D + 1) + of_tile] = sum;
+    const float over = !whole_tile ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+    const int64_t to = !whole_tile ? of_tile * D : ((int64_t)(p.first + joined_token) * (c.G * c.R) + piece.g * c.R + joined_row - joined_token * c.R) * D;
+    if (!whole_tile && lane % 8 == 0) parts[F::kRows * D + of_tile] = most, parts[F::kRows * (D + 1) + of_tile] = sum;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) {
       floatx4 y = {};
@@ -644,62 +742,98 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
       for (int w = 0; w < kWaves; ++w) y += *reinterpret_cast<const floatx4 *>(all + w * kEach + of_tile * kStride + 32 * e + 4 * (lane % 8)) * factor[w];
       y *= over;
       const int64_t at = to + 32 * e + 4 * (lane % 8);
-      if (p.cuts > 1) *reinterpret_cast<floatx4 *>(parts + at) = y;
+      if (!whole_tile) *reinterpret_cast<floatx4 *>(parts + at) = y;
       else if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
       else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
     }
   }
 }
 
-// Joins the cuts of a tile's rows: a workgroup per 32 rows of a tile that is cut
+template <int D, bool FEW, bool WIDE, bool SHAPED>
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(FEW && D == 128 ? 1 : 2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
+  using F = Form<D, FEW>;
+  __shared__ __attribute__((aligned(1024))) char lds[F::kLds];
+  __shared__ int odd_first, odd_last;                    // steps with values that are not finite, of those that not every row sees
+  Chunk<F, FEW> k(c, r, a);
+  Piece p;
+  if (!FEW || k.span == kNone) {
+    if (piece_of(p, k, c, r, a, (int)blockIdx.x)) attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last);
+    return;
+  }
+  if constexpr (FEW) {
+    if (blockIdx.x >= F::kSlots) return;
+    int b, item;
+    if (!step_of(p.q, b, item, p.begin, k, c, r, a, (unsigned long long)blockIdx.x * (unsigned)k.span)) return;
+    for (int left = k.span;;) {
+      p.end = min(p.q.steps, p.begin + left);
+      p.slot = p.begin > 0 ? 2 * blockIdx.x : p.end < p.q.steps ? 2 * blockIdx.x + 1 : -1;
+      set_item(p, c, item);
+      attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last);
+      left -= p.end - p.begin;
+      if (left <= 0) return;
+      p.begin = 0;
+      if (++item == p.q.tiles * c.G) {
+        item = 0;
+        do {
+          if (++b >= r.batch) return;
+          p.q = of_lane(sequence_at<F>(c, r, a, b), 0);
+        } while (p.q.tiles == 0);
+      }
+      __syncthreads();                                   // LDS is free again
+    }
+  }
+}
+
+// Joins the results of a tile's pieces: a workgroup per 32 rows of a tile that is cut
 constexpr int kJoinRows = 32, kJoinThreads = 256;
 
 template <int D, bool FEW, bool WIDE>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(Pool c, Rows r, Attend a) {
   using F = Form<D, FEW>;
-  const int tile_index = blockIdx.x / (F::kRows / kJoinRows);
+  const int index = blockIdx.x / (F::kRows / kJoinRows);
+  Chunk<F, FEW> k(c, r, a);
+  if (k.span == kNone) return;
   Piece p;
-  p.there = false;
-  int tiles_before = 0;
-  with_plan<F>(c, r, a, [&](const Sequence &q, const int cuts, const int, const int cut_upto, const int, const int cut_before) {
-    const int mine = cuts > 1 ? q.tiles * c.G : 0, upto = wave_scan(mine);
-    const uint64_t ended = __ballot(tiles_before + upto <= tile_index);
-    if (ended == ~0ull) {
-      tiles_before += uniform(__shfl(upto, 63));
-      return false;
-    }
-    const int at = __popcll(ended);
-    auto of = [&](const int x) { return __builtin_amdgcn_readlane(x, at); };
-    p.there = true;
-    p.first = of(q.first), p.n = of(q.n), p.cuts = of(cuts);
-    const int tiles = of(q.tiles), within = tile_index - tiles_before - (of(upto) - tiles * c.G), rank = uniform(within / c.G);
-    p.g = within - rank * c.G;
-    p.tile = tiles - 1 - rank;
-    p.apart = tiles * c.G;
-    p.slot = cut_before + of(cut_upto) - tiles * c.G * p.cuts + within;
-    return true;
-  });
-  if (!p.there) return;
+  if constexpr (FEW) {                                   // the item in which stretch index + 1 begins, if it is the first stretch that begins in it
+    int b, item;
+    const unsigned long long at = (unsigned long long)(index + 1) * (unsigned)k.span;
+    if (!step_of(p.q, b, item, p.begin, k, c, r, a, at) || p.begin == 0 || p.begin > k.span) return;
+    set_item(p, c, item);
+    p.cuts = 1 + (p.q.steps - p.begin + k.span - 1) / k.span;
+    p.slot = 2 * index + 1;
+    p.apart = 2;                                         // (the first piece's is 2 index + 1, the others' are 2 (index + 1), ...)
+  } else {
+    if (!k.find(c, r, a, &Plan::cut_tiles, index)) return;
+    const int cuts = cuts_of(k.q, k.span), items = k.q.tiles * c.G, mine = cuts > 1 ? items : 0, within_chunk = index - k.first(&Plan::cut_tiles), upto = wave_scan(mine);
+    const uint64_t ended = __ballot(upto <= within_chunk);
+    if (ended == ~0ull) return;
+    const int at = __popcll(ended), cut_upto = wave_scan(mine * cuts);
+    p.q = of_lane(k.q, at);
+    p.cuts = of_lane(cuts, at);
+    const int within = within_chunk - of_lane(upto - mine, at);
+    set_item(p, c, within);
+    p.slot = k.first(&Plan::cut_pieces) + of_lane(cut_upto - mine * cuts, at) + within;
+    p.apart = p.q.tiles * c.G;
+  }
   constexpr int kLanes = D / 4, kTogether = kJoinThreads / kLanes;      // a row's lanes, four elements each; rows at a time
 #pragma unroll 1
-  for (int k = 0; k < kJoinRows; k += kTogether) {
-    const int of_tile = blockIdx.x % (F::kRows / kJoinRows) * kJoinRows + k + threadIdx.x / kLanes, row = p.tile * F::kRows + of_tile, token = row / c.R, head = p.g * c.R + row - token * c.R;
-    if (token >= p.n) return;
-    const float *part = a.parts + (int64_t)p.slot * F::kPartFloats;
-    const int64_t apart = (int64_t)p.apart * F::kPartFloats;
+  for (int i = 0; i < kJoinRows; i += kTogether) {
+    const int of_tile = blockIdx.x % (F::kRows / kJoinRows) * kJoinRows + i + threadIdx.x / kLanes, row = p.tile * F::kRows + of_tile, token = row / c.R, head = p.g * c.R + row - token * c.R;
+    if (token >= p.q.n) return;
+    auto part = [&](const int cut) { return a.parts + (int64_t)(FEW && cut > 0 ? p.slot - 1 + cut * p.apart : p.slot + cut * p.apart) * F::kPartFloats; };
     float m = -1e30f, l = 0.f;
 #pragma unroll 4
-    for (int cut = 0; cut < p.cuts; ++cut) m = fmaxf(m, part[cut * apart + F::kRows * D + of_tile]);
+    for (int cut = 0; cut < p.cuts; ++cut) m = fmaxf(m, part(cut)[F::kRows * D + of_tile]);
     floatx4 o = {};
 #pragma unroll 4
     for (int cut = 0; cut < p.cuts; ++cut) {
-      const float *one = part + cut * apart;
+      const float *one = part(cut);
       const float factor = __builtin_amdgcn_exp2f(one[F::kRows * D + of_tile] - m);
       l += one[F::kRows * (D + 1) + of_tile] * factor;
       o += *reinterpret_cast<const floatx4 *>(one + of_tile * D + 4 * (threadIdx.x % kLanes)) * factor;
     }
     o *= l == 0.f ? 0.f : 1.f / l;
-    const int64_t at = ((int64_t)(p.first + token) * (c.G * c.R) + head) * D + 4 * (threadIdx.x % kLanes);
+    const int64_t at = ((int64_t)(p.q.first + token) * (c.G * c.R) + head) * D + 4 * (threadIdx.x % kLanes);
     if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = o;
     else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
   }
@@ -793,12 +927,12 @@ int okv_rope_append(const okv_layer_pool *c, const okv_rows *r, const okv_rope *
 
 int64_t okv_chunk_workspace_bytes(const okv_layer_pool *c) {
   if (const char *why = shape_problem(c)) return report(OKV_EINVAL, "okv_chunk_workspace_bytes: %s", why);
-  // A tile that is cut has less than twice as many cuts as its steps are spans, which are kPieces at most
+  // Cut into equal pieces, a tile has less than twice as many as its steps are spans, which are kPieces at most; of a stretch two are kept
   auto of = [&](auto form) {
     using F = decltype(form);
-    return pool_of(c).capacity <= F::kUncut * F::kStep ? (int64_t)0 : (int64_t)2 * F::kPieces * F::kPartFloats * 4;
+    return pool_of(c).capacity <= F::kUncut * F::kStep ? (int64_t)0 : (int64_t)F::kParts * F::kPartFloats * 4;
   };
-  return c->head_dim == 128 ? std::max(of(Form<128, true>{}), of(Form<128, false>{})) : std::max(of(Form<64, true>{}), of(Form<64, false>{}));
+  return kPlanBytes + (c->head_dim == 128 ? std::max(of(Form<128, true>{}), of(Form<128, false>{})) : std::max(of(Form<64, true>{}), of(Form<64, false>{})));
 }
 
 int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *a, const void *q, int64_t q_stride, void *out, void *stream) {
@@ -814,7 +948,7 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
   if (!q || !out) return report(OKV_EINVAL, "%s: NULL pointer", who);
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(a->slopes, 4) || !aligned(a->prefix, 4)) return report(OKV_EINVAL, "%s: q and out must be 16-byte aligned, slopes and prefix 4", who);
   const int64_t need = okv_chunk_workspace_bytes(c);
-  if (need && (!a->workspace || a->workspace_bytes < need || !aligned(a->workspace, 256)))
+  if ((!a->workspace || a->workspace_bytes < need || !aligned(a->workspace, 256)))
     return report(OKV_ENOSPC, "%s: the workspace must be %lld bytes, 256-byte aligned", who, (long long)need);
   const Pool pool = pool_of(c);
   const Rows rows{r->seqs, r->starts, r->lens, r->batch, r->n_rows};
@@ -823,8 +957,8 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
   const float scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)d);
   x.scale = a->cap != 0.f ? 2.f * kLog2e * (scale / a->cap) : scale * kLog2e, x.cap = a->cap * kLog2e;
   x.window = a->window, x.slopes = a->slopes, x.prefix = a->prefix;
-  x.parts = static_cast<float *>(a->workspace);
-  x.parts = static_cast<float *>(a->workspace);
+  x.plan = static_cast<Plan *>(a->workspace), x.parts = reinterpret_cast<float *>(static_cast<char *>(a->workspace) + kPlanBytes);
+  x.plan = static_cast<Plan *>(a->workspace), x.parts = reinterpret_cast<float *>(static_cast<char *>(a->workspace) + kPlanBytes);
   const bool wide = a->out_dtype == 1, shaped = a->cap != 0.f || a->slopes;
   // How many rows a sequence brings is on the device: by the mean
   const int64_t all_rows = (int64_t)r->n_rows * pool.R;
@@ -835,14 +969,16 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
     constexpr bool FEW = decltype(few_)::value, WIDE = decltype(wide_)::value;
     using F = Form<D, FEW>;
     x.may_cut = pool.capacity > F::kUncut * F::kStep;
-    // a tile of rows begins at a sequence's first row; cutting adds at most kPieces
-    const int64_t tiles = (all_rows + F::kRows - 1) / F::kRows + std::min(r->batch, r->n_rows), pieces = tiles * pool.G + (x.may_cut ? F::kPieces : 0);
+    // a tile of rows begins at a sequence's first row; cutting into equal pieces adds at most kPieces, stretches are kSlots
+    const int64_t tiles = (all_rows + F::kRows - 1) / F::kRows + std::min(r->batch, r->n_rows), items = tiles * pool.G;
+    const int64_t pieces = !x.may_cut ? items : FEW ? std::max<int64_t>(items, F::kSlots) : items + F::kPieces;
     if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
+    if (r->batch > 64) hipLaunchKernelGGL((plan_kernel<F, FEW>), dim3(1), dim3(kPlanThreads), 0, s, pool, rows, x);
     if (shaped) hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, true>), dim3((unsigned)pieces), dim3(64 * kWaves), 0, s, pool, rows, x);
     else hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, false>), dim3((unsigned)pieces), dim3(64 * kWaves), 0, s, pool, rows, x);
-    // (tiles that are cut have more steps than a span)
-    if (x.may_cut)
-      hipLaunchKernelGGL((join_kernel<D, FEW, WIDE>), dim3((unsigned)(std::min<int64_t>(F::kPieces, tiles * pool.G) * (F::kRows / kJoinRows))), dim3(kJoinThreads), 0, s, pool, rows, x);
+    // (tiles that are cut into equal pieces have more steps than a span; a stretch but the first begins at most one)
+    const int64_t joined = FEW ? F::kSlots - 1 : std::min<int64_t>(F::kPieces, items);
+    if (x.may_cut) hipLaunchKernelGGL((join_kernel<D, FEW, WIDE>), dim3((unsigned)(joined * (F::kRows / kJoinRows))), dim3(kJoinThreads), 0, s, pool, rows, x);
     return hip_result(who);
   };
   auto typed = [&](auto d_) {

@@ -167,6 +167,20 @@ def test_many_sequences():
     check_rows(p, q, attended(p, q, n_new), n_new)
 
 
+@pytest.mark.parametrize("most,H,G", [(3, 4, 1), (200, 2, 2)])
+def test_many_long_sequences(most, H, G):
+    """More sequences than a wavefront has lanes, some of them long: few rows each, and hundreds of some."""
+    rng = np.random.default_rng(most)
+    n_new = [int(x) for x in rng.integers(0, 4, 130)]
+    n_new[7], n_new[70], n_new[129] = most, 1, most
+    lens = [n + int(x) for n, x in zip(n_new, rng.integers(0, 600, 130))]
+    lens[70], lens[129], lens[12] = 9000, 2500, n_new[12]
+    p = Paged(H, G, 64, 256, lens, seed=2)
+    q = queries(sum(n_new), H, 64)
+    for kw in (dict(), dict(window=700, prefix=[int(x) for x in rng.integers(0, 20, 130)])):
+        check_rows(p, q, attended(p, q, n_new, torch.float32, **kw), n_new, some=3, **kw)
+
+
 def test_strided_rows():
     p = Paged(4, 2, 128, 64, [100, 30], seed=3)
     both = queries(24, 9, 128)
