@@ -162,6 +162,7 @@ struct Attend {
   const float *slopes;
   const int32_t *prefix;
   Plan *plan;                            // in the workspace
+  char *cuts;                            // in the workspace
   float *parts;                          // results of pieces of rows' keys: kRows x D sums, and behind them kRows maxima and kRows sums of weights
 };
 
@@ -169,21 +170,23 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kRaise = 8.f;            // the maximum is raised when a score is this far above it
 // Weights are 2^(s - m + kLift): at most 2^15, and normal numbers in fp16 down to 2^-21 of the largest
 constexpr float kLift = 7.f;
-constexpr int kWaves = 4, kRing = 2;     // blocks of keys, and of values, in LDS
+constexpr int kRing = 2;                 // blocks of keys, and of values, in LDS
 
 // Rows are the n R rows (tokens, and for each its R query heads) of a sequence and KV head; a wavefront has 32 of them, whose blocks of keys go by.
 // Few rows: a workgroup has 32, each wavefront every fourth block of 32 keys, and joins them.  Many: a workgroup has 128, a wavefront 32, and all share blocks of 64 keys.
 template <int D, bool FEW>
 struct Form {
+  static constexpr int kWaves = FEW && D == 128 ? 2 : 4, kThreads = 64 * kWaves;
   static constexpr int kRows = FEW ? 32 : 32 * kWaves, kKeys = FEW ? 32 : 64, kStep = FEW ? kWaves * kKeys : kKeys;      // keys of a step of the workgroup
   static constexpr int kBlockBytes = kKeys * D * 2, kLoads = kBlockBytes / 1024 / (FEW ? 1 : kWaves);                   // loads of a wavefront per block of keys (or values)
   static constexpr int kLds = (FEW ? kWaves : 1) * 2 * kRing * kBlockBytes;
   static constexpr int kPartFloats = kRows * (D + 2);
   // How keys are cut (see Plan): workgroups that run at a time, and in steps what a piece costs beside its own, what joining does, and what is never cut
-  static constexpr int kSlots = FEW && D == 128 ? 256 : 512, kUncut = 512 / kStep;
+  static constexpr int kSlots = 512, kUncut = 512 / kStep, kLeast = 256 / kStep;
   static constexpr float kPerPiece = FEW ? 1.f : 4.f, kPerJoin = FEW ? 3.f : 10.f;
   static constexpr int kPieces = 1024;                  // that steps come to at most, where tiles are cut into equal pieces
-  static constexpr int kParts = 2 * (FEW ? kSlots : kPieces);                  // results of pieces
+  __host__ __device__ static int stretches(const int G) { return kSlots / G > 1 ? kSlots / G : 1; }
+  __host__ __device__ static int64_t parts(const int G) { return 2 * (FEW ? (int64_t)stretches(G) * G : (int64_t)kPieces); }      // results of pieces
 };
 
 __device__ __forceinline__ half8 transposed(const char *first, const char *second) {
@@ -201,12 +204,20 @@ __device__ __forceinline__ const char *uniform(const char *p) {
 }
 // One 16-byte-per-lane load from `base` + off straight into LDS: lane l's bytes land at lds + 16 l.  Written as assembly because the compiler, which cannot tell the block being
 // written from the one being read, waits for all such loads in front of every LDS read otherwise.  m0 is left as it was found.
+// ONCE: nobody else reads these bytes soon, past the caches (5 tokens for each of 32 sequences of up to 4096: 82 -> 76 us; with shared blocks 42 -> 45).
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const char *base, const uint32_t off, const uint32_t lds) {
   uint32_t found;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-               : "=&s"(found)
-               : "s"(uniform((int)lds)), "v"(off), "s"(uniform(base))
-               : "memory");
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 nt\n\ts_mov_b32 m0, %0"
+                 : "=&s"(found)
+                 : "s"(uniform((int)lds)), "v"(off), "s"(uniform(base))
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(found)
+                 : "s"(uniform((int)lds)), "v"(off), "s"(uniform(base))
+                 : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_for_loads() {      // until N are outstanding
@@ -237,7 +248,8 @@ __device__ __forceinline__ Keys keys_of(const int n, const int len, const int pr
 // What workgroups do.  The rows of every sequence and KV head are cut into tiles (`tiles` of a sequence, each for G heads: its items), whose keys are walked in steps.  Where workgroups that take an item
 // each would leave much of the chip idle, keys are cut among them, and a second launch joins the results.
 //   many rows   every tile of a sequence is cut into as many pieces (`cuts`), of `span` steps at most
-//   few rows    all items' steps, one item after the other, are shared out in stretches of `span`: a workgroup takes a stretch, which ends some items, holds some and begins one
+//   few rows    the steps of all tiles, one tile after the other, are shared out in stretches of `span`: G workgroups take a stretch, one for each head, which ends some tiles, holds some and
+//               begins one.  (Heads side by side: their keys adjoin in memory.)
 // Lengths are on the device: every wavefront finds this out for itself, a lane per sequence; beyond 64 sequences a launch of one workgroup adds up chunks of 64 first.
 constexpr int kNone = 0x3fffffff;
 struct Sequence {
@@ -247,10 +259,17 @@ struct Sequence {
 struct Plan {                            // in the workspace, for more than 64 sequences; before each chunk of 64, and behind the last
   int span, unused;
   int pieces[OKV_CHUNK_MAX_BATCH / 64 + 1], cut_pieces[OKV_CHUNK_MAX_BATCH / 64 + 1], cut_tiles[OKV_CHUNK_MAX_BATCH / 64 + 1];
-  unsigned long long steps[OKV_CHUNK_MAX_BATCH / 64 + 1];
+  unsigned long long steps[OKV_CHUNK_MAX_BATCH / 64 + 1];      // of one head
 };
 constexpr int64_t kPlanBytes = 2048;
 static_assert(sizeof(Plan) <= kPlanBytes, "");
+// A tile that is cut, for the launch that joins its pieces, behind the plan: few rows, of the workgroup that takes its second piece; many, in order
+struct Cut {
+  int first, n, tile, g;                 // of its sequence: the first row, and rows
+  int slot, slot1, apart, cuts;          // its pieces' results: slot, slot1, slot1 + apart, ..; cuts 0: there is none
+};
+constexpr int kMostCuts = 1024;
+constexpr int64_t kCutBytes = 16 + kMostCuts * (int64_t)sizeof(Cut);      // (many rows: how many there are comes first)
 
 template <class F>
 __device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, const Attend &a, const int b) {
@@ -294,8 +313,8 @@ __device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum
   float best = time(items, longest);
   int span = kNone;
   if constexpr (FEW) {
-    const float even = ceilf(work * (1.0001f / F::kSlots));
-    if (longest > F::kUncut && even + (items * (1.f / F::kSlots) + 1.f) * F::kPerPiece + F::kPerJoin < best) span = (int)fminf(even, 1e9f);
+    const float stretches = (float)F::stretches(c.G), even = fmaxf(ceilf(work * 1.0001f / (stretches * c.G)), (float)F::kLeast);
+    if (longest > F::kUncut && even + (items / (stretches * c.G) + 1.f) * F::kPerPiece + F::kPerJoin < best) span = (int)fminf(even, 1e9f);
   } else {
     const int least = max(1, (int)fminf(ceilf(work * (1.0001f / F::kPieces)), 1e9f));
     if (best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return span;
@@ -335,6 +354,10 @@ struct Chunk {
     q = sequence_at<F>(c, r, a, b0 + lane);
     return true;
   }
+  __device__ __forceinline__ int cut_tiles(const Pool &c, const Rows &r) const {      // of all sequences (before find())
+    if (plan) return plan->cut_tiles[(r.batch + 63) / 64];
+    return uniform(__shfl(wave_scan(cuts_of(q, span) > 1 ? q.tiles * c.G : 0), 63));
+  }
   template <class T>
   __device__ __forceinline__ T first(const T (Plan::*before)[OKV_CHUNK_MAX_BATCH / 64 + 1]) const { return plan ? (plan->*before)[at] : 0; }
 };
@@ -343,7 +366,7 @@ struct Piece {
   Sequence q;
   int tile, g, begin, end;               // steps of its tile's q.steps
   int slot;                              // of its results in the workspace, below 0: it is whole
-  int cuts, apart;                       // (joining) slots of the tile's, and from one to the next
+  int cuts, cut, cut_tile, apart;        // pieces of the tile, and which one this is; the number of the tile among those that are cut; slots from a piece to the next
 };
 __device__ __forceinline__ int of_lane(const int x, const int lane) { return __builtin_amdgcn_readlane(x, lane); }
 __device__ __forceinline__ Sequence of_lane(const Sequence &q, const int lane) {
@@ -374,14 +397,17 @@ __device__ __forceinline__ bool piece_of(Piece &p, Chunk<F, FEW> &k, const Pool 
   if (p.cuts > 1) {
     const int cut_mine = cuts > 1 ? mine : 0, cut_upto = wave_scan(cut_mine);
     p.slot = k.first(&Plan::cut_pieces) + of_lane(cut_upto - cut_mine, at) + within;
+    p.cut = cut, p.apart = items;
+    const int tiles_mine = cuts > 1 ? k.q.tiles * c.G : 0, tiles_upto = wave_scan(tiles_mine);
+    p.cut_tile = k.first(&Plan::cut_tiles) + of_lane(tiles_upto - tiles_mine, at) + within - cut * items;
   }
   return true;
 }
-// Where step `step` of all items' lies: its sequence (its number: b), the item and the step of the item
+// Where step `step` of all tiles' lies: its sequence (its number: b), the tile (its rank: those that see the most keys first) and the step of the tile
 template <class F, bool FEW>
-__device__ __forceinline__ bool step_of(Sequence &q, int &b, int &item, int &within, Chunk<F, FEW> &k, const Pool &c, const Rows &r, const Attend &a, const unsigned long long step) {
+__device__ __forceinline__ bool step_of(Sequence &q, int &b, int &rank, int &within, Chunk<F, FEW> &k, const Pool &c, const Rows &r, const Attend &a, const unsigned long long step) {
   if (!k.find(c, r, a, &Plan::steps, step)) return false;
-  const unsigned long long mine = (unsigned long long)((unsigned)k.q.tiles * (unsigned)c.G) * (unsigned)k.q.steps, within_chunk = step - k.first(&Plan::steps);
+  const unsigned long long mine = (unsigned long long)(unsigned)k.q.tiles * (unsigned)k.q.steps, within_chunk = step - k.first(&Plan::steps);
   const unsigned long long upto = wave_scan(mine);
   const uint64_t ended = __ballot(upto <= within_chunk);
   if (ended == ~0ull) return false;
@@ -390,8 +416,8 @@ __device__ __forceinline__ bool step_of(Sequence &q, int &b, int &item, int &wit
   const unsigned long long rest = within_chunk - ((unsigned long long)(unsigned)of_lane((int)(before >> 32), at) << 32 | (unsigned)of_lane((int)before, at));
   q = of_lane(k.q, at);
   b = k.b0 + at;
-  item = uniform((int)(rest / (unsigned)q.steps));
-  within = uniform((int)(rest - (unsigned long long)(unsigned)item * (unsigned)q.steps));
+  rank = uniform((int)(rest / (unsigned)q.steps));
+  within = uniform((int)(rest - (unsigned long long)(unsigned)rank * (unsigned)q.steps));
   return true;
 }
 
@@ -427,7 +453,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pool c, Rows r, Atte
   for (int i = 0; i < kPlanEach; ++i) {                  // chunk 16 i + wave
     const int cuts = cuts_of(q[i], span), items = q[i].tiles * c.G, chunk = i * kPlanWaves + wave;
     const int pieces = wave_scan(items * cuts), cut_pieces = wave_scan(cuts > 1 ? items * cuts : 0), cut_tiles = wave_scan(cuts > 1 ? items : 0);
-    const unsigned long long steps = wave_scan((unsigned long long)(unsigned)items * (unsigned)q[i].steps);
+    const unsigned long long steps = wave_scan((unsigned long long)(unsigned)q[i].tiles * (unsigned)q[i].steps);
     if (lane == 63 && chunk < chunks) plan.pieces[chunk + 1] = pieces, plan.cut_pieces[chunk + 1] = cut_pieces, plan.cut_tiles[chunk + 1] = cut_tiles, plan.steps[chunk + 1] = steps;
   }
   __threadfence_block();
@@ -440,10 +466,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pool c, Rows r, Atte
   if (lane == 0) plan.span = span, plan.pieces[0] = plan.cut_pieces[0] = plan.cut_tiles[0] = 0, plan.steps[0] = 0;
 }
 
-template <int D, bool FEW, bool WIDE, bool SHAPED>
-__device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, const Piece &piece, char *const lds, int &odd_first, int &odd_last) {
+// `meanwhile` is called while the first blocks are on their way
+template <int D, bool FEW, bool WIDE, bool SHAPED, class Meanwhile>
+__device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, const Piece &piece, char *const lds, int &odd_first, int &odd_last, const Meanwhile &meanwhile) {
   using F = Form<D, FEW>;
-  constexpr int kLoads = F::kLoads, kKeys = F::kKeys, kRowBytes = 2 * D, kParts = kKeys / 32;
+  constexpr int kWaves = F::kWaves, kLoads = F::kLoads, kKeys = F::kKeys, kRowBytes = 2 * D, kParts = kKeys / 32;
   const Sequence &p = piece.q;
   if (threadIdx.x == 0) odd_first = INT_MAX, odd_last = -1;      // (a barrier comes before their use)
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -484,7 +511,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
   // sixteen rows' same piece, and the four pieces of 32 elements of four rows, are in different banks.  A load brings 1 KiB, 512 / D rows of a tile of 16.  FEW: a
   // wavefront has rings of its own and loads all of its blocks; else load j of a block is wavefront j % 4's.
   constexpr int kTileLoads = 16 * kRowBytes / 1024, kUnits = D / 8, kBases = FEW ? kLoads / kTileLoads : kLoads;
-  static_assert(kWaves % kTileLoads == 0, "a wavefront's loads of a shared block are of the same rows of their tiles");
+  static_assert(FEW || kWaves % kTileLoads == 0, "a wavefront's loads of a shared block are of the same rows of their tiles");
   const int lane_row = lane / kUnits;
   const uint32_t lane_base = lane_row * kRowBytes + 16 * ((lane % kUnits) ^ (D == 128 ? 4 * lane_row : 4 * ((lane_row >> 1) & 1) | (lane_row >> 2)));
   auto lane_offset = [&](const int j) { return (lane_base ^ (j * (D == 128 ? 16 : 32))) + j * 1024; };         // of load j of a tile
@@ -496,12 +523,12 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
   const int64_t slab = (int64_t)2 * c.G * D << (4 + c.st_log2);
   const int last_tile = (p.len - 1) >> 4;
   int held_from = INT_MIN / 2, held = p.s;              // lane l: the block in entry held_from + l of the sequence's row of the table
-  const char *value_base[kBases];
-  auto load = [&](const char *(&bases)[kBases], const uint32_t more, const int slot) {
+  const char *bases[kBases];             // of the keys that were loaded last
+  auto load = [&](const uint32_t more, const int slot) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
-      if constexpr (FEW) load_to_lds(bases[j / kTileLoads] + more, lane_offset(j % kTileLoads), lds0 + slot * F::kBlockBytes + j * 1024);
-      else load_to_lds(bases[j] + more, shared_offset, lds0 + slot * F::kBlockBytes + (j * kWaves + wave) * 1024);
+      if constexpr (FEW) load_to_lds<true>(bases[j / kTileLoads] + more, lane_offset(j % kTileLoads), lds0 + slot * F::kBlockBytes + j * 1024);
+      else load_to_lds<false>(bases[j] + more, shared_offset, lds0 + slot * F::kBlockBytes + (j * kWaves + wave) * 1024);
   };
   auto load_keys = [&](const int i, const int slot) {
     const int t0 = uniform(key_at_step(i)) / 16 + (FEW ? 0 : wave / kTileLoads);
@@ -513,12 +540,12 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
         held = min(max(table_row[min(e + lane, c.width - 1)], 0), c.n_blocks - 1);
       }
       const int block = __builtin_amdgcn_readlane(held, c.table ? e - held_from : 0);
-      value_base[j] = uniform(pool + 2 * (block * c.block_elems + (tb >> c.st_log2) * slab + (int64_t)(tb & ((1 << c.st_log2) - 1)) * (c.gg * 16 * D)));
+      bases[j] = uniform(pool + 2 * (block * c.block_elems + (tb >> c.st_log2) * slab + (int64_t)(tb & ((1 << c.st_log2) - 1)) * (c.gg * 16 * D)));
     }
-    load(value_base, 0, slot);
+    load(0, slot);
   };
   const uint32_t behind = 2 * v_offset<D>(c);
-  auto load_values = [&](const int slot) { load(value_base, behind, kRing + slot); };      // of the keys that were loaded last
+  auto load_values = [&](const int slot) { load(behind, kRing + slot); };      // of the keys that were loaded last
 
   // where this lane's operands begin in a block; xor 32 k (keys' k-th 16 elements) or 64 e (values' e-th 32 elements)
   const int x4 = (lane >> 2) & 3, p4 = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
@@ -549,6 +576,26 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     }
   };
 
+  // A number that is not finite may be of a key that some row does not see, and 0 times it is not 0: it is taken out, and added at the end where it is seen
+  auto take_out = [&](const int i, char *const v0) {
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      u32x4 *at = reinterpret_cast<u32x4 *>(v0 + (FEW ? j : j * kWaves + wave) * 1024 + 16 * lane), w = *at;
+      uint32_t any = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t bad = ((w[k] & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+        w[k] &= ~(bad - (bad >> 15));
+        any |= bad;
+      }
+      if (any) {
+        *at = w;
+        odd = true;
+      }
+    }
+    if (odd) atomicMin(&odd_first, i), atomicMax(&odd_last, i);
+  };
   auto step = [&](const int i, const int slot, floatx16 (&x)[kParts], floatx16 (&next)[kParts]) {
     wait_for_loads<0>();
     if constexpr (!FEW) barrier_leaving_loads();         // the next block of keys and this one of values are there, those before free
@@ -558,24 +605,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     const int key0 = uniform(key_at_step(i));
     char *const v0 = mine + (kRing + slot) * F::kBlockBytes;
     if (!all_see(key0)) {
-      // A number that is not finite may be of a key that some row does not see, and 0 times it is not 0: it is taken out here, and added at the end where it is seen
-      bool odd = false;
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        u32x4 *at = reinterpret_cast<u32x4 *>(v0 + (FEW ? j : j * kWaves + wave) * 1024 + 16 * lane), w = *at;
-        uint32_t any = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t bad = ((w[k] & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
-          w[k] &= ~(bad - (bad >> 15));
-          any |= bad;
-        }
-        if (any) {
-          *at = w;
-          odd = true;
-        }
-      }
-      if (odd) atomicMin(&odd_first, i), atomicMax(&odd_last, i);
+      take_out(i, v0);
       if constexpr (!FEW) __syncthreads();
     }
     if (!in_sight(key0)) {
@@ -655,13 +685,16 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       }
   };
 
+  if (total == 0) meanwhile();
   if (total > 0) {
     load_keys(0, 0);
+    floatx16 x[kParts], y[kParts];
     load_values(0);
     load_keys(1, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    meanwhile();
     wait_for_loads<2 * kLoads>();
-    barrier_leaving_loads();
-    floatx16 x[kParts], y[kParts];
+    if constexpr (!FEW) barrier_leaving_loads();
     if (in_sight(uniform(key_at_step(0)))) score(x, 0);
     for (int i = 0;; i += 2) {
       step(i, 0, x, y);
@@ -722,7 +755,9 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       for (int i = 0; i < 4; ++i) *reinterpret_cast<floatx4 *>(own + col * kStride + 32 * e + 8 * i + 4 * half) = floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
     if (half == 0) own[32 * kStride + col] = m, own[32 * kStride + 32 + col] = l;
     __syncthreads();
-    const int of_tile = wave * 8 + lane / 8, joined_row = piece.tile * 32 + of_tile, joined_token = joined_row / c.R;
+#pragma unroll 1
+    for (int k = 0; k < 32 / kWaves; k += 8) {
+    const int of_tile = wave * (32 / kWaves) + k + lane / 8, joined_row = piece.tile * 32 + of_tile, joined_token = joined_row / c.R;
     if (joined_token >= p.n) return;
     float most = -1e30f, sum = 0.f, factor[kWaves];
 #pragma unroll
@@ -746,97 +781,112 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       else if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
       else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
     }
+    }
   }
 }
 
 template <int D, bool FEW, bool WIDE, bool SHAPED>
-__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(FEW && D == 128 ? 1 : 2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
+__global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgpu_waves_per_eu(FEW && D == 128 ? 1 : 2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
   using F = Form<D, FEW>;
   __shared__ __attribute__((aligned(1024))) char lds[F::kLds];
   __shared__ int odd_first, odd_last;                    // steps with values that are not finite, of those that not every row sees
   Chunk<F, FEW> k(c, r, a);
   Piece p;
+  Cut *const cut = reinterpret_cast<Cut *>(a.cuts + 16);
   if (!FEW || k.span == kNone) {
-    if (piece_of(p, k, c, r, a, (int)blockIdx.x)) attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last);
+    if constexpr (FEW) {
+      if (a.may_cut && (int)blockIdx.x < F::stretches(c.G) * c.G && threadIdx.x == 0) cut[blockIdx.x].cuts = 0;
+    } else if (a.may_cut && blockIdx.x == 0) {
+      const int all = k.cut_tiles(c, r);
+      if (threadIdx.x == 0) *reinterpret_cast<int *>(a.cuts) = all;
+    }
+    if (!piece_of(p, k, c, r, a, (int)blockIdx.x)) return;
+    if (!FEW && p.slot >= 0 && p.cut == 0 && threadIdx.x == 0) cut[p.cut_tile] = {p.q.first, p.q.n, p.tile, p.g, p.slot, p.slot + p.apart, p.apart, p.cuts};
+    attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last, [] {});
     return;
   }
   if constexpr (FEW) {
-    if (blockIdx.x >= F::kSlots) return;
-    int b, item;
-    if (!step_of(p.q, b, item, p.begin, k, c, r, a, (unsigned long long)blockIdx.x * (unsigned)k.span)) return;
+    const int stretch = uniform((int)blockIdx.x / c.G), g = (int)blockIdx.x - stretch * c.G;
+    if (stretch >= F::stretches(c.G)) return;
+    int b, rank;
+    const bool there = step_of(p.q, b, rank, p.begin, k, c, r, a, (unsigned long long)(unsigned)stretch * (unsigned)k.span);
+    p.g = g;
+    if (threadIdx.x == 0) {                              // (the first stretch that begins in a tile says so)
+      Cut one{};
+      if (there && p.begin > 0 && p.begin <= k.span)
+        one = {p.q.first, p.q.n, p.q.tiles - 1 - rank, g, (2 * stretch - 1) * c.G + g, 2 * stretch * c.G + g, 2 * c.G, 1 + (p.q.steps - p.begin + k.span - 1) / k.span};
+      cut[blockIdx.x] = one;
+    }
+    if (!there) return;
     for (int left = k.span;;) {
+      p.tile = p.q.tiles - 1 - rank;
       p.end = min(p.q.steps, p.begin + left);
-      p.slot = p.begin > 0 ? 2 * blockIdx.x : p.end < p.q.steps ? 2 * blockIdx.x + 1 : -1;
-      set_item(p, c, item);
-      attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last);
+      p.slot = p.begin > 0 ? 2 * stretch * c.G + g : p.end < p.q.steps ? (2 * stretch + 1) * c.G + g : -1;
       left -= p.end - p.begin;
-      if (left <= 0) return;
-      p.begin = 0;
-      if (++item == p.q.tiles * c.G) {
-        item = 0;
+      Sequence next = p.q;
+      bool more = left > 0;
+      auto look_ahead = [&] {
+        if (!more || ++rank < p.q.tiles) return;
+        rank = 0;
         do {
-          if (++b >= r.batch) return;
-          p.q = of_lane(sequence_at<F>(c, r, a, b), 0);
-        } while (p.q.tiles == 0);
-      }
+          if (!(more = ++b < r.batch)) return;
+          next = of_lane(sequence_at<F>(c, r, a, b), 0);
+        } while (next.tiles == 0);
+      };
+      attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last, look_ahead);
+      if (!more) return;
+      p.q = next, p.begin = 0;
       __syncthreads();                                   // LDS is free again
     }
   }
 }
 
-// Joins the results of a tile's pieces: a workgroup per 32 rows of a tile that is cut
-constexpr int kJoinRows = 32, kJoinThreads = 256;
+// Joins the results of a tile's pieces, a workgroup for some rows
+constexpr int kJoinThreads = 256;
+template <int D>
+constexpr int kJoinLanes = D / 4;                        // of a row, four elements each
+template <int D>
+constexpr int kJoinRows = kJoinThreads / kJoinLanes<D>;
 
 template <int D, bool FEW, bool WIDE>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(Pool c, Rows r, Attend a) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(Pool c, Attend a) {
   using F = Form<D, FEW>;
-  const int index = blockIdx.x / (F::kRows / kJoinRows);
-  Chunk<F, FEW> k(c, r, a);
-  if (k.span == kNone) return;
-  Piece p;
-  if constexpr (FEW) {                                   // the item in which stretch index + 1 begins, if it is the first stretch that begins in it
-    int b, item;
-    const unsigned long long at = (unsigned long long)(index + 1) * (unsigned)k.span;
-    if (!step_of(p.q, b, item, p.begin, k, c, r, a, at) || p.begin == 0 || p.begin > k.span) return;
-    set_item(p, c, item);
-    p.cuts = 1 + (p.q.steps - p.begin + k.span - 1) / k.span;
-    p.slot = 2 * index + 1;
-    p.apart = 2;                                         // (the first piece's is 2 index + 1, the others' are 2 (index + 1), ...)
-  } else {
-    if (!k.find(c, r, a, &Plan::cut_tiles, index)) return;
-    const int cuts = cuts_of(k.q, k.span), items = k.q.tiles * c.G, mine = cuts > 1 ? items : 0, within_chunk = index - k.first(&Plan::cut_tiles), upto = wave_scan(mine);
-    const uint64_t ended = __ballot(upto <= within_chunk);
-    if (ended == ~0ull) return;
-    const int at = __popcll(ended), cut_upto = wave_scan(mine * cuts);
-    p.q = of_lane(k.q, at);
-    p.cuts = of_lane(cuts, at);
-    const int within = within_chunk - of_lane(upto - mine, at);
-    set_item(p, c, within);
-    p.slot = k.first(&Plan::cut_pieces) + of_lane(cut_upto - mine * cuts, at) + within;
-    p.apart = p.q.tiles * c.G;
-  }
-  constexpr int kLanes = D / 4, kTogether = kJoinThreads / kLanes;      // a row's lanes, four elements each; rows at a time
-#pragma unroll 1
-  for (int i = 0; i < kJoinRows; i += kTogether) {
-    const int of_tile = blockIdx.x % (F::kRows / kJoinRows) * kJoinRows + i + threadIdx.x / kLanes, row = p.tile * F::kRows + of_tile, token = row / c.R, head = p.g * c.R + row - token * c.R;
-    if (token >= p.q.n) return;
-    auto part = [&](const int cut) { return a.parts + (int64_t)(FEW && cut > 0 ? p.slot - 1 + cut * p.apart : p.slot + cut * p.apart) * F::kPartFloats; };
-    float m = -1e30f, l = 0.f;
-#pragma unroll 4
-    for (int cut = 0; cut < p.cuts; ++cut) m = fmaxf(m, part(cut)[F::kRows * D + of_tile]);
-    floatx4 o = {};
-#pragma unroll 4
-    for (int cut = 0; cut < p.cuts; ++cut) {
-      const float *one = part(cut);
-      const float factor = __builtin_amdgcn_exp2f(one[F::kRows * D + of_tile] - m);
+  constexpr int kLanes = kJoinLanes<D>;
+  const int index = blockIdx.x / (F::kRows / kJoinRows<D>), lane = threadIdx.x % kLanes;
+  if (!FEW && index >= *reinterpret_cast<const int *>(a.cuts)) return;
+  const Cut t = reinterpret_cast<const Cut *>(a.cuts + 16)[index];
+  const int of_tile = blockIdx.x % (F::kRows / kJoinRows<D>) * kJoinRows<D> + threadIdx.x / kLanes, row = t.tile * F::kRows + of_tile, token = row / c.R, head = t.g * c.R + row - token * c.R;
+  if (t.cuts == 0 || token >= t.n) return;
+  auto part = [&](const int cut) { return a.parts + (int64_t)(cut ? t.slot1 + (cut - 1) * t.apart : t.slot) * F::kPartFloats; };
+  float m = -1e30f, l = 0.f;
+  for (int cut = lane; cut < t.cuts; cut += kLanes) m = fmaxf(m, part(cut)[F::kRows * D + of_tile]);
+#pragma unroll
+  for (int o = kLanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  floatx4 o = {};
+  for (int cut0 = 0; cut0 < t.cuts; cut0 += kLanes) {
+    float factor = 0.f;
+    if (cut0 + lane < t.cuts) {
+      const float *one = part(cut0 + lane);
+      factor = __builtin_amdgcn_exp2f(one[F::kRows * D + of_tile] - m);
       l += one[F::kRows * (D + 1) + of_tile] * factor;
-      o += *reinterpret_cast<const floatx4 *>(one + of_tile * D + 4 * (threadIdx.x % kLanes)) * factor;
     }
-    o *= l == 0.f ? 0.f : 1.f / l;
-    const int64_t at = ((int64_t)(p.q.first + token) * (c.G * c.R) + head) * D + 4 * (threadIdx.x % kLanes);
-    if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = o;
-    else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
+    for (int j0 = 0; j0 < min(kLanes, t.cuts - cut0); j0 += 8) {      // (past the last: that one again, 0 times)
+      floatx4 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const floatx4 *>(part(min(cut0 + j0 + j, t.cuts - 1)) + of_tile * D + 4 * lane);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float by = __shfl(factor, j0 + j, kLanes);
+        if (by != 0.f) o += v[j] * by;
+      }
+    }
   }
+#pragma unroll
+  for (int o = kLanes / 2; o; o >>= 1) l += __shfl_xor(l, o);
+  o *= l == 0.f ? 0.f : 1.f / l;
+  const int64_t at = ((int64_t)(t.first + token) * (c.G * c.R) + head) * D + 4 * lane;
+  if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = o;
+  else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)o[0], (_Float16)o[1], (_Float16)o[2], (_Float16)o[3]};
 }
 
 // ---- host -------------------------------------------------------------------------------------------
@@ -930,9 +980,9 @@ int64_t okv_chunk_workspace_bytes(const okv_layer_pool *c) {
   // Cut into equal pieces, a tile has less than twice as many as its steps are spans, which are kPieces at most; of a stretch two are kept
   auto of = [&](auto form) {
     using F = decltype(form);
-    return pool_of(c).capacity <= F::kUncut * F::kStep ? (int64_t)0 : (int64_t)F::kParts * F::kPartFloats * 4;
+    return pool_of(c).capacity <= F::kUncut * F::kStep ? (int64_t)0 : F::parts(c->n_kv_heads) * F::kPartFloats * 4;
   };
-  return kPlanBytes + (c->head_dim == 128 ? std::max(of(Form<128, true>{}), of(Form<128, false>{})) : std::max(of(Form<64, true>{}), of(Form<64, false>{})));
+  return kPlanBytes + kCutBytes + (c->head_dim == 128 ? std::max(of(Form<128, true>{}), of(Form<128, false>{})) : std::max(of(Form<64, true>{}), of(Form<64, false>{})));
 }
 
 int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *a, const void *q, int64_t q_stride, void *out, void *stream) {
@@ -957,8 +1007,8 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
   const float scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)d);
   x.scale = a->cap != 0.f ? 2.f * kLog2e * (scale / a->cap) : scale * kLog2e, x.cap = a->cap * kLog2e;
   x.window = a->window, x.slopes = a->slopes, x.prefix = a->prefix;
-  x.plan = static_cast<Plan *>(a->workspace), x.parts = reinterpret_cast<float *>(static_cast<char *>(a->workspace) + kPlanBytes);
-  x.plan = static_cast<Plan *>(a->workspace), x.parts = reinterpret_cast<float *>(static_cast<char *>(a->workspace) + kPlanBytes);
+  x.plan = static_cast<Plan *>(a->workspace), x.cuts = static_cast<char *>(a->workspace) + kPlanBytes, x.parts = reinterpret_cast<float *>(x.cuts + kCutBytes);
+  x.plan = static_cast<Plan *>(a->workspace), x.cuts = static_cast<char *>(a->workspace) + kPlanBytes, x.parts = reinterpret_cast<float *>(x.cuts + kCutBytes);
   const bool wide = a->out_dtype == 1, shaped = a->cap != 0.f || a->slopes;
   // How many rows a sequence brings is on the device: by the mean
   const int64_t all_rows = (int64_t)r->n_rows * pool.R;
@@ -971,14 +1021,15 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
     x.may_cut = pool.capacity > F::kUncut * F::kStep;
     // a tile of rows begins at a sequence's first row; cutting into equal pieces adds at most kPieces, stretches are kSlots
     const int64_t tiles = (all_rows + F::kRows - 1) / F::kRows + std::min(r->batch, r->n_rows), items = tiles * pool.G;
-    const int64_t pieces = !x.may_cut ? items : FEW ? std::max<int64_t>(items, F::kSlots) : items + F::kPieces;
+    const int64_t pieces = !x.may_cut ? items : FEW ? std::max<int64_t>(items, F::stretches(pool.G) * pool.G) : items + F::kPieces;
     if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
     if (r->batch > 64) hipLaunchKernelGGL((plan_kernel<F, FEW>), dim3(1), dim3(kPlanThreads), 0, s, pool, rows, x);
-    if (shaped) hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, true>), dim3((unsigned)pieces), dim3(64 * kWaves), 0, s, pool, rows, x);
-    else hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, false>), dim3((unsigned)pieces), dim3(64 * kWaves), 0, s, pool, rows, x);
-    // (tiles that are cut into equal pieces have more steps than a span; a stretch but the first begins at most one)
-    const int64_t joined = FEW ? F::kSlots - 1 : std::min<int64_t>(F::kPieces, items);
-    if (x.may_cut) hipLaunchKernelGGL((join_kernel<D, FEW, WIDE>), dim3((unsigned)(joined * (F::kRows / kJoinRows))), dim3(kJoinThreads), 0, s, pool, rows, x);
+    if (shaped) hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, true>), dim3((unsigned)pieces), dim3(F::kThreads), 0, s, pool, rows, x);
+    else hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, false>), dim3((unsigned)pieces), dim3(F::kThreads), 0, s, pool, rows, x);
+    // (tiles that are cut into equal pieces have more steps than a span)
+    static_assert(F::kSlots <= kMostCuts && F::kPieces <= kMostCuts, "");
+    const int64_t joined = FEW ? F::stretches(pool.G) * pool.G : std::min<int64_t>(F::kPieces, items);
+    if (x.may_cut) hipLaunchKernelGGL((join_kernel<D, FEW, WIDE>), dim3((unsigned)(joined * (F::kRows / kJoinRows<D>))), dim3(kJoinThreads), 0, s, pool, x);
     return hip_result(who);
   };
   auto typed = [&](auto d_) {
