@@ -321,7 +321,7 @@ __device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum
     for (int i = 0; i < 12; ++i) {
       const float of_all = i == 8 ? .5f : i == 9 ? 1.f / 1.5f : i == 10 ? 1.f / 3.f : 1.f;
       const int s = uniform(max(least, (int)ceilf(i < 8 ? longest / (float)(i + 2) : work * (of_all / F::kSlots))));
-      const float pieces = sum([&](const Sequence &q) { return (float)q.tiles * (float)cuts_of(q, s); }) * c.G;
+      const float over = 1.f / (float)s, pieces = sum([&](const Sequence &q) { return (float)q.tiles * ceilf((float)q.steps * over); }) * c.G;
       const float t = time(pieces, fminf(longest, (float)s)) + F::kPerJoin;
       if (t < best) best = t, span = s;
     }
@@ -659,6 +659,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       for (int e = 0; e < D / 32; ++e) o[e] *= scale;
       m = to;
     }
+    __builtin_amdgcn_s_setprio(1);
     // The next block's scores under this one's weights (past the end, or out of sight: for nothing)
     score(next, slot ^ 1);
     half8 hi[2 * kParts], lo[WIDE ? 2 * kParts : 1];
@@ -683,6 +684,28 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
         o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, hi[t], o[e], 0, 0, 0);
         if constexpr (WIDE) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo[t], o[e], 0, 0, 0);
       }
+    if constexpr (!FEW) {
+      // The order of what comes before, as far as operands allow: keys read eight operands ahead, two products of scores with 6 (D = 64: 12) other instructions and 2 (5) exponentials beside them, one of results with 4 and
+      // 1.  us of 8 prompts of 2048 to 4096 (32 heads x 128) / a chunk of 512 behind some 58 000 keys: 928 / 478, with four products in a row 936 / 505, fewer instructions beside them
+      // 1005 / 530, left to the compiler 965 / 500; without the priority that the products' wavefront has over the other one of its SIMD 957 / 504, with neither 980 / 518
+      constexpr int kScores = kParts * D / 16, kResults = 2 * kParts * (D / 32) * (WIDE ? 2 : 1);
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);      // reads of LDS; 8: products, 2: other vector instructions, 0x400: exponentials
+#pragma unroll
+      for (int k = 0; k < kScores / 2; ++k) {
+        __builtin_amdgcn_sched_group_barrier(8, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(2, 100 / kScores, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 40 / kScores, 0);
+      }
+#pragma unroll
+      for (int k = 0; k < kResults; ++k) {
+        __builtin_amdgcn_sched_group_barrier(8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(2, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   if (total == 0) meanwhile();
