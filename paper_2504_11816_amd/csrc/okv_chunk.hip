@@ -81,7 +81,7 @@ __device__ __forceinline__ int sequence_of_row(const Rows &r, const int row) {  
   for (int b0 = 0; b0 < r.batch; b0 += 64) {
     const uint64_t ended = __ballot(b0 + lane < r.batch && r.starts[min(b0 + lane, r.batch - 1) + 1] <= row);
     b += __popcll(ended);
-    if (ended != ~0ull) break;
+    if (ended != ~(uint64_t)0) break;
   }
   return b < r.batch && r.starts[b] <= row ? b : -1;
 }
@@ -259,7 +259,7 @@ struct Sequence {
 struct Plan {                            // in the workspace, for more than 64 sequences; before each chunk of 64, and behind the last
   int span, unused;
   int pieces[OKV_CHUNK_MAX_BATCH / 64 + 1], cut_pieces[OKV_CHUNK_MAX_BATCH / 64 + 1], cut_tiles[OKV_CHUNK_MAX_BATCH / 64 + 1];
-  unsigned long long steps[OKV_CHUNK_MAX_BATCH / 64 + 1];      // of one head
+  uint64_t steps[OKV_CHUNK_MAX_BATCH / 64 + 1];      // of one head
 };
 constexpr int64_t kPlanBytes = 2048;
 static_assert(sizeof(Plan) <= kPlanBytes, "");
@@ -287,16 +287,6 @@ __device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, co
   q.tiles = (int)(((int64_t)q.n * c.R + F::kRows - 1) / F::kRows);
   if (q.tiles) q.steps = max(keys_of<F>(q.n, q.len, q.prefix, a.window, c.R, q.tiles - 1).total, 1);      // (an item without keys is a step, too: its rows are 0)
   return q;
-}
-template <class T>
-__device__ __forceinline__ T wave_scan(T x) {             // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const T other = __shfl_up(x, o);
-    if (lane >= o) x += other;
-  }
-  return x;
 }
 __device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { return (int)(((unsigned)q.steps + (unsigned)span - 1) / (unsigned)span); }
 
@@ -356,7 +346,7 @@ struct Chunk {
   }
   __device__ __forceinline__ int cut_tiles(const Pool &c, const Rows &r) const {      // of all sequences (before find())
     if (plan) return plan->cut_tiles[(r.batch + 63) / 64];
-    return uniform(__shfl(wave_scan(cuts_of(q, span) > 1 ? q.tiles * c.G : 0), 63));
+    return lane_value(wave_scan(cuts_of(q, span) > 1 ? q.tiles * c.G : 0), 63);
   }
   template <class T>
   __device__ __forceinline__ T first(const T (Plan::*before)[OKV_CHUNK_MAX_BATCH / 64 + 1]) const { return plan ? (plan->*before)[at] : 0; }
@@ -368,9 +358,8 @@ struct Piece {
   int slot;                              // of its results in the workspace, below 0: it is whole
   int cuts, cut, cut_tile, apart;        // pieces of the tile, and which one this is; the number of the tile among those that are cut; slots from a piece to the next
 };
-__device__ __forceinline__ int of_lane(const int x, const int lane) { return __builtin_amdgcn_readlane(x, lane); }
 __device__ __forceinline__ Sequence of_lane(const Sequence &q, const int lane) {
-  return {of_lane(q.first, lane), of_lane(q.n, lane), of_lane(q.s, lane), of_lane(q.len, lane), of_lane(q.prefix, lane), of_lane(q.tiles, lane), of_lane(q.steps, lane)};
+  return {lane_value(q.first, lane), lane_value(q.n, lane), lane_value(q.s, lane), lane_value(q.len, lane), lane_value(q.prefix, lane), lane_value(q.tiles, lane), lane_value(q.steps, lane)};
 }
 // Items of a sequence: the heads of a tile next to each other, so that those of a head are on the same XCD where they are a multiple of eight; tiles that see the most keys first
 __device__ __forceinline__ void set_item(Piece &p, const Pool &c, const int item) {
@@ -385,39 +374,38 @@ __device__ __forceinline__ bool piece_of(Piece &p, Chunk<F, FEW> &k, const Pool 
   const int cuts = cuts_of(k.q, k.span), mine = k.q.tiles * c.G * cuts, within_chunk = index - k.first(&Plan::pieces);
   const int upto = wave_scan(mine);
   const uint64_t ended = __ballot(upto <= within_chunk);
-  if (ended == ~0ull) return false;
+  if (ended == ~(uint64_t)0) return false;
   const int at = __popcll(ended);
   p.q = of_lane(k.q, at);
-  p.cuts = of_lane(cuts, at);
-  const int within = within_chunk - of_lane(upto - mine, at), items = p.q.tiles * c.G, cut = uniform(within / items);
+  p.cuts = lane_value(cuts, at);
+  const int within = within_chunk - lane_value(upto - mine, at), items = p.q.tiles * c.G, cut = uniform(within / items);
   set_item(p, c, within - cut * items);
   p.begin = uniform((int)((uint64_t)(unsigned)p.q.steps * (unsigned)cut / (unsigned)p.cuts));
   p.end = uniform((int)((uint64_t)(unsigned)p.q.steps * (unsigned)(cut + 1) / (unsigned)p.cuts));
   p.slot = -1;
   if (p.cuts > 1) {
     const int cut_mine = cuts > 1 ? mine : 0, cut_upto = wave_scan(cut_mine);
-    p.slot = k.first(&Plan::cut_pieces) + of_lane(cut_upto - cut_mine, at) + within;
+    p.slot = k.first(&Plan::cut_pieces) + lane_value(cut_upto - cut_mine, at) + within;
     p.cut = cut, p.apart = items;
     const int tiles_mine = cuts > 1 ? k.q.tiles * c.G : 0, tiles_upto = wave_scan(tiles_mine);
-    p.cut_tile = k.first(&Plan::cut_tiles) + of_lane(tiles_upto - tiles_mine, at) + within - cut * items;
+    p.cut_tile = k.first(&Plan::cut_tiles) + lane_value(tiles_upto - tiles_mine, at) + within - cut * items;
   }
   return true;
 }
 // Where step `step` of all tiles' lies: its sequence (its number: b), the tile (its rank: those that see the most keys first) and the step of the tile
 template <class F, bool FEW>
-__device__ __forceinline__ bool step_of(Sequence &q, int &b, int &rank, int &within, Chunk<F, FEW> &k, const Pool &c, const Rows &r, const Attend &a, const unsigned long long step) {
+__device__ __forceinline__ bool step_of(Sequence &q, int &b, int &rank, int &within, Chunk<F, FEW> &k, const Pool &c, const Rows &r, const Attend &a, const uint64_t step) {
   if (!k.find(c, r, a, &Plan::steps, step)) return false;
-  const unsigned long long mine = (unsigned long long)(unsigned)k.q.tiles * (unsigned)k.q.steps, within_chunk = step - k.first(&Plan::steps);
-  const unsigned long long upto = wave_scan(mine);
+  const uint64_t mine = (uint64_t)(unsigned)k.q.tiles * (unsigned)k.q.steps, within_chunk = step - k.first(&Plan::steps);
+  const uint64_t upto = wave_scan(mine);
   const uint64_t ended = __ballot(upto <= within_chunk);
-  if (ended == ~0ull) return false;
+  if (ended == ~(uint64_t)0) return false;
   const int at = __popcll(ended);
-  const unsigned long long before = upto - mine;
-  const unsigned long long rest = within_chunk - ((unsigned long long)(unsigned)of_lane((int)(before >> 32), at) << 32 | (unsigned)of_lane((int)before, at));
+  const uint64_t rest = within_chunk - lane_value(upto - mine, at);
   q = of_lane(k.q, at);
   b = k.b0 + at;
   rank = uniform((int)(rest / (unsigned)q.steps));
-  within = uniform((int)(rest - (unsigned long long)(unsigned)rank * (unsigned)q.steps));
+  within = uniform((int)(rest - (uint64_t)(unsigned)rank * (unsigned)q.steps));
   return true;
 }
 
@@ -453,7 +441,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pool c, Rows r, Atte
   for (int i = 0; i < kPlanEach; ++i) {                  // chunk 16 i + wave
     const int cuts = cuts_of(q[i], span), items = q[i].tiles * c.G, chunk = i * kPlanWaves + wave;
     const int pieces = wave_scan(items * cuts), cut_pieces = wave_scan(cuts > 1 ? items * cuts : 0), cut_tiles = wave_scan(cuts > 1 ? items : 0);
-    const unsigned long long steps = wave_scan((unsigned long long)(unsigned)q[i].tiles * (unsigned)q[i].steps);
+    const uint64_t steps = wave_scan((uint64_t)(unsigned)q[i].tiles * (unsigned)q[i].steps);
     if (lane == 63 && chunk < chunks) plan.pieces[chunk + 1] = pieces, plan.cut_pieces[chunk + 1] = cut_pieces, plan.cut_tiles[chunk + 1] = cut_tiles, plan.steps[chunk + 1] = steps;
   }
   __threadfence_block();
@@ -461,7 +449,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pool c, Rows r, Atte
   if (wave) return;
   const bool there = lane < chunks;
   const int pieces = wave_scan(there ? plan.pieces[lane + 1] : 0), cut_pieces = wave_scan(there ? plan.cut_pieces[lane + 1] : 0), cut_tiles = wave_scan(there ? plan.cut_tiles[lane + 1] : 0);
-  const unsigned long long steps = wave_scan(there ? plan.steps[lane + 1] : 0ull);
+  const uint64_t steps = wave_scan(there ? plan.steps[lane + 1] : (uint64_t)0);
   if (there) plan.pieces[lane + 1] = pieces, plan.cut_pieces[lane + 1] = cut_pieces, plan.cut_tiles[lane + 1] = cut_tiles, plan.steps[lane + 1] = steps;
   if (lane == 0) plan.span = span, plan.pieces[0] = plan.cut_pieces[0] = plan.cut_tiles[0] = 0, plan.steps[0] = 0;
 }
@@ -832,7 +820,7 @@ __global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgp
     const int stretch = uniform((int)blockIdx.x / c.G), g = (int)blockIdx.x - stretch * c.G;
     if (stretch >= F::stretches(c.G)) return;
     int b, rank;
-    const bool there = step_of(p.q, b, rank, p.begin, k, c, r, a, (unsigned long long)(unsigned)stretch * (unsigned)k.span);
+    const bool there = step_of(p.q, b, rank, p.begin, k, c, r, a, (uint64_t)(unsigned)stretch * (unsigned)k.span);
     p.g = g;
     if (threadIdx.x == 0) {                              // (the first stretch that begins in a tile says so)
       Cut one{};

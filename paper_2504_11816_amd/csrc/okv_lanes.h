@@ -52,4 +52,27 @@ __device__ __forceinline__ float row_sum(float v) {      // over the lane's row 
 }
 __device__ __forceinline__ float wave_sum(float v) { return row_sum(sum_with_lane_xor<16>(sum_with_lane_xor<32>(v))); }
 
+// The value that DPP control CTRL brings to each lane, 0 where it brings none; ROWS: the rows of 16 lanes that take it
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int brought(const int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t brought(const uint64_t v) { return (uint64_t)(uint32_t)brought<CTRL, ROWS>((int)(v >> 32)) << 32 | (uint32_t)brought<CTRL, ROWS>((int)v); }
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double brought(const double v) { return __builtin_bit_cast(double, brought<CTRL, ROWS>(__builtin_bit_cast(uint64_t, v))); }
+// Sums over the lanes up to each one, itself included: within rows of 16 (lanes 1, 2, 4 and 8 before), then the last lane of a row on to the next row, and lane 31 to the upper half
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v += brought<0x111>(v);
+  v += brought<0x112>(v);
+  v += brought<0x114>(v);
+  v += brought<0x118>(v);
+  v += brought<0x142, 0xa>(v);
+  return v + brought<0x143, 0xc>(v);
+}
+// Lane `from`'s value, in scalar registers
+__device__ __forceinline__ int lane_value(const int v, const int from) { return __builtin_amdgcn_readlane(v, from); }
+__device__ __forceinline__ uint64_t lane_value(const uint64_t v, const int from) { return (uint64_t)(uint32_t)lane_value((int)(v >> 32), from) << 32 | (uint32_t)lane_value((int)v, from); }
+__device__ __forceinline__ double lane_value(const double v, const int from) { return __builtin_bit_cast(double, lane_value(__builtin_bit_cast(uint64_t, v), from)); }
+__device__ __forceinline__ double wave_sum(const double v) { return lane_value(wave_scan(v), 63); }
+
 }  // namespace okv

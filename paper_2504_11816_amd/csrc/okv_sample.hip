@@ -233,63 +233,55 @@ __device__ __forceinline__ Turn turn_of(const Verify &a, const int b) {
   return t;
 }
 
-// Weights of the row that the next token is drawn from, kPart tokens at a time: a wavefront has kPart / 64 = 32 consecutive ones in each lane
+// Weights of the row that the next token is drawn from, kPart tokens at a time, 32 in each lane of a wavefront: four at a time side by side (to be added up), or one after the other (to find a
+// token; 64 lanes' 32 in a row are 64 lines a load)
 constexpr int kPart = 2048, kOfLane = kPart / 64;
+template <bool IN_A_ROW>
 struct Weights {
   float p[kOfLane], q[kOfLane];
-  int without;                           // place in the lane of the token that a certain draft takes off, -1: none
+  int without, i0;                       // the token that a certain draft takes off, -1: none; this lane's first
+  __device__ __forceinline__ static int place(const int i) { return IN_A_ROW ? i : i / 4 * 256 + i % 4; }      // of a lane's i-th behind its first
   __device__ __forceinline__ Weights(const Verify &a, const int b, const Turn &t, const int part) {
     const int64_t at = t.first + t.accepted;
-    const int i0 = part * kPart + (threadIdx.x & 63) * kOfLane, n = a.vocab - i0;
+    i0 = part * kPart + (int)(threadIdx.x & 63) * (IN_A_ROW ? kOfLane : 4);
     const bool rejected = t.accepted < t.n;
-    read(p, a.target + (at + b) * a.target_stride + i0, n);
-    if (rejected && a.draft) read(q, a.draft + at * a.draft_stride + i0, n);
+    read(p, a.target + (at + b) * a.target_stride + i0, a.vocab - i0);
+    if (rejected && a.draft) read(q, a.draft + at * a.draft_stride + i0, a.vocab - i0);
     else
 #pragma unroll
       for (int i = 0; i < kOfLane; ++i) q[i] = 0.f;
-    without = rejected && !a.draft ? a.drafts[at] - i0 : -1;
+    without = rejected && !a.draft ? a.drafts[at] : -1;
   }
   __device__ __forceinline__ static void read(float (&to)[kOfLane], const float *from, const int n) {
-    if (n >= kOfLane) {
 #pragma unroll
-      for (int i = 0; i < kOfLane / 4; ++i) {
-        const floatx4 v = reinterpret_cast<const floatx4 *>(from)[i];
+    for (int i = 0; i < kOfLane; i += 4) {
+      if (place(i) + 4 <= n) {
+        const floatx4 v = *reinterpret_cast<const floatx4 *>(from + place(i));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) to[4 * i + j] = v[j];
+        for (int j = 0; j < 4; ++j) to[i + j] = v[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[i + j] = place(i) + j < n ? from[place(i) + j] : 0.f;
       }
-      return;
     }
-#pragma unroll
-    for (int i = 0; i < kOfLane; ++i) to[i] = i < n ? from[i] : 0.f;
   }
   __device__ __forceinline__ static double counted(const double w) { return w > 0. && w < INFINITY ? w : 0.; }
-  __device__ __forceinline__ double one(const int i, const bool all) const { return counted(all ? p[i] : i == without ? 0. : (double)p[i] - (double)q[i]); }
+  __device__ __forceinline__ double one(const int i, const bool all) const { return counted(all ? p[i] : i0 + place(i) == without ? 0. : (double)p[i] - (double)q[i]); }
 };
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-// A part's sum over rest(), or over all()
-__device__ __forceinline__ double sum_of(const Weights &w, const bool all) {
+// A part's sum: of what the target has above the draft, or (all) of the target
+__device__ __forceinline__ double sum_of(const Verify &a, const int b, const Turn &t, const int part, const bool all) {
+  const Weights<false> w(a, b, t, part);
   double sum = 0.;
 #pragma unroll
   for (int i = 0; i < kOfLane; ++i) sum += w.one(i, all);
-  return wave_sum64(sum);
+  return wave_sum(sum);
 }
 // The first lane whose `mine` and those before it come to more than x less `before`, and the sum before it; should rounding leave none, the last that is not 0 (-1: all are)
 __device__ __forceinline__ int lane_of(const double mine, const double x, double &before) {
-  const int lane = threadIdx.x & 63;
-  double upto = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double other = __shfl_up(upto, o);
-    if (lane >= o) upto += other;
-  }
+  const double upto = wave_scan(mine);
   const uint64_t above = __ballot(mine > 0. && before + upto > x), some = __ballot(mine > 0.);
   const int at = above ? __ffsll((unsigned long long)above) - 1 : 63 - __clzll((long long)some);
-  if (above) before += __shfl(upto - mine, at);
-  else before += __shfl(upto, 63);
+  before += above ? lane_value(upto - mine, at) : lane_value(upto, 63);
   return above ? at : some ? at | 64 : -1;             // (| 64: of those so far)
 }
 // Where u lies among the parts' sums, by a wavefront: the part (-1: all sums are 0), the sum before it (below 0: rounding has left none, it is the last part with a weight and its last token),
@@ -302,7 +294,7 @@ __device__ __forceinline__ Place place_of(const double *sums, const int parts, c
   const int lane = threadIdx.x & 63;
   double total = 0.;
   for (int i = lane; i < parts; i += 64) total += sums[i];
-  Place p{-1, 0., (double)u * wave_sum64(total)};
+  Place p{-1, 0., (double)u * wave_sum(total)};
   for (int i0 = 0; i0 < parts; i0 += 64) {
     const int at = lane_of(i0 + lane < parts ? sums[i0 + lane] : 0., p.x, p.before);
     if (at < 0) continue;
@@ -313,7 +305,7 @@ __device__ __forceinline__ Place place_of(const double *sums, const int parts, c
   return p;
 }
 // The token in its part, by a wavefront that has the part's weights
-__device__ __forceinline__ int token_in(const Weights &w, const Place &p, const bool all) {
+__device__ __forceinline__ int token_in(const Weights<true> &w, const Place &p, const bool all) {
   double mine = 0.;
 #pragma unroll
   for (int i = 0; i < kOfLane; ++i) mine += w.one(i, all);
@@ -330,15 +322,30 @@ __device__ __forceinline__ int token_in(const Weights &w, const Place &p, const 
     before += v;
     if (v > 0. && !found) token = i, found = at < 64 && before > x;
   }
-  return p.part * kPart + (at & 63) * kOfLane + __shfl(token, at & 63);
+  return p.part * kPart + (at & 63) * kOfLane + lane_value(token, at & 63);
 }
-// The token that u draws, by a wavefront: rest and all are the parts' sums
-__device__ __forceinline__ int next_token(const Verify &a, const int b, const Turn &t, const double *rest, const double *all, const int parts, const float u) {
-  Place p = place_of(rest, parts, u);
+// The token that u draws, by a wavefront, from the parts' sums
+__device__ __forceinline__ int next_token(const Verify &a, const int b, const Turn &t, const double *sums, const int parts, const float u) {
+  Place p = place_of(sums, parts, u);
   const bool fallback = p.part < 0;
-  if (fallback) p = place_of(all, parts, u);
+  if (fallback) {                                        // nothing above the draft: from all of the target
+    double x = 0.;
+    for (int part = 0; part < parts; ++part) x += sum_of(a, b, t, part, true);
+    p.x = (double)u * x, p.before = 0.;
+    int last = -1;
+    for (int part = 0; part < parts; ++part) {
+      const double sum = sum_of(a, b, t, part, true);
+      if (sum > 0.) last = part;
+      if (sum > 0. && p.before + sum > p.x) {
+        p.part = part;
+        break;
+      }
+      p.before += sum;
+    }
+    if (p.part < 0) p.part = last, p.before = -1.;
+  }
   if (p.part < 0) return -1;
-  const Weights w(a, b, t, p.part);
+  const Weights<true> w(a, b, t, p.part);
   return token_in(w, p, fallback);
 }
 __device__ __forceinline__ void write_tokens(const Verify &a, const int b, const Turn &t, const int token) {
@@ -350,32 +357,30 @@ __device__ __forceinline__ void write_tokens(const Verify &a, const int b, const
   }
 }
 
-// A workgroup per sequence, a wavefront per part: few tokens, in one launch
-constexpr int kOneWaves = 16;
+// A workgroup per sequence, in one launch: few tokens
+constexpr int kOneWaves = 8, kOneParts = 16;
 __global__ void __launch_bounds__(64 * kOneWaves) verify_kernel(Verify a) {
-  __shared__ double sums[2][kOneWaves];
+  __shared__ double sums[kOneParts];
   const int b = blockIdx.x, wave = threadIdx.x >> 6, parts = (a.vocab + kPart - 1) / kPart;
   const Turn t = turn_of(a, b);
   const float u = a.uniforms[t.first + b + t.n];
-  if (wave < parts) {
-    const Weights w(a, b, t, wave);
-    const double rest = sum_of(w, false), all = sum_of(w, true);
-    if ((threadIdx.x & 63) == 0) sums[0][wave] = rest, sums[1][wave] = all;
+  for (int part = wave; part < parts; part += kOneWaves) {
+    const double sum = sum_of(a, b, t, part, false);
+    if ((threadIdx.x & 63) == 0) sums[part] = sum;
   }
   __syncthreads();
-  if (wave == 0) write_tokens(a, b, t, next_token(a, b, t, sums[0], sums[1], parts, u));
+  if (wave == 0) write_tokens(a, b, t, next_token(a, b, t, sums, parts, u));
 }
 
-// Many tokens: a wavefront per part of every sequence, then one per sequence.  sums [batch][2][parts]
+// Many tokens: a wavefront per part of every sequence, then one per sequence.  sums [batch][parts]
 constexpr int kPartWaves = 4;
 __global__ void __launch_bounds__(64 * kPartWaves) parts_kernel(Verify a, double *sums) {
   const int b = blockIdx.y, part = blockIdx.x * kPartWaves + (threadIdx.x >> 6), parts = (a.vocab + kPart - 1) / kPart;
   if (part >= parts) return;
   const Turn t = turn_of(a, b);
-  const Weights w(a, b, t, part);
-  const double rest = sum_of(w, false), all = sum_of(w, true);
+  const double sum = sum_of(a, b, t, part, false);
   if ((threadIdx.x & 63) == 0) {
-    sums[((int64_t)b * 2) * parts + part] = rest, sums[((int64_t)b * 2 + 1) * parts + part] = all;
+    sums[(int64_t)b * parts + part] = sum;
     if (part == 0) a.accepted[b] = t.accepted;
   }
 }
@@ -384,8 +389,7 @@ __global__ void __launch_bounds__(64) token_kernel(Verify a, const double *sums)
   Turn t = rows_of(a, b);
   t.accepted = min(max(a.accepted[b], 0), t.n);
   const float u = a.uniforms[t.first + b + t.n];
-  sums += (int64_t)b * 2 * parts;
-  write_tokens(a, b, t, next_token(a, b, t, sums, sums + parts, parts, u));
+  write_tokens(a, b, t, next_token(a, b, t, sums + (int64_t)b * parts, parts, u));
 }
 
 bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -442,7 +446,7 @@ int okv_token_probs(const void *logits, int32_t dtype, int64_t stride, const flo
 int64_t okv_verify_workspace_bytes(int32_t max_batch, int32_t vocab) {
   if (max_batch < 0 || max_batch > OKV_VERIFY_MAX_BATCH || vocab < 1 || vocab > OKV_SAMPLE_MAX_VOCAB)
     return report(OKV_EINVAL, "okv_verify_workspace_bytes: batch must be in [0, 4096] and vocab in [1, 2^24]");
-  return (int64_t)max_batch * ((vocab + kPart - 1) / kPart) * 2 * 8;
+  return (int64_t)max_batch * ((vocab + kPart - 1) / kPart) * 8;
 }
 
 int okv_verify(const float *target, int64_t target_stride, const float *draft_probs, int64_t draft_stride, const int32_t *drafts, const int32_t *starts,
@@ -462,7 +466,7 @@ int okv_verify(const float *target, int64_t target_stride, const float *draft_pr
   Verify a{target, draft_probs, target_stride, draft_stride, drafts, starts, uniforms, tokens, accepted, rejected, batch, n_rows, vocab};
   const int32_t parts = (vocab + kPart - 1) / kPart;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (parts <= kOneWaves) {
+  if (parts <= kOneParts) {
     hipLaunchKernelGGL(verify_kernel, dim3((unsigned)batch), dim3(64 * kOneWaves), 0, s, a);
   } else {
     hipLaunchKernelGGL(parts_kernel, dim3((unsigned)((parts + kPartWaves - 1) / kPartWaves), (unsigned)batch), dim3(64 * kPartWaves), 0, s, a, static_cast<double *>(workspace));
