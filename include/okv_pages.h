@@ -92,7 +92,8 @@ int okv_pages_fork(const okv_pages *p, int32_t n, const int32_t *src, const int3
 int okv_pages_free(const okv_pages *p, int32_t n, const int32_t *seqs, void *stream);
 
 /* Sequence seqs[i] loses its last n_drop[i] >= 0 tokens (drafted ones that were rejected); pages that no token of it is in any longer
- * belong to it no more.  OKV_ESTATE, and nothing changes, where a sequence has fewer tokens, where the page that its new last token leaves partly
+ * belong to it no more.  Nothing is done while status[0] and status[3] both hold a code (the tokens that are to go
+ * were never added).  OKV_ESTATE, and nothing changes, where a sequence has fewer tokens, where the page that its new last token leaves partly
  * filled is shared (a shared page is full), and where a row array no longer holds the rows of a group that becomes partly filled (with rows = 32: the
  * new length is no multiple of 32 and lies below the last one that the old length has passed).
  *   seqs [n] distinct, or NULL: i;  n_drop [n] */

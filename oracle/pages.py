@@ -73,6 +73,8 @@ class Model:
 
     def shrink(self, seqs, n_drop, row_counts=()):
         """row_counts: the rows of a group of each row array."""
+        if self.refused and self.status:
+            return
         for s, n in zip(seqs, n_drop):
             if not 0 <= s < len(self.lens) or n <= 0:
                 continue

@@ -134,12 +134,21 @@ class Cache16:
             raise ValueError(f"out must be a contiguous fp16 or fp32 tensor {list(q.shape)} on {device}")
         at = self._whose(layer, rows, starts, lens, seqs)
         a = self._chunk
-        if slopes is not None:
-            need("slopes", slopes, torch.float32, (self.H,), device)
-        if prefix is not None and (prefix.dtype is not torch.int32 or prefix.dim() != 1 or not prefix.is_contiguous() or prefix.device != device
-                                   or prefix.shape[0] < (self._rows.batch if seqs is None else self.max_seqs)):
-            raise ValueError(f"prefix must be an int32 vector on {device} with an entry per row of the table (per sequence where seqs is None)")
+        if slopes is not None or prefix is not None:
+            self._vectors(slopes, prefix, self._rows.batch if seqs is None else self.max_seqs)
         a.scale, a.cap, a.window, a.slopes, a.prefix, a.out_dtype = scale, cap, window, _address(slopes), _address(prefix), out.dtype is torch.float32
         rc = self._attend(at, self._rows_ref, self._chunk_ref, q.data_ptr(), q_stride, out.data_ptr(), binding.current_stream(device))
         if rc:
             binding._check(rc)
+
+    def _vectors(self, slopes, prefix, entries):
+        if slopes is not None:
+            need("slopes", slopes, torch.float32, (self.H,), self.device)
+        if prefix is not None and (prefix.dtype is not torch.int32 or prefix.dim() != 1 or not prefix.is_contiguous() or prefix.device != self.device or prefix.shape[0] < entries):
+            raise ValueError(f"prefix must be an int32 vector on {self.device} with an entry per row of the table (per sequence where seqs is None)")
+
+    def check_how(self, scale=0.0, cap=0.0, window=0, slopes=None, prefix=None):
+        """Raises unless attend() takes these, with sequences by their rows of the table."""
+        if not (0 <= scale < math.inf and 0 <= cap < math.inf and 0 <= window < 1 << 31):
+            raise ValueError("scale and cap must be finite and not negative, window too")
+        self._vectors(slopes, prefix, self.max_seqs)

@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(kMoveThreads) free_kernel(State s, const int32
 // Whether the call fits the state, a thread per sequence; then the pages, a wavefront per sequence
 __global__ void __launch_bounds__(kThreads) shrink_kernel(State s, const int32_t *seqs, const int32_t *n_drop, int n, RowCounts tails) {
   __shared__ int bad;
+  if (s.status[0] != 0 && s.status[3] != 0) return;      // the tokens that are to go never came
   if (threadIdx.x == 0) bad = 0;
   __syncthreads();
   for (int j = threadIdx.x; j < n; j += kThreads) {

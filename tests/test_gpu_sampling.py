@@ -304,6 +304,20 @@ def test_rows_beside_pages():
     p.do("shrink", [0], [3])
 
 
+def test_nothing_is_taken_back_that_was_refused():
+    """A step whose pages could not be taken added nothing: giving its rejected tokens back must not shorten what was there."""
+    p = Shrunk(n_pages=4)
+    p.do("extend", [0, 1], [20, 30])
+    p.do("extend", [0, 1], [5, 5])                           # no page is left for both
+    assert p.model.status == binding.OKV_ENOSPC
+    p.do("shrink", [0, 1], [4, 2])
+    assert p.lens.tolist()[:2] == [20, 30]
+    with pytest.raises(binding.OkvError):
+        p.pages.check()
+    p.model.status, p.model.refused = 0, False
+    p.do("shrink", [0, 1], [4, 2])
+
+
 def test_many_sequences_shrink_at_once():
     rng = np.random.default_rng(0)
     p = Shrunk(S=1500, width=5, n_pages=7000)

@@ -1,0 +1,195 @@
+"""Whole decoder layers over the fp16 cache with several tokens a sequence, a speculative step made of the new calls, and the example that serves with them.
+
+Tolerance of whole layers as for one token a sequence: a different rounding decision at one fp16 store moves a value by 2^-11 relative, and four products and two norms follow one
+another: 1.5e-2 + 1.5e-2 |oracle| against the oracle that rounds to fp16 where the GPU stores fp16."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import chunk as oracle
+from oracle import decode_layer as dl
+from oracle import linear4 as oracle4
+from paper_2504_11816_amd.cache16 import Cache16, Rope
+from paper_2504_11816_amd.compressed import CompressedLayer, Scratch, decoder_chunk
+from paper_2504_11816_amd.harness import LayerWeights
+from paper_2504_11816_amd.sampling import Sampler
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def ids(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+
+
+def starts_of(n):
+    return ids(np.concatenate([[0], np.cumsum(n)]))
+
+
+H, G, D, H2 = 8, 2, 64, 1024
+H1, KV = H * D, G * D
+
+
+def cache(L=1, **kw):
+    return Cache16(**{**dict(n_layers=L, n_q_heads=H, n_kv_heads=G, head_dim=D, page_tokens=32, n_pages=40, max_seqs=4, max_pages_per_seq=8, device=DEV), **kw})
+
+
+@pytest.mark.parametrize("how", [dict(), dict(window=20, prefix=True), dict(cap=8.0), dict(turned=False)], ids=str)
+def test_decoder_layers_against_the_definition(how):
+    """A prompt in two chunks beside a token at a time, then drafts that are partly given back, against the same tokens in 64 bits."""
+    how = dict(how)
+    rng = np.random.default_rng(3)
+    turned = how.pop("turned", True)
+    if how.pop("prefix", False):
+        how["prefix"] = ids([0, 3, 5, 2])
+    prefix_of = how["prefix"].tolist() if "prefix" in how else [0] * 4
+    w = LayerWeights(H1, H2, 5, 0, DEV, kv_cols=KV)
+    layers, c, scratch = [CompressedLayer(w)], cache(), Scratch(128, H1, H2, KV, DEV)
+    rope = Rope.of(D, device=DEV) if turned else None
+    freq = 10000.0 ** (-np.arange(0, D, 2) / D) if turned else np.zeros(0)
+    p = w.numpy()
+    stacked = oracle4.quantise(w.wqkv.cpu().numpy(), 128, False)
+    p.update(wq=stacked[:H1], wk=stacked[H1:H1 + KV], wv=stacked[H1 + KV:])
+    p.update({n: oracle4.quantise(w.t[n].cpu().numpy(), 128, False) for n in ("wo", "w1", "w2")})
+    seqs, held = [2, 0, 3], [[np.zeros((0, G, D)), np.zeros((0, G, D))] for _ in range(3)]
+    for n, drop in (([40, 1, 0], [0, 0, 0]), ([33, 1, 70], [0, 0, 0]), ([5, 5, 5], [2, 5, 0]), ([1, 4, 2], [1, 0, 2]), ([3, 3, 3], [0, 0, 0])):
+        first = rng.standard_normal((sum(n), H1)).astype(np.float16)
+        x = torch.tensor(first).to(DEV)
+        decoder_chunk(c, layers, scratch, x, starts_of(n), ids(seqs), ids(n), rope=rope, **how)
+        q, k, v = dl.qkv(first.astype(np.float64), p, fp16_between=True)
+        t, row = np.empty((sum(n), H1)), 0
+        for b, m in enumerate(n):
+            pos = len(held[b][0]) + np.arange(m)
+            kb = dl.round16(oracle.rotate(k[row:row + m].reshape(m, G, D), pos, freq, False))
+            qb = dl.round16(oracle.rotate(q[row:row + m].reshape(m, H, D), pos, freq, False))
+            held[b] = [np.concatenate([held[b][0], kb]), np.concatenate([held[b][1], v[row:row + m].reshape(m, G, D)])]
+            for j in range(m):
+                for h in range(H):
+                    g = h // (H // G)
+                    t[row + j, h * D:(h + 1) * D] = oracle.attend(qb[j, h], held[b][0][:, g], held[b][1][:, g], pos[j], cap=how.get("cap", 0.0), window=how.get("window", 0),
+                                                                  prefix=min(prefix_of[seqs[b]], len(held[b][0])))[0]
+            row += m
+        want = dl.after_attention(first.astype(np.float64), dl.round16(t), p, fp16_between=True)
+        got = x.double().cpu().numpy()
+        assert np.isfinite(got).all() and (np.abs(got - want) <= 1.5e-2 + 1.5e-2 * np.abs(want)).all(), n
+        c.pages.shrink(ids(seqs), ids(drop))
+        held = [[y[:len(y) - m] for y in kv] for kv, m in zip(held, drop)]
+    c.pages.check()
+    assert [c.lens.tolist()[s] for s in seqs] == [len(kv[0]) for kv in held]
+    assert int((c.refs > 0).sum()) == sum(-(-len(kv[0]) // 32) for kv in held)
+
+
+def test_a_captured_step_of_drafts():
+    """Chunk, probabilities, verification and giving back in one graph, replayed with eager work between, against the calls one by one."""
+    V, B, k, L = 512, 3, 3, 2
+    layers = [CompressedLayer(LayerWeights(H1, H2, 7, l, DEV, kv_cols=KV)) for l in range(L)]
+    scratch, rope = Scratch(64, H1, H2, KV, DEV), Rope.of(D, device=DEV)
+    head = torch.randn((H1, V), device=DEV).half()
+    starts, drafts_at, n_new = ids(np.arange(B + 1) * (k + 1)), ids(np.arange(B + 1) * k), ids([k + 1] * B)
+    seqs, u, drafts = ids([3, 0, 2]), torch.rand(B * (k + 1), device=DEV), torch.randint(0, V, (B * k,), device=DEV).int()
+    first = torch.randn((B * (k + 1), H1), device=DEV).half()
+    sampler = Sampler(max_batch=B * (k + 1), vocab=V, device=DEV)
+
+    def make():
+        c = cache(L)
+        c.pages.extend(seqs, ids([31, 5, 0]))
+        c.pool.normal_(generator=torch.Generator(device=DEV).manual_seed(4))
+        return c, [torch.empty(n, dtype=torch.int32, device=DEV) for n in (B * (k + 1), B, B)], torch.empty((B * (k + 1), V), device=DEV), torch.empty_like(first)
+
+    def step(c, out, p, x):
+        x.copy_(first)
+        decoder_chunk(c, layers, scratch, x, starts, seqs, n_new, rope=rope)
+        sampler.probs((x @ head * 0.02).float(), p)
+        p.clamp_(min=1e-4)
+        sampler.verify(p, drafts, drafts_at, u, *out)
+        c.pages.shrink(seqs, out[2])
+
+    eager, captured = make(), make()
+    step(*make())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*captured)
+    for i in range(5):
+        g = torch.Generator(device=DEV).manual_seed(i)
+        first.copy_(torch.randn(first.shape, generator=g, device=DEV))
+        u.copy_(torch.rand(u.shape, generator=g, device=DEV))
+        u[::4] *= 1e-3                                        # (the first draft is accepted now and then)
+        graph.replay()
+        torch.randn(1 << 14, device=DEV).sum().item()
+        step(*eager)
+        for a, b in zip(eager[1], captured[1]):
+            assert torch.equal(a, b), i
+        assert torch.equal(eager[2], captured[2]) and torch.equal(eager[3], captured[3])
+        for name in ("lens", "table", "refs", "pool"):
+            assert torch.equal(getattr(eager[0], name), getattr(captured[0], name)), (i, name)
+    eager[0].pages.check()
+    assert len(set(eager[0].lens.tolist())) > 2
+
+
+def test_steps_that_do_not_fit_change_nothing():
+    w = [CompressedLayer(LayerWeights(H1, H2, 5, 0, DEV, kv_cols=KV))]
+    c, scratch, x = cache(), Scratch(16, H1, H2, KV, DEV), torch.randn((6, H1), device=DEV).half()
+    c.pages.extend(ids([0, 1]), ids([10, 20]))
+    good = dict(cache=c, layers=w, scratch=scratch, x=x, starts=ids([0, 2, 6]), seqs=ids([1, 0]), n_new=ids([2, 4]), rope=Rope.of(D, device=DEV))
+    before = [t.clone() for t in (c.pool, c.table, c.lens, c.refs)]
+    for bad in (dict(x=x.float()), dict(x=x[:, :128].contiguous()), dict(x=torch.empty((17, H1), dtype=torch.float16, device=DEV)), dict(x=x[:0]), dict(starts=ids([0, 2])), dict(starts=ids([0, 2, 6]).long()),
+                dict(seqs=ids([1])), dict(n_new=ids([1])), dict(n_new=ids([2, 4]).cpu()), dict(layers=[]), dict(layers=w * 2), dict(scratch=Scratch(16, 2 * H1, H2, KV, DEV)), dict(rope=Rope.of(128, device=DEV)),
+                dict(cap=-1.0), dict(cap=float("nan")), dict(window=-1), dict(scale=float("inf")), dict(slopes=torch.ones(3, device=DEV)), dict(prefix=ids([1]))):
+        with pytest.raises(ValueError):
+            decoder_chunk(**{**good, **bad})
+        assert all(torch.equal(a, b) for a, b in zip(before, (c.pool, c.table, c.lens, c.refs)))
+    decoder_chunk(**good)
+    assert c.lens.tolist()[:2] == [14, 22]
+
+
+def test_pages_that_are_short_leave_the_cache_as_it_was():
+    w = [CompressedLayer(LayerWeights(H1, H2, 5, 0, DEV, kv_cols=KV))]
+    c, scratch, x = cache(n_pages=3), Scratch(80, H1, H2, KV, DEV), torch.randn((80, H1), device=DEV).half()
+    c.pages.extend(ids([0, 1]), ids([32, 20]))
+    before = [t.clone() for t in (c.pool, c.table, c.lens, c.refs)]
+    for _ in range(2):
+        decoder_chunk(c, w, scratch, x, ids([0, 40, 80]), ids([0, 1]), ids([40, 40]))
+        assert all(torch.equal(a, b) for a, b in zip(before, (c.pool, c.table, c.lens, c.refs)))
+    with pytest.raises(Exception, match="no room"):
+        c.pages.check()
+    decoder_chunk(c, w, scratch, x[:10].contiguous(), ids([0, 10]), ids([1]), ids([10]))
+    c.pages.check()
+    assert c.lens.tolist()[:2] == [32, 30]
+
+
+def load():
+    spec = importlib.util.spec_from_file_location("serve_speculative", os.path.join(ROOT, "examples", "serve_speculative.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+@pytest.mark.parametrize("window", (0, 64))
+def test_the_example(window):
+    """Runs, and both caches hold what the tokens by themselves give (in one chunk of a fresh cache): rows that were rejected have left no trace."""
+    r = load().serve(prompts=3, drafts=3, steps=6, layers=2, draft_layers=1, longest=150, window=window)
+    assert 0 < sum(len(a) for a in r["answers"]) == r["accepted"] + 18
+    for c in (r["target"], r["draft"]):
+        for b in range(3):
+            tokens = torch.tensor([*r["prompts"][b], *r["answers"][b]][:-1], device=DEV)
+            n = len(tokens)
+            assert int(c.lens[b]) == n
+            fresh = Cache16(n_layers=c.L, n_q_heads=c.H, n_kv_heads=c.G, head_dim=c.d, page_tokens=c.T, n_pages=8, max_seqs=1, max_pages_per_seq=8, device=DEV)
+            x = r["embed"][tokens]
+            decoder_chunk(fresh, r["model"][:c.L], Scratch(n, x.shape[1], 4096, c.G * c.d, DEV), x, ids([0, n]), ids([0]), ids([n]), rope=r["rope"], window=window)
+            pages = -(-n // c.T)
+            a, z = c.pool[:, c.table[b, :pages].long()].float(), fresh.pool[:, fresh.table[0, :pages].long()].float()
+            # rows behind the last token: of rejected tokens in one, none in the other
+            slot = torch.arange(pages * c.T, device=DEV).view(pages, -1, 16)
+            there = (slot < n).view(1, pages, -1, 1, 1, 16, 1)
+            shape = (c.L, pages, c.T // 16, 2, c.G, 16, c.d)      # (a slab of a tile, or several tiles of few heads: heads and tiles are in the same places in both)
+            if c.pages.arrays[0].c.unit_tokens == 16:
+                a, z = a.view(shape) * there, z.view(shape) * there
+            else:
+                full = n // c.T
+                a, z = a[:, :full], z[:, :full]
+            assert (a - z).abs().max() <= 1.5e-2 * 4 + 1.5e-2 * z.abs().max()
