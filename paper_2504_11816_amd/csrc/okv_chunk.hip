@@ -184,7 +184,7 @@ struct Form {
   // How keys are cut (see Plan): workgroups that run at a time, and in steps what a piece costs beside its own, what joining does, and what is never cut
   static constexpr int kSlots = 512, kUncut = 512 / kStep, kLeast = 256 / kStep;
   static constexpr float kPerPiece = FEW ? 1.f : 4.f, kPerJoin = FEW ? 3.f : 10.f;
-  static constexpr int kPieces = 1024;                  // that steps come to at most, where tiles are cut into equal pieces
+  static constexpr int kPieces = 512;                   // that steps come to at most, where tiles are cut into equal pieces
   __host__ __device__ static int stretches(const int G) { return kSlots / G > 1 ? kSlots / G : 1; }
   __host__ __device__ static int64_t parts(const int G) { return 2 * (FEW ? (int64_t)stretches(G) * G : (int64_t)kPieces); }      // results of pieces
 };
@@ -292,32 +292,34 @@ __device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { retu
 
 // The span that is expected to take the least time, kNone: nothing is cut.  P pieces of up to s steps (W in all) on kSlots workgroups at a time take s + kPerPiece where P <= kSlots, else
 // (W + P kPerPiece) / kSlots and half a piece until the last one has ended; kPerJoin is added where any are cut.  sum(f) and most(f): over all sequences.
-template <class F, bool FEW, class Sum, class Most>
-__device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum &sum, const Most &most) {
+// pieces_at(s, work, items): how many with spans of s, a lane a span.
+template <class F, bool FEW, class Sum, class Most, class PiecesAt>
+__device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum &sum, const Most &most, const PiecesAt &pieces_at) {
   if (!a.may_cut) return kNone;
   const float work = sum([](const Sequence &q) { return (float)q.tiles * (float)q.steps; }) * c.G, items = sum([](const Sequence &q) { return (float)q.tiles; }) * c.G;
   const float longest = most([](const Sequence &q) { return (float)q.steps; });
   auto time = [&](const float pieces, const float s) {
     return pieces <= F::kSlots ? s + F::kPerPiece : (work + pieces * F::kPerPiece) * (1.f / F::kSlots) + .5f * (s + F::kPerPiece);
   };
-  float best = time(items, longest);
-  int span = kNone;
+  const float best = time(items, longest);
   if constexpr (FEW) {
     const float stretches = (float)F::stretches(c.G), even = fmaxf(ceilf(work * 1.0001f / (stretches * c.G)), (float)F::kLeast);
-    if (longest > F::kUncut && even + (items / (stretches * c.G) + 1.f) * F::kPerPiece + F::kPerJoin < best) span = (int)fminf(even, 1e9f);
+    if (longest > F::kUncut && even + (items / (stretches * c.G) + 1.f) * F::kPerPiece + F::kPerJoin < best) return uniform((int)fminf(even, 1e9f));
+    return kNone;
   } else {
-    const int least = max(1, (int)fminf(ceilf(work * (1.0001f / F::kPieces)), 1e9f));
-    if (best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return span;
-    for (int i = 0; i < 12; ++i) {
-      const float of_all = i == 8 ? .5f : i == 9 ? 1.f / 1.5f : i == 10 ? 1.f / 3.f : 1.f;
-      const int s = uniform(max(least, (int)ceilf(i < 8 ? longest / (float)(i + 2) : work * (of_all / F::kSlots))));
-      const float over = 1.f / (float)s, pieces = sum([&](const Sequence &q) { return (float)q.tiles * ceilf((float)q.steps * over); }) * c.G;
-      const float t = time(pieces, fminf(longest, (float)s)) + F::kPerJoin;
-      if (t < best) best = t, span = s;
-    }
+    if (best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return kNone;
+    // a lane a span: the longest item in 2 .. 49 pieces, and from a fourth to four times an even share
+    const int lane = threadIdx.x & 63;
+    const float least = fmaxf(1.f, ceilf(work * (1.0001f / F::kPieces)));
+    const float s = fminf(fmaxf(ceilf(lane < 48 ? longest / (float)(lane + 2) : work * ((float)(lane - 47) * .25f / F::kSlots)), least), 1e9f);
+    const float pieces = pieces_at(s, work, items);
+    const float mine = time(pieces, fminf(longest, s)) + F::kPerJoin, shortest = -wave_max(-mine);
+    if (!(shortest < best)) return kNone;
+    return __builtin_amdgcn_readlane((int)s, __ffsll((unsigned long long)__ballot(mine == shortest)) - 1);
   }
-  return uniform(span);
 }
+
+__device__ __forceinline__ float about(const float s, const float work, const float items) { return fmaxf(items, work / s + .5f * items); }      // pieces, on the average
 
 // The chunk of 64 sequences with the index-th of what `before` counts, a lane a sequence
 template <class F, bool FEW>
@@ -332,7 +334,13 @@ struct Chunk {
       return;
     }
     q = sequence_at<F>(c, r, a, threadIdx.x & 63);
-    span = span_of<F, FEW>(c, a, [&](const auto &f) { return wave_sum(f(q)); }, [&](const auto &f) { return wave_max(f(q)); });
+    span = span_of<F, FEW>(c, a, [&](const auto &f) { return wave_sum(f(q)); }, [&](const auto &f) { return wave_max(f(q)); }, [&](const float s, const float work, const float items) {
+      if (r.batch > 16) return about(s, work, items);
+      const float over = 1.f / s;
+      float pieces = 0.f;
+      for (int b = 0; b < r.batch; ++b) pieces += (float)lane_value(q.tiles, b) * ceilf((float)lane_value(q.steps, b) * over);
+      return pieces * c.G;
+    });
   }
   template <class T>
   __device__ __forceinline__ bool find(const Pool &c, const Rows &r, const Attend &a, const T (Plan::*before)[OKV_CHUNK_MAX_BATCH / 64 + 1], const T index) {
@@ -367,6 +375,13 @@ __device__ __forceinline__ void set_item(Piece &p, const Pool &c, const int item
   p.g = item - rank * c.G;
   p.tile = p.q.tiles - 1 - rank;
 }
+// all part / parts, rounded down; in 32 bits where they suffice (a division of 64 is 150 instructions)
+__device__ __forceinline__ int share(const int all, const int part, const int parts) {
+  if (all == parts) return part;
+  if (parts == 1) return part ? all : 0;
+  if ((unsigned)all < 65536u && (unsigned)part < 65536u) return uniform((int)((unsigned)all * (unsigned)part / (unsigned)parts));
+  return uniform((int)((uint64_t)(unsigned)all * (unsigned)part / (unsigned)parts));
+}
 // The index-th piece, where items are whole or cut into equal pieces.  A sequence's first cuts come first: tiles read the same keys together
 template <class F, bool FEW>
 __device__ __forceinline__ bool piece_of(Piece &p, Chunk<F, FEW> &k, const Pool &c, const Rows &r, const Attend &a, const int index) {
@@ -380,8 +395,7 @@ __device__ __forceinline__ bool piece_of(Piece &p, Chunk<F, FEW> &k, const Pool 
   p.cuts = lane_value(cuts, at);
   const int within = within_chunk - lane_value(upto - mine, at), items = p.q.tiles * c.G, cut = uniform(within / items);
   set_item(p, c, within - cut * items);
-  p.begin = uniform((int)((uint64_t)(unsigned)p.q.steps * (unsigned)cut / (unsigned)p.cuts));
-  p.end = uniform((int)((uint64_t)(unsigned)p.q.steps * (unsigned)(cut + 1) / (unsigned)p.cuts));
+  p.begin = share(p.q.steps, cut, p.cuts), p.end = share(p.q.steps, cut + 1, p.cuts);
   p.slot = -1;
   if (p.cuts > 1) {
     const int cut_mine = cuts > 1 ? mine : 0, cut_upto = wave_scan(cut_mine);
@@ -435,7 +449,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pool c, Rows r, Atte
     for (int i = 0; i < kPlanEach; ++i) x = largest ? fmaxf(x, f(q[i])) : x + f(q[i]);
     return all(x, largest);
   };
-  const int span = span_of<F, FEW>(c, a, [&](const auto &f) { return each(f, false); }, [&](const auto &f) { return each(f, true); });
+  const int span = span_of<F, FEW>(c, a, [&](const auto &f) { return each(f, false); }, [&](const auto &f) { return each(f, true); }, about);
   Plan &plan = *a.plan;
 #pragma unroll
   for (int i = 0; i < kPlanEach; ++i) {                  // chunk 16 i + wave
@@ -480,8 +494,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
   Keys keys = keys_of<F>(p.n, p.len, p.prefix, a.window, c.R, piece.tile);
   keys.ahead = uniform(keys.ahead), keys.first = uniform(keys.first), keys.total = uniform(keys.total);
   const bool whole_tile = piece.slot < 0;
-  const int i0 = whole_tile ? 0 : uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)piece.begin / (unsigned)p.steps));
-  const int total = whole_tile ? keys.total : uniform((int)((uint64_t)(unsigned)keys.total * (unsigned)piece.end / (unsigned)p.steps)) - i0;
+  const int i0 = whole_tile ? 0 : share(keys.total, piece.begin, p.steps), total = whole_tile ? keys.total : share(keys.total, piece.end, p.steps) - i0;
   auto key_at_step = [&](const int i) {                // this wavefront's first key of a step; past the end: the last again
     const int j = i0 + min(i, total - 1);
     return (j < keys.ahead ? j : keys.first + j - keys.ahead) * F::kStep + (FEW ? wave * kKeys : 0);
