@@ -183,7 +183,7 @@ struct Form {
   static constexpr int kPartFloats = kRows * (D + 2);
   // How keys are cut (see Plan): workgroups that run at a time, and in steps what a piece costs beside its own, what joining does, and what is never cut
   static constexpr int kSlots = 512, kUncut = 512 / kStep, kLeast = 256 / kStep;
-  static constexpr float kPerPiece = FEW ? 1.f : 4.f, kPerJoin = FEW ? 3.f : 10.f;
+  static constexpr float kPerPiece = FEW ? 1.f : 6.f, kPerJoin = FEW ? 3.f : 6.f;
   static constexpr int kPieces = 512;                   // that steps come to at most, where tiles are cut into equal pieces
   __host__ __device__ static int stretches(const int G) { return kSlots / G > 1 ? kSlots / G : 1; }
   __host__ __device__ static int64_t parts(const int G) { return 2 * (FEW ? (int64_t)stretches(G) * G : (int64_t)kPieces); }      // results of pieces
@@ -290,16 +290,18 @@ __device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, co
 }
 __device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { return (int)(((unsigned)q.steps + (unsigned)span - 1) / (unsigned)span); }
 
-// The span that is expected to take the least time, kNone: nothing is cut.  P pieces of up to s steps (W in all) on kSlots workgroups at a time take s + kPerPiece where P <= kSlots, else
-// (W + P kPerPiece) / kSlots and half a piece until the last one has ended; kPerJoin is added where any are cut.  sum(f) and most(f): over all sequences.
-// pieces_at(s, work, items): how many with spans of s, a lane a span.
+// The span that is expected to take the least time, kNone: nothing is cut.  P pieces of up to s steps (W in all) on kSlots workgroups at a time, two to a compute unit, take s + kPerPiece where
+// P <= kSlots, kAlone of that where each has a unit to itself, else (W + P kPerPiece) / kSlots and half a piece until the last one has ended; kPerJoin is added where any are cut.  us with kAlone .6 / 1: 8
+// sequences of 32 tokens 31.0 / 34.6, 5 of 33 to 301 (40 heads x 64) 37.0 / 40.5, 16 of 1 to 600 behind 6000 338 / 330; with kPerPiece 4 and kPerJoin 10, 1000 rows of 8 heads 54.9 (38.5).
+// sum(f) and most(f): over all sequences; pieces_at(s, work, items): how many with spans of s, a lane a span.
+constexpr float kAlone = .6f;
 template <class F, bool FEW, class Sum, class Most, class PiecesAt>
 __device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum &sum, const Most &most, const PiecesAt &pieces_at) {
   if (!a.may_cut) return kNone;
   const float work = sum([](const Sequence &q) { return (float)q.tiles * (float)q.steps; }) * c.G, items = sum([](const Sequence &q) { return (float)q.tiles; }) * c.G;
   const float longest = most([](const Sequence &q) { return (float)q.steps; });
   auto time = [&](const float pieces, const float s) {
-    return pieces <= F::kSlots ? s + F::kPerPiece : (work + pieces * F::kPerPiece) * (1.f / F::kSlots) + .5f * (s + F::kPerPiece);
+    return pieces <= F::kSlots / 2 ? kAlone * (s + F::kPerPiece) : pieces <= F::kSlots ? s + F::kPerPiece : (work + pieces * F::kPerPiece) * (1.f / F::kSlots) + .5f * (s + F::kPerPiece);
   };
   const float best = time(items, longest);
   if constexpr (FEW) {
