@@ -41,6 +41,7 @@ class Cache16:
 
     def __init__(self, *, n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_pages_per_seq, pool=None, table=None, device="cuda:0"):
         self.device = torch.empty(0, device=device).device      # "cuda" is the current device's "cuda:n", as its tensors say
+        self._index = self.device.index
         self.L, self.H, self.G, self.d, self.T, self.max_seqs = n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, max_seqs
         if n_layers < 1 or page_tokens < 16:
             raise ValueError("a cache has at least one layer, and pages of at least 16 tokens")
@@ -79,11 +80,11 @@ class Cache16:
         if not 0 <= layer < self.L:
             raise ValueError(f"layer must be in [0, {self.L})")
         batch = starts.shape[0] - 1 if starts.dim() == 1 else -1
-        if starts.dtype is not int32 or batch < 0 or not starts.is_contiguous() or starts.device != device:
+        if starts.dtype is not int32 or batch < 0 or not starts.is_contiguous() or starts.get_device() != self._index:
             raise ValueError(f"starts must be an int32 vector of an entry more than there are sequences, on {device}")
-        if lens.dtype is not int32 or lens.dim() != 1 or not lens.is_contiguous() or lens.device != device or lens.shape[0] < (batch if seqs is None else self.max_seqs):
+        if lens.dtype is not int32 or lens.dim() != 1 or not lens.is_contiguous() or lens.get_device() != self._index or lens.shape[0] < (batch if seqs is None else self.max_seqs):
             raise ValueError(f"lens must be an int32 vector on {device} with an entry per row of the table (per sequence where seqs is None)")
-        if seqs is not None and (seqs.dtype is not int32 or seqs.shape != (batch,) or not seqs.is_contiguous() or seqs.device != device):
+        if seqs is not None and (seqs.dtype is not int32 or seqs.shape != (batch,) or not seqs.is_contiguous() or seqs.get_device() != self._index):
             need("seqs", seqs, int32, (batch,), device)
         r = self._rows
         r.batch, r.n_rows, r.seqs, r.starts, r.lens = batch, rows, _address(seqs), starts.data_ptr(), lens.data_ptr()
@@ -92,9 +93,12 @@ class Cache16:
     def _heads(self, name, t, rows, heads):
         """The stride of rows of heads, which are contiguous in a row."""
         d = self.d
-        if t.dtype is not torch.float16 or t.shape != (rows, heads, d) or t.device != self.device or (rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d))):
-            raise ValueError(f"{name} must be fp16 [{rows}][{heads}][{d}] on {self.device}, the heads of a row contiguous; it is {t.dtype} {list(t.shape)} on {t.device}")
-        return t.stride(0) if rows > 1 else heads * d
+        if t.dtype is torch.float16 and t.shape == (rows, heads, d) and t.get_device() == self._index:
+            if t.is_contiguous():
+                return heads * d
+            if t.stride(2) == 1 and (heads == 1 or t.stride(1) == d):
+                return t.stride(0) if rows > 1 else heads * d
+        raise ValueError(f"{name} must be fp16 [{rows}][{heads}][{d}] on {self.device}, the heads of a row contiguous; it is {t.dtype} {list(t.shape)} on {t.device}")
 
     def append(self, layer, k, v, starts, lens, seqs=None, q=None, q_out=None, rope=None, positions=None):
         """Rows starts[b] .. starts[b + 1] - 1 of k and v (fp16 [rows][G][d], rows strided alike) become the last tokens of sequence b, which has lens[...] of them with
@@ -130,7 +134,7 @@ class Cache16:
         them.  slopes (fp32 [H]): scores fall by slopes[h] times the distance.  prefix (int32, by row of the table): that many tokens are seen by all."""
         rows, device = q.shape[0], self.device
         q_stride = self._heads("q", q, rows, self.H)
-        if out.dtype not in (torch.float16, torch.float32) or out.shape != q.shape or not out.is_contiguous() or out.device != device:
+        if out.dtype not in (torch.float16, torch.float32) or out.shape != q.shape or not out.is_contiguous() or out.get_device() != self._index:
             raise ValueError(f"out must be a contiguous fp16 or fp32 tensor {list(q.shape)} on {device}")
         at = self._whose(layer, rows, starts, lens, seqs)
         a = self._chunk

@@ -18,7 +18,7 @@ class Sampler:
 
     def __init__(self, *, max_batch, vocab, device="cuda:0"):
         self.device = torch.empty(0, device=device).device
-        self.max_batch, self.vocab = max_batch, vocab
+        self.max_batch, self.vocab, self._index = max_batch, vocab, self.device.index
         lib = binding.lib()
         sizes = [int(lib.okv_token_probs_workspace_bytes(max_batch, vocab)), int(lib.okv_verify_workspace_bytes(min(max_batch, 4096), vocab))]
         binding._check(min(*sizes, 0))
@@ -28,9 +28,12 @@ class Sampler:
 
     def _table(self, name, t, dtypes, rows):
         """The stride of rows of vocab numbers."""
-        if t.dtype not in dtypes or t.shape != (rows, self.vocab) or t.device != self.device or (rows and self.vocab > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name} must be {' or '.join(map(str, dtypes))} [{rows}][{self.vocab}] on {self.device}, rows contiguous; it is {t.dtype} {list(t.shape)} on {t.device}")
-        return t.stride(0) if rows > 1 else self.vocab
+        if t.dtype in dtypes and t.shape == (rows, self.vocab) and t.get_device() == self._index:
+            if t.is_contiguous():
+                return self.vocab
+            if self.vocab == 1 or t.stride(1) == 1:
+                return t.stride(0) if rows > 1 else self.vocab
+        raise ValueError(f"{name} must be {' or '.join(map(str, dtypes))} [{rows}][{self.vocab}] on {self.device}, rows contiguous; it is {t.dtype} {list(t.shape)} on {t.device}")
 
     def probs(self, logits, out, temperature=None):
         """out (fp32) = softmax of each row of logits (fp16 or fp32 [rows][vocab], rows may be strided) / temperature (fp32 [rows], or None: 1).  Temperature 0: 1 at the
@@ -55,7 +58,7 @@ class Sampler:
         if not 0 <= batch <= self.max_batch:
             raise ValueError(f"starts must have an entry more than there are sequences, of which there is room for {self.max_batch}")
         for name, t, size in (("drafts", drafts, n), ("starts", starts, batch + 1), ("tokens", tokens, n + batch), ("accepted", accepted, batch), ("rejected", rejected, batch)):
-            if t is not None and (t.dtype is not torch.int32 or t.shape != (size,) or not t.is_contiguous() or t.device != device):
+            if t is not None and (t.dtype is not torch.int32 or t.shape != (size,) or not t.is_contiguous() or t.get_device() != self._index):
                 need(name, t, torch.int32, (size,), device)
         need("uniforms", uniforms, torch.float32, (n + batch,), device)
         stride = self._table("target", target, (torch.float32,), n + batch)
