@@ -73,12 +73,12 @@ int okv_rope_append(const okv_layer_pool *c, const okv_rows *r, const okv_rope *
  *     s_i = scale (q . k_i);   s_i = cap tanh(s_i / cap) with a cap;   s_i -= slopes[h] |p - i| with slopes
  *     out = sum_i softmax_i(s) v_i
  * A row that sees no key is 0 (p < 0: the sequence has fewer tokens than rows).  A score of -infinity leaves its key out (0 if no key
- * is left), one that is infinite or NaN makes the row NaN.  What lies at keys that a row does not see, infinities and NaN included, does not
+ * is left), one that is +infinity or NaN makes the row NaN; an infinite or NaN value makes what it goes into infinite or NaN.  What lies at keys that a row does not see, infinities and NaN included, does not
  * change it.  Weights are fp16 in the second product for an fp16 result (each off by 2^-12 of itself, or 2^-32 of the largest), two fp16
  * numbers for an fp32 one (2^-22); sums are fp32. */
 typedef struct okv_chunk {
-  float scale;                 /* 0: 1 / sqrt(d)                                                                        */
-  float cap;                   /* 0: none; else positive                                                                */
+  float scale;                 /* 0: 1 / sqrt(d); else in [1e-30, 1e30]                                                 */
+  float cap;                   /* 0: none; else in [1e-30, 1e30]                                                        */
   int32_t window;              /* 0: none                                                                               */
   const float *slopes;         /* [H], or NULL                                                                          */
   const int32_t *prefix;       /* [max_seqs], by row of block_table, or NULL                                            */

@@ -133,6 +133,8 @@ class Cache16:
         out fp16 or fp32 [rows][H][d], contiguous.  scale 0: 1 / sqrt(d).  cap: scores become cap tanh(score / cap).  window: a row sees that many tokens, its own among
         them.  slopes (fp32 [H]): scores fall by slopes[h] times the distance.  prefix (int32, by row of the table): that many tokens are seen by all."""
         rows, device = q.shape[0], self.device
+        if window >= 1 << 31:
+            raise ValueError("window must be below 2^31")
         q_stride = self._heads("q", q, rows, self.H)
         if out.dtype not in (torch.float16, torch.float32) or out.shape != q.shape or not out.is_contiguous() or out.get_device() != self._index:
             raise ValueError(f"out must be a contiguous fp16 or fp32 tensor {list(q.shape)} on {device}")
@@ -153,6 +155,6 @@ class Cache16:
 
     def check_how(self, scale=0.0, cap=0.0, window=0, slopes=None, prefix=None):
         """Raises unless attend() takes these, with sequences by their rows of the table."""
-        if not (0 <= scale < math.inf and 0 <= cap < math.inf and 0 <= window < 1 << 31):
-            raise ValueError("scale and cap must be finite and not negative, window too")
+        if not (all(x == 0 or 1e-30 <= x <= 1e30 for x in (scale, cap)) and 0 <= window < 1 << 31):
+            raise ValueError("scale and cap must be 0 or in [1e-30, 1e30], window in [0, 2^31)")
         self._vectors(slopes, prefix, self.max_seqs)

@@ -109,6 +109,7 @@ __global__ void __launch_bounds__(kAppendWaves * 64) append_kernel(Pool c, Rows 
   const int s = r.seqs ? r.seqs[b] : b;
   int first, last, len = 0;
   rows_of(r, b, first, last);
+  if (row < first || row >= last) return;                // (starts that do not ascend)
   const bool known = s >= 0 && s < c.max_seqs;
   if (known) len = min(max(r.lens[s], 0), c.capacity);
   const int token = len - (last - row);
@@ -180,6 +181,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kRaise = 8.f;            // the maximum is raised when a score is this far above it
 // Weights are 2^(s - m + kLift): at most 2^15, and normal numbers in fp16 down to 2^-21 of the largest
 constexpr float kLift = 7.f;
+constexpr float kLowest = -3e38f;        // the maximum of no scores: finite, so that less it -infinity is that
 constexpr int kRing = 2;                 // blocks of keys, and of values, in LDS
 
 // Rows are the n R rows (tokens, and for each its R query heads) of a sequence and KV head; a wavefront has 32 of them, whose blocks of keys go by.
@@ -405,7 +407,9 @@ __device__ __forceinline__ bool piece_of(Piece &p, Chunk<F, FEW> &k, const Pool 
   const int at = __popcll(ended);
   p.q = of_lane(k.q, at);
   p.cuts = lane_value(cuts, at);
-  const int within = within_chunk - lane_value(upto - mine, at), items = p.q.tiles * c.G, cut = uniform(within / items);
+  const int within = within_chunk - lane_value(upto - mine, at), items = p.q.tiles * c.G;
+  if ((unsigned)within >= (unsigned)(items * p.cuts)) return false;      // (starts that do not ascend: sums past 2^31)
+  const int cut = uniform(within / items);
   set_item(p, c, within - cut * items);
   p.begin = share(p.q.steps, cut, p.cuts), p.end = share(p.q.steps, cut + 1, p.cuts);
   p.slot = -1;
@@ -576,7 +580,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
   floatx16 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = floatx16{};
-  float m = -1e30f, l = 0.f;
+  float m = kLowest, l = 0.f;
   // scores: keys 32 b + 8 (i / 4) + 4 half + i % 4 of this lane's row
   auto score = [&](floatx16 (&x)[kParts], const int slot) {
     const char *k0 = mine + slot * F::kBlockBytes;
@@ -795,7 +799,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     for (int k = 0; k < 32 / kWaves; k += 8) {
     const int of_tile = wave * (32 / kWaves) + k + lane / 8, joined_row = piece.tile * 32 + of_tile, joined_token = joined_row / c.R;
     if (joined_token >= p.n) return;
-    float most = -1e30f, sum = 0.f, factor[kWaves];
+    float most = kLowest, sum = 0.f, factor[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) most = fmaxf(most, all[w * kEach + 32 * kStride + of_tile]);
 #pragma unroll
@@ -894,7 +898,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Pool c, Attend a) {
   const int of_tile = blockIdx.x % (F::kRows / kJoinRows<D>) * kJoinRows<D> + threadIdx.x / kLanes, row = t.tile * F::kRows + of_tile, token = row / c.R, head = t.g * c.R + row - token * c.R;
   if (t.cuts == 0 || token >= t.n) return;
   auto part = [&](const int cut) { return a.parts + (int64_t)(cut ? t.slot1 + (cut - 1) * t.apart : t.slot) * F::kPartFloats; };
-  float m = -1e30f, l = 0.f;
+  float m = kLowest, l = 0.f;
   for (int cut = lane; cut < t.cuts; cut += kLanes) m = fmaxf(m, part(cut)[F::kRows * D + of_tile]);
 #pragma unroll
   for (int o = kLanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
@@ -1025,7 +1029,9 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
   const char *const who = "okv_chunk_attn";
   if (const char *why = problem(c, r)) return report(OKV_EINVAL, "%s: %s", who, why);
   if (!a) return report(OKV_EINVAL, "%s: NULL pointer", who);
-  if (!(a->scale >= 0.f && a->scale < INFINITY) || !(a->cap >= 0.f && a->cap < INFINITY)) return report(OKV_EINVAL, "%s: scale and cap must be finite and not negative", who);
+  // (below 1e-30 a product with them, or their quotient, would leave the range of fp32)
+  for (const float x : {a->scale, a->cap})
+    if (x != 0.f && !(x >= 1e-30f && x <= 1e30f)) return report(OKV_EINVAL, "%s: scale and cap must be 0 or in [1e-30, 1e30]", who);
   if (a->window < 0) return report(OKV_EINVAL, "%s: window must not be negative", who);
   if (a->out_dtype != 0 && a->out_dtype != 1) return report(OKV_EINVAL, "%s: out_dtype must be 0 or 1", who);
   const int32_t d = c->head_dim;

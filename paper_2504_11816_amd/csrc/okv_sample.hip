@@ -3,8 +3,8 @@
 // Probabilities are bound by HBM, 2 or 4 bytes read and 4 written a logit: 320 rows of 131072 fp16 logits 17 us for the pieces' sums (84 MB, 4.9 TB/s) and 43 for the quotients (168 MB written, the
 // logits from the memory-side cache).  5 rows of 32000: one launch of 5.7 us.
 // Verification reads one row of the target and one of the draft a sequence: 64 sequences of 131072 tokens 14 us (67 MB, 4.8 TB/s), and 7 to find the tokens; 4 of 32000 in one launch of 12.5 us, which is a
-// chain of dependent loads (starts, drafts, their probabilities, the row, the part again).  Sums are in 64 bits: with 32 a random number next to a border between tokens would fall on its wrong side in
-// about one of ten draws from 131072 tokens (an error of 2^-24 of the sum, against borders 2^-17 apart, some hundred roundings).
+// chain of dependent loads (starts, drafts, their probabilities, the row, the part again).  Sums are in 64 bits: an error of 2^-24 of the sum would
+// put one draw of 64 from 131072 equal tokens on the wrong side of a border between two.
 #include "okv_sample.h"
 #include "okv_lanes.h"
 #include "okv_report.h"

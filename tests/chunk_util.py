@@ -20,13 +20,13 @@ def starts_of(n):
 class Paged:
     """Sequences of lens tokens, in rows `seqs` of a table of more rows, their pages shuffled; every number of the pool is set (behind a sequence's end: `behind`)."""
 
-    def __init__(self, H, G, d, T, lens, seed=0, behind=None, extra=0):
+    def __init__(self, H, G, d, T, lens, seed=0, behind=None, room=0):
         rng = np.random.default_rng(seed)
         self.H, self.G, self.d, self.T, self.lens = H, G, d, T, list(lens)
         B = len(lens)
         self.seqs = [int(x) for x in rng.permutation(B + 2)[:B]]
         need = [-(-n // T) for n in lens]
-        width, n_pages = max([*need, 1]) + 1, sum(need) + 2 + extra
+        width, n_pages = max([*need, room // T]) + 1, sum(need) + 2      # room: tokens that a sequence can have at least (what is chosen goes by that, too)
         ids_of = rng.permutation(n_pages)
         table, at = np.full((B + 2, width), -1, dtype=np.int32), 0
         for s, n in zip(self.seqs, need):

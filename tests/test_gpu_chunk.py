@@ -33,11 +33,13 @@ def attended(p, q, n_new, dtype=torch.float16, prefix=None, slopes=None, **kw):
 
 
 @pytest.mark.parametrize("dtype", (torch.float16, torch.float32), ids=str)
+@pytest.mark.parametrize("room,times", [(0, 1), (3000, 1), (3000, 3)])
 @pytest.mark.parametrize("H,G,d", HEADS)
-def test_rows_of_every_kind(H, G, d, dtype):
-    """One token, none, whole prompts, chunks behind long contexts; lengths about tiles' and blocks' ends."""
+def test_rows_of_every_kind(H, G, d, room, times, dtype):
+    """One token, none, whole prompts, chunks behind long contexts; lengths about tiles' and blocks' ends.  In small caches and large ones, with few rows and with many."""
     lens, n_new = [1, 40, 17, 64, 65, 200, 129, 33], [1, 1, 17, 64, 2, 0, 40, 5]
-    p = Paged(H, G, d, 32, lens, seed=H + d)
+    lens, n_new = [n * times for n in lens], [n * times for n in n_new]
+    p = Paged(H, G, d, 32, lens, seed=H + d, room=room)
     q = queries(sum(n_new), H, d)
     check_rows(p, q, attended(p, q, n_new, dtype), n_new)
 
@@ -52,13 +54,14 @@ def test_pages_of_every_size(T):
 @pytest.mark.parametrize("kw", [dict(window=1), dict(window=7), dict(window=64), dict(window=100), dict(window=1 << 30), dict(prefix=[3, 0, 200, 30]), dict(prefix=[500, 1, 64, 33], window=20),
                                 dict(prefix=[4, 4, 4, 4], window=1), dict(cap=5.0), dict(cap=30.0, window=50, prefix=[1, 2, 3, 4]), dict(slopes=True), dict(slopes=True, prefix=[90, 0, 140, 2]),
                                 dict(slopes=True, cap=10.0, window=33), dict(scale=0.5), dict(scale=0.01, cap=0.3)], ids=str)
+@pytest.mark.parametrize("room", (0, 3000))
 @pytest.mark.parametrize("dtype", (torch.float16, torch.float32), ids=str)
-def test_masks_caps_and_biases(kw, dtype):
+def test_masks_caps_and_biases(kw, dtype, room):
     kw = dict(kw)
     if kw.get("slopes"):
         kw["slopes"] = [2.0 ** -(i + 1) for i in range(6)]
     n_new = [100, 3, 77, 40]
-    p = Paged(6, 3, 64, 16, [260, 70, 141, 40], seed=11)
+    p = Paged(6, 3, 64, 16, [260, 70, 141, 40], seed=11, room=room)
     q = queries(sum(n_new), 6, 64, size=3.0)
     check_rows(p, q, attended(p, q, n_new, dtype, **kw), n_new, **kw)
 
@@ -87,11 +90,14 @@ def test_one_key_takes_the_weight():
         check_rows(p, q, out, [9])
 
 
-def test_what_rows_do_not_see_does_not_change_them():
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("room", (0, 3000))
+def test_what_rows_do_not_see_does_not_change_them(room, d):
     """Infinities and NaN behind a sequence's end, and at keys that some rows of a tile see and others do not."""
     n_new, lens = [40, 5], [90, 33]
-    p = Paged(4, 2, 64, 32, lens, seed=6, behind=np.float16(np.nan))
-    q = queries(45, 4, 64)
+    p = Paged(4, 2, d, 32, lens, seed=6, behind=np.float16(np.nan), room=room)
+    clean = Paged(4, 2, d, 32, lens, seed=6, room=room)
+    q = queries(45, 4, d)
     check_rows(p, q, attended(p, q, n_new), n_new)
     for value, kv in ((np.inf, 1), (-np.inf, 1), (np.nan, 1), (np.nan, 0)):
         for token in (70, 89):
@@ -102,7 +108,7 @@ def test_what_rows_do_not_see_does_not_change_them():
             out = attended(p, q, n_new, dtype)
             with np.errstate(invalid="ignore"):
                 early = [j for j in range(40) if 50 + j < 70]
-                want = attended(Paged(4, 2, 64, 32, lens, seed=6), q, n_new, dtype)
+                want = attended(clean, q, n_new, dtype)
                 assert torch.equal(out[early], want[early]) and torch.equal(out[40:], want[40:])
                 late = out[early[-1] + 1:40, 2:].float().cpu().numpy()
                 if kv == 0:
@@ -114,7 +120,7 @@ def test_what_rows_do_not_see_does_not_change_them():
                         assert (late[..., 5] == np.inf).all()
         for token in (70, 89):                               # as it was
             o = p.offset(0, kv, 1, token)
-            p.pool[o + 5] = Paged(4, 2, 64, 32, lens, seed=6).pool[o + 5]
+            p.pool[o + 5] = clean.pool[o + 5]
     # a window that a number has left
     o = p.offset(0, 1, 0, 45)
     p.pool[o] = np.inf
@@ -156,6 +162,25 @@ def test_rows_before_the_first_token_and_rows_of_no_sequence():
     lens[p.seqs[0]], lens[p.seqs[1]] = -7, 1 << 30
     p.cache.attend(1, q, out, ids([0, 5, 9]), lens, ids(p.seqs))
     assert not out[:5].any() and torch.isfinite(out[5:9]).all()
+
+
+def test_starts_that_do_not_ascend_stay_within_the_buffers():
+    for room in (0, 3000):
+        p = Paged(4, 2, 64, 16, [20, 30, 40], seed=1, room=room)
+        q, out = queries(12, 4, 64), torch.full((14, 4, 64), math.nan, dtype=torch.float16, device=DEV)
+        for starts in ([0, 9, 3, 20], [-5, 4, 100, 7], [12, 12, 12, 12], [5, 3, 1, 0]):
+            p.cache.attend(1, q, out[1:13], ids(starts), p.cache.lens, ids(p.seqs))
+            p.cache.append(0, q[:, :2], q[:, 2:], ids(starts), p.cache.lens, ids(p.seqs))
+        assert torch.isnan(out[0]).all() and torch.isnan(out[13]).all()
+
+
+def test_scores_far_below_zero():
+    """A bias that puts every score below -1e30: the nearest key takes the weight."""
+    p = Paged(2, 2, 64, 16, [40], seed=1)
+    q = queries(40, 2, 64)
+    out = attended(p, q, [40], torch.float32, slopes=[1e31, 1e35], prefix=[0], window=0)
+    v = [p.rows(0, 1, g) for g in range(2)]
+    assert all(torch.equal(out[j, h].cpu(), torch.from_numpy(v[h][j].astype(np.float32))) for j in range(40) for h in range(2))
 
 
 def test_many_sequences():
@@ -374,7 +399,9 @@ def test_wrong_tensors_are_refused():
                 dict(slopes=torch.ones(3, device=DEV)), dict(slopes=torch.ones(4, device=DEV, dtype=torch.float64)), dict(prefix=ids([1])), dict(prefix=torch.ones(4, device=DEV))):
         with pytest.raises(ValueError):
             c.attend(**{**good, **bad})
-    for bad in (dict(cap=-1.0), dict(cap=math.nan), dict(scale=-0.5), dict(window=-3)):
+    with pytest.raises(ValueError):
+        c.attend(**good, window=1 << 32)
+    for bad in (dict(cap=-1.0), dict(cap=math.nan), dict(cap=1e-39), dict(scale=-0.5), dict(scale=1e-40), dict(scale=1e31), dict(window=-3)):
         with pytest.raises(binding.OkvError):
             c.attend(**{**good, **bad})
     rope = Rope.of(64, device=DEV)
