@@ -631,26 +631,32 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     }
     const bool whole = (key0 + kKeys - 1 <= pos0 && key0 >= from1) || key0 + kKeys <= p.prefix;
     const int apart = pos - key0 - 4 * half;             // from the lane's first key to its row
-    float by = a.scale;
+    float by = a.scale, shift = 0.f;                     // scores in units of log 2 are by x + shift
     if constexpr (SHAPED) {
-      // (in units of log 2 from here on)  tanh(y) = 1 - 2 / (e^2y + 1): off by 3 2^-24 of 1, whatever y
+      // tanh(y) = 1 - 2 / (e^2y + 1): off by 3 2^-24 of 1, whatever y
       if (a.cap != 0.f) {
 #pragma unroll
         for (int b = 0; b < kParts; ++b)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[b][j] = fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[b][j] * a.scale) + 1.f), a.cap);
-      } else {
-#pragma unroll
-        for (int b = 0; b < kParts; ++b) x[b] *= a.scale;
+          for (int j = 0; j < 16; ++j) x[b][j] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(x[b][j] * a.scale));
+        by = 2.f * a.cap, shift = a.cap;
       }
       if (a.slopes) {
         const float far = (float)apart;
+        if (key0 + kKeys - 1 <= pos0) {                  // all keys before all rows: the distance is a difference
+          const float nearest = fmaf(-slope, far, shift);
 #pragma unroll
-        for (int b = 0; b < kParts; ++b)
+          for (int b = 0; b < kParts; ++b)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[b][j] = fmaf(-slope, fabsf(far - (float)(32 * b + 8 * (j / 4) + j % 4)), x[b][j]);
+            for (int j = 0; j < 16; ++j) x[b][j] = fmaf(x[b][j], by, fmaf(slope, (float)(32 * b + 8 * (j / 4) + j % 4), nearest));
+        } else {
+#pragma unroll
+          for (int b = 0; b < kParts; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[b][j] = fmaf(-slope, fabsf(far - (float)(32 * b + 8 * (j / 4) + j % 4)), fmaf(x[b][j], by, shift));
+        }
+        by = 1.f, shift = 0.f;
       }
-      by = 1.f;
     }
     if (!whole) {
       const int fixed = p.prefix - key0 - 4 * half, upto = max(apart, fixed - 1), below = from - key0 - 4 * half;
@@ -668,7 +674,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     for (int b = 0; b < kParts; ++b)
 #pragma unroll
       for (int j = 0; j < 16; j += 2) top = fmaxf(fmaxf(top, x[b][j]), x[b][j + 1]);
-    top = max_with_lane_xor<32>(top) * by;
+    top = fmaf(max_with_lane_xor<32>(top), by, shift);
     if (__ballot(top > m + kRaise)) {
       const float to = top > m + kRaise ? top : m, scale = __builtin_amdgcn_exp2f(m - to);
       l *= scale;
@@ -680,7 +686,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     // The next block's scores under this one's weights (past the end, or out of sight: for nothing)
     score(next, slot ^ 1);
     half8 hi[2 * kParts], lo[WIDE ? 2 * kParts : 1];
-    const float less = kLift - m;
+    const float less = kLift - m + shift;
     float sums[4] = {};
 #pragma unroll
     for (int b = 0; b < kParts; ++b)
@@ -767,9 +773,32 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
   l = sum_with_lane_xor<32>(l);
   float *parts = a.parts + (int64_t)max(piece.slot, 0) * F::kPartFloats;
   if constexpr (!FEW) {
-    if (token >= p.n) return;
     const int of_tile = wave * 32 + col;
     const float over = !whole_tile ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    if (!WIDE && whole_tile) {
+      // Whole rows through LDS (each wavefront's in a place of its own), 16 bytes a lane
+      constexpr int kStride = kRowBytes + 16;
+      char *const own = lds + wave * (32 * kStride);
+      static_assert(kWaves * 32 * kStride <= F::kLds, "");
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          half4 y;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = (_Float16)(o[e][4 * i + j] * over);
+          *reinterpret_cast<half4 *>(own + col * kStride + 64 * e + 16 * i + 8 * half) = y;
+        }
+#pragma unroll
+      for (int k = 0; k < 32; k += 64 / kUnits) {
+        const int r0 = row0 + k + lane_row, their_token = r0 / c.R;
+        const u32x4 y = *reinterpret_cast<const u32x4 *>(own + (k + lane_row) * kStride + 16 * (lane % kUnits));
+        if (their_token < p.n)
+          *reinterpret_cast<u32x4 *>(static_cast<_Float16 *>(a.out) + ((int64_t)(p.first + their_token) * (c.G * c.R) + piece.g * c.R + r0 - their_token * c.R) * D + 8 * (lane % kUnits)) = y;
+      }
+      return;
+    }
+    if (token >= p.n) return;
     const int64_t to = !whole_tile ? of_tile * D : ((int64_t)(p.first + token) * (c.G * c.R) + head) * D;
     if (!whole_tile && half == 0) parts[F::kRows * D + of_tile] = m, parts[F::kRows * (D + 1) + of_tile] = l;
 #pragma unroll
@@ -779,10 +808,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
         floatx4 y;
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = o[e][4 * i + j] * over;
-        const int64_t at = to + 32 * e + 8 * i + 4 * half;
-        if (!whole_tile) *reinterpret_cast<floatx4 *>(parts + at) = y;
-        else if constexpr (WIDE) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.out) + at) = y;
-        else *reinterpret_cast<half4 *>(static_cast<_Float16 *>(a.out) + at) = half4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
+        *reinterpret_cast<floatx4 *>((!whole_tile ? parts : static_cast<float *>(a.out)) + to + 32 * e + 8 * i + 4 * half) = y;
       }
   } else {
     // The wavefronts' results through LDS (each has written to rings of its own only): a row's D sums, then the maxima and the sums of weights
