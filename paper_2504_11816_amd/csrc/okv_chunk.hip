@@ -182,6 +182,7 @@ constexpr float kRaise = 8.f;            // the maximum is raised when a score i
 // Weights are 2^(s - m + kLift): at most 2^15, and normal numbers in fp16 down to 2^-21 of the largest
 constexpr float kLift = 7.f;
 constexpr float kLowest = -3e38f;        // the maximum of no scores: finite, so that less it -infinity is that
+constexpr float kNearCap = 64 * kLog2e;   // above it: see the tanh
 constexpr int kRing = 2;                 // blocks of keys, and of values, in LDS
 
 // Rows are the n R rows (tokens, and for each its R query heads) of a sequence and KV head; a wavefront has 32 of them, whose blocks of keys go by.
@@ -633,8 +634,21 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     const int apart = pos - key0 - 4 * half;             // from the lane's first key to its row
     float by = a.scale, shift = 0.f;                     // scores in units of log 2 are by x + shift
     if constexpr (SHAPED) {
-      // tanh(y) = 1 - 2 / (e^2y + 1): off by 3 2^-24 of 1, whatever y
-      if (a.cap != 0.f) {
+      // tanh(y) = 1 - 2 / (e^2y + 1) is off by 3 2^-24 of 1, whatever y: of a cap that is far above the scores more than they bear.  There (kNearCap) small y take their series, up to y^9: off by 2^-26 of itself
+      // below 1/4, and by 12 2^-24 above.  us of 4 times 700 to
+      // 1024 rows behind up to 8000 tokens, 16 / 8 heads x 128, cap 50: 170, with both for every cap 227
+      if (a.cap > kNearCap) {
+#pragma unroll
+        for (int b = 0; b < kParts; ++b)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float z = x[b][j] * a.scale, y = z * (.5f / kLog2e), yy = y * y;
+            const float series = fmaf(fmaf(fmaf(fmaf(62.f / 2835, yy, -17.f / 315), yy, 2.f / 15), yy, -1.f / 3) * yy, y, y);
+            const float far = fmaf(2.f, __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(z)), 1.f);
+            x[b][j] = fabsf(y) < .25f ? series : far;
+          }
+        by = a.cap;
+      } else if (a.cap != 0.f) {
 #pragma unroll
         for (int b = 0; b < kParts; ++b)
 #pragma unroll
@@ -1055,7 +1069,7 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
   const char *const who = "okv_chunk_attn";
   if (const char *why = problem(c, r)) return report(OKV_EINVAL, "%s: %s", who, why);
   if (!a) return report(OKV_EINVAL, "%s: NULL pointer", who);
-  // (below 1e-30 a product with them, or their quotient, would leave the range of fp32)
+  // (below 1e-30 a product with them would leave the range of fp32; a quotient above 1e30, whose scores are the cap anyway, is that)
   for (const float x : {a->scale, a->cap})
     if (x != 0.f && !(x >= 1e-30f && x <= 1e30f)) return report(OKV_EINVAL, "%s: scale and cap must be 0 or in [1e-30, 1e30]", who);
   if (a->window < 0) return report(OKV_EINVAL, "%s: window must not be negative", who);
@@ -1073,9 +1087,8 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
   Attend x;
   x.q = static_cast<const _Float16 *>(q), x.out = out, x.q_stride = q_stride;
   const float scale = a->scale != 0.f ? a->scale : 1.f / sqrtf((float)d);
-  x.scale = a->cap != 0.f ? 2.f * kLog2e * (scale / a->cap) : scale * kLog2e, x.cap = a->cap * kLog2e;
+  x.scale = a->cap != 0.f ? 2.f * kLog2e * std::min(scale / a->cap, 1e30f) : scale * kLog2e, x.cap = a->cap * kLog2e;
   x.window = a->window, x.slopes = a->slopes, x.prefix = a->prefix;
-  x.plan = static_cast<Plan *>(a->workspace), x.cuts = static_cast<char *>(a->workspace) + kPlanBytes, x.parts = reinterpret_cast<float *>(x.cuts + kCutBytes);
   x.plan = static_cast<Plan *>(a->workspace), x.cuts = static_cast<char *>(a->workspace) + kPlanBytes, x.parts = reinterpret_cast<float *>(x.cuts + kCutBytes);
   const bool wide = a->out_dtype == 1, shaped = a->cap != 0.f || a->slopes;
   // How many rows a sequence brings is on the device: by the mean.  Where contexts are short, so many that the wavefronts of a workgroup would walk them one after the other take less time side by side: us of 8

@@ -1,4 +1,6 @@
 """A paged fp16 cache on the GPU and its tokens on the CPU, for tests of steps with several tokens a sequence; what such a step may be off by."""
+import math
+
 import numpy as np
 import torch
 
@@ -67,7 +69,8 @@ def check_rows(p, q, out, n_new, *, scale=0.0, cap=0.0, window=0, slopes=None, p
     """Every row (or every `some`-th) of out against the oracle.  What a result may be off by, A the weighted mean of |v|:
 
     weights     each off by 2^-11 of itself (fp16, half a step) or 2^-22 (two fp16 numbers), beside sums that are not:  A 2^-11 or A 2^-22
-    scores      d products summed in 32 bits, the scale, the cap's tanh (4 units of what it is multiplied with) and the bias: e <= (d + 8) 2^-24 S + 8 cap 2^-24 + 2^-22 bias, which
+    scores      d products summed in 32 bits, the scale, the cap's tanh (4 units of what it is multiplied with; a cap above 64 is relative: 16 units of a score, which
+                is at most S and cap) and the bias: e <= (d + 8) 2^-24 S + 8 cap 2^-24 + 2^-22 bias (with a cap the first is at most 2 cap), which
                 changes a weight by e and the sum by e:  2 e A;  exponents are products and differences of numbers of up to 2 S: 4 S 2^-24 each, and 2^-22 of the exponential
     sums        of n numbers in 32 bits, numerator and denominator: 2 n 2^-24 A
     the result  half a step of its type, 2^-11 (2^-24), and for fp16 the smallest number, 2^-25"""
@@ -86,7 +89,7 @@ def check_rows(p, q, out, n_new, *, scale=0.0, cap=0.0, window=0, slopes=None, p
                 slope = 0.0 if slopes is None else float(slopes[h])
                 want, A, S = oracle.attend(q[row, h], K, V, pos, scale, cap, window, slope, 0 if prefix is None else min(prefix[b], p.lens[b]))
                 bias = slope * p.lens[b]
-                e = (p.d + 8) * 2.0 ** -24 * S + 8 * cap * 2.0 ** -24 + 2.0 ** -22 * bias
+                e = min((p.d + 8) * 2.0 ** -24 * S, 2 * cap if cap else math.inf) + (8 * cap if cap <= 64 else 16 * min(S, cap)) * 2.0 ** -24 + 2.0 ** -22 * bias
                 tol = A * ((2.0 ** -22 if out32 else 2.0 ** -11) + 2 * e + 4 * (min(S, cap) if cap else S) * 2.0 ** -24 + 4 * bias * 2.0 ** -24 + 2.0 ** -22 + 2 * (p.lens[b] + 2) * 2.0 ** -24)
                 tol = tol + (2.0 ** -24 if out32 else 2.0 ** -11) * np.abs(want) + (0 if out32 else 2.0 ** -25)
                 same = (got[row, h] == want) | (np.isnan(got[row, h]) & np.isnan(want))

@@ -66,6 +66,20 @@ def test_masks_caps_and_biases(kw, dtype, room):
     check_rows(p, q, attended(p, q, n_new, dtype, **kw), n_new, **kw)
 
 
+@pytest.mark.parametrize("kw", [dict(cap=64.5), dict(cap=1000.0), dict(cap=1e6, slopes=True), dict(cap=1e30), dict(cap=1e30, scale=1e-10), dict(scale=30.0, cap=200.0),
+                                dict(scale=1e30, cap=1e-30)], ids=str)
+@pytest.mark.parametrize("n_new", ([100, 3, 77, 40], [5, 3, 1, 4]), ids=("many", "few"))
+@pytest.mark.parametrize("d", (64, 128))
+def test_caps_far_above_and_below_the_scores(kw, n_new, d):
+    kw = dict(kw)
+    if kw.get("slopes"):
+        kw["slopes"] = [2.0 ** -(i + 1) for i in range(6)]
+    p = Paged(6, 3, d, 16, [260, 70, 141, 40], seed=12, room=3000)
+    q = queries(sum(n_new), 6, d, size=3.0)
+    for dtype in (torch.float16, torch.float32):
+        check_rows(p, q, attended(p, q, n_new, dtype, **kw), n_new, **kw)
+
+
 def test_long_contexts():
     """Few rows over tens of thousands of keys, and some hundreds of rows: cut among workgroups."""
     for n_new, lens in (([5, 1], [30001, 20000]), ([300], [9000]), ([1, 600, 2], [5, 4000, 12345])):
