@@ -1,7 +1,7 @@
 // From logits to tokens (include/okv_sample.h): probabilities, and drafted tokens held against them, for gfx950.
 //
-// Probabilities are bound by HBM, 2 or 4 bytes read and 4 written a logit: 320 rows of 131072 fp16 logits 17 us for the pieces' sums (84 MB, 4.9 TB/s) and 43 for the quotients (168 MB written, the
-// logits from the memory-side cache).  5 rows of 32000: one launch of 5.7 us.
+// Probabilities are bound by HBM, 2 or 4 bytes read and 4 written a logit: 320 rows of 131072 fp16 logits 17 us for the pieces' sums (84 MB, 4.9 TB/s) and 38 for the quotients (168 MB written, the
+// logits from the memory-side cache).  5 rows of 32000: one launch of 5.9 us.
 // Verification reads one row of the target and one of the draft a sequence: 64 sequences of 131072 tokens 14 us (67 MB, 4.8 TB/s), and 7 to find the tokens; 4 of 32000 in one launch of 12.5 us, which is a
 // chain of dependent loads (starts, drafts, their probabilities, the row, the part again).  Sums are in 64 bits: an error of 2^-24 of the sum would
 // put one draw of 64 from 131072 equal tokens on the wrong side of a border between two.
@@ -24,16 +24,17 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Rows begin anywhere: vectors of elements that are aligned as one of them is
-typedef _Float16 half8 __attribute__((ext_vector_type(8), aligned(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---- probabilities --------------------------------------------------------------------------------
 //
 // Every logit is read and every probability written once where a row fits the registers of a workgroup: one launch.  Longer rows are cut into pieces of as many workgroups, in two launches: the
-// largest number and the sum of every piece, then the quotients, whose logits come from the memory-side cache.
+// largest number and the sum of every piece, then the quotients, whose logits come from the memory-side cache.  A wavefront's store is 1 KiB in a row (four numbers a lane; the first launch, which stores
+// nothing, reads eight); past the caches they leave the logits there: us of 320 / 64 rows of 131072 fp16 logits 56 / 14.3, stores kept in the caches 69 / 15.6, eight numbers a lane 70 / 17.4
+// and past the caches 84 / 19.9, the first launch four a lane 58.6 / 15.3, a workgroup a row in one launch 88 / 29.5.
 
 constexpr int kRowThreads = 1024, kPieceThreads = 256;
-constexpr int kEach = 32;                // logits of a thread, eight in a row at a time
+constexpr int kEach = 32;                // logits of a thread, in runs
 constexpr int kOneLaunch = kRowThreads * kEach;
 constexpr int kPieceLogits = kPieceThreads * kEach;
 
@@ -43,44 +44,46 @@ struct Seen {
   int at, unused;
 };
 
-template <class T>
-__device__ __forceinline__ void load8(const T *x, const int n, float (&to)[8]) {      // n of them are there, -infinity for the others
-  if (n >= 8) {
-    if constexpr (sizeof(T) == 2) {
-      const half8 v = *reinterpret_cast<const half8 *>(x);
+template <int RUN, class T>
+__device__ __forceinline__ void load_run(const T *x, const int n, float (&to)[RUN]) {      // n of them are there, -infinity for the others
+  typedef T numbers __attribute__((ext_vector_type(16 / sizeof(T) < RUN ? 16 / sizeof(T) : RUN), aligned(sizeof(T))));
+  constexpr int kVector = sizeof(numbers) / sizeof(T);
+  if (n >= RUN) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) to[i] = (float)v[i];
-    } else {
-      const floatx4 u = reinterpret_cast<const floatx4 *>(x)[0], v = reinterpret_cast<const floatx4 *>(x)[1];
+    for (int k = 0; k < RUN; k += kVector) {
+      const numbers v = *reinterpret_cast<const numbers *>(x + k);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) to[i] = u[i], to[4 + i] = v[i];
+      for (int i = 0; i < kVector; ++i) to[k + i] = (float)v[i];
     }
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) to[i] = i < n ? (float)x[i] : -INFINITY;
+  for (int i = 0; i < RUN; ++i) to[i] = i < n ? (float)x[i] : -INFINITY;
 }
-__device__ __forceinline__ void store8(float *y, const int n, const float (&x)[8]) {
-  if (n >= 8) {
-    reinterpret_cast<floatx4 *>(y)[0] = floatx4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<floatx4 *>(y)[1] = floatx4{x[4], x[5], x[6], x[7]};
+// ONCE: past the caches, which have the logits of other pieces
+template <bool ONCE>
+__device__ __forceinline__ void store_run(float *y, const int n, const float (&x)[4]) {
+  if (n >= 4) {
+    const floatx4 v = {x[0], x[1], x[2], x[3]};
+    if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<floatx4 *>(y));
+    else *reinterpret_cast<floatx4 *>(y) = v;
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 4; ++i)
     if (i < n) y[i] = x[i];
 }
 
-// THREADS threads' numbers of a piece of a row, eight from 8 (i THREADS + thread) on each: their largest, first place (at temperature 0), exponentials in their stead, and the sum
-template <int THREADS>
-__device__ __forceinline__ Seen seen_by_all(float (&x)[kEach / 8][8], const float t, const float by, float *shared) {
+// THREADS threads' numbers of a piece of a row, RUN from RUN (i THREADS + thread) on each: their largest, first place (at temperature 0), exponentials in their stead, and the sum
+template <int THREADS, int RUN>
+__device__ __forceinline__ Seen seen_by_all(float (&x)[kEach / RUN][RUN], const float t, const float by, float *shared) {
   constexpr int kWaves = THREADS / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Seen s{-INFINITY, 0.f, 0x7fffffff, 0};
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i)
+  for (int i = 0; i < kEach / RUN; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s.top = fmaxf(s.top, x[i][j]);
+    for (int j = 0; j < RUN; ++j) s.top = fmaxf(s.top, x[i][j]);
   s.top = wave_max(s.top);
   if (lane == 0) shared[wave] = s.top;
   __syncthreads();
@@ -89,10 +92,10 @@ __device__ __forceinline__ Seen seen_by_all(float (&x)[kEach / 8][8], const floa
   __syncthreads();
   if (t == 0.f) {
 #pragma unroll
-    for (int i = kEach / 8 - 1; i >= 0; --i)
+    for (int i = kEach / RUN - 1; i >= 0; --i)
 #pragma unroll
-      for (int j = 7; j >= 0; --j)
-        if (x[i][j] == s.top) s.at = 8 * (i * THREADS + (int)threadIdx.x) + j;
+      for (int j = RUN - 1; j >= 0; --j)
+        if (x[i][j] == s.top) s.at = RUN * (i * THREADS + (int)threadIdx.x) + j;
 #pragma unroll
     for (int o = 32; o; o >>= 1) s.at = min(s.at, __shfl_xor(s.at, o));
     if (lane == 0) shared[wave] = __builtin_bit_cast(float, s.at);
@@ -104,9 +107,9 @@ __device__ __forceinline__ Seen seen_by_all(float (&x)[kEach / 8][8], const floa
   }
   const float less = s.top == -INFINITY ? 0.f : s.top;
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i)
+  for (int i = 0; i < kEach / RUN; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s.sum += x[i][j] = __builtin_amdgcn_exp2f((x[i][j] - less) * by);
+    for (int j = 0; j < RUN; ++j) s.sum += x[i][j] = __builtin_amdgcn_exp2f((x[i][j] - less) * by);
   s.sum = wave_sum(s.sum);
   if (lane == 0) shared[wave] = s.sum;
   __syncthreads();
@@ -123,21 +126,21 @@ __global__ void __launch_bounds__(kRowThreads) row_probs_kernel(const T *logits,
   __shared__ float shared[kRowThreads / 64];
   const T *x = logits + blockIdx.x * stride;
   float *y = out + blockIdx.x * out_stride;
-  float v[kEach / 8][8];
+  float v[kEach / 4][4];
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i) {
-    const int at = 8 * (i * kRowThreads + (int)threadIdx.x);
-    load8(x + at, vocab - at, v[i]);
+  for (int i = 0; i < kEach / 4; ++i) {
+    const int at = 4 * (i * kRowThreads + (int)threadIdx.x);
+    load_run(x + at, vocab - at, v[i]);
   }
   const float t = temperature ? temperature[blockIdx.x] : 1.f;
-  const Seen s = seen_by_all<kRowThreads>(v, t, per_temperature(t), shared);
+  const Seen s = seen_by_all<kRowThreads, 4>(v, t, per_temperature(t), shared);
   const float over = s.sum == 0.f ? 0.f : 1.f / s.sum;
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i) {
-    const int at = 8 * (i * kRowThreads + (int)threadIdx.x);
+  for (int i = 0; i < kEach / 4; ++i) {
+    const int at = 4 * (i * kRowThreads + (int)threadIdx.x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = t == 0.f ? (at + j == s.at ? 1.f : 0.f) : v[i][j] * over;
-    store8(y + at, vocab - at, v[i]);
+    for (int j = 0; j < 4; ++j) v[i][j] = t == 0.f ? (at + j == s.at ? 1.f : 0.f) : v[i][j] * over;
+    store_run<false>(y + at, vocab - at, v[i]);
   }
 }
 
@@ -150,24 +153,24 @@ __global__ void __launch_bounds__(kPieceThreads) piece_seen_kernel(const T *logi
 #pragma unroll
   for (int i = 0; i < kEach / 8; ++i) {
     const int at = first + 8 * (i * kPieceThreads + (int)threadIdx.x);
-    load8(x + at, vocab - at, v[i]);
+    load_run(x + at, vocab - at, v[i]);
   }
   const float t = temperature ? temperature[row] : 1.f;
-  Seen s = seen_by_all<kPieceThreads>(v, t, per_temperature(t), shared);
+  Seen s = seen_by_all<kPieceThreads, 8>(v, t, per_temperature(t), shared);
   if (s.at != 0x7fffffff) s.at += first;
   if (threadIdx.x == 0) seen[(int64_t)row * gridDim.x + blockIdx.x] = s;
 }
-template <class T>
+template <bool ONCE, class T>
 __global__ void __launch_bounds__(kPieceThreads) piece_probs_kernel(const T *logits, const int64_t stride, const float *temperature, float *out, const int64_t out_stride, const int vocab,
                                                                     const Seen *seen) {
   const int first = blockIdx.x * kPieceLogits, row = blockIdx.y, lane = threadIdx.x & 63, pieces = gridDim.x;
   const T *x = logits + row * stride;
   float *y = out + row * out_stride;
-  float v[kEach / 8][8];
+  float v[kEach / 4][4];
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i) {
-    const int at = first + 8 * (i * kPieceThreads + (int)threadIdx.x);
-    load8(x + at, vocab - at, v[i]);
+  for (int i = 0; i < kEach / 4; ++i) {
+    const int at = first + 4 * (i * kPieceThreads + (int)threadIdx.x);
+    load_run(x + at, vocab - at, v[i]);
   }
   const float t = temperature ? temperature[row] : 1.f, by = per_temperature(t);
   float top = -INFINITY, sum = 0.f;
@@ -185,11 +188,11 @@ __global__ void __launch_bounds__(kPieceThreads) piece_probs_kernel(const T *log
   for (int o = 32; o; o >>= 1) at_top = min(at_top, __shfl_xor(at_top, o));
   const float over = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i) {
-    const int at = first + 8 * (i * kPieceThreads + (int)threadIdx.x);
+  for (int i = 0; i < kEach / 4; ++i) {
+    const int at = first + 4 * (i * kPieceThreads + (int)threadIdx.x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = t == 0.f ? (at + j == at_top ? 1.f : 0.f) : __builtin_amdgcn_exp2f((v[i][j] - less) * by) * over;
-    store8(y + at, vocab - at, v[i]);
+    for (int j = 0; j < 4; ++j) v[i][j] = t == 0.f ? (at + j == at_top ? 1.f : 0.f) : __builtin_amdgcn_exp2f((v[i][j] - less) * by) * over;
+    store_run<ONCE>(y + at, vocab - at, v[i]);
   }
 }
 
@@ -441,7 +444,12 @@ int okv_token_probs(const void *logits, int32_t dtype, int64_t stride, const flo
       const float *const t = temperature ? temperature + first : nullptr;
       Seen *const at = seen + (int64_t)first * pieces;
       hipLaunchKernelGGL(piece_seen_kernel, grid, dim3(kPieceThreads), 0, s, x + first * stride, stride, t, vocab, at);
-      hipLaunchKernelGGL(piece_probs_kernel, grid, dim3(kPieceThreads), 0, s, x + first * stride, stride, t, out + first * out_stride, out_stride, vocab, static_cast<const Seen *>(at));
+      // (of 256 rows of 50001, most of which are not aligned: 22 us, past the caches 24)
+      auto probs = [&](auto once) {
+        hipLaunchKernelGGL((piece_probs_kernel<decltype(once)::value>), grid, dim3(kPieceThreads), 0, s, x + first * stride, stride, t, out + first * out_stride, out_stride, vocab, static_cast<const Seen *>(at));
+      };
+      if (aligned(out, 16) && out_stride % 4 == 0) probs(std::true_type{});
+      else probs(std::false_type{});
     }
   };
   if (dtype == 0) run(static_cast<const _Float16 *>(logits));
