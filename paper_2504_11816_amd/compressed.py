@@ -125,6 +125,8 @@ def _check_chunk(cache, layers, scratch, x, starts, seqs, n_new, rope, how):
     need("starts", starts, torch.int32, (batch + 1,), cache.device)
     if not 1 <= x.shape[0] <= 4096:
         raise ValueError("a call takes 1 to 4096 rows")
+    if batch > 4096:
+        raise ValueError("a call takes at most 4096 sequences")
     if rope is not None and (rope.device != cache.device or rope.rotated > cache.d):
         raise ValueError(f"the rope must be on {cache.device} and turn at most {cache.d} elements")
     cache.check_how(**how)

@@ -136,7 +136,8 @@ def test_steps_that_do_not_fit_change_nothing():
     c.pages.extend(ids([0, 1]), ids([10, 20]))
     good = dict(cache=c, layers=w, scratch=scratch, x=x, starts=ids([0, 2, 6]), seqs=ids([1, 0]), n_new=ids([2, 4]), rope=Rope.of(D, device=DEV))
     before = [t.clone() for t in (c.pool, c.table, c.lens, c.refs)]
-    for bad in (dict(x=x.float()), dict(x=x[:, :128].contiguous()), dict(x=torch.empty((17, H1), dtype=torch.float16, device=DEV)), dict(x=x[:0]), dict(starts=ids([0, 2])), dict(starts=ids([0, 2, 6]).long()),
+    many = ids([0] * 4097)
+    for bad in (dict(starts=ids([0] * 4098), seqs=many, n_new=many), dict(x=x.float()), dict(x=x[:, :128].contiguous()), dict(x=torch.empty((17, H1), dtype=torch.float16, device=DEV)), dict(x=x[:0]), dict(starts=ids([0, 2])), dict(starts=ids([0, 2, 6]).long()),
                 dict(seqs=ids([1])), dict(n_new=ids([1])), dict(n_new=ids([2, 4]).cpu()), dict(layers=[]), dict(layers=w * 2), dict(scratch=Scratch(16, 2 * H1, H2, KV, DEV)), dict(rope=Rope.of(128, device=DEV)),
                 dict(cap=-1.0), dict(cap=float("nan")), dict(window=-1), dict(scale=float("inf")), dict(slopes=torch.ones(3, device=DEV)), dict(prefix=ids([1]))):
         with pytest.raises(ValueError):
