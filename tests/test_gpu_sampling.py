@@ -90,6 +90,28 @@ def test_strided_logits():
         assert (out[:, :5] == 7).all() and (out[:, 5005:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", (torch.float16, torch.float32), ids=str)
+@pytest.mark.parametrize("at, to, columns", [(0, 4, 40004), (1, 5, 40009), (3, 4, 40010), (0, 1, 40004)])
+def test_long_rows_that_are_strided(at, to, columns, dtype):
+    """Rows whose places are aligned for wide stores, and others."""
+    x = torch.randn((5, 40003), device=DEV).to(dtype)
+    out = torch.full((5, columns), 7.0, device=DEV)
+    Sampler(max_batch=5, vocab=39998, device=DEV).probs(x[:, at:at + 39998], out[:, to:to + 39998])
+    check_probs(x[:, at:at + 39998], None, out[:, to:to + 39998])
+    assert (out[:, :to] == 7).all() and (out[:, to + 39998:] == 7).all()
+
+
+def test_more_long_rows_than_a_grid_has():
+    rows, vocab = 32770, 32800
+    x = torch.randn((rows, vocab), device=DEV, dtype=torch.float16)
+    out = torch.empty((rows, vocab), device=DEV)
+    t = torch.ones(rows, device=DEV)
+    t[32768] = 0.5
+    Sampler(max_batch=rows, vocab=vocab, device=DEV).probs(x, out, t)
+    some = [0, 1, 20000, 32767, 32768, 32769]
+    check_probs(x[some], t[some], out[some])
+
+
 # ---- verification ---------------------------------------------------------------------------------
 
 def inputs(vocab, n, seed, peaked=1.5, agree=0.7):
