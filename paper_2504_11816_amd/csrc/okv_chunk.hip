@@ -1,13 +1,13 @@
 // Several new tokens of a sequence at once over the fp16 cache (include/okv_chunk.h): appending with rotation, and attention of the rows, for gfx950.
 //
-// Appending moves 4 d (H + 2 G) bytes a row and is bound by HBM: 24 prompts of 100 to 2000 tokens, 32 / 8 heads x 128, 119 us (608 MB, 5.1 TB/s).
+// Appending moves 4 d (H + 2 G) bytes a row and is bound by HBM: 24 prompts of 100 to 2000 tokens, 32 / 8 heads x 128, 119 us (607 MB, 5.1 TB/s).
 //
 // Attention, out = sum_i softmax_i(s) v_i with the running maximum and sum of one pass.  Scores are the product K (rows: keys) x Q^T (columns: the rows of a KV head's queries, 32 of them in a
 // wavefront): a lane then has 16 keys of one row, so the maximum and the sum take one exchange between halves of the wavefront, and the weights are where the second product, V^T x weights, wants
 // them if its keys are taken in the order 4 h .. 4 h + 3, 8 + 4 h .. 11 + 4 h of every 16 (h the half).  V^T's operand comes from LDS by the load that transposes four rows of 16.
 // Keys and values go from memory straight into LDS, two blocks ahead.  Many rows: bound by the matrix cores and the vector unit beside them (2.1 us a block of 64 keys and 128 rows, two workgroups to a
-// compute unit: 1024 cycles of products and 850 of softmax for each wavefront); a chunk of 512 tokens behind some 58 000 keys 480 us, 0.99 PFLOP/s, 8 prompts of 2048 to 4096 (32 heads x 128) 918 us,
-// 0.83 PFLOP/s.  Few rows: bound by HBM; 5 tokens for each of 32 sequences of up to 4096 keys, 32 / 8 heads x 128, 62 us (337 MB, 5.4 TB/s) and 5 to join.
+// compute unit: 1024 cycles of products and 850 of softmax for each wavefront); a chunk of 512 tokens behind some 58 000 keys 476 us, 1.00 PFLOP/s, 8 prompts of 2048 to 4096 (32 heads x 128) 900 us,
+// 0.85 PFLOP/s.  Few rows: bound by HBM; 5 tokens for each of 32 sequences of up to 4096 keys, 32 / 8 heads x 128, 62 us (337 MB, 5.4 TB/s) and 5 to join.
 // For an fp16 result weights are fp16 numbers in the second product; for fp32 two each (hi + lo), half as many products again.
 #include "okv_chunk.h"
 #include "okv_host.h"
@@ -98,6 +98,8 @@ __device__ __forceinline__ int sequence_of_row(const Rows &r, const int row) {  
 
 constexpr int kAppendWaves = 4;
 
+// Stores stay in the caches: past them (and loads too) 24 prompts of 100 to 2000 tokens take 109 us instead of 119, but the attention that comes next and reads what is new takes as much more (8 prompts of 2048
+// behind as many, 32 / 8 heads x 128, both launches: 410 us either way; 16 of 300, 40 heads x 64: 72, past them 76 to 89).
 // A wavefront per row.  A lane has 16 elements of a head, which are eight pairs (or none that turn), and the same ones of every 64 / (D / 16)-th head after it:
 // the sines of its pairs are computed once.
 template <int D>
@@ -155,8 +157,8 @@ __global__ void __launch_bounds__(kAppendWaves * 64) append_kernel(Pool c, Rows 
     _Float16 *to = c.kv + at + head_offset<D>(c, g);
     move(a.k + row * a.kv_stride + g * D, to);
     const _Float16 *v = a.v + row * a.kv_stride + g * D;
-    *reinterpret_cast<half8 *>(to + v_offset<D>(c) + 16 * unit) = *reinterpret_cast<const half8 *>(v + 16 * unit);
-    *reinterpret_cast<half8 *>(to + v_offset<D>(c) + 16 * unit + 8) = *reinterpret_cast<const half8 *>(v + 16 * unit + 8);
+    *reinterpret_cast<half8 *>(to + v_offset<D>(c) + 8 * unit) = *reinterpret_cast<const half8 *>(v + 8 * unit);
+    *reinterpret_cast<half8 *>(to + v_offset<D>(c) + 8 * unit + D / 2) = *reinterpret_cast<const half8 *>(v + 8 * unit + D / 2);
   }
 }
 
