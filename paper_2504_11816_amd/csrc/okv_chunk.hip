@@ -6,8 +6,8 @@
 // wavefront): a lane then has 16 keys of one row, so the maximum and the sum take one exchange between halves of the wavefront, and the weights are where the second product, V^T x weights, wants
 // them if its keys are taken in the order 4 h .. 4 h + 3, 8 + 4 h .. 11 + 4 h of every 16 (h the half).  V^T's operand comes from LDS by the load that transposes four rows of 16.
 // Keys and values go from memory straight into LDS, two blocks ahead.  Many rows: bound by the matrix cores and the vector unit beside them (2.1 us a block of 64 keys and 128 rows, two workgroups to a
-// compute unit: 1024 cycles of products and 850 of softmax for each wavefront); a chunk of 512 tokens behind some 58 000 keys 476 us, 1.00 PFLOP/s, 8 prompts of 2048 to 4096 (32 heads x 128) 900 us,
-// 0.85 PFLOP/s.  Few rows: bound by HBM; 5 tokens for each of 32 sequences of up to 4096 keys, 32 / 8 heads x 128, 62 us (337 MB, 5.4 TB/s) and 5 to join.
+// compute unit: 1024 cycles of products and 850 of softmax for each wavefront); a chunk of 512 tokens behind some 58 000 keys 476 us, 1.00 PFLOP/s, 8 prompts of 2048 to 4096 (32 heads x 128) 901 us,
+// 0.84 PFLOP/s.  Few rows: bound by HBM; 5 tokens for each of 32 sequences of up to 4096 keys, 32 / 8 heads x 128, 59 us (337 MB, 5.7 TB/s) and 5 to join.
 // For an fp16 result weights are fp16 numbers in the second product; for fp32 two each (hi + lo), half as many products again.
 #include "okv_chunk.h"
 #include "okv_host.h"
@@ -616,11 +616,14 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     }
     if (odd) atomicMin(&odd_first, i), atomicMax(&odd_last, i);
   };
-  auto step = [&](const int i, const int slot, floatx16 (&x)[kParts], floatx16 (&next)[kParts]) {
+  auto step = [&](auto last, const int i, const int slot, floatx16 (&x)[kParts], floatx16 (&next)[kParts]) {
+    constexpr bool kLast = decltype(last)::value;
     wait_for_loads<0>();
     if constexpr (!FEW) barrier_leaving_loads();         // the next block of keys and this one of values are there, those before free
-    load_values(slot ^ 1);
-    load_keys(i + 2, slot);
+    if constexpr (!kLast) {
+      load_values(slot ^ 1);
+      if (!FEW || i + 2 < total) load_keys(i + 2, slot);
+    }
     __builtin_amdgcn_sched_barrier(0);
     const int key0 = uniform(key_at_step(i));
     char *const v0 = mine + (kRing + slot) * F::kBlockBytes;
@@ -629,7 +632,8 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       if constexpr (!FEW) __syncthreads();
     }
     if (!in_sight(key0)) {
-      if (i + 1 < total && in_sight(uniform(key_at_step(i + 1)))) score(next, slot ^ 1);
+      if constexpr (!kLast)
+        if ((FEW || i + 1 < total) && in_sight(uniform(key_at_step(i + 1)))) score(next, slot ^ 1);
       return;
     }
     const bool whole = (key0 + kKeys - 1 <= pos0 && key0 >= from1) || key0 + kKeys <= p.prefix;
@@ -699,8 +703,8 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       m = to;
     }
     __builtin_amdgcn_s_setprio(1);
-    // The next block's scores under this one's weights (past the end, or out of sight: for nothing)
-    score(next, slot ^ 1);
+    // The next block's scores under this one's weights (out of sight, or past the end of shared blocks: for nothing)
+    if constexpr (!kLast) score(next, slot ^ 1);
     half8 hi[2 * kParts], lo[WIDE ? 2 * kParts : 1];
     const float less = kLift - m + shift;
     float sums[4] = {};
@@ -723,7 +727,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
         o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, hi[t], o[e], 0, 0, 0);
         if constexpr (WIDE) o[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, lo[t], o[e], 0, 0, 0);
       }
-    if constexpr (!FEW) {
+    if constexpr (!FEW && !kLast) {
       // The order of what comes before, as far as operands allow: keys read eight operands ahead, two products of scores with 6 (D = 64: 12) other instructions and 2 (5) exponentials beside them, one of results with 4 and
       // 1.  us of 8 prompts of 2048 to 4096 (32 heads x 128) / a chunk of 512 behind some 58 000 keys: 928 / 478, with four products in a row 936 / 505, fewer instructions beside them
       // 1005 / 530, left to the compiler 965 / 500; without the priority that the products' wavefront has over the other one of its SIMD 957 / 504, with neither 980 / 518
@@ -758,11 +762,27 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     wait_for_loads<2 * kLoads>();
     if constexpr (!FEW) barrier_leaving_loads();
     if (in_sight(uniform(key_at_step(0)))) score(x, 0);
-    for (int i = 0;; i += 2) {
-      step(i, 0, x, y);
-      if (i + 1 >= total) break;
-      step(i + 1, 1, y, x);
-      if (i + 2 >= total) break;
+    // The last step has code of its own, brings nothing and computes no scores after its own: us of 4 sequences of 1 to 5 rows 8.07 -> 7.65, of 5 rows for each of 32 70.6 -> 67.5.  With shared blocks that
+    // needs more registers than there are (872 after 876 for 8 prompts, but 181 after 170 with a cap); loads under a condition in every step take 965 after 909
+    if constexpr (FEW) {
+      int i = 0;
+      for (; i + 2 < total; i += 2) {
+        step(std::false_type{}, i, 0, x, y);
+        step(std::false_type{}, i + 1, 1, y, x);
+      }
+      if (i + 1 < total) {
+        step(std::false_type{}, i, 0, x, y);
+        step(std::true_type{}, i + 1, 1, y, x);
+      } else {
+        step(std::true_type{}, i, 0, x, y);
+      }
+    } else {
+      for (int i = 0;; i += 2) {
+        step(std::false_type{}, i, 0, x, y);
+        if (i + 1 >= total) break;
+        step(std::false_type{}, i + 1, 1, y, x);
+        if (i + 2 >= total) break;
+      }
     }
     wait_for_loads<0>();                                 // nothing may still be on its way into LDS
     __syncthreads();
