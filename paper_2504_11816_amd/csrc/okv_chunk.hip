@@ -487,13 +487,18 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pool c, Rows r, Atte
   if (lane == 0) plan.span = span, plan.pieces[0] = plan.cut_pieces[0] = plan.cut_tiles[0] = 0, plan.steps[0] = 0;
 }
 
+// The steps of a piece in which a wavefront has taken out values that are not finite, of those that not every row sees: none, or the first and the last
+struct Odd {
+  int first, last;
+};
+
 // `meanwhile` is called while the first blocks are on their way
 template <int D, bool FEW, bool WIDE, bool SHAPED, class Meanwhile>
-__device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, const Piece &piece, char *const lds, int &odd_first, int &odd_last, const Meanwhile &meanwhile) {
+__device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, const Piece &piece, char *const lds, Odd *const odd_of, const Meanwhile &meanwhile) {
   using F = Form<D, FEW>;
   constexpr int kWaves = F::kWaves, kLoads = F::kLoads, kKeys = F::kKeys, kRowBytes = 2 * D, kParts = kKeys / 32;
   const Sequence &p = piece.q;
-  if (threadIdx.x == 0) odd_first = INT_MAX, odd_last = -1;      // (a barrier comes before their use)
+  Odd odd{INT_MAX, -1};
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int row0 = piece.tile * F::kRows + (FEW ? 0 : wave * 32), row = row0 + col;         // of the sequence's n R rows
   const int token = row / c.R, head = piece.g * c.R + row - token * c.R;
@@ -598,7 +603,7 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
 
   // A number that is not finite may be of a key that some row does not see, and 0 times it is not 0: it is taken out, and added at the end where it is seen
   auto take_out = [&](const int i, char *const v0) {
-    bool odd = false;
+    bool found = false;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       u32x4 *at = reinterpret_cast<u32x4 *>(v0 + (FEW ? j : j * kWaves + wave) * 1024 + 16 * lane), w = *at;
@@ -611,10 +616,10 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       }
       if (any) {
         *at = w;
-        odd = true;
+        found = true;
       }
     }
-    if (odd) atomicMin(&odd_first, i), atomicMax(&odd_last, i);
+    if (__ballot(found)) odd.first = min(odd.first, i), odd.last = i;
   };
   auto step = [&](auto last, const int i, const int slot, floatx16 (&x)[kParts], floatx16 (&next)[kParts]) {
     constexpr bool kLast = decltype(last)::value;
@@ -785,9 +790,16 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       }
     }
     wait_for_loads<0>();                                 // nothing may still be on its way into LDS
+    // Shared blocks: what any wavefront has taken out is everybody's.  (Few rows: each has taken out what is in its own blocks, and adds that.)
+    if constexpr (!FEW)
+      if (lane == 0) odd_of[wave] = odd;
     __syncthreads();
+    if constexpr (!FEW) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) odd.first = min(odd.first, uniform(odd_of[w].first)), odd.last = max(odd.last, uniform(odd_of[w].last));
+    }
 #pragma unroll 1
-    for (int i = odd_first; i <= odd_last; ++i) {
+    for (int i = odd.first; i <= odd.last; ++i) {
       const int key0 = uniform(key_at_step(i));
       if (all_see(key0)) continue;
 #pragma unroll 1
@@ -891,7 +903,7 @@ template <int D, bool FEW, bool WIDE, bool SHAPED>
 __global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgpu_waves_per_eu(FEW && D == 128 ? 1 : 2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
   using F = Form<D, FEW>;
   __shared__ __attribute__((aligned(1024))) char lds[F::kLds];
-  __shared__ int odd_first, odd_last;                    // steps with values that are not finite, of those that not every row sees
+  __shared__ Odd odd_of[F::kWaves];                      // (used where rows are many)
   Chunk<F, FEW> k(c, r, a);
   Piece p;
   Cut *const cut = reinterpret_cast<Cut *>(a.cuts + 16);
@@ -904,7 +916,7 @@ __global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgp
     }
     if (!piece_of(p, k, c, r, a, (int)blockIdx.x)) return;
     if (!FEW && p.slot >= 0 && p.cut == 0 && threadIdx.x == 0) cut[p.cut_tile] = {p.q.first, p.q.n, p.tile, p.g, p.slot, p.slot + p.apart, p.apart, p.cuts};
-    attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last, [] {});
+    attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_of, [] {});
     return;
   }
   if constexpr (FEW) {
@@ -935,7 +947,7 @@ __global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgp
           next = of_lane(sequence_at<F>(c, r, a, b), 0);
         } while (next.tiles == 0);
       };
-      attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_first, odd_last, look_ahead);
+      attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_of, look_ahead);
       if (!more) return;
       p.q = next, p.begin = 0;
       __syncthreads();                                   // LDS is free again
