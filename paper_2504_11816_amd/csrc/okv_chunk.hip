@@ -172,6 +172,7 @@ struct Attend {
   float scale, cap;                      // of scores in units of log 2: scale log2(e), or with a cap 2 log2(e) scale / cap and cap log2(e)
   int32_t window;                        // 0: none
   int32_t may_cut;                       // whether keys may be cut among workgroups (a second launch joins them)
+  int32_t most_items;                    // what the launch has workgroups for (see span_of)
   const float *slopes;
   const int32_t *prefix;
   Plan *plan;                            // in the workspace
@@ -309,6 +310,8 @@ __device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { retu
 // P <= kSlots, kAlone of that where each has a unit to itself, else (W + P kPerPiece) / kSlots and half a piece until the last one has ended; kPerJoin is added where any are cut.  us with kAlone .6 / 1: 8
 // sequences of 32 tokens 31.0 / 34.6, 5 of 33 to 301 (40 heads x 64) 37.0 / 40.5, 16 of 1 to 600 behind 6000 338 / 330; with kPerPiece 4 and kPerJoin 10, 1000 rows of 8 heads 54.9 (38.5).
 // sum(f) and most(f): over all sequences; pieces_at(s, work, items): how many with spans of s, a lane a span.
+// Many rows: starts that do not ascend may come to more items than n_rows rows have; some pieces then have no workgroup, and what says where a cut tile's results are would not be written for the launch
+// that joins them: nothing is cut.  (Few rows: as many workgroups as there are stretches, whatever the starts.)
 constexpr float kAlone = .6f;
 template <class F, bool FEW, class Sum, class Most, class PiecesAt>
 __device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum &sum, const Most &most, const PiecesAt &pieces_at) {
@@ -324,7 +327,7 @@ __device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum
     if (longest > F::kUncut && even + (items / (stretches * c.G) + 1.f) * F::kPerPiece + F::kPerJoin < best) return uniform((int)fminf(even, 1e9f));
     return kNone;
   } else {
-    if (best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return kNone;
+    if (items > (float)a.most_items || best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return kNone;      // (items of a launch are below 2^24: the sum is exact)
     // a lane a span: the longest item in 2 .. 49 pieces, and from a fourth to four times an even share
     const int lane = threadIdx.x & 63;
     const float least = fmaxf(1.f, ceilf(work * (1.0001f / F::kPieces)));
@@ -1139,6 +1142,7 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
     const int64_t tiles = (all_rows + F::kRows - 1) / F::kRows + std::min(r->batch, r->n_rows), items = tiles * pool.G;
     const int64_t pieces = !x.may_cut ? items : FEW ? std::max<int64_t>(items, F::stretches(pool.G) * pool.G) : items + F::kPieces;
     if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
+    x.most_items = (int32_t)items;
     if (r->batch > 64) hipLaunchKernelGGL((plan_kernel<F, FEW>), dim3(1), dim3(kPlanThreads), 0, s, pool, rows, x);
     if (shaped) hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, true>), dim3((unsigned)pieces), dim3(F::kThreads), 0, s, pool, rows, x);
     else hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, false>), dim3((unsigned)pieces), dim3(F::kThreads), 0, s, pool, rows, x);
