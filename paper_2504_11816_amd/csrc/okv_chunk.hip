@@ -987,14 +987,15 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Pool c, Attend a) {
       factor = __builtin_amdgcn_exp2f(one[F::kRows * D + of_tile] - m);
       l += one[F::kRows * (D + 1) + of_tile] * factor;
     }
-    for (int j0 = 0; j0 < min(kLanes, t.cuts - cut0); j0 += 8) {      // (past the last: that one again, 0 times)
+    for (int j0 = 0; j0 < min(kLanes, t.cuts - cut0); j0 += 8) {      // (past the last: that one again, for nothing)
       floatx4 v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const floatx4 *>(part(min(cut0 + j0 + j, t.cuts - 1)) + of_tile * D + 4 * lane);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
+        // (0 times a piece far below the largest counts, too: it makes a number that is not finite NaN)
         const float by = __shfl(factor, j0 + j, kLanes);
-        if (by != 0.f) o += v[j] * by;
+        if (cut0 + j0 + j < t.cuts) o += v[j] * by;
       }
     }
   }

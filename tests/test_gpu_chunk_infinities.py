@@ -57,3 +57,20 @@ def test_values_that_are_not_finite_in_long_contexts(n_new, H, G, d, dtype):
                 places = sorted({t for t in (lens[b] - 1, lens[b] - 2, lens[b] - n, lens[b] - n // 2 - 1, lens[b] - window - n + 1, lens[b] - window - 1, lens[b] - window - 33) if 0 <= t < lens[b]})
                 odd += [(b, (i + part) % G, t, values[(i + part) % 3]) for i, t in enumerate(places) if i % 3 == part]
             check(p, odd, q, n_new, dtype, window)
+
+
+@pytest.mark.parametrize("dtype", (torch.float16, torch.float32), ids=str)
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("n_new", ([4, 2], [200, 90]), ids=("few", "many"))
+def test_values_that_are_not_finite_far_below_the_largest_score(n_new, d, dtype):
+    """A key with a score of hundreds in one piece of the keys, a value that is not finite in another, whose weights are 2^-126 of the largest and less: the result is infinite or NaN however the keys were cut."""
+    lens = [9000, 7000]
+    p = Paged(4, 2, d, 64, lens, seed=d)
+    for b in range(2):
+        for g in range(2):
+            p.pool[p.offset(b, 0, g, lens[b] - n_new[b] - 300)] = 2000.0
+    p.upload()
+    q = torch.randn((sum(n_new), 4, d), generator=torch.Generator().manual_seed(4)).half().to(DEV)
+    q[:, :, 0] = 4.0                                         # 2000 * 4 / sqrt(d): 707 and more above the others
+    for value in (np.inf, -np.inf, np.nan):
+        check(p, [(0, 0, 5, value), (1, 1, 2000, value)], q, n_new, dtype)
