@@ -171,8 +171,7 @@ struct Attend {
   int64_t q_stride;
   float scale, cap;                      // of scores in units of log 2: scale log2(e), or with a cap 2 log2(e) scale / cap and cap log2(e)
   int32_t window;                        // 0: none
-  int32_t may_cut;                       // whether keys may be cut among workgroups (a second launch joins them)
-  int32_t most_items;                    // what the launch has workgroups for (see span_of)
+  int32_t may_cut;                       // whether keys may be cut among workgroups (a second launch joins them): 0, or the most items that the launch has workgroups for (see span_of)
   const float *slopes;
   const int32_t *prefix;
   Plan *plan;                            // in the workspace
@@ -327,7 +326,7 @@ __device__ __forceinline__ int span_of(const Pool &c, const Attend &a, const Sum
     if (longest > F::kUncut && even + (items / (stretches * c.G) + 1.f) * F::kPerPiece + F::kPerJoin < best) return uniform((int)fminf(even, 1e9f));
     return kNone;
   } else {
-    if (items > (float)a.most_items || best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return kNone;      // (items of a launch are below 2^24: the sum is exact)
+    if (items > (float)a.may_cut || best < 1.2f * fmaxf(F::kPerJoin, work * (1.f / F::kSlots))) return kNone;      // (items of a launch are below 2^24: the sum is exact)
     // a lane a span: the longest item in 2 .. 49 pieces, and from a fourth to four times an even share
     const int lane = threadIdx.x & 63;
     const float least = fmaxf(1.f, ceilf(work * (1.0001f / F::kPieces)));
@@ -497,11 +496,13 @@ struct Odd {
 
 // `meanwhile` is called while the first blocks are on their way
 template <int D, bool FEW, bool WIDE, bool SHAPED, class Meanwhile>
-__device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, const Piece &piece, char *const lds, Odd *const odd_of, const Meanwhile &meanwhile) {
+__device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, const Piece &piece, char *const lds, Odd &shared_odd, const Meanwhile &meanwhile) {
   using F = Form<D, FEW>;
   constexpr int kWaves = F::kWaves, kLoads = F::kLoads, kKeys = F::kKeys, kRowBytes = 2 * D, kParts = kKeys / 32;
   const Sequence &p = piece.q;
+  // Few rows: each wavefront's own, in registers.  Many: everybody's, in LDS, set before the barrier that comes before the first step
   Odd odd{INT_MAX, -1};
+  if (!FEW && threadIdx.x == 0) shared_odd = odd;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int row0 = piece.tile * F::kRows + (FEW ? 0 : wave * 32), row = row0 + col;         // of the sequence's n R rows
   const int token = row / c.R, head = piece.g * c.R + row - token * c.R;
@@ -622,7 +623,11 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
         found = true;
       }
     }
-    if (__ballot(found)) odd.first = min(odd.first, i), odd.last = i;
+    if constexpr (FEW) {
+      if (__ballot(found)) odd.first = min(odd.first, i), odd.last = i;
+    } else if (found) {
+      atomicMin(&shared_odd.first, i), atomicMax(&shared_odd.last, i);
+    }
   };
   auto step = [&](auto last, const int i, const int slot, floatx16 (&x)[kParts], floatx16 (&next)[kParts]) {
     constexpr bool kLast = decltype(last)::value;
@@ -768,7 +773,10 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
     __builtin_amdgcn_sched_barrier(0);
     meanwhile();
     wait_for_loads<2 * kLoads>();
-    if constexpr (!FEW) barrier_leaving_loads();
+    if constexpr (!FEW) {
+      __builtin_amdgcn_s_waitcnt(0xc07f);                // (what thread 0 has set is in LDS)
+      barrier_leaving_loads();
+    }
     if (in_sight(uniform(key_at_step(0)))) score(x, 0);
     // The last step has code of its own, brings nothing and computes no scores after its own: us of 4 sequences of 1 to 5 rows 8.07 -> 7.65, of 5 rows for each of 32 70.6 -> 67.5.  With shared blocks that
     // needs more registers than there are (872 after 876 for 8 prompts, but 181 after 170 with a cap); loads under a condition in every step take 965 after 909
@@ -793,14 +801,8 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
       }
     }
     wait_for_loads<0>();                                 // nothing may still be on its way into LDS
-    // Shared blocks: what any wavefront has taken out is everybody's.  (Few rows: each has taken out what is in its own blocks, and adds that.)
-    if constexpr (!FEW)
-      if (lane == 0) odd_of[wave] = odd;
     __syncthreads();
-    if constexpr (!FEW) {
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) odd.first = min(odd.first, uniform(odd_of[w].first)), odd.last = max(odd.last, uniform(odd_of[w].last));
-    }
+    if constexpr (!FEW) odd = {uniform(shared_odd.first), uniform(shared_odd.last)};
 #pragma unroll 1
     for (int i = odd.first; i <= odd.last; ++i) {
       const int key0 = uniform(key_at_step(i));
@@ -906,7 +908,7 @@ template <int D, bool FEW, bool WIDE, bool SHAPED>
 __global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgpu_waves_per_eu(FEW && D == 128 ? 1 : 2, 2))) chunk_kernel(Pool c, Rows r, Attend a) {
   using F = Form<D, FEW>;
   __shared__ __attribute__((aligned(1024))) char lds[F::kLds];
-  __shared__ Odd odd_of[F::kWaves];                      // (used where rows are many)
+  __shared__ Odd shared_odd;
   Chunk<F, FEW> k(c, r, a);
   Piece p;
   Cut *const cut = reinterpret_cast<Cut *>(a.cuts + 16);
@@ -919,7 +921,7 @@ __global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgp
     }
     if (!piece_of(p, k, c, r, a, (int)blockIdx.x)) return;
     if (!FEW && p.slot >= 0 && p.cut == 0 && threadIdx.x == 0) cut[p.cut_tile] = {p.q.first, p.q.n, p.tile, p.g, p.slot, p.slot + p.apart, p.apart, p.cuts};
-    attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_of, [] {});
+    attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, shared_odd, [] {});
     return;
   }
   if constexpr (FEW) {
@@ -950,7 +952,7 @@ __global__ void __launch_bounds__((Form<D, FEW>::kThreads)) __attribute__((amdgp
           next = of_lane(sequence_at<F>(c, r, a, b), 0);
         } while (next.tiles == 0);
       };
-      attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, odd_of, look_ahead);
+      attend_piece<D, FEW, WIDE, SHAPED>(c, a, p, lds, shared_odd, look_ahead);
       if (!more) return;
       p.q = next, p.begin = 0;
       __syncthreads();                                   // LDS is free again
@@ -1143,7 +1145,7 @@ int okv_chunk_attn(const okv_layer_pool *c, const okv_rows *r, const okv_chunk *
     const int64_t tiles = (all_rows + F::kRows - 1) / F::kRows + std::min(r->batch, r->n_rows), items = tiles * pool.G;
     const int64_t pieces = !x.may_cut ? items : FEW ? std::max<int64_t>(items, F::stretches(pool.G) * pool.G) : items + F::kPieces;
     if (pieces > 0x7fffffff / 256) return report(OKV_EINVAL, "%s: too many rows for a call", who);
-    x.most_items = (int32_t)items;
+    if (x.may_cut) x.may_cut = (int32_t)items;
     if (r->batch > 64) hipLaunchKernelGGL((plan_kernel<F, FEW>), dim3(1), dim3(kPlanThreads), 0, s, pool, rows, x);
     if (shaped) hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, true>), dim3((unsigned)pieces), dim3(F::kThreads), 0, s, pool, rows, x);
     else hipLaunchKernelGGL((chunk_kernel<D, FEW, WIDE, false>), dim3((unsigned)pieces), dim3(F::kThreads), 0, s, pool, rows, x);
