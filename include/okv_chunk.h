@@ -9,8 +9,8 @@
  * Conventions as in okv.h: C ABI, every pointer DEVICE unless labelled, the caller owns all memory, calls enqueue on the
  * stream and return at once; OKV_OK or a negative OKV_E* code; okv_last_error(NULL) has the message.  No call
  * allocates, copies or waits: all may be captured in a graph.  Lengths, starts, rows of the table and page numbers are read
- * on the device: a length is taken as at least 0 and at most the capacity, wrong rows of the table are passed over and wrong
- * pages give wrong numbers, no access outside the buffers.
+ * on the device: a length is taken as at least 0 (and in attention at most the capacity), wrong rows of the table are passed
+ * over and wrong pages give wrong numbers, no access outside the buffers.
  */
 #ifndef OKV_CHUNK_H
 #define OKV_CHUNK_H
@@ -60,7 +60,7 @@ typedef struct okv_rope {
 } okv_rope;
 
 /* Row i of n rows of a sequence of len tokens becomes its token len - n + i: keys turned, values as they are.  Tokens before 0
- * or past the capacity are not stored.
+ * or past the capacity (a len may be above it) are not stored; their queries are turned by their positions all the same.
  *   k, v   fp16 [n_rows][G][d], rows kv_stride elements apart (a multiple of 8, at least G * d), 16-byte aligned
  *   q      fp16 [n_rows][H][d] (q_stride likewise) and q_out (q_out_stride): turned queries; NULL: there are none.  q_out may be q
  *          (with the same stride), and overlap nothing else

@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(kAppendWaves * 64) append_kernel(Pool c, Rows 
   rows_of(r, b, first, last);
   if (row < first || row >= last) return;                // (starts that do not ascend)
   const bool known = s >= 0 && s < c.max_seqs;
-  if (known) len = min(max(r.lens[s], 0), c.capacity);
-  const int token = len - (last - row);
+  if (known) len = max(r.lens[s], 0);
+  const int token = len - (last - row);                  // (past the capacity: turned like others, and not stored)
   constexpr int kUnits = D / 16, kHeads = 64 / kUnits;
   const int unit = lane % kUnits, slot = lane / kUnits, turning = a.rotated / 16;
   const bool turns = a.turns && unit < turning;
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kAppendWaves * 64) append_kernel(Pool c, Rows 
   };
   if (a.q)
     for (int h = slot; h < a.H; h += kHeads) move(a.q + row * a.q_stride + h * D, a.q_out + row * a.q_out_stride + h * D);
-  if (!known || token < 0 || (c.refused && *c.refused)) return;
+  if (!known || token < 0 || token >= c.capacity || (c.refused && *c.refused)) return;
   const int64_t at = tile_at<D>(c, c.table + (int64_t)s * c.width, s, token >> 4) + (token & 15) * D;
   for (int g = slot; g < c.G; g += kHeads) {
     _Float16 *to = c.kv + at + head_offset<D>(c, g);

@@ -1,0 +1,57 @@
+"""Rows whose tokens the pool has no place for."""
+import numpy as np
+import pytest
+import torch
+
+from chunk_util import DEV, ids
+from oracle import chunk as oracle
+from oracle import kv_layout
+from paper_2504_11816_amd.cache16 import Cache16, Rope
+
+pytestmark = pytest.mark.gpu
+
+
+def filled(H, G, d, T, per_seq, seqs=2, seed=0):
+    """A cache whose sequences may have per_seq pages each, all of them in the table, every number set."""
+    n_pages = per_seq * seqs
+    c = Cache16(n_layers=1, n_q_heads=H, n_kv_heads=G, head_dim=d, page_tokens=T, n_pages=n_pages, max_seqs=seqs, max_pages_per_seq=per_seq, device=DEV)
+    rng = np.random.default_rng(seed)
+    c.table.copy_(torch.from_numpy(rng.permutation(n_pages).astype(np.int32).reshape(seqs, per_seq)))
+    c.pool.copy_(torch.from_numpy(rng.standard_normal(tuple(c.pool.shape)).astype(np.float16)))
+    return c
+
+
+def layout_of(c):
+    return dict(kind="paged", G=c.G, d=c.d, T=c.T, block_table=c.table.cpu().numpy())
+
+
+def normal(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).half().to(DEV)
+
+
+@pytest.mark.parametrize("G,d", [(2, 64), (4, 128)])
+@pytest.mark.parametrize("over", (1, 2, 4, 30, 1 << 30, (1 << 31) - 1 - 64))
+def test_tokens_past_the_capacity_are_not_stored(over, G, d):
+    """Row i of n is token len - n + i whatever the capacity: those that fit are at their own places, turned by them, earlier tokens stay bit for bit, and queries are turned by their own positions."""
+    T, per_seq, n = 16, 4, 4
+    capacity = T * per_seq
+    c = filled(G, G, d, T, per_seq, seed=G)
+    before, layout = c.pool.cpu().numpy().reshape(-1).copy(), layout_of(c)
+    k, v, q = normal(1, n, G, d), normal(2, n, G, d), normal(3, n, G, d)
+    q_out = torch.empty_like(q)
+    c.append(0, k, v, ids([0, n]), ids([0, capacity + over]), ids([1]), q=q, q_out=q_out, rope=Rope.of(d, device=DEV))
+    tokens = [capacity + over - n + i for i in range(n)]
+    freq = 10000.0 ** (-np.arange(0, d, 2) / d)
+    turned, want, places = oracle.rotate(k.cpu().numpy(), tokens, freq, False), before.astype(np.float64), np.zeros(before.shape, dtype=bool)
+    for i, t in enumerate(tokens):
+        if t < capacity:
+            for g in range(G):
+                a, z = kv_layout.token_row_offset(layout, 1, 0, g, t), kv_layout.token_row_offset(layout, 1, 1, g, t)
+                want[a:a + d], want[z:z + d], places[a:a + d] = turned[i, g], v[i, g].cpu().numpy(), True
+    got = c.pool.cpu().numpy().reshape(-1)
+    assert np.array_equal(got[~places], want[~places])
+    # (a turned number: half a step of itself, factors off by 2^-22 and, of positions of 2^31, an angle off by some 2^-53 of itself: 2^-19 of numbers of up to 5)
+    size = 2.0 ** -19 * 2 * 5
+    assert (np.abs(got - want) <= 2.0 ** -11 * np.abs(want) + size)[places].all()
+    qw = oracle.rotate(q.cpu().numpy(), tokens, freq, False)
+    assert (np.abs(q_out.cpu().numpy() - qw) <= 2.0 ** -11 * np.abs(qw) + size).all()
