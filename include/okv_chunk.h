@@ -9,7 +9,7 @@
  * Conventions as in okv.h: C ABI, every pointer DEVICE unless labelled, the caller owns all memory, calls enqueue on the
  * stream and return at once; OKV_OK or a negative OKV_E* code; okv_last_error(NULL) has the message.  No call
  * allocates, copies or waits: all may be captured in a graph.  Lengths, starts, rows of the table and page numbers are read
- * on the device: a length is taken as at least 0 (and in attention at most the capacity), wrong rows of the table are passed
+ * on the device: a length is taken as at least 0, what lies past the capacity is not there, wrong rows of the table are passed
  * over and wrong pages give wrong numbers, no access outside the buffers.
  */
 #ifndef OKV_CHUNK_H
@@ -72,7 +72,7 @@ int okv_rope_append(const okv_layer_pool *c, const okv_rows *r, const okv_rope *
  * those below the sequence's prefix, wherever they are.  Scores, in fp32:
  *     s_i = scale (q . k_i);   s_i = cap tanh(s_i / cap) with a cap;   s_i -= slopes[h] |p - i| with slopes
  *     out = sum_i softmax_i(s) v_i
- * A row that sees no key is 0 (p < 0: the sequence has fewer tokens than rows).  A score of -infinity leaves its key out (0 if no key
+ * A row that sees no key is 0 (p < 0: the sequence has fewer tokens than rows).  Rows of tokens past the capacity (a len may be above it) attend as the pool's last token does.  A score of -infinity leaves its key out (0 if no key
  * is left), one that is +infinity or NaN makes the row NaN; an infinite or NaN value makes what it goes into infinite or NaN.  What lies at keys that a row does not see, infinities and NaN included, does not
  * change it.  Weights are fp16 in the second product for an fp16 result (each off by 2^-12 of itself, or 2^-32 of the largest), two fp16
  * numbers for an fp32 one (2^-22); sums are fp32. */

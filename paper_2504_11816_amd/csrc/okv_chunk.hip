@@ -251,8 +251,8 @@ struct Keys {
   int ahead, first, total;
 };
 template <class F>
-__device__ __forceinline__ Keys keys_of(const int n, const int len, const int prefix, const int window, const int R, const int tile) {
-  const int pos0 = len - n + tile * F::kRows / R, pos1 = len - n + min((tile * F::kRows + F::kRows - 1) / R, n - 1);
+__device__ __forceinline__ Keys keys_of(const int n, const int base, const int len, const int prefix, const int window, const int R, const int tile) {
+  const int pos0 = min(base + tile * F::kRows / R, len - 1), pos1 = min(base + min((tile * F::kRows + F::kRows - 1) / R, n - 1), len - 1);
   Keys k;
   k.first = window == 0 || pos0 < window ? 0 : (pos0 - window + 1) / F::kStep;
   k.ahead = min((prefix + F::kStep - 1) / F::kStep, k.first);
@@ -268,7 +268,8 @@ __device__ __forceinline__ Keys keys_of(const int n, const int len, const int pr
 // Lengths are on the device: every wavefront finds this out for itself, a lane per sequence; beyond 64 sequences a launch of one workgroup adds up chunks of 64 first.
 constexpr int kNone = 0x3fffffff;
 struct Sequence {
-  int first, n, s, len, prefix;          // its first row, its rows, its row of the table (below 0: there is none), its tokens, those of its prefix
+  int first, n, s, len, prefix;          // its first row, its rows, its row of the table (below 0: there is none), its tokens (at most the capacity), those of its prefix
+  int base;                              // the first row's position: rows past the capacity, which the pool has no tokens of, have the last token's
   int tiles, steps;                      // steps: of its last tile, which sees the most keys; others' are taken to be as many
 };
 struct Plan {                            // in the workspace, for more than 64 sequences; before each chunk of 64, and behind the last
@@ -288,19 +289,22 @@ constexpr int64_t kCutBytes = 16 + kMostCuts * (int64_t)sizeof(Cut);      // (ma
 
 template <class F>
 __device__ __forceinline__ Sequence sequence_at(const Pool &c, const Rows &r, const Attend &a, const int b) {
-  Sequence q{0, 0, -1, 0, 0, 0, 0};
+  Sequence q{0, 0, -1, 0, 0, 0, 0, 0};
   if (b >= r.batch) return q;
   int last;
   rows_of(r, b, q.first, last);
   q.n = last - q.first;
+  q.base = -q.n;
   const int s = r.seqs ? r.seqs[b] : b;
   if (s >= 0 && s < c.max_seqs) {
     q.s = s;
-    q.len = min(max(r.lens[s], 0), c.capacity);
+    const int lens = max(r.lens[s], 0);
+    q.len = min(lens, c.capacity);
+    q.base = min(lens - q.n, q.len);
     if (a.prefix) q.prefix = min(max(a.prefix[s], 0), q.len);
   }
   q.tiles = (int)(((int64_t)q.n * c.R + F::kRows - 1) / F::kRows);
-  if (q.tiles) q.steps = max(keys_of<F>(q.n, q.len, q.prefix, a.window, c.R, q.tiles - 1).total, 1);      // (an item without keys is a step, too: its rows are 0)
+  if (q.tiles) q.steps = max(keys_of<F>(q.n, q.base, q.len, q.prefix, a.window, c.R, q.tiles - 1).total, 1);      // (an item without keys is a step, too: its rows are 0)
   return q;
 }
 __device__ __forceinline__ int cuts_of(const Sequence &q, const int span) { return (int)(((unsigned)q.steps + (unsigned)span - 1) / (unsigned)span); }
@@ -386,7 +390,7 @@ struct Piece {
   int cuts, cut, cut_tile, apart;        // pieces of the tile, and which one this is; the number of the tile among those that are cut; slots from a piece to the next
 };
 __device__ __forceinline__ Sequence of_lane(const Sequence &q, const int lane) {
-  return {lane_value(q.first, lane), lane_value(q.n, lane), lane_value(q.s, lane), lane_value(q.len, lane), lane_value(q.prefix, lane), lane_value(q.tiles, lane), lane_value(q.steps, lane)};
+  return {lane_value(q.first, lane), lane_value(q.n, lane), lane_value(q.s, lane), lane_value(q.len, lane), lane_value(q.prefix, lane), lane_value(q.base, lane), lane_value(q.tiles, lane), lane_value(q.steps, lane)};
 }
 // Items of a sequence: the heads of a tile next to each other, so that those of a head are on the same XCD where they are a multiple of eight; tiles that see the most keys first
 __device__ __forceinline__ void set_item(Piece &p, const Pool &c, const int item) {
@@ -506,20 +510,21 @@ __device__ __forceinline__ void attend_piece(const Pool &c, const Attend &a, con
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int row0 = piece.tile * F::kRows + (FEW ? 0 : wave * 32), row = row0 + col;         // of the sequence's n R rows
   const int token = row / c.R, head = piece.g * c.R + row - token * c.R;
-  const int base = p.len - p.n, pos = base + token;
+  auto position = [&](const int token) { return min(p.base + token, p.len - 1); };
+  const int pos = position(token);
   auto first_seen = [&](const int pos) { return a.window == 0 || pos < a.window ? 0 : pos - a.window + 1; };      // (but for the prefix)
   const int from = first_seen(pos);
   // of this wavefront's rows, and of the tile's
   const int token0 = uniform(row0 / c.R), token1 = min(uniform((row0 + 31) / c.R), p.n - 1);
   const bool idle = token0 >= p.n;
-  const int pos0 = base + token0, pos1 = base + token1, from0 = first_seen(pos0), from1 = first_seen(pos1);
-  const int tile_pos0 = base + uniform(piece.tile * F::kRows / c.R), tile_pos1 = base + min(uniform((piece.tile * F::kRows + F::kRows - 1) / c.R), p.n - 1);
+  const int pos0 = position(token0), pos1 = position(token1), from0 = first_seen(pos0), from1 = first_seen(pos1);
+  const int tile_pos0 = position(uniform(piece.tile * F::kRows / c.R)), tile_pos1 = position(min(uniform((piece.tile * F::kRows + F::kRows - 1) / c.R), p.n - 1));
   const int tile_from1 = first_seen(tile_pos1);
   auto all_see = [&](const int key0) { return (key0 + kKeys - 1 <= tile_pos0 && key0 >= tile_from1) || key0 + kKeys <= p.prefix; };      // rows of the tile
   auto in_sight = [&](const int key0) { return !idle && ((key0 <= pos1 && key0 + kKeys > from0) || key0 < p.prefix); };                  // of some row of the wavefront
 
   // this piece's steps of the tile's
-  Keys keys = keys_of<F>(p.n, p.len, p.prefix, a.window, c.R, piece.tile);
+  Keys keys = keys_of<F>(p.n, p.base, p.len, p.prefix, a.window, c.R, piece.tile);
   keys.ahead = uniform(keys.ahead), keys.first = uniform(keys.first), keys.total = uniform(keys.total);
   const bool whole_tile = piece.slot < 0;
   const int i0 = whole_tile ? 0 : share(keys.total, piece.begin, p.steps), total = whole_tile ? keys.total : share(keys.total, piece.end, p.steps) - i0;

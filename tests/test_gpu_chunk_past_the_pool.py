@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from chunk_util import DEV, ids
+from chunk_util import DEV, check_rows, ids, starts_of
 from oracle import chunk as oracle
 from oracle import kv_layout
 from paper_2504_11816_amd.cache16 import Cache16, Rope
@@ -55,3 +55,41 @@ def test_tokens_past_the_capacity_are_not_stored(over, G, d):
     assert (np.abs(got - want) <= 2.0 ** -11 * np.abs(want) + size)[places].all()
     qw = oracle.rotate(q.cpu().numpy(), tokens, freq, False)
     assert (np.abs(q_out.cpu().numpy() - qw) <= 2.0 ** -11 * np.abs(qw) + size).all()
+
+
+class Tokens:
+    """What check_rows asks of a cache."""
+
+    def __init__(self, c, seq):
+        self.H, self.G, self.d, self.lens = c.H, c.G, c.d, [c.T * c.table.shape[1]]
+        self.pool, self.layout, self.seq = c.pool.cpu().numpy().reshape(-1), layout_of(c), seq
+
+    def rows(self, b, kv, g):
+        return kv_layout.gather_rows(self.pool, self.layout, self.seq, kv, g, self.lens[b])
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(window=9), dict(window=40, prefix=5), dict(slopes=True), dict(cap=4.0, window=100)], ids=str)
+@pytest.mark.parametrize("n,over", [(5, 2), (150, 20), (3, 3), (4, 9), (150, 1 << 30), (70, (1 << 31) - 1 - 2048)])
+@pytest.mark.parametrize("H,G,d,per_seq", [(4, 2, 64, 12), (3, 3, 128, 12), (4, 2, 64, 128)])
+def test_attention_past_the_capacity(H, G, d, per_seq, n, over, kw):
+    """A row's position is its token's place: rows whose tokens the pool has attend from there, as they do in a call without those behind them; rows past it attend as its last token does.  In small caches and in
+    those whose keys may be cut, few rows and many."""
+    T = 16
+    capacity = T * per_seq
+    over = min(over, (1 << 31) - 1 - capacity)
+    c = filled(H, G, d, T, per_seq, seed=d + per_seq)
+    q, kw = normal(n, n, H, d), dict(kw)
+    how = dict(kw)
+    if kw.get("slopes"):
+        kw["slopes"] = [2.0 ** -(i + 1) for i in range(H)]
+        how["slopes"] = torch.tensor(kw["slopes"], device=DEV)
+    if kw.get("prefix"):
+        how["prefix"], kw["prefix"] = ids([0, kw["prefix"]]), [kw["prefix"]]
+    for dtype in (torch.float16, torch.float32):
+        out = torch.full(q.shape, np.nan, dtype=dtype, device=DEV)
+        c.attend(0, q, out, starts_of([n]), ids([0, capacity + over]), ids([1]), **how)
+        p, there = Tokens(c, 1), max(0, n - over)
+        if there:
+            check_rows(p, q[:there], out[:there], [there], **kw)
+        for j in {there, (there + n) // 2, n - 1}:
+            check_rows(p, q[j:j + 1], out[j:j + 1], [1], **kw)
