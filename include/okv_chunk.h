@@ -10,7 +10,7 @@
  * stream and return at once; OKV_OK or a negative OKV_E* code; okv_last_error(NULL) has the message.  No call
  * allocates, copies or waits: all may be captured in a graph.  Lengths, starts, rows of the table and page numbers are read
  * on the device: a length is taken as at least 0, what lies past the capacity is not there, wrong rows of the table are passed
- * over and wrong pages give wrong numbers, no access outside the buffers.
+ * over, nothing is stored in wrong pages and reading them gives wrong numbers, no access outside the buffers.
  */
 #ifndef OKV_CHUNK_H
 #define OKV_CHUNK_H

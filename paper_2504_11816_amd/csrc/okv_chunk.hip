@@ -152,7 +152,10 @@ __global__ void __launch_bounds__(kAppendWaves * 64) append_kernel(Pool c, Rows 
   if (a.q)
     for (int h = slot; h < a.H; h += kHeads) move(a.q + row * a.q_stride + h * D, a.q_out + row * a.q_out_stride + h * D);
   if (!known || token < 0 || token >= c.capacity || (c.refused && *c.refused)) return;
-  const int64_t at = tile_at<D>(c, c.table + (int64_t)s * c.width, s, token >> 4) + (token & 15) * D;
+  const int32_t *table_row = c.table + (int64_t)s * c.width;
+  // (a page that is none of the pool's: there is no place for the token, and another sequence's would lose its own)
+  if (c.table && (unsigned)table_row[token >> 4 >> c.log2_tiles] >= (unsigned)c.n_blocks) return;
+  const int64_t at = tile_at<D>(c, table_row, s, token >> 4) + (token & 15) * D;
   for (int g = slot; g < c.G; g += kHeads) {
     _Float16 *to = c.kv + at + head_offset<D>(c, g);
     move(a.k + row * a.kv_stride + g * D, to);

@@ -1,4 +1,4 @@
-"""Rows whose tokens the pool has no place for."""
+"""Rows whose tokens the pool has no place for: past the capacity, and in pages that the table does not name."""
 import numpy as np
 import pytest
 import torch
@@ -93,3 +93,22 @@ def test_attention_past_the_capacity(H, G, d, per_seq, n, over, kw):
             check_rows(p, q[:there], out[:there], [there], **kw)
         for j in {there, (there + n) // 2, n - 1}:
             check_rows(p, q[j:j + 1], out[j:j + 1], [1], **kw)
+
+
+@pytest.mark.parametrize("missing", (-1, -5, 8, 1 << 30))
+def test_rows_of_pages_that_the_table_does_not_name_are_not_stored(missing):
+    """Nothing goes into a page that is another sequence's."""
+    T, G, d = 16, 2, 64
+    c = filled(G, G, d, T, 4)
+    c.table[1, 2] = missing
+    before, layout = c.pool.cpu().numpy().reshape(-1).copy(), layout_of(c)
+    k, v = normal(1, 24, G, d), normal(2, 24, G, d)
+    c.append(0, k, v, ids([0, 24]), ids([0, 52]), ids([1]))      # tokens 28 .. 51: the missing page's are 32 .. 47
+    want = before.copy()
+    for i, t in enumerate(range(28, 52)):
+        if t // T != 2:
+            for g in range(G):
+                for kv, x in ((0, k), (1, v)):
+                    a = kv_layout.token_row_offset(layout, 1, kv, g, t)
+                    want[a:a + d] = x[i, g].cpu().numpy()
+    assert np.array_equal(c.pool.cpu().numpy().reshape(-1), want)
