@@ -20,7 +20,8 @@ extern "C" {
 
 /* out[r][i] = softmax_i(logits[r][i] / t_r), sums in fp32.
  *   logits       fp16 (dtype 0) or fp32 (1) [rows][vocab], rows `stride` elements apart (at least vocab), aligned to their size
- *   temperature  fp32 [rows], or NULL: 1.  0: 1 at the first of the row's largest logits, 0 elsewhere.  Negative or NaN: the row is NaN
+ *   temperature  fp32 [rows], or NULL: 1.  0: 1 at the first of the row's largest logits, 0 elsewhere.  Infinite: the same for every logit above
+ *                -infinity.  Negative or NaN: the row is NaN
  *   out          fp32 [rows][vocab], rows out_stride elements apart; not overlapping logits
  * A logit of -infinity has probability 0, a row of nothing else is 0.  One that is infinite or NaN makes its row NaN (an infinite
  * one at temperature 0 is the largest, and NaN is passed over there). */

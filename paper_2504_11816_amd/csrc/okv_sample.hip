@@ -118,8 +118,9 @@ __device__ __forceinline__ Seen seen_by_all(float (&x)[kEach / RUN][RUN], const 
   for (int w = 0; w < kWaves; ++w) s.sum += shared[w];
   return s;
 }
-// (x - top) / t in units of log 2.  A temperature below 1e-30 is as good as that: the largest take all
-__device__ __forceinline__ float per_temperature(const float t) { return t >= 0.f ? kLog2e / fmaxf(t, 1e-30f) : NAN; }
+// (x - top) / t in units of log 2.  A temperature below 1e-30 is as good as that: the largest take all.  Of an infinite one the smallest number there is stays, with which differences of finite logits come
+// to less than 2^-20 and those of -infinity (0 times which is NaN) to that.
+__device__ __forceinline__ float per_temperature(const float t) { return t >= 0.f ? fmaxf(kLog2e / fmaxf(t, 1e-30f), 0x1p-149f) : NAN; }
 
 template <class T>
 __global__ void __launch_bounds__(kRowThreads) row_probs_kernel(const T *logits, const int64_t stride, const float *temperature, float *out, const int64_t out_stride, const int vocab) {
