@@ -155,6 +155,6 @@ class Cache16:
 
     def check_how(self, scale=0.0, cap=0.0, window=0, slopes=None, prefix=None):
         """Raises unless attend() takes these, with sequences by their rows of the table."""
-        if not (all(x == 0 or 1e-30 <= x <= 1e30 for x in (scale, cap)) and 0 <= window < 1 << 31):
-            raise ValueError("scale and cap must be 0 or in [1e-30, 1e30], window in [0, 2^31)")
+        if not (all(x == 0 or 1e-30 <= x <= 1e30 for x in (scale, cap)) and hasattr(window, "__index__") and 0 <= window < 1 << 31):
+            raise ValueError("scale and cap must be 0 or in [1e-30, 1e30], window a whole number in [0, 2^31)")
         self._vectors(slopes, prefix, self.max_seqs)

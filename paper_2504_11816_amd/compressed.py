@@ -51,9 +51,11 @@ class Scratch:
         return (b[:batch] for b in (self.a, self.q, self.k, self.v, self.t, self.y, self.z, self.u))
 
 
-def _check_widths(cache, layers, scratch, x, rows):
+def _check_widths(cache, layers, scratch, x, rows, eps):
     h1, kv = cache.H * cache.d, cache.G * cache.d
     need("x", x, torch.float16, (rows, h1), cache.device)
+    if x.data_ptr() % 16 or not eps >= 0:                    # (the first norm would refuse them, when lengths have grown)
+        raise ValueError("x must be 16-byte aligned, and eps not negative")
     h2 = scratch.u.shape[1]
     if len(layers) != cache.L or any(w.h1 != h1 or w.kv_cols != kv or w.h2 != h2 for w in layers):
         raise ValueError(f"there must be {cache.L} layers of widths {h1}, {kv} and {h2}, as the cache and the scratch have them")
@@ -61,13 +63,13 @@ def _check_widths(cache, layers, scratch, x, rows):
         raise ValueError(f"the scratch must be for widths {h1} and {kv}, on {cache.device}")
 
 
-def _check(cache, layers, scratch, x, seqs):
+def _check(cache, layers, scratch, x, seqs, eps):
     """Raises before anything has changed: lengths that have grown, or layers that have appended, would stay so."""
     B = x.shape[0]
     need("seqs", seqs, torch.int32, (B,), cache.device)
     if cache.out_dtype is not torch.float16:
         raise ValueError("the cache's results go into products: out_dtype must be torch.float16")
-    _check_widths(cache, layers, scratch, x, B)
+    _check_widths(cache, layers, scratch, x, B, eps)
 
 
 def decoder_step(cache, layers, scratch, x, seqs, eps=1e-5):
@@ -76,7 +78,7 @@ def decoder_step(cache, layers, scratch, x, seqs, eps=1e-5):
     says so in cache.pages.check(): it is then as it was before the step, and x means nothing.  Arguments that do not fit raise a ValueError, and change
     nothing."""
     rows = scratch.rows(x.shape[0])
-    _check(cache, layers, scratch, x, seqs)
+    _check(cache, layers, scratch, x, seqs, eps)
     B, stream = x.shape[0], binding.current_stream(x.device)
     a, q, k, v, t, y, z, u = rows
     h1 = x.shape[1]
@@ -99,7 +101,7 @@ def decoder_chunk(cache, layers, scratch, x, starts, seqs, n_new, rope=None, eps
     GPU's side; a cache that is out of pages says so in cache.pages.check(): it is then as it was, and x means nothing.  Arguments that do not fit raise a ValueError, and
     change nothing."""
     rows = scratch.rows(x.shape[0])
-    _check_chunk(cache, layers, scratch, x, starts, seqs, n_new, rope, how)
+    _check_chunk(cache, layers, scratch, x, starts, seqs, n_new, rope, how, eps)
     m, stream = x.shape[0], binding.current_stream(x.device)
     a, q, k, v, t, y, z, u = rows
     h1 = x.shape[1]
@@ -117,8 +119,8 @@ def decoder_chunk(cache, layers, scratch, x, starts, seqs, n_new, rope=None, eps
         w.ff2(u, x, residual=y)
 
 
-def _check_chunk(cache, layers, scratch, x, starts, seqs, n_new, rope, how):
-    _check_widths(cache, layers, scratch, x, x.shape[0])
+def _check_chunk(cache, layers, scratch, x, starts, seqs, n_new, rope, how, eps):
+    _check_widths(cache, layers, scratch, x, x.shape[0], eps)
     batch = seqs.shape[0] if seqs.dim() == 1 else -1
     need("seqs", seqs, torch.int32, (batch,), cache.device)
     need("n_new", n_new, torch.int32, (batch,), cache.device)
