@@ -54,8 +54,8 @@ class Scratch:
 def _check_widths(cache, layers, scratch, x, rows, eps):
     h1, kv = cache.H * cache.d, cache.G * cache.d
     need("x", x, torch.float16, (rows, h1), cache.device)
-    if x.data_ptr() % 16 or not eps >= 0:                    # (the first norm would refuse them, when lengths have grown)
-        raise ValueError("x must be 16-byte aligned, and eps not negative")
+    if h1 > 16384 or x.data_ptr() % 16 or not eps >= 0:      # (the first norm would refuse them, when lengths have grown)
+        raise ValueError("x must be at most 16384 wide and 16-byte aligned, and eps not negative")
     h2 = scratch.u.shape[1]
     if len(layers) != cache.L or any(w.h1 != h1 or w.kv_cols != kv or w.h2 != h2 for w in layers):
         raise ValueError(f"there must be {cache.L} layers of widths {h1}, {kv} and {h2}, as the cache and the scratch have them")

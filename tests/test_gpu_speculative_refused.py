@@ -1,5 +1,6 @@
 """Steps of whole layers that do not fit, refused before lengths grow."""
 import math
+import types
 
 import numpy as np
 import pytest
@@ -53,3 +54,14 @@ def test_steps_that_a_later_call_would_refuse():
     refuses(lambda **kw: decoder_step(**{**good, **kw}), c, (c.codes, c.scales, c.tails, c.table, c.lens, c.refs), [dict(x=between(2)), dict(eps=-1.0), dict(eps=math.nan)])
     decoder_step(**good)
     assert c.lens.tolist()[:2] == [11, 21]
+
+
+def test_layers_that_are_wider_than_a_norm():
+    """(The weights are never reached.)"""
+    heads, kv_heads = 272, 17
+    h1, kv = heads * D, kv_heads * D
+    layers, scratch, x = [types.SimpleNamespace(h1=h1, kv_cols=kv, h2=64)], Scratch(2, h1, 64, kv, DEV), torch.zeros((2, h1), dtype=torch.float16, device=DEV)
+    how = dict(n_layers=1, n_q_heads=heads, n_kv_heads=kv_heads, head_dim=D, page_tokens=32, n_pages=2, max_seqs=2, max_pages_per_seq=1, device=DEV)
+    c, c8 = Cache16(**how), Cache8(**how)
+    refuses(lambda: decoder_chunk(c, layers, scratch, x, ids([0, 2]), ids([0]), ids([2])), c, (c.table, c.lens, c.refs), [dict()])
+    refuses(lambda: decoder_step(c8, layers, scratch, x, ids([0, 1])), c8, (c8.table, c8.lens, c8.refs), [dict()])
