@@ -72,9 +72,10 @@ int okv_rope_append(const okv_layer_pool *c, const okv_rows *r, const okv_rope *
  * those below the sequence's prefix, wherever they are.  Scores, in fp32:
  *     s_i = scale (q . k_i);   s_i = cap tanh(s_i / cap) with a cap;   s_i -= slopes[h] |p - i| with slopes
  *     out = sum_i softmax_i(s) v_i
- * A row that sees no key is 0 (p < 0: the sequence has fewer tokens than rows).  Rows of tokens past the capacity (a len may be above it) attend as the pool's last token does.  A score of -infinity leaves its key out (0 if no key
- * is left), one that is +infinity or NaN makes the row NaN; an infinite or NaN value makes what it goes into infinite or NaN.  What lies at keys that a row does not see, infinities and NaN included, does not
- * change it.  Weights are fp16 in the second product for an fp16 result (each off by 2^-12 of itself, or 2^-32 of the largest), two fp16
+ * A row that sees no key is 0 (p < 0: the sequence has fewer tokens than rows).  Rows of tokens past the capacity (a len may be above it) attend as
+ * the last token within it does.  A score of -infinity leaves its key out (0 if no key is left), one that is +infinity or NaN makes the row NaN; an infinite or NaN value makes the rows that see its key infinite or NaN in that
+ * element, whatever the key's weight, 0 included.  What lies at keys that a row does not see, infinities and NaN included, does not
+ * change it.  Weights are fp16 in the second product for an fp16 result (each off by 2^-11 of itself at most, or 2^-32 of the largest), two fp16
  * numbers for an fp32 one (2^-22); sums are fp32. */
 typedef struct okv_chunk {
   float scale;                 /* 0: 1 / sqrt(d); else in [1e-30, 1e30]                                                 */

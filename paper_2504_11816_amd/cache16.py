@@ -8,7 +8,8 @@
     cache.pages.shrink(seqs, rejected)                                           # drafted tokens that were rejected go again
 
 Pools are laid out as okv.h says: okv_decode_attn_static reads them too.  Every call runs the library's kernels on the current stream, allocates nothing and does
-not wait: it may be captured in a graph.
+not wait: it may be captured in a graph.  Calls of one Cache16 follow one another on one stream, and come from one thread at a time: they share its workspace.  Calls that
+may run at the same time need caches of their own (over the same pool and table, if they only attend).
 """
 import ctypes
 import math
@@ -66,7 +67,6 @@ class Cache16:
             x = binding.OkvLayerPool.from_buffer_copy(c)
             x.pool = pool[l].data_ptr()
             self._layers.append((x, ctypes.byref(x)))
-        # calls over one cache follow one another on one stream
         self.workspace = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.device)
         self._rows = binding.OkvRows()
         self._rows_ref = ctypes.byref(self._rows)

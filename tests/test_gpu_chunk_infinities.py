@@ -74,3 +74,21 @@ def test_values_that_are_not_finite_far_below_the_largest_score(n_new, d, dtype)
     q[:, :, 0] = 4.0                                         # 2000 * 4 / sqrt(d): 707 and more above the others
     for value in (np.inf, -np.inf, np.nan):
         check(p, [(0, 0, 5, value), (1, 1, 2000, value)], q, n_new, dtype)
+
+
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("room", (0, 5000))
+@pytest.mark.parametrize("n_new", ([4], [300]), ids=("few", "many"))
+def test_values_that_are_not_finite_count_at_keys_without_weight(n_new, room, d):
+    """A score of -infinity gives its key no weight; its value, where it is not finite, is seen all the same."""
+    lens = [700]
+    p = Paged(4, 2, d, 64, lens, seed=d, room=room)
+    places = (3, 500, 697)
+    for token in places:
+        p.pool[p.offset(0, 0, 1, token)] = -np.inf
+    p.upload()
+    q = torch.randn((n_new[0], 4, d), generator=torch.Generator().manual_seed(4)).half().to(DEV)
+    q[:, :, 0] = 1.0
+    for dtype in (torch.float16, torch.float32):
+        for token in places:
+            check(p, [(0, 1, token, np.inf)], q, n_new, dtype)
