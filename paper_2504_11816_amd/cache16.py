@@ -13,6 +13,7 @@ may run at the same time need caches of their own (over the same pool and table,
 """
 import ctypes
 import math
+import operator
 
 import torch
 
@@ -155,6 +156,10 @@ class Cache16:
 
     def check_how(self, scale=0.0, cap=0.0, window=0, slopes=None, prefix=None):
         """Raises unless attend() takes these, with sequences by their rows of the table."""
-        if not (all(x == 0 or 1e-30 <= x <= 1e30 for x in (scale, cap)) and hasattr(window, "__index__") and 0 <= window < 1 << 31):
+        try:
+            good = all(x == 0 or 1e-30 <= x <= 1e30 for x in (scale, cap)) and 0 <= operator.index(window) < 1 << 31
+        except TypeError:
+            good = False
+        if not good:
             raise ValueError("scale and cap must be 0 or in [1e-30, 1e30], window a whole number in [0, 2^31)")
         self._vectors(slopes, prefix, self.max_seqs)

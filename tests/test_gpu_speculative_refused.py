@@ -40,7 +40,7 @@ def test_chunks_that_a_later_call_would_refuse():
     layers, scratch = [CompressedLayer(LayerWeights(H1, H2, 5, 0, DEV, kv_cols=KV))], Scratch(16, H1, H2, KV, DEV)
     c.pages.extend(ids([0, 1]), ids([10, 20]))
     good = dict(cache=c, layers=layers, scratch=scratch, x=torch.randn((6, H1), device=DEV).half(), starts=ids([0, 2, 6]), seqs=ids([1, 0]), n_new=ids([2, 4]), rope=Rope.of(D, device=DEV))
-    bad = [dict(x=between(6)), dict(eps=-1.0), dict(eps=math.nan), dict(window=2.5), dict(window=math.nan)]
+    bad = [dict(x=between(6)), dict(eps=-1.0), dict(eps=math.nan), dict(window=2.5), dict(window=math.nan), dict(window=torch.tensor(2.5)), dict(cap="1")]
     refuses(lambda **kw: decoder_chunk(**{**good, **kw}), c, (c.pool, c.table, c.lens, c.refs), bad)
     decoder_chunk(**good, window=np.int64(7), eps=0)
     assert c.lens.tolist()[:2] == [14, 22]
